@@ -382,6 +382,98 @@ int fairkv_append(const void *k_new, const void *v_new, int32_t B, int32_t Hkv, 
  * and step; re-plan with fairkv_plan every few hundred steps. */
 int fairkv_plan_grow(fairkv_item *items, int32_t n_items, int32_t B, int32_t Hkv, int32_t *len, const int32_t *cap);
 
+/* ---- a step over a growing cache: append the new tokens, attend, keep what was accepted -----------
+ *
+ * The entry points above plan on the host, for lengths that stay as the compressor left them.  While a sequence is
+ * decoded its lengths grow, by one token a step or by the accepted part of a draft, and they are known on the GPU first.
+ * The three calls of such a step read lengths there and nowhere else: nothing is planned on the host, and a step captured
+ * into a graph may be replayed while the cache grows.
+ *
+ *     fairkv_append_rotated       the new tokens' heads: norm, rotation by position, keys and values into the cache
+ *     fairkv_decode_attn_tree     every new token attends over the cache and over the new tokens that are its ancestors
+ *     fairkv_accept               the rows of the accepted path move to the front of the draft's, the others are dropped
+ *
+ * fairkv_cache says where a layer's rows are.  Pair p = b * Hkv + h, token t >= 0:
+ *   packed (off given, pages null)   row off[p] + t
+ *   paged (pages given, off null)    row pages[p * max_pages + t / page_rows] * page_rows + t % page_rows
+ * A pair may hold cap[p] tokens (paged: and max_pages * page_rows).  Rows of different pairs must not overlap; pages that no
+ * token lies in are not looked at.  A pair whose off, or a token whose page, lies outside the n_rows rows has no such row:
+ * such tokens are not attended to, and nothing is appended or moved there. */
+enum { FAIRKV_MAX_DRAFT = 64,     /* most new tokens of a sequence in one call */
+       FAIRKV_CACHE_SCALES = 32 };
+
+typedef struct {
+    void *k, *v;             /* device [n_rows][D] of type dtype, 16-byte aligned */
+    int64_t n_rows;
+    const int64_t *off;      /* device [B][Hkv], or NULL */
+    const int32_t *pages;    /* device [B][Hkv][max_pages], or NULL */
+    const int32_t *cap;      /* device [B][Hkv] */
+    int32_t max_pages;       /* 0 for a packed cache */
+    int32_t page_rows;       /* a power of two, 16 or more; 0 for a packed cache */
+    int32_t B, Hkv, D;       /* D 64 or 128 */
+    int32_t dtype;           /* FAIRKV_BF16, FAIRKV_E4M3 or (append, accept) FAIRKV_F32 */
+    int32_t n_scales;        /* E4M3: 1, or Hkv (at most FAIRKV_CACHE_SCALES): a stored byte of head h stands for byte * k_scale[h]; else 0 */
+    float k_scale[FAIRKV_CACHE_SCALES], v_scale[FAIRKV_CACHE_SCALES];   /* finite, not 0 */
+} fairkv_cache;              /* a host struct; 336 bytes */
+
+/* What is done to the heads of new queries and keys before they are used, all of it in fp32, rounded once at the end:
+ *   x = x / sqrt(mean(x^2) + eps) * norm      over the D elements of a head; q_norm, k_norm device float [D], NULL: not done
+ *   (x_a, x_b) = (x_a cos - x_b sin, x_b cos + x_a sin)   for the rot / 2 pairs of the first rot elements: a = i, b = i + rot / 2,
+ *       or with `pairs` set a = 2 i, b = 2 i + 1.  table: device float [n_pos][rot], the cosines of the rot / 2 angles of a position
+ *       and then their sines (made in as many bits as far positions want), 16-byte aligned; NULL: not done.
+ *   pos        device int32 [B][q_len]: the new tokens' positions (the nodes of a tree at one depth share one). */
+typedef struct {
+    const float *q_norm, *k_norm;
+    const float *table;
+    const int32_t *pos;
+    float eps;               /* >= 0 */
+    int32_t n_pos, rot;      /* rot a multiple of 16, at most D */
+    int32_t pairs;
+} fairkv_rotation;
+
+/* Norm and rotation of q_len new tokens per sequence; queries go to q_out, keys and values into the cache as tokens
+ * len[p] .. len[p] + n - 1 of every pair, with len_out[p] = len[p] + n, n = n_new[b].
+ * q, k_new, v_new   device, of type dtype (BF16, or F32 with an F32 cache): token (b, i) at element (b * q_len + i) * stride, its Hq (Hkv)
+ *                   heads one behind the other; strides in elements, at least Hq * D (Hkv * D), so that all three may lie in one
+ *                   projection's output.  16-byte aligned, strides multiples of 16 bytes.
+ * q_out             device [B][q_len][Hq][D] of type dtype; may be q where q's tokens follow one another
+ * n_new             device [B]: how many of the q_len tokens a sequence has (taken into 0 .. q_len), or NULL: all.  What is behind them is not
+ *                   read, and the queries there are left as they are.
+ * len_out           device [B][Hkv]; may be len
+ * bad               device counter or NULL: plus one for every pair that is left alone (its length kept, none of its rows written), because
+ *                   it has no room for all n, a row of them lies outside the cache or a position outside the table, and for every token whose
+ *                   queries are left alone because its position lies outside the table.
+ * An E4M3 cache takes x / scale rounded to nearest even, what is beyond +-448 as +-448.
+ * Enqueues one kernel; no synchronisation.  FAIRKV_EUNSUPPORTED: q_len > FAIRKV_MAX_DRAFT, types, D. */
+int fairkv_append_rotated(const fairkv_cache *cache, const fairkv_rotation *r, const void *q, int64_t q_stride, const void *k_new,
+                          int64_t k_stride, const void *v_new, int64_t v_stride, void *q_out, int32_t q_len, int32_t Hq, int32_t dtype,
+                          const int32_t *n_new, const int32_t *len, int32_t *len_out, int32_t *bad, void *hip_stream);
+
+/* Attention of a draft tree.  The last n = n_new[b] of the len[p] rows of every pair are the draft's (fairkv_append_rotated has put
+ * them there); node i < n of sequence b sees every row in front of them and draft row j < n iff bit j of tree[b][i] is set: its ancestors'
+ * bits and, as a rule, its own.  tree == NULL: nodes 0 .. i, a chain; q_len = 1 is a plain decode step.
+ * out = softmax(scale * q . K^T) V over the rows that are seen, in fp32, and lse = log sum exp of the scaled scores; a node that sees
+ * nothing gets out = 0 and lse = -inf.  An infinite or NaN row counts for the nodes that see it only.  Nodes i >= n are left as they are.
+ * q          device bf16 [B][q_len][Hq][D], 16-byte aligned; Hq a multiple of Hkv, any Hq / Hkv up to 16
+ * tree       device uint64 [B][q_len], or NULL
+ * workspace  device, fairkv_tree_workspace_bytes(cache, Hq, q_len, n_slots) bytes, 16-byte aligned.  It need not be cleared; nothing in it is
+ *            kept from call to call.  Calls that share one must be ordered on one stream.
+ * n_slots    workgroups to balance over: the GPU's compute units
+ * out        device [B][q_len][Hq][D] of out_dtype (FAIRKV_F32 or FAIRKV_BF16); lse device float [B][q_len][Hq] or NULL
+ * Lengths below 0 count as 0, those beyond the cache's rows (paged: max_pages * page_rows) as that many.
+ * Enqueues two kernels; no synchronisation.  FAIRKV_EUNSUPPORTED: q_len > FAIRKV_MAX_DRAFT, an F32 cache, D, Hq / Hkv > 16. */
+size_t fairkv_tree_workspace_bytes(const fairkv_cache *cache, int32_t Hq, int32_t q_len, int32_t n_slots);
+int fairkv_decode_attn_tree(const fairkv_cache *cache, const void *q, const uint64_t *tree, const int32_t *n_new, const int32_t *len,
+                            void *workspace, size_t workspace_bytes, int32_t n_slots, void *out, float *lse, int32_t q_len, int32_t Hq,
+                            int32_t out_dtype, float scale, void *hip_stream);
+
+/* Keeps n_path[b] of the n = n_new[b] draft rows at the end of every pair: draft row path[b][i] becomes draft row i for i < n_path[b], and
+ * len_out[p] = len[p] - n + n_path[b].  path: device int32 [B][q_len], in any order, what is behind n_path[b] is not read; n_path device [B].
+ * A pair is left alone (its length kept) and counted in *bad if n_path[b] is not in 0 .. n, an entry not in 0 .. n - 1, its length below n,
+ * or a row outside the cache.  len_out may be len; bad may be NULL.  Enqueues one kernel; no synchronisation. */
+int fairkv_accept(const fairkv_cache *cache, const int32_t *path, const int32_t *n_path, const int32_t *n_new, const int32_t *len,
+                  int32_t *len_out, int32_t q_len, int32_t *bad, void *hip_stream);
+
 /* The measurement aids (the decode kernel with wall-clock stamps, the reader that only streams) are declared in
  * fairkv_measure.h: they are in the library for the benchmark, not for callers of the method. */
 

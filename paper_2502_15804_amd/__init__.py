@@ -24,6 +24,8 @@ FAIRKV_SHORT_PAIR_TOKENS = 96
 FAIRKV_STATIC_WORKSPACE_BYTES = 8 << 20
 FAIRKV_POLICY_NAIVE, FAIRKV_POLICY_LPT, FAIRKV_POLICY_LPT_SPLIT, FAIRKV_POLICY_FAIR = 0, 1, 2, 3
 
+FAIRKV_MAX_DRAFT, FAIRKV_CACHE_SCALES = 64, 32
+
 FAIRKV_PLACE_AUTO, FAIRKV_PLACE_EXACT, FAIRKV_PLACE_GREEDY = 0, 1, 2
 
 EXPORTS = ("fairkv_default_params", "fairkv_plan", "fairkv_workspace_bytes", "fairkv_workspace_counter_bytes",
@@ -31,6 +33,7 @@ EXPORTS = ("fairkv_default_params", "fairkv_plan", "fairkv_workspace_bytes", "fa
            "fairkv_decode_attn_multi", "fairkv_decode_attn_kv8", "fairkv_decode_attn_kv8_per_head",
            "fairkv_decode_attn_static", "fairkv_decode_attn_trace",
            "fairkv_place", "fairkv_pack", "fairkv_append", "fairkv_plan_grow", "fairkv_stream_probe", "fairkv_stream_probe_shape", "fairkv_workspace_reset",
+           "fairkv_append_rotated", "fairkv_decode_attn_tree", "fairkv_tree_workspace_bytes", "fairkv_accept",
            "fairkv_strerror", "fairkv_version")
 
 
@@ -61,6 +64,18 @@ class fairkv_place_summary(ctypes.Structure):
     _fields_ = [("den", ctypes.c_int64), ("delta_num", ctypes.c_int64), ("max_load_num", ctypes.c_int64),
                 ("min_load_num", ctypes.c_int64), ("efficiency", ctypes.c_double), ("n_shares", ctypes.c_int32),
                 ("exact", ctypes.c_int32)]
+
+
+class fairkv_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_rows", ctypes.c_int64), ("off", ctypes.c_void_p),
+                ("pages", ctypes.c_void_p), ("cap", ctypes.c_void_p)] + [
+        (n, ctypes.c_int32) for n in ("max_pages", "page_rows", "B", "Hkv", "D", "dtype", "n_scales")] + [
+        (n, ctypes.c_float * FAIRKV_CACHE_SCALES) for n in ("k_scale", "v_scale")]
+
+
+class fairkv_rotation(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q_norm", "k_norm", "table", "pos")] + [("eps", ctypes.c_float)] + [
+        (n, ctypes.c_int32) for n in ("n_pos", "rot", "pairs")]
 
 
 SHARE_DTYPE = np.dtype([(n, np.int32) for n, _ in fairkv_share._fields_])
@@ -139,6 +154,16 @@ def lib() -> ctypes.CDLL:
         L.fairkv_decode_attn_trace.restype = ctypes.c_int
         L.fairkv_decode_attn_trace.argtypes = [vp, vp, vp, ctypes.c_int64, vp, vp, i32, vp, i32, i32, vp, ctypes.c_size_t,
                                                vp, vp, i32, i32, i32, i32, ctypes.c_float, vp, ctypes.c_size_t, vp]
+        cache_p = ctypes.POINTER(fairkv_cache)
+        L.fairkv_append_rotated.restype = ctypes.c_int
+        L.fairkv_append_rotated.argtypes = [cache_p, ctypes.POINTER(fairkv_rotation), vp, ctypes.c_int64, vp, ctypes.c_int64, vp, ctypes.c_int64,
+                                            vp, i32, i32, i32, vp, vp, vp, vp, vp]
+        L.fairkv_tree_workspace_bytes.restype = ctypes.c_size_t
+        L.fairkv_tree_workspace_bytes.argtypes = [cache_p, i32, i32, i32]
+        L.fairkv_decode_attn_tree.restype = ctypes.c_int
+        L.fairkv_decode_attn_tree.argtypes = [cache_p, vp, vp, vp, vp, vp, ctypes.c_size_t, i32, vp, vp, i32, i32, i32, ctypes.c_float, vp]
+        L.fairkv_accept.restype = ctypes.c_int
+        L.fairkv_accept.argtypes = [cache_p, vp, vp, vp, vp, vp, i32, vp, vp]
         L.fairkv_strerror.restype = ctypes.c_char_p
         L.fairkv_strerror.argtypes = [ctypes.c_int]
         L.fairkv_version.restype = ctypes.c_int
@@ -289,7 +314,8 @@ def _native():
         loader.exec_module(m)
         m.init(ITEM_DTYPE, *(ctypes.cast(f, ctypes.c_void_p).value for f in (
             L.fairkv_decode_attn_multi, L.fairkv_decode_attn_static, L.fairkv_decode_attn_trace, L.fairkv_decode_attn_kv8,
-            L.fairkv_decode_attn_kv8_per_head, L.fairkv_pack, L.fairkv_append)))
+            L.fairkv_decode_attn_kv8_per_head, L.fairkv_pack, L.fairkv_append, L.fairkv_append_rotated, L.fairkv_decode_attn_tree,
+            L.fairkv_accept)))
         _native_module = m
     return _native_module
 
@@ -380,6 +406,88 @@ def fairkv_plan_grow(items: np.ndarray, B: int, Hkv: int, lens: np.ndarray, cap:
     rc = lib().fairkv_plan_grow(items.ctypes.data, items.size, int(B), int(Hkv), lens.ctypes.data, cap.ctypes.data)
     if rc != FAIRKV_OK:
         raise FairKVError(rc, "fairkv_plan_grow")
+
+
+class Cache:
+    """One layer's growing cache: where the rows of its pairs are (fairkv_cache in the header).
+
+    k, v [n_rows, D] bfloat16, float32 or 8-bit floats (torch.float8_e4m3fn, or uint8 holding the same bytes); cap int32 [B, Hkv]: the
+    tokens a pair may hold.  Packed: off int64 [B, Hkv].  Paged: pages int32 [B, Hkv, max_pages] (or [B * Hkv, max_pages]) and page_rows.
+    k_scale, v_scale: of an 8-bit cache, a number or one per KV head (1).  All tensors are on one GPU and contiguous; the cache keeps them
+    and reads what is in them at every call, so pages may be entered into `pages` as sequences grow.
+    """
+
+    def __init__(self, k, v, cap, off=None, pages=None, page_rows=None, k_scale=None, v_scale=None):
+        torch = _torch()[0]
+        codes = {torch.bfloat16: FAIRKV_BF16, torch.float32: FAIRKV_F32, torch.float8_e4m3fn: FAIRKV_E4M3, torch.uint8: FAIRKV_E4M3}
+        if k.dtype not in codes or v.dtype != k.dtype:
+            raise TypeError("k and v must share bfloat16, float32 or 8-bit floats")
+        if k.dim() != 2 or v.shape != k.shape or cap.dim() != 2:
+            raise ValueError("k and v must be [n_rows, D], cap [B, Hkv]")
+        if (off is None) == (pages is None) or (pages is None) != (page_rows is None):
+            raise ValueError("a cache has either off, or pages and page_rows")
+        B, Hkv = cap.shape
+        if cap.dtype != torch.int32 or (off is not None and (off.dtype != torch.int64 or off.numel() != cap.numel())):
+            raise ValueError("cap must be int32 [B, Hkv], off int64 of its size")
+        if pages is not None and (pages.dtype != torch.int32 or pages.dim() not in (2, 3) or pages.shape[:-1].numel() != cap.numel()):
+            raise ValueError("pages must be int32 [B, Hkv, max_pages]")
+        _check_dev(k=k, v=v, cap=cap, off=off, pages=pages)
+        if any(t is not None and t.device != k.device for t in (v, cap, off, pages)):
+            raise ValueError("the tensors of a cache must be on one device")
+        c = fairkv_cache(k=_ptr(k), v=_ptr(v), n_rows=k.shape[0], off=_ptr(off), pages=_ptr(pages), cap=_ptr(cap),
+                         max_pages=pages.shape[-1] if pages is not None else 0, page_rows=int(page_rows or 0), B=B, Hkv=Hkv, D=k.shape[1],
+                         dtype=codes[k.dtype])
+        if c.dtype == FAIRKV_E4M3:
+            c.n_scales = Hkv if np.ndim(k_scale) or np.ndim(v_scale) else 1
+            if c.n_scales > FAIRKV_CACHE_SCALES:
+                raise ValueError(f"scales for at most {FAIRKV_CACHE_SCALES} KV heads")
+            for to, scale in ((c.k_scale, k_scale), (c.v_scale, v_scale)):
+                to[:c.n_scales] = np.broadcast_to(np.asarray(1.0 if scale is None else scale, dtype=np.float32), (c.n_scales,)).tolist()
+        elif k_scale is not None or v_scale is not None:
+            raise ValueError("scales belong to an 8-bit cache")
+        from .runtime import device_compute_units
+        self.k, self.v, self.cap, self.off, self.pages = k, v, cap, off, pages       # kept alive: the struct has their addresses
+        self.struct, self.address, self.device = c, ctypes.addressof(c), k.get_device()
+        self.n_slots = device_compute_units(k.device)
+
+
+def fairkv_append_rotated(cache, lens, q, k_new, v_new, q_out, table=None, pos=None, q_norm=None, k_norm=None, eps=1e-6, pairs=False,
+                          n_new=None, lens_out=None, bad=None, stream=None):
+    """Enqueue the append of a step's new tokens, their query and key heads normalised and rotated (see the header).
+
+    q, q_out [B, q_len, Hq, D] (or [B, Hq, D]), k_new, v_new [B, q_len, Hkv, D] (or [B, Hkv, D]), bfloat16 or float32; q, k_new and v_new may be
+    slices of one projection's output.  table float32 [n_pos, rot] with pos int32 [B, q_len]; q_norm, k_norm float32 [D]; n_new int32 [B];
+    lens, lens_out int32 [B, Hkv] (lens_out=None: in place); bad int32 [1].  Queries go to q_out, which may be q."""
+    rc = (_native_module or _native()).append_rotated((_pt or _torch())[1], cache.address, cache.device, lens, q, k_new, v_new, q_out, table, pos, q_norm,
+                                                      k_norm, eps, pairs, n_new, lens_out, bad, stream)
+    if rc != FAIRKV_OK:
+        raise FairKVError(rc, "fairkv_append_rotated")
+
+
+def fairkv_tree_workspace_bytes(cache, Hq: int, q_len: int, n_slots=None) -> int:
+    """Bytes of the workspace of fairkv_decode_attn_tree; 0 for a shape that it does not take."""
+    return int(lib().fairkv_tree_workspace_bytes(ctypes.byref(cache.struct), int(Hq), int(q_len), cache.n_slots if n_slots is None else int(n_slots)))
+
+
+def fairkv_decode_attn_tree(cache, lens, q, workspace, out, lse, scale, tree=None, n_new=None, n_slots=None, stream=None):
+    """Enqueue the attention of a draft tree over the cache and the draft's own rows, the last of every pair (see the header).
+
+    q bfloat16 [B, q_len, Hq, D] (or [B, Hq, D]); tree int64 or uint64 [B, q_len]: bit j of node i's word says that it sees node j (None: a chain);
+    n_new int32 [B] or None; lens int32 [B, Hkv]; workspace of fairkv_tree_workspace_bytes; out bfloat16 or float32 of q's shape; lse
+    float32 [B, q_len, Hq] or None.  Nothing is allocated or synchronised here."""
+    rc = (_native_module or _native()).decode_tree((_pt or _torch())[1], cache.address, cache.device, lens, q, workspace, out, lse, scale, tree, n_new,
+                                                   cache.n_slots if n_slots is None else n_slots, stream)
+    if rc != FAIRKV_OK:
+        raise FairKVError(rc, "fairkv_decode_attn_tree")
+
+
+def fairkv_accept(cache, lens, path, n_path, n_new=None, lens_out=None, bad=None, stream=None):
+    """Enqueue the end of a step: of the draft's rows those of the accepted path are kept (see the header).
+
+    path int32 [B, q_len], n_path int32 [B]; n_new as in the step's append; lens, lens_out int32 [B, Hkv] (lens_out=None: in place); bad int32 [1]."""
+    rc = (_native_module or _native()).accept((_pt or _torch())[1], cache.address, cache.device, lens, path, n_path, n_new, lens_out, bad, stream)
+    if rc != FAIRKV_OK:
+        raise FairKVError(rc, "fairkv_accept")
 
 
 def fairkv_workspace_reset(workspace, n_pairs, stream=None):

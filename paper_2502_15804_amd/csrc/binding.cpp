@@ -8,8 +8,10 @@
 #include <Python.h>
 #define NPY_NO_DEPRECATED_API NPY_2_0_API_VERSION
 #include <numpy/arrayobject.h>
+#include <c10/core/DeviceGuard.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <exception>
 
@@ -25,6 +27,9 @@ decltype(&fairkv_decode_attn_kv8) decode_kv8;
 decltype(&fairkv_decode_attn_kv8_per_head) decode_kv8_per_head;
 decltype(&fairkv_pack) pack_rows;
 decltype(&fairkv_append) append_rows;
+decltype(&fairkv_append_rotated) append_rotated_rows;
+decltype(&fairkv_decode_attn_tree) decode_tree_attn;
+decltype(&fairkv_accept) accept_rows;
 PyArray_Descr *item_descr;      // of the plan's item array
 
 struct Refused {};              // a Python exception is set
@@ -325,19 +330,166 @@ PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---- a step over a growing cache ----
+// A cache is the address of its fairkv_cache, whose tensors its owner has checked, and its GPU.
+struct CacheArg {
+    const fairkv_cache *c;
+    c10::DeviceIndex device;
+    CacheArg(PyObject *address, PyObject *index) : c(static_cast<const fairkv_cache *>(PyLong_AsVoidPtr(address))), device(static_cast<c10::DeviceIndex>(index_of(index)))
+    {
+        if (PyErr_Occurred()) throw Refused{};
+        if (!c) refuse(PyExc_ValueError, "not a cache");
+    }
+    int64_t pairs() const { return static_cast<int64_t>(c->B) * c->Hkv; }
+    // A tensor on the cache's GPU, of any strides.
+    const at::Tensor &here(PyObject *o, const char *name, bool optional = false) const
+    {
+        const at::Tensor &t = tensor(o, name, optional);
+        if (t.defined() && (!t.is_cuda() || t.get_device() != device)) {
+            PyErr_Format(PyExc_ValueError, "%s must be on the cache's device", name);
+            throw Refused{};
+        }
+        return t;
+    }
+    // ... that is contiguous, of a type and with so many elements (-1: any number)
+    const at::Tensor &flat(PyObject *o, const char *name, at::ScalarType type, int64_t numel, bool optional = false) const
+    {
+        const at::Tensor &t = here(o, name, optional);
+        if (!t.defined()) return t;
+        on_device(t, name);
+        if (!is(t, type) || (numel >= 0 && t.numel() != numel)) {
+            PyErr_Format(PyExc_ValueError, "%s must have %lld elements of type %s", name, static_cast<long long>(numel), c10::toString(type));
+            throw Refused{};
+        }
+        return t;
+    }
+    c10::DeviceGuard guard() const { return c10::DeviceGuard(c10::Device(c10::DeviceType::CUDA, device)); }
+};
+template <class T>
+T *data(const at::Tensor &t)
+{
+    return static_cast<T *>(ptr(t));
+}
+
+// Elements between the tokens of x [B, n, H, D] (or [B, H, D]), whose heads lie one behind the other.
+int64_t token_stride(const at::Tensor &x, const char *name)
+{
+    const int64_t B = x.size(0), n = x.dim() == 4 ? x.size(1) : 1, H = x.size(-2), D = x.size(-1);
+    const int64_t stride = n > 1 ? x.stride(1) : B > 1 ? x.stride(0) : H * D;
+    if ((D > 1 && x.stride(-1) != 1) || (H > 1 && x.stride(-2) != D) || (n > 1 && B > 1 && x.stride(0) != n * stride)) {
+        PyErr_Format(PyExc_ValueError, "%s must have its heads one behind the other and one distance between its tokens", name);
+        throw Refused{};
+    }
+    return stride;
+}
+
+// (current, cache, device, lens, q, k_new, v_new, q_out, table, pos, q_norm, k_norm, eps, pairs, n_new, lens_out, bad, stream)
+PyObject *append_rotated(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 18, [&]() -> int {
+        const CacheArg cache(a[1], a[2]);
+        const fairkv_cache *c = cache.c;
+        const at::Tensor &q = cache.here(a[4], "q"), &k = cache.here(a[5], "k_new"), &v = cache.here(a[6], "v_new"), &q_out = cache.here(a[7], "q_out");
+        const bool multi = q.dim() == 4;
+        if (!multi && q.dim() != 3) refuse(PyExc_ValueError, "q must be [B, Hq, D] or [B, q_len, Hq, D]");
+        const int64_t B = c->B, n_new_max = multi ? q.size(1) : 1;
+        if (q.size(0) != B || q.size(-1) != c->D || k.dim() != q.dim() || k.size(0) != B || k.size(-1) != c->D || k.size(-2) != c->Hkv ||
+            (multi && k.size(1) != n_new_max) || v.sizes() != k.sizes() || q_out.sizes() != q.sizes())
+            refuse(PyExc_ValueError, "shape mismatch");
+        if (!is_q_or_out(q) || k.scalar_type() != q.scalar_type() || v.scalar_type() != q.scalar_type() || q_out.scalar_type() != q.scalar_type())
+            refuse(PyExc_TypeError, "q, k_new, v_new and q_out must share bf16 or fp32");
+        on_device(q_out, "q_out");
+        const int64_t tokens = B * n_new_max;
+        const at::Tensor &lens = cache.flat(a[3], "lens", at::kInt, cache.pairs()), &table = cache.flat(a[8], "table", at::kFloat, -1, true),
+                         &pos = cache.flat(a[9], "pos", at::kInt, tokens, true), &q_norm = cache.flat(a[10], "q_norm", at::kFloat, c->D, true),
+                         &k_norm = cache.flat(a[11], "k_norm", at::kFloat, c->D, true), &count = cache.flat(a[14], "n_new", at::kInt, B, true),
+                         &lens_out = cache.flat(a[15], "lens_out", at::kInt, cache.pairs(), true), &bad = cache.flat(a[16], "bad", at::kInt, 1, true);
+        if (table.defined() && (table.dim() != 2 || !pos.defined())) refuse(PyExc_ValueError, "table must be [n_pos, rot] and come with pos");
+        if (table.defined() && table.size(0) > INT32_MAX) refuse(PyExc_ValueError, "too many positions");
+        const int pairs = PyObject_IsTrue(a[13]);
+        if (pairs < 0) throw Refused{};
+        fairkv_rotation r{};
+        r.q_norm = data<const float>(q_norm), r.k_norm = data<const float>(k_norm), r.table = data<const float>(table), r.pos = data<const int32_t>(pos);
+        r.eps = float_of(a[12]);
+        r.n_pos = table.defined() ? static_cast<int32_t>(table.size(0)) : 0;
+        r.rot = table.defined() ? static_cast<int32_t>(std::min<int64_t>(table.size(1), INT32_MAX)) : 0;
+        r.pairs = pairs;
+        const int64_t qs = token_stride(q, "q"), ks = token_stride(k, "k_new"), vs = token_stride(v, "v_new");
+        void *st = stream_of(a[17], a[0], q);
+        const c10::DeviceGuard guard = cache.guard();
+        return unlocked([&] {
+            return append_rotated_rows(c, &r, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, q_out.data_ptr(), static_cast<int32_t>(n_new_max),
+                                       static_cast<int32_t>(q.size(-2)), dtype_code(q), data<const int32_t>(count), data<const int32_t>(lens),
+                                       data<int32_t>(lens_out.defined() ? lens_out : lens), data<int32_t>(bad), st);
+        });
+    });
+}
+
+// (current, cache, device, lens, q, workspace, out, lse, scale, tree, n_new, n_slots, stream)
+PyObject *decode_tree(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 13, [&]() -> int {
+        const CacheArg cache(a[1], a[2]);
+        const fairkv_cache *c = cache.c;
+        const at::Tensor &q = cache.here(a[4], "q"), &workspace = cache.here(a[5], "workspace"), &out = cache.here(a[6], "out");
+        on_device(q, "q"), on_device(workspace, "workspace"), on_device(out, "out");
+        const bool multi = q.dim() == 4;
+        if (!multi && q.dim() != 3) refuse(PyExc_ValueError, "q must be [B, Hq, D] or [B, q_len, Hq, D]");
+        if (q.size(0) != c->B || q.size(-1) != c->D || out.sizes() != q.sizes()) refuse(PyExc_ValueError, "shape mismatch");
+        if (!is(q, at::kBFloat16) || !is_q_or_out(out)) refuse(PyExc_TypeError, "q must be bf16, out bf16 or fp32");
+        const int64_t q_len = multi ? q.size(1) : 1, Hq = q.size(-2);
+        if (q_len > INT32_MAX || Hq > INT32_MAX) refuse(PyExc_ValueError, "shape mismatch");
+        const at::Tensor &lens = cache.flat(a[3], "lens", at::kInt, cache.pairs()), &lse = cache.flat(a[7], "lse", at::kFloat, c->B * q_len * Hq, true),
+                         &tree = cache.here(a[9], "tree", true), &count = cache.flat(a[10], "n_new", at::kInt, c->B, true);
+        if (tree.defined()) {
+            on_device(tree, "tree");
+            if ((!is(tree, at::kLong) && !is(tree, at::kUInt64)) || tree.numel() != c->B * q_len)
+                refuse(PyExc_ValueError, "tree must have a 64-bit word for every new token");
+        }
+        const float scale = float_of(a[8]);
+        const int32_t n_slots = index_of(a[11]);
+        void *st = stream_of(a[12], a[0], q);
+        const c10::DeviceGuard guard = cache.guard();
+        return unlocked([&] {
+            return decode_tree_attn(c, q.data_ptr(), data<const uint64_t>(tree), data<const int32_t>(count), data<const int32_t>(lens), workspace.data_ptr(),
+                                    workspace.nbytes(), n_slots, out.data_ptr(), data<float>(lse), static_cast<int32_t>(q_len), static_cast<int32_t>(Hq),
+                                    dtype_code(out), scale, st);
+        });
+    });
+}
+
+// (current, cache, device, lens, path, n_path, n_new, lens_out, bad, stream)
+PyObject *accept(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 10, [&]() -> int {
+        const CacheArg cache(a[1], a[2]);
+        const int64_t B = cache.c->B;
+        const at::Tensor &lens = cache.flat(a[3], "lens", at::kInt, cache.pairs()), &path = cache.flat(a[4], "path", at::kInt, -1),
+                         &n_path = cache.flat(a[5], "n_path", at::kInt, B), &count = cache.flat(a[6], "n_new", at::kInt, B, true),
+                         &lens_out = cache.flat(a[7], "lens_out", at::kInt, cache.pairs(), true), &bad = cache.flat(a[8], "bad", at::kInt, 1, true);
+        if (path.dim() != 2 || path.size(0) != B || path.size(1) > INT32_MAX) refuse(PyExc_ValueError, "path must be [B, q_len]");
+        void *st = stream_of(a[9], a[0], path);
+        const c10::DeviceGuard guard = cache.guard();
+        return unlocked([&] {
+            return accept_rows(cache.c, data<const int32_t>(path), data<const int32_t>(n_path), data<const int32_t>(count), data<const int32_t>(lens),
+                               data<int32_t>(lens_out.defined() ? lens_out : lens), static_cast<int32_t>(path.size(1)), data<int32_t>(bad), st);
+        });
+    });
+}
+
 // (dtype of the plan's items, addresses of the library's functions in the order of the pointers above)
 PyObject *init(PyObject *, PyObject *args)
 {
     PyObject *dtype;
-    unsigned long long f[7];
-    if (!PyArg_ParseTuple(args, "OKKKKKKK", &dtype, f, f + 1, f + 2, f + 3, f + 4, f + 5, f + 6)) return nullptr;
+    unsigned long long f[10];
+    if (!PyArg_ParseTuple(args, "OKKKKKKKKKK", &dtype, f, f + 1, f + 2, f + 3, f + 4, f + 5, f + 6, f + 7, f + 8, f + 9)) return nullptr;
     if (!PyArray_DescrCheck(dtype)) return PyErr_Format(PyExc_TypeError, "a numpy dtype is expected");
     Py_INCREF(dtype);
     Py_XDECREF(reinterpret_cast<PyObject *>(item_descr));
     item_descr = reinterpret_cast<PyArray_Descr *>(dtype);
     auto set = [&](auto &fn, int i) { fn = reinterpret_cast<std::decay_t<decltype(fn)>>(static_cast<uintptr_t>(f[i])); };
     set(decode_multi, 0), set(decode_static, 1), set(decode_trace, 2), set(decode_kv8, 3), set(decode_kv8_per_head, 4);
-    set(pack_rows, 5), set(append_rows, 6);
+    set(pack_rows, 5), set(append_rows, 6), set(append_rotated_rows, 7), set(decode_tree_attn, 8), set(accept_rows, 9);
     Py_RETURN_NONE;
 }
 
@@ -350,6 +502,9 @@ PyMethodDef methods[] = {
     {"decode_8bit", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(decode_8bit)), METH_FASTCALL, nullptr},
     {"pack", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(pack)), METH_FASTCALL, nullptr},
     {"append", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(append)), METH_FASTCALL, nullptr},
+    {"append_rotated", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(append_rotated)), METH_FASTCALL, nullptr},
+    {"decode_tree", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(decode_tree)), METH_FASTCALL, nullptr},
+    {"accept", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(accept)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,226 @@
+// C ABI of a step over a growing cache: argument checks, kernel selection and launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "append_rotated.h"
+#include "decode_tree.h"
+#include "fairkv.h"
+
+namespace {
+
+using namespace fairkv;
+
+bool aligned(const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+int launched() { return hipGetLastError() == hipSuccess ? FAIRKV_OK : FAIRKV_EHIP; }
+
+int check_cache(const fairkv_cache *c)
+{
+    if (!c || !c->k || !c->v || !c->cap || (c->off == nullptr) == (c->pages == nullptr)) return FAIRKV_EINVAL;
+    if (c->B < 1 || c->Hkv < 1 || c->D < 1 || c->n_rows < 0 || !aligned(c->k, 16) || !aligned(c->v, 16)) return FAIRKV_EINVAL;
+    if (static_cast<int64_t>(c->B) * c->Hkv > INT32_MAX / 2) return FAIRKV_EINVAL;
+    if (c->pages && (c->max_pages < 1 || c->page_rows < 16 || (c->page_rows & (c->page_rows - 1)) != 0 || c->page_rows > (1 << 30))) return FAIRKV_EINVAL;
+    if (c->off && (c->max_pages != 0 || c->page_rows != 0)) return FAIRKV_EINVAL;
+    if (c->dtype != FAIRKV_BF16 && c->dtype != FAIRKV_F32 && c->dtype != FAIRKV_E4M3) return FAIRKV_EUNSUPPORTED;
+    if (c->D != 64 && c->D != 128) return FAIRKV_EUNSUPPORTED;
+    if (c->dtype != FAIRKV_E4M3) return c->n_scales == 0 ? FAIRKV_OK : FAIRKV_EINVAL;
+    if (c->n_scales > FAIRKV_CACHE_SCALES) return FAIRKV_EUNSUPPORTED;
+    if (c->n_scales != 1 && c->n_scales != c->Hkv) return FAIRKV_EINVAL;
+    for (int32_t h = 0; h < c->n_scales; ++h)
+        if (!std::isfinite(c->k_scale[h]) || !std::isfinite(c->v_scale[h]) || c->k_scale[h] == 0.f || c->v_scale[h] == 0.f) return FAIRKV_EINVAL;
+    return FAIRKV_OK;
+}
+
+RowMap row_map(const fairkv_cache *c)
+{
+    int shift = 0;
+    while (c->pages && (1 << shift) < c->page_rows) ++shift;
+    return RowMap{c->off, c->pages, c->n_rows, c->max_pages, shift};
+}
+
+template <typename T, typename C>
+void launch_rotated(int D, unsigned grid, hipStream_t st, const RotateArgs &a)
+{
+    if (D == 64)
+        hipLaunchKernelGGL((fairkv_append_rotated_kernel<T, C, 64>), dim3(grid), dim3(256), 0, st, a);
+    else
+        hipLaunchKernelGGL((fairkv_append_rotated_kernel<T, C, 128>), dim3(grid), dim3(256), 0, st, a);
+}
+
+}  // namespace
+
+extern "C" int fairkv_append_rotated(const fairkv_cache *c, const fairkv_rotation *r, const void *q, int64_t q_stride, const void *k_new,
+                                     int64_t k_stride, const void *v_new, int64_t v_stride, void *q_out, int32_t q_len, int32_t Hq,
+                                     int32_t dtype, const int32_t *n_new, const int32_t *len, int32_t *len_out, int32_t *bad, void *hip_stream)
+{
+    if (const int rc = check_cache(c)) return rc;
+    if (!r || !q || !k_new || !v_new || !q_out || !len || !len_out || q_len < 1 || Hq < 1) return FAIRKV_EINVAL;
+    if (dtype != FAIRKV_BF16 && dtype != FAIRKV_F32) return FAIRKV_EUNSUPPORTED;
+    if ((dtype == FAIRKV_F32) != (c->dtype == FAIRKV_F32) || q_len > FAIRKV_MAX_DRAFT) return FAIRKV_EUNSUPPORTED;
+    const int64_t elem = dtype == FAIRKV_BF16 ? 2 : 4, tokens = static_cast<int64_t>(c->B) * q_len;
+    if (q_stride < static_cast<int64_t>(Hq) * c->D || k_stride < static_cast<int64_t>(c->Hkv) * c->D || v_stride < static_cast<int64_t>(c->Hkv) * c->D)
+        return FAIRKV_EINVAL;
+    if (q_stride * elem % 16 != 0 || k_stride * elem % 16 != 0 || v_stride * elem % 16 != 0) return FAIRKV_EINVAL;
+    if (!aligned(q, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(q_out, 16)) return FAIRKV_EINVAL;
+    if ((r->q_norm || r->k_norm) && !(r->eps >= 0.f && std::isfinite(r->eps))) return FAIRKV_EINVAL;
+    if (r->table && (!r->pos || r->n_pos < 1 || r->rot < 16 || r->rot % 16 != 0 || r->rot > c->D || !aligned(r->table, 16))) return FAIRKV_EINVAL;
+    if (tokens > INT32_MAX || q_out == k_new || q_out == v_new) return FAIRKV_EINVAL;
+    if (q_out == q && q_stride != static_cast<int64_t>(Hq) * c->D) return FAIRKV_EINVAL;
+
+    RotateArgs a{};
+    a.q = static_cast<const char *>(q), a.k_new = static_cast<const char *>(k_new), a.v_new = static_cast<const char *>(v_new);
+    a.q_out = static_cast<char *>(q_out), a.k = static_cast<char *>(c->k), a.v = static_cast<char *>(c->v);
+    a.q_norm = r->q_norm, a.k_norm = r->k_norm, a.table = r->table, a.pos = r->pos;
+    a.n_new = n_new, a.len = len, a.cap = c->cap, a.len_out = len_out, a.bad = bad;
+    a.rows = row_map(c);
+    a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride;
+    a.B = c->B, a.Hq = Hq, a.Hkv = c->Hkv, a.q_len = q_len, a.n_pos = r->n_pos, a.rot = r->table ? r->rot : 0, a.pairs = r->pairs;
+    a.eps = r->eps;
+    a.n_scales = c->n_scales;
+    for (int32_t h = 0; h < c->n_scales; ++h) a.k_scale[h] = 1.f / c->k_scale[h], a.v_scale[h] = 1.f / c->v_scale[h];
+    const int slots = 256 / (c->D / kRow8);
+    a.head_slots = 1;
+    while (a.head_slots * 2 <= std::min(Hq, slots)) a.head_slots *= 2;
+    const int64_t tokens_each = slots / a.head_slots, pairs_each = std::max(1, slots / q_len);
+    a.q_groups = static_cast<int32_t>((tokens + tokens_each - 1) / tokens_each);
+    const int64_t grid = a.q_groups + (static_cast<int64_t>(c->B) * c->Hkv + pairs_each - 1) / pairs_each;
+    if (grid > INT32_MAX) return FAIRKV_EINVAL;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (dtype == FAIRKV_F32)
+        launch_rotated<float, float>(c->D, static_cast<unsigned>(grid), st, a);
+    else if (c->dtype == FAIRKV_BF16)
+        launch_rotated<uint16_t, uint16_t>(c->D, static_cast<unsigned>(grid), st, a);
+    else
+        launch_rotated<uint16_t, uint8_t>(c->D, static_cast<unsigned>(grid), st, a);
+    return launched();
+}
+
+extern "C" int fairkv_accept(const fairkv_cache *c, const int32_t *path, const int32_t *n_path, const int32_t *n_new, const int32_t *len,
+                             int32_t *len_out, int32_t q_len, int32_t *bad, void *hip_stream)
+{
+    if (const int rc = check_cache(c)) return rc;
+    if (!path || !n_path || !len || !len_out || q_len < 1) return FAIRKV_EINVAL;
+    if (q_len > FAIRKV_MAX_DRAFT) return FAIRKV_EUNSUPPORTED;
+    const AcceptArgs a{static_cast<char *>(c->k), static_cast<char *>(c->v), path, n_path, n_new, len, len_out, bad, row_map(c), c->B, c->Hkv, q_len};
+    const int rb = c->D * (c->dtype == FAIRKV_E4M3 ? 1 : c->dtype == FAIRKV_BF16 ? 2 : 4), slots = 256 / (rb / 16), each = std::max(1, slots / q_len);
+    const dim3 grid(static_cast<unsigned>((c->B * c->Hkv + each - 1) / each));
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (rb == 64)
+        hipLaunchKernelGGL(fairkv_accept_kernel<64>, grid, dim3(256), 0, st, a);
+    else if (rb == 128)
+        hipLaunchKernelGGL(fairkv_accept_kernel<128>, grid, dim3(256), 0, st, a);
+    else if (rb == 256)
+        hipLaunchKernelGGL(fairkv_accept_kernel<256>, grid, dim3(256), 0, st, a);
+    else
+        hipLaunchKernelGGL(fairkv_accept_kernel<512>, grid, dim3(256), 0, st, a);
+    return launched();
+}
+
+// ---- attention of a draft tree --------------------------------------------------------------------
+namespace {
+
+// How the columns of a pair are dealt: `waves` waves side by side (32 columns each), `blocks` workgroups, and the slots of each of those.
+struct TreeShape {
+    int32_t waves, blocks, slots;
+};
+TreeShape tree_shape(int32_t cols, int32_t n_slots)
+{
+    TreeShape s{};
+    s.waves = cols <= 32 ? 1 : cols <= 64 ? 2 : cols <= 128 ? 4 : 8;
+    s.blocks = (cols + 32 * s.waves - 1) / (32 * s.waves);
+    s.slots = std::max(1, n_slots / s.blocks);
+    return s;
+}
+
+struct TreeSpace {
+    size_t cut, ml, o;
+};
+TreeSpace tree_space(const TreeShape &s, int32_t D)
+{
+    const size_t groups = static_cast<size_t>(s.blocks) * s.slots, cols = 32 * static_cast<size_t>(s.waves);
+    return {align256(groups * 2 * sizeof(int32_t)), align256(groups * 2 * cols * 2 * sizeof(float)), align256(groups * 2 * cols * D * sizeof(float))};
+}
+
+int check_tree(const fairkv_cache *c, int32_t Hq, int32_t q_len, int32_t n_slots)
+{
+    if (const int rc = check_cache(c)) return rc;
+    if (Hq < 1 || q_len < 1 || n_slots < 1 || Hq % c->Hkv != 0) return FAIRKV_EINVAL;
+    if (c->dtype == FAIRKV_F32 || q_len > FAIRKV_MAX_DRAFT || Hq / c->Hkv > 16 || n_slots > 65536) return FAIRKV_EUNSUPPORTED;
+    return FAIRKV_OK;
+}
+
+template <int D, bool KV8, int WC, int WT, int STAGES, bool FINE>
+void launch_tree_kernel(const TreeArgs &a, int32_t blocks, hipStream_t st)
+{
+    hipLaunchKernelGGL((fairkv_decode_tree_kernel<D, KV8, WC, WT, STAGES, FINE>), dim3(static_cast<unsigned>(a.n_slots), static_cast<unsigned>(blocks)),
+                       dim3(WC * WT * 64), 0, st, a);
+    constexpr int CB = WC * kTreeCols;
+    hipLaunchKernelGGL((fairkv_tree_merge_kernel<D, CB>), dim3(static_cast<unsigned>(a.n_slots), static_cast<unsigned>(blocks), std::min(8, CB * D / 1024)),
+                       dim3(256), 0, st, a);
+}
+
+template <int D, bool KV8>
+void launch_tree(int waves, bool fine, const TreeArgs &a, int32_t blocks, hipStream_t st)
+{
+    switch (waves) {
+    case 1: return launch_tree_kernel<D, KV8, 1, 4, 2, true>(a, blocks, st);
+    case 2: return launch_tree_kernel<D, KV8, 2, 4, 2, true>(a, blocks, st);
+    case 4: return fine ? launch_tree_kernel<D, KV8, 4, 2, 3, true>(a, blocks, st) : launch_tree_kernel<D, KV8, 4, 2, 3, false>(a, blocks, st);
+    default: return fine ? launch_tree_kernel<D, KV8, 8, 1, 4, true>(a, blocks, st) : launch_tree_kernel<D, KV8, 8, 1, 4, false>(a, blocks, st);
+    }
+}
+
+}  // namespace
+
+extern "C" size_t fairkv_tree_workspace_bytes(const fairkv_cache *c, int32_t Hq, int32_t q_len, int32_t n_slots)
+{
+    if (check_tree(c, Hq, q_len, n_slots) != FAIRKV_OK) return 0;
+    const TreeSpace s = tree_space(tree_shape(Hq / c->Hkv * q_len, n_slots), c->D);
+    return s.cut + s.ml + s.o;
+}
+
+extern "C" int fairkv_decode_attn_tree(const fairkv_cache *c, const void *q, const uint64_t *tree, const int32_t *n_new, const int32_t *len,
+                                       void *workspace, size_t workspace_bytes, int32_t n_slots, void *out, float *lse, int32_t q_len, int32_t Hq,
+                                       int32_t out_dtype, float scale, void *hip_stream)
+{
+    if (const int rc = check_tree(c, Hq, q_len, n_slots)) return rc;
+    if (!q || !len || !out || !std::isfinite(scale)) return FAIRKV_EINVAL;
+    if (out_dtype != FAIRKV_BF16 && out_dtype != FAIRKV_F32) return FAIRKV_EUNSUPPORTED;
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16) || (tree && !aligned(tree, 8))) return FAIRKV_EINVAL;
+    if (static_cast<int64_t>(c->B) * q_len * Hq * c->D > INT32_MAX) return FAIRKV_EINVAL;
+    const TreeShape shape = tree_shape(Hq / c->Hkv * q_len, n_slots);
+    const TreeSpace space = tree_space(shape, c->D);
+    if (!workspace || workspace_bytes < space.cut + space.ml + space.o) return FAIRKV_EWORKSPACE;
+
+    TreeArgs a{};
+    a.q = q, a.k = c->k, a.v = c->v;
+    a.rows = row_map(c);
+    a.len = len, a.n_new = n_new, a.tree = reinterpret_cast<const int64_t *>(tree);
+    a.out = out, a.lse = lse;
+    char *ws = static_cast<char *>(workspace);
+    a.cut = reinterpret_cast<int32_t *>(ws);
+    a.part_ml = reinterpret_cast<float *>(ws + space.cut);
+    a.part_o = reinterpret_cast<float *>(ws + space.cut + space.ml);
+    a.B = c->B, a.Hq = Hq, a.Hkv = c->Hkv, a.G = Hq / c->Hkv, a.q_len = q_len, a.cols = a.G * q_len;
+    a.n_slots = shape.slots;
+    // 2^31 - 2^16 tokens: what is added to a token's number inside a tile or a batch of pages does not wrap around
+    const int64_t rows = c->n_rows < 1 ? 0 : c->pages ? static_cast<int64_t>(c->max_pages) * c->page_rows : c->n_rows;
+    a.max_len = static_cast<int32_t>(std::min<int64_t>(rows, INT32_MAX - 65535));
+    a.out_dtype = out_dtype;
+    a.n_scales = c->n_scales;
+    a.scale_log2 = scale * kLog2e;
+    for (int h = 0; h < kCacheScales; ++h) {
+        a.k_scale[h] = h < c->n_scales ? c->k_scale[h] : 1.f;
+        a.v_scale[h] = h < c->n_scales ? c->v_scale[h] : 1.f;
+    }
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const bool fine = out_dtype == FAIRKV_F32;
+    if (c->dtype == FAIRKV_E4M3)
+        c->D == 128 ? launch_tree<128, true>(shape.waves, fine, a, shape.blocks, st) : launch_tree<64, true>(shape.waves, fine, a, shape.blocks, st);
+    else
+        c->D == 128 ? launch_tree<128, false>(shape.waves, fine, a, shape.blocks, st) : launch_tree<64, false>(shape.waves, fine, a, shape.blocks, st);
+    return launched();
+}
