@@ -456,13 +456,16 @@ int fairkv_append_rotated(const fairkv_cache *cache, const fairkv_rotation *r, c
  * nothing gets out = 0 and lse = -inf.  An infinite or NaN row counts for the nodes that see it only.  Nodes i >= n are left as they are.
  * q          device bf16 [B][q_len][Hq][D], 16-byte aligned; Hq a multiple of Hkv, any Hq / Hkv up to 16
  * tree       device uint64 [B][q_len], or NULL
- * workspace  device, fairkv_tree_workspace_bytes(cache, Hq, q_len, n_slots) bytes, 16-byte aligned.  It need not be cleared; nothing in it is
- *            kept from call to call.  Calls that share one must be ordered on one stream.
+ * workspace  device, fairkv_tree_workspace_bytes(cache, Hq, q_len, n_slots) bytes, 16-byte aligned.  Its first fairkv_tree_counter_bytes(n_slots)
+ *            bytes must be zero before the first use (fairkv_tree_workspace_reset); every completed call leaves them zero, and nothing else
+ *            in it is kept from call to call, so calls of any shapes with one n_slots that are ordered on one stream may share it.
  * n_slots    workgroups to balance over: the GPU's compute units
  * out        device [B][q_len][Hq][D] of out_dtype (FAIRKV_F32 or FAIRKV_BF16); lse device float [B][q_len][Hq] or NULL
  * Lengths below 0 count as 0, those beyond the cache's rows (paged: max_pages * page_rows) as that many.
- * Enqueues two kernels; no synchronisation.  FAIRKV_EUNSUPPORTED: q_len > FAIRKV_MAX_DRAFT, an F32 cache, D, Hq / Hkv > 16. */
+ * Enqueues one kernel; no synchronisation.  FAIRKV_EUNSUPPORTED: q_len > FAIRKV_MAX_DRAFT, an F32 cache, D, Hq / Hkv > 16. */
+size_t fairkv_tree_counter_bytes(int32_t n_slots);
 size_t fairkv_tree_workspace_bytes(const fairkv_cache *cache, int32_t Hq, int32_t q_len, int32_t n_slots);
+int fairkv_tree_workspace_reset(void *workspace, size_t workspace_bytes, int32_t n_slots, void *hip_stream);
 int fairkv_decode_attn_tree(const fairkv_cache *cache, const void *q, const uint64_t *tree, const int32_t *n_new, const int32_t *len,
                             void *workspace, size_t workspace_bytes, int32_t n_slots, void *out, float *lse, int32_t q_len, int32_t Hq,
                             int32_t out_dtype, float scale, void *hip_stream);

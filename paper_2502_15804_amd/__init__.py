@@ -33,7 +33,7 @@ EXPORTS = ("fairkv_default_params", "fairkv_plan", "fairkv_workspace_bytes", "fa
            "fairkv_decode_attn_multi", "fairkv_decode_attn_kv8", "fairkv_decode_attn_kv8_per_head",
            "fairkv_decode_attn_static", "fairkv_decode_attn_trace",
            "fairkv_place", "fairkv_pack", "fairkv_append", "fairkv_plan_grow", "fairkv_stream_probe", "fairkv_stream_probe_shape", "fairkv_workspace_reset",
-           "fairkv_append_rotated", "fairkv_decode_attn_tree", "fairkv_tree_workspace_bytes", "fairkv_accept",
+           "fairkv_append_rotated", "fairkv_decode_attn_tree", "fairkv_tree_workspace_bytes", "fairkv_tree_counter_bytes", "fairkv_tree_workspace_reset", "fairkv_accept",
            "fairkv_strerror", "fairkv_version")
 
 
@@ -160,6 +160,10 @@ def lib() -> ctypes.CDLL:
                                             vp, i32, i32, i32, vp, vp, vp, vp, vp]
         L.fairkv_tree_workspace_bytes.restype = ctypes.c_size_t
         L.fairkv_tree_workspace_bytes.argtypes = [cache_p, i32, i32, i32]
+        L.fairkv_tree_counter_bytes.restype = ctypes.c_size_t
+        L.fairkv_tree_counter_bytes.argtypes = [i32]
+        L.fairkv_tree_workspace_reset.restype = ctypes.c_int
+        L.fairkv_tree_workspace_reset.argtypes = [vp, ctypes.c_size_t, i32, vp]
         L.fairkv_decode_attn_tree.restype = ctypes.c_int
         L.fairkv_decode_attn_tree.argtypes = [cache_p, vp, vp, vp, vp, vp, ctypes.c_size_t, i32, vp, vp, i32, i32, i32, ctypes.c_float, vp]
         L.fairkv_accept.restype = ctypes.c_int
@@ -469,11 +473,24 @@ def fairkv_tree_workspace_bytes(cache, Hq: int, q_len: int, n_slots=None) -> int
     return int(lib().fairkv_tree_workspace_bytes(ctypes.byref(cache.struct), int(Hq), int(q_len), cache.n_slots if n_slots is None else int(n_slots)))
 
 
+def fairkv_tree_counter_bytes(n_slots: int) -> int:
+    return int(lib().fairkv_tree_counter_bytes(int(n_slots)))
+
+
+def fairkv_tree_workspace_reset(workspace, n_slots, stream=None):
+    """Enqueue the kernel that zeroes the counter bytes of a device workspace (see the header)."""
+    _check_dev(workspace=workspace)
+    rc = lib().fairkv_tree_workspace_reset(_ptr(workspace), workspace.numel() * workspace.element_size(), int(n_slots), _stream(stream, workspace))
+    if rc != FAIRKV_OK:
+        raise FairKVError(rc, "fairkv_tree_workspace_reset")
+
+
 def fairkv_decode_attn_tree(cache, lens, q, workspace, out, lse, scale, tree=None, n_new=None, n_slots=None, stream=None):
     """Enqueue the attention of a draft tree over the cache and the draft's own rows, the last of every pair (see the header).
 
     q bfloat16 [B, q_len, Hq, D] (or [B, Hq, D]); tree int64 or uint64 [B, q_len]: bit j of node i's word says that it sees node j (None: a chain);
-    n_new int32 [B] or None; lens int32 [B, Hkv]; workspace of fairkv_tree_workspace_bytes; out bfloat16 or float32 of q's shape; lse
+    n_new int32 [B] or None; lens int32 [B, Hkv]; workspace uint8 of fairkv_tree_workspace_bytes, zero-filled
+    before its first use; out bfloat16 or float32 of q's shape; lse
     float32 [B, q_len, Hq] or None.  Nothing is allocated or synchronised here."""
     rc = (_native_module or _native()).decode_tree((_pt or _torch())[1], cache.address, cache.device, lens, q, workspace, out, lse, scale, tree, n_new,
                                                    cache.n_slots if n_slots is None else n_slots, stream)

@@ -22,6 +22,8 @@
 #include "cache_rows.h"
 #include "decode_mfma.h"
 
+#include <type_traits>
+
 namespace fairkv {
 
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
@@ -29,7 +31,10 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 
 constexpr int kTreeTok = 32;          // tokens of a tile
 constexpr int kTreeCols = 32;         // columns of a wave
-constexpr int kTreeOverhead = 3;      // what a pair costs a workgroup beside its tiles, in tiles
+constexpr int kJoin = 8;              // pieces of a pair that are added up at once
+constexpr int kLevels = 6;            // of such sums, for pairs in up to 8^6 pieces
+constexpr int kTreeSlots = 65536;     // most workgroups of a block of columns
+static_assert(kTreeSlots <= 1 << 3 * kLevels && kJoin == 8, "levels");
 
 struct TreeArgs {
     const void *q, *k, *v;
@@ -39,9 +44,9 @@ struct TreeArgs {
     const int64_t *tree;              // [B][q_len] or null: node i sees nodes 0 .. i
     void *out;
     float *lse;
-    float *part_o;                    // [slots][D / 4][columns of a workgroup][4]
-    float *part_ml;                   // [slots][columns of a workgroup][2]
-    int32_t *cut;                     // [column blocks][n_slots][2]: the pair whose first piece a workgroup had, and its pieces (0: none was cut)
+    float *part_o;                    // [column blocks][n_slots][2][D / 4][columns of a workgroup][4]
+    float *part_ml;                   // [column blocks][n_slots][2][columns of a workgroup][2]
+    int32_t *arrivals;                // [column blocks][kLevels][n_slots][2], 0 between calls
     int32_t B, Hq, Hkv, G, q_len, cols, n_slots, max_len, out_dtype, n_scales;
     float scale_log2;
     float k_scale[kCacheScales], v_scale[kCacheScales];
@@ -105,9 +110,37 @@ __device__ __forceinline__ int32_t tree_new(const TreeArgs &a, int b)
 __device__ __forceinline__ int32_t tree_len(const TreeArgs &a, int pair) { return min(max(a.len[pair], 0), a.max_len); }
 __device__ __forceinline__ int32_t tiles_of(int32_t len) { return (len + kTreeTok - 1) / kTreeTok; }
 
-// FINE: a weight enters the second product as two bf16 numbers (its rounding and what that leaves), in twice the instructions: an output in
-// fp32 keeps fp32's accuracy.  Without, its error is that of weights rounded to 8 bits, about as large as a bf16 output's own rounding.
-template <int D, bool KV8, int WC, int WT, int STAGES, bool FINE>
+// x plus those of the lanes below, by steps of the wave's own data paths.
+__device__ __forceinline__ int64_t wave_upto(int64_t x)
+{
+    auto step = [&](auto ctrl, auto rows, auto banks) __attribute__((always_inline)) {
+        const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(x), ctrl(), rows(), banks(), false);
+        const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(x >> 32), ctrl(), rows(), banks(), false);
+        x += static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
+    };
+#define FAIRKV_N(n) std::integral_constant<int, n>{}
+    step(FAIRKV_N(0x111), FAIRKV_N(0xf), FAIRKV_N(0xf));      // from 1, 2, 4, 8 lanes below in the row of 16
+    step(FAIRKV_N(0x112), FAIRKV_N(0xf), FAIRKV_N(0xf));
+    step(FAIRKV_N(0x114), FAIRKV_N(0xf), FAIRKV_N(0xf));
+    step(FAIRKV_N(0x118), FAIRKV_N(0xf), FAIRKV_N(0xf));
+    step(FAIRKV_N(0x142), FAIRKV_N(0xa), FAIRKV_N(0xf));      // from the end of the row below, of both rows below
+    step(FAIRKV_N(0x143), FAIRKV_N(0xc), FAIRKV_N(0xf));
+#undef FAIRKV_N
+    return x;
+}
+
+// A run of tiles of one pair.
+struct TreePiece {
+    int pair, b, h;
+    int32_t len, nn, tiles, tile0, tile1;
+    int64_t off;                      // first row of a packed pair, -1 if its run does not fit the cache
+    int64_t first;                    // place of the pair's first tile in the line
+};
+
+// PARTS: a weight enters the second product as so many bf16 numbers, each the rounding of what those before leave, in as many times the
+// instructions.  Three keep an fp32 output's accuracy; one is off by 2^-8 of a weight, which adds 0.4 times to the error that a bf16 output's own
+// rounding makes.
+template <int D, bool KV8, int WC, int WT, int STAGES, int PARTS>
 __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(TreeArgs a)
 {
     constexpr int NW = WC * WT, NT = NW * 64, CB = WC * kTreeCols;
@@ -119,34 +152,51 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
     constexpr int NSL = D / 16, NDB = D / 32;
     constexpr int kAhead = WC == 1 ? STAGES : STAGES - 1;       // tiles on their way while one is waited for
     constexpr int RING = WT * STAGES * STAGEB;
-    constexpr int FOLDROW = D + 4;
-    constexpr int FOLD = (WT - 1) * CB * (FOLDROW + 2) * 4;
+    constexpr int kBlock = kTreeCols * 32 * 4;        // bytes of 32 coordinates of a wave's columns
+    constexpr int kOverhead = WC == 1 ? 3 : 5;        // what a pair costs a workgroup beside its tiles, in tiles
+    constexpr int kRound = WT == 1 ? 0 : WC == 1 ? (NDB < 2 ? NDB : 2) : 1;      // such blocks of a group that are folded at once
+    constexpr int FOLD = (WT - 1) * WC * kRound * kBlock;
     static_assert(LOADS * kAhead < 64, "vmcnt is a 6-bit counter");
+    static_assert(WT == 1 || NDB % kRound == 0, "rounds");
 
-    __shared__ __attribute__((aligned(1024))) char lds[RING > FOLD ? RING : FOLD];
-    __shared__ int64_t scan[NW + 3];                  // totals of the waves; the pair the workgroup starts in and where it begins
+    constexpr int kTable = NT * 16;                   // what a pair's piece needs to know, of up to NT pairs; before the first fold
+    __shared__ __attribute__((aligned(1024))) char lds[RING + (FOLD > kTable ? FOLD : kTable)];
+    __shared__ float2 st_ml[WT][CB];
+    __shared__ int64_t scan[NW + 2];                  // totals of the waves; the pair the workgroup starts with and where it ends
+    __shared__ int32_t counted;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wc = wave % WC, wt = wave / WC;
     const int l32 = lane & 31, hi = lane >> 5;
     const int n_pairs = a.B * a.Hkv, c0 = blockIdx.y * CB;
     const int my_slot = blockIdx.x;
-    int32_t *cut = a.cut + (static_cast<size_t>(blockIdx.y) * a.n_slots + my_slot) * 2;
-    if (threadIdx.x == 0) cut[1] = 0;
 
-    // ---- this workgroup's share of the line ----
-    int64_t begin, end, share, at;
+    // ---- this workgroup's share of the line, which it walks from its end to its beginning: the piece at its end, whose pair goes on in the
+    //      next workgroup, is done first, so that it is there when that one, having done the pair's other piece last, adds the two up ----
+    int4 *const table = reinterpret_cast<int4 *>(lds + RING);
+    const bool in_table = n_pairs <= NT;
+    auto pair_entry = [&](int p) __attribute__((always_inline)) {      // length, new tokens, first row (-1: a run that does not fit the cache)
+        const int32_t len = tree_len(a, p);
+        int64_t off = a.rows.pages ? 0 : a.rows.off[p];
+        if (off < 0 || (!a.rows.pages && static_cast<uint64_t>(off) + static_cast<uint32_t>(len) > static_cast<uint64_t>(a.rows.n_rows))) off = -1;
+        return int4{len, tree_new(a, p / a.Hkv), static_cast<int32_t>(off), static_cast<int32_t>(off >> 32)};
+    };
+    int64_t begin, end, share, at;                    // at: where the pair ends
     int pair;
+    bool small;                                       // places of the line fit 31 bits
     {
         const int run = (n_pairs + NT - 1) / NT, p0 = min(static_cast<int>(threadIdx.x) * run, n_pairs), p1 = min(p0 + run, n_pairs);
         int64_t mine = 0;
-        for (int p = p0; p < p1; ++p) mine += kTreeOverhead + tiles_of(tree_len(a, p));
-        int64_t upto = mine;
-#pragma unroll
-        for (int o = 1; o < 64; o *= 2) {
-            const int64_t x = __shfl_up(upto, o, 64);
-            if (lane >= o) upto += x;
+        if (in_table) {
+            if (p0 < p1) {
+                const int4 e = pair_entry(p0);
+                table[p0] = e;
+                mine = kOverhead + tiles_of(e.x);
+            }
+        } else {
+            for (int p = p0; p < p1; ++p) mine += kOverhead + tiles_of(tree_len(a, p));
         }
+        const int64_t upto = wave_upto(mine);
         if (lane == 63) scan[wave] = upto;
         if (threadIdx.x == 0) scan[NW] = -1;
         __syncthreads();
@@ -156,24 +206,28 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
             if (w < wave) before += scan[w];
             total += scan[w];
         }
-        share = (total + a.n_slots - 1) / a.n_slots;
+        total = uniform64(total);
+        small = total < (1ll << 30);
+        share = small ? static_cast<uint32_t>(static_cast<uint32_t>(total) + a.n_slots - 1) / static_cast<uint32_t>(a.n_slots) : (total + a.n_slots - 1) / a.n_slots;
+        share = uniform64(share);
         begin = share * my_slot;
         end = begin + share;
         before += upto - mine;
-        if (before <= begin && begin < before + mine) {
+        const int64_t target = min(end, total) - 1;
+        if (begin < total && before <= target && target < before + mine) {
             int p = p0;
-            for (; p < p1; ++p) {
-                const int cost = kTreeOverhead + tiles_of(tree_len(a, p));
-                if (begin < before + cost) break;
-                before += cost;
-            }
+            if (!in_table)
+                for (; p < p1; ++p) {
+                    const int cost = kOverhead + tiles_of(tree_len(a, p));
+                    if (target < before + cost) break;
+                    before += cost;
+                }
             scan[NW] = p;
-            scan[NW + 1] = before;
+            scan[NW + 1] = before + (in_table ? mine : kOverhead + tiles_of(tree_len(a, p)));
         }
         __syncthreads();
         pair = __builtin_amdgcn_readfirstlane(static_cast<int>(scan[NW]));
         at = uniform64(scan[NW + 1]);
-        begin = uniform64(begin), end = uniform64(end), share = uniform64(share);
     }
     if (pair < 0) return;                             // nothing is left of the line
 
@@ -182,53 +236,169 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
     const Column column(a, min(col, a.cols - 1));
     const uint32_t ring = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(FAIRKV_LDS_PTR(lds))) + wt * (STAGES * STAGEB);
     const int ld_row = lane / PPR, ld_col = lane % PPR;
-    uint32_t k_rd[NSL], v_rd[NDB][2];                 // where the lane reads in stage 0: its row of K; of V for the first 16 tokens
-#pragma unroll
-    for (int s = 0; s < NSL; ++s)
-        k_rd[s] = ring + l32 * ROWB + (KV8 ? (s ^ k_swizzle<ROWB>(l32)) * 16 + hi * 8 : ((2 * s + hi) ^ k_swizzle<ROWB>(l32)) * 16);
+    // Where the lane reads in stage 0: its row of K, and its share of the transposing reads of V.  Pieces further on in a row are a bit pattern
+    // away, since swizzles are patterns too, rows further on whole rows: swizzles repeat every 8 (8-bit: 16) rows.
+    const uint32_t k_rd = (ring + l32 * ROWB + k_swizzle<ROWB>(l32) * 16 + (KV8 ? hi * 8 : 0)) ^ (KV8 ? 0 : hi * 16);
     const int x16 = lane & 15, dq = lane >> 4 & 1;
-#pragma unroll
-    for (int nb = 0; nb < NDB; ++nb) {
-        if constexpr (KV8) {
-            const int e = x16 >> 1, r = (e < 4 ? e : e + 4) + 4 * hi;
-            v_rd[nb][0] = ring + TILEB + r * ROWB + ((2 * nb + dq) ^ v_swizzle<ROWB, true>(r)) * 16 + (x16 & 1) * 8;
-            v_rd[nb][1] = 0;
-        } else {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int r = 8 * u + 4 * hi + (x16 >> 2);
-                v_rd[nb][u] = ring + TILEB + r * ROWB + ((4 * nb + 2 * dq + ((x16 & 3) >> 1)) ^ v_swizzle<ROWB, false>(r)) * 16 + (x16 & 1) * 8;
-            }
-        }
-    }
+    const int v_row = KV8 ? (x16 < 8 ? x16 >> 1 : (x16 >> 1) + 4) + 4 * hi : 4 * hi + (x16 >> 2);
+    const uint32_t v_rd = ring + TILEB + v_row * ROWB + ((KV8 ? dq : 2 * dq + ((x16 & 3) >> 1)) ^ v_swizzle<ROWB, KV8>(v_row)) * 16 + (x16 & 1) * 8;
     const char *const k_base = static_cast<const char *>(a.k), *const v_base = static_cast<const char *>(a.v);
 
-    for (; pair < n_pairs && at < end; ++pair) {
-        const int b = pair / a.Hkv, h = pair - b * a.Hkv;
-        const int32_t len = __builtin_amdgcn_readfirstlane(tree_len(a, pair)), tiles = tiles_of(len), nn = __builtin_amdgcn_readfirstlane(tree_new(a, b));
-        const int64_t first = at + kTreeOverhead;     // place of the pair's first tile
-        at = first + tiles;
-        const int32_t tile0 = static_cast<int32_t>(max(begin - first, static_cast<int64_t>(0)));
-        const int32_t tile1 = static_cast<int32_t>(min(end - first, static_cast<int64_t>(tiles)));
-        const bool empty = tiles == 0 && begin < first && first <= end;      // a pair without rows belongs to one workgroup too
-        if ((tile1 <= tile0 && !empty) || c0 >= nn * a.G) continue;
-        const bool whole = tile0 == 0 && tile1 == tiles;
-        const int32_t base = len - nn;                // rows in front of the draft
-        const bool active = col < nn * a.G;
+    // ---- the pieces of the share: what 64 pairs' pieces need to know is held in lanes ----
+    int held = pair;                                  // the pair of lane 0; lane i has the i-th before it
+    int4 entry;
+    entry = in_table ? table[max(pair - lane, 0)] : pair_entry(max(pair - lane, 0));
+    auto next_piece = [&](TreePiece &pc) __attribute__((always_inline)) {      // false: the share has no more
+        while (pair >= 0) {
+            if (held - pair >= 64) {
+                held = pair;
+                entry = pair_entry(max(pair - lane, 0));
+            }
+            const int i = held - pair;
+            pc.pair = pair;
+            pc.b = pair / a.Hkv, pc.h = pair - pc.b * a.Hkv;
+            pc.len = __builtin_amdgcn_readlane(entry.x, i), pc.nn = __builtin_amdgcn_readlane(entry.y, i);
+            pc.off = static_cast<int64_t>((static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(entry.w, i))) << 32) |
+                                          static_cast<uint32_t>(__builtin_amdgcn_readlane(entry.z, i)));
+            pc.tiles = tiles_of(pc.len);
+            pc.first = at - pc.tiles;
+            at = pc.first - kOverhead;
+            pair = at <= begin ? -1 : pair - 1;
+            pc.tile0 = static_cast<int32_t>(max(begin - pc.first, static_cast<int64_t>(0)));
+            pc.tile1 = static_cast<int32_t>(min(end - pc.first, static_cast<int64_t>(pc.tiles)));
+            const bool empty = pc.tiles == 0 && begin < pc.first && pc.first <= end;      // a pair without rows belongs to one workgroup too
+            if ((pc.tile1 > pc.tile0 || empty) && c0 < pc.nn * a.G) return true;
+        }
+        return false;
+    };
 
-        // ---- queries, and what the column sees of the draft ----
-        const uint32_t q_row = column.row(a, b, h);
-        bf16x8_t qb[NSL];
+    // The group's tiles of a piece: tile0 + wt, + WT, ...  Lane i holds the first cache rows of tile i's two halves of 16 tokens, for 64 tiles at
+    // a time: -1 where the cache has none.  A half lies in one page.
+    struct Rows {
+        uint32_t lo[2], hi[2];
+        __device__ __forceinline__ int64_t get(int half, int i) const
+        {
+            return static_cast<int64_t>((static_cast<uint64_t>(__builtin_amdgcn_readlane(hi[half], i)) << 32) | static_cast<uint32_t>(__builtin_amdgcn_readlane(lo[half], i)));
+        }
+    };
+    auto fetch_pages = [&](const TreePiece &pc, int step) __attribute__((always_inline)) {      // page numbers of steps step .. step + 63, not waited for
+        int2 ids = {0, 0};
+        if (a.rows.pages && pc.len > 0) {
+            const int t = min((pc.tile0 + wt + (step + lane) * WT) * kTreeTok, pc.len - 1);
+            const int32_t *of_pair = a.rows.pages + static_cast<int64_t>(pc.pair) * a.rows.max_pages;
+            ids = {of_pair[t >> a.rows.page_shift], of_pair[min(t + 16, pc.len - 1) >> a.rows.page_shift]};
+        }
+        return ids;
+    };
+    auto rows_of = [&](const TreePiece &pc, int step, int2 ids) __attribute__((always_inline)) {
+        Rows x;
+        const int t = min((pc.tile0 + wt + (step + lane) * WT) * kTreeTok, max(pc.len - 1, 0) & ~15);
 #pragma unroll
-        for (int s = 0; s < NSL; ++s)
-            qb[s] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t *>(static_cast<const char *>(a.q) + (static_cast<size_t>(q_row) * D + 16 * s + 8 * hi) * 2));
-        uint64_t sees = a.tree ? static_cast<uint64_t>(a.tree[b * a.q_len + column.node]) : ~0ull >> (63 - column.node);
-        sees &= nn >= 64 ? ~0ull : (1ull << nn) - 1;
-        const int sc = a.n_scales > 1 ? h : 0;
-        const float s_mul = KV8 ? a.scale_log2 * a.k_scale[sc] : a.scale_log2;
-        const int64_t off = a.rows.pages ? 0 : uniform64(a.rows.off[pair]);
-        const bool run_ok = a.rows.pages || (off >= 0 && static_cast<uint64_t>(off) + static_cast<uint32_t>(len) <= static_cast<uint64_t>(a.rows.n_rows));
+        for (int half = 0; half < 2; ++half) {
+            const int th = half ? min(t + 16, max(pc.len - 1, 0) & ~15) : t;
+            const int64_t row = a.rows.pages ? a.rows.row_of_page(half ? ids.y : ids.x, th) : pc.off < 0 ? -1 : pc.off + th;
+            x.lo[half] = static_cast<uint32_t>(row), x.hi[half] = static_cast<uint32_t>(row >> 32);
+            asm volatile("" : "+v"(x.lo[half]), "+v"(x.hi[half]));      // page numbers are waited for here and not where the lanes are read
+        }
+        return x;
+    };
+    // This wave's share of a stage: with more than one wave side by side all of it K or all of it V.  Rows past the end of the pair are its last
+    // row again, rows that the cache does not have the cache's first one: their weights are 0.  `missing` says of every stage which of its two
+    // halves the cache does not have.
+    static_assert(WC == 1 || LPT % LOADS == 0, "a wave loads K or V");
+    const int load0 = wc * LOADS;                     // the wave's first load of a stage
+    auto is_v = [&](int x) __attribute__((always_inline)) { return WC == 1 ? x >= LPT : load0 >= LPT; };
+    auto nth = [&](int x) __attribute__((always_inline)) { return WC == 1 ? x % LPT : load0 % LPT + x; };      // load of the tile of K or V
+    auto swizzled = [&](int x) __attribute__((always_inline)) {      // byte of its row that the lane fetches in load x
+        const int r = nth(x) * RPI + ld_row;
+        return static_cast<uint32_t>((ld_col ^ (is_v(x) ? v_swizzle<ROWB, KV8>(r) : k_swizzle<ROWB>(r))) * 16);
+    };
+    // The lane's offset in a load of whole rows, from the first row of the load: swizzles repeat every kTurns loads.
+    constexpr int kTurns = ROWB / 64 < LOADS ? ROWB / 64 : LOADS, kKinds = WC == 1 ? 2 : 1;
+    uint32_t full_offset[kKinds][kTurns];
+#pragma unroll
+    for (int kind = 0; kind < kKinds; ++kind)
+#pragma unroll
+        for (int x = 0; x < kTurns; ++x) {
+            full_offset[kind][x] = ld_row * ROWB + swizzled(kind * LPT + x);
+            asm volatile("" : "+v"(full_offset[kind][x]));
+        }
+    uint32_t missing = 0;
+    auto fetch = [&](const TreePiece &pc, const Rows &rows, int step, int at_stage) __attribute__((always_inline)) {
+        const int last = pc.len - 1 - (pc.tile0 + wt + step * WT) * kTreeTok;
+        const uint32_t stage = ring + at_stage * STAGEB;
+        const int64_t row0 = rows.get(0, step & 63), row1 = rows.get(1, step & 63);
+        const bool full = last >= kTreeTok - 1 && (row0 | row1) >= 0;
+        missing &= ~(3u << 2 * at_stage);
+        if (full) {
+#pragma unroll
+            for (int x = 0; x < LOADS; ++x) {
+                if (2 * LPT < WC && load0 >= 2 * LPT) break;
+                load16_to_lds((is_v(x) ? v_base : k_base) + ((nth(x) * RPI >= 16 ? row1 : row0) + nth(x) * RPI % 16) * ROWB,
+                              full_offset[WC == 1 && x >= LPT ? 1 : 0][x % kTurns], stage + (is_v(x) ? TILEB : 0) + nth(x) * 1024);
+            }
+        } else {
+            missing |= ((row0 < 0 ? 1u : 0u) | (row1 < 0 ? 2u : 0u)) << 2 * at_stage;
+#pragma unroll
+            for (int x = 0; x < LOADS; ++x) {
+                if (2 * LPT < WC && load0 >= 2 * LPT) break;
+                const bool upper = nth(x) * RPI >= 16;
+                const int64_t row = upper ? row1 : row0;
+                const int behind = row < 0 ? 0 : min(nth(x) * RPI + ld_row, last) - (upper && last >= 16 ? 16 : 0);
+                load16_to_lds((is_v(x) ? v_base : k_base) + max(row, static_cast<int64_t>(0)) * ROWB, behind * ROWB + swizzled(x),
+                              stage + (is_v(x) ? TILEB : 0) + nth(x) * 1024);
+            }
+        }
+    };
+    auto mine_of = [&](const TreePiece &pc) __attribute__((always_inline)) { return max(0, (pc.tile1 - pc.tile0 - wt + WT - 1) / WT); };
+    auto begin_ring = [&](const TreePiece &pc, const Rows &rows) __attribute__((always_inline)) {
+        const int n = mine_of(pc);
+#pragma clang loop unroll(disable)                    // 20 KB of instructions less, which come from memory once per launch
+        for (int s = 0; s < min(n, kAhead); ++s) fetch(pc, rows, s, s);
+    };
+    auto wait_stage = [&](int later) __attribute__((always_inline)) {      // all but the loads of `later` stages have landed
+        if (later <= 0)
+            wait_vmcnt<0>();
+        else if (later == 1)
+            wait_vmcnt<LOADS>();
+        else if (later == 2)
+            wait_vmcnt<2 * LOADS>();
+        else
+            wait_vmcnt<3 * LOADS>();
+    };
+    static_assert(kAhead <= 4, "stages waited for");
+    // The lane's column of the queries, and what it sees of the draft.
+    struct Queries {
+        bf16x8_t q[NSL];
+        uint64_t sees;
+    };
+    auto fetch_queries = [&](const TreePiece &pc) __attribute__((always_inline)) {
+        Queries x;
+        const char *row = static_cast<const char *>(a.q) + static_cast<size_t>(column.row(a, pc.b, pc.h)) * (2 * D);
+#pragma unroll
+        for (int s = 0; s < NSL; ++s) x.q[s] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t *>(row + 32 * s + 16 * hi));
+        x.sees = a.tree ? static_cast<uint64_t>(a.tree[pc.b * a.q_len + column.node]) : ~0ull >> (63 - column.node);
+        return x;
+    };
 
+    TreePiece pc;
+    if (!next_piece(pc)) return;
+    Rows rows = rows_of(pc, 0, fetch_pages(pc, 0));
+    begin_ring(pc, rows);
+    Queries qs = fetch_queries(pc);
+
+    for (;;) {
+        TreePiece ahead;
+        const bool more = next_piece(ahead);
+        int2 pages_ahead = {0, 0};
+        if (more) pages_ahead = fetch_pages(ahead, 0);
+
+        const int32_t base = pc.len - pc.nn;          // rows in front of the draft
+        const uint64_t sees = qs.sees & (pc.nn >= 64 ? ~0ull : (1ull << pc.nn) - 1);
+        const int sc = a.n_scales > 1 ? pc.h : 0;
+        // Scores to log2 units by a factor above 0 (a mask's -inf stays one; a factor of 0 is one under which every score is): the sign goes into q.
+        const float s_mul = KV8 ? a.scale_log2 * a.k_scale[sc] : a.scale_log2, s_abs = fmaxf(fabsf(s_mul), 1e-37f);
+        const int n_mine = mine_of(pc), n_steps = (pc.tile1 - pc.tile0 + WT - 1) / WT;
         f32x16_t o[NDB];
         float m_run = -INFINITY, l_run = 0.f;
 #pragma unroll
@@ -236,115 +406,80 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[nb][i] = 0.f;
 
-        // The group's tiles: tile0 + wt, + WT, ...  Pages of 64 of them are held in lanes, those of the first and of the second 16 tokens.
-        const int n_steps = (tile1 - tile0 + WT - 1) / WT;
-        const int n_mine = max(0, (tile1 - tile0 - wt + WT - 1) / WT);
-        int32_t page_lo = 0, page_hi = 0;
-        auto fetch_pages = [&](int step) __attribute__((always_inline)) {      // of steps step .. step + 63
-            const int t = min((tile0 + wt + (step + lane) * WT) * kTreeTok, len - 1);
-            const int32_t *ids = a.rows.pages + static_cast<int64_t>(pair) * a.rows.max_pages;
-            page_lo = ids[t >> a.rows.page_shift];
-            page_hi = ids[min(t + 16, len - 1) >> a.rows.page_shift];
-            drain_vmem();
+        auto more_rows = [&](int step) __attribute__((always_inline)) {
+            rows = rows_of(pc, step, fetch_pages(pc, step));
+            __builtin_amdgcn_s_waitcnt(0x0F70);       // said to the compiler, which would wait in every turn of the loop
         };
-        // First row of 16 tokens from token t on, -1 if the cache has none there.
-        auto row_of = [&](int step, int half, int32_t t) __attribute__((always_inline)) -> int64_t {
-            if (!a.rows.pages) return run_ok ? off + t : -1;
-            return a.rows.row_of_page(__builtin_amdgcn_readlane(half ? page_hi : page_lo, step & 63), t);
-        };
-        // This wave's share of a stage.  Rows past the end of the pair are its last row again, rows that the cache does not have the cache's first
-        // one: their weights are 0.  `missing` says of every stage which of its two halves the cache does not have.
-        uint32_t missing = 0;
-        auto fetch = [&](int step) __attribute__((always_inline)) {
-            const int32_t t0 = (tile0 + wt + step * WT) * kTreeTok;
-            const int last = len - 1 - t0, at_stage = step % STAGES;
-            const uint32_t stage = ring + at_stage * STAGEB;
-            const int64_t row0 = row_of(step, 0, t0), row1 = last >= 16 ? row_of(step, 1, t0 + 16) : row0;
-            missing = (missing & ~(3u << 2 * at_stage)) | ((row0 < 0 ? 1u : 0u) | (row1 < 0 ? 2u : 0u)) << 2 * at_stage;
+        // The queries are here before the loop: waited for inside it, every turn would wait for all tiles.
 #pragma unroll
-            for (int x = 0; x < LOADS; ++x) {
-                const int load = wc * LOADS + x;
-                if (2 * LPT < WC && load >= 2 * LPT) break;
-                const bool is_v = load >= LPT;
-                const int i = is_v ? load - LPT : load;
-                const bool upper = i * RPI >= 16;
-                const int64_t row = upper ? row1 : row0;
-                const int r = i * RPI + ld_row, behind = row < 0 ? 0 : min(r, last) - (upper && last >= 16 ? 16 : 0);      // rows behind `row`
-                const int swizzled = ld_col ^ (is_v ? v_swizzle<ROWB, KV8>(r) : k_swizzle<ROWB>(r));
-                load16_to_lds((is_v ? v_base : k_base) + max(row, static_cast<int64_t>(0)) * ROWB, behind * ROWB + swizzled * 16,
-                              stage + (is_v ? TILEB : 0) + i * 1024);
-            }
-        };
-        auto wait_stage = [&](int later) __attribute__((always_inline)) {      // all but the loads of `later` stages have landed
-            if (later <= 0)
-                wait_vmcnt<0>();
-            else if (later == 1)
-                wait_vmcnt<LOADS>();
-            else if (later == 2)
-                wait_vmcnt<2 * LOADS>();
-            else
-                wait_vmcnt<3 * LOADS>();
-        };
-        static_assert(kAhead <= 4, "stages waited for");
-
-        __builtin_amdgcn_s_waitcnt(0x0F70);           // the queries are here: the ring's loads are counted from now on
-        if (a.rows.pages && n_mine > 0) fetch_pages(0);
+        for (int s = 0; s < NSL; ++s) asm volatile("" : "+v"(qs.q[s]));
+        if (s_mul < 0.f) {
 #pragma unroll
-        for (int s = 0; s < kAhead; ++s)
-            if (s < n_mine) fetch(s);
+            for (int s = 0; s < NSL; ++s) qs.q[s] = __builtin_bit_cast(bf16x8_t, __builtin_bit_cast(u32x4_t, qs.q[s]) ^ 0x80008000u);
+        }
 
-        for (int step = 0; step < (WC == 1 ? n_mine : n_steps); ++step) {
+        int c_stage = 0, free_stage = WC == 1 ? 0 : STAGES - 1;      // the stage of this step, and the one that is filled in it
+        auto turn = [&]() __attribute__((always_inline)) {
+            c_stage = c_stage == STAGES - 1 ? 0 : c_stage + 1;
+            free_stage = free_stage == STAGES - 1 ? 0 : free_stage + 1;
+        };
+        for (int step = 0; step < (WC == 1 ? n_mine : n_steps); ++step, turn()) {
             wait_stage(min(n_mine - 1 - step, kAhead - 1));
             if constexpr (WC > 1) {
                 // every wave's loads of this stage have landed, and every wave is through with the stage before, which the next loads fill
                 asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
                 const int next = step + kAhead;
                 if (next < n_mine) {
-                    if (a.rows.pages && (next & 63) == 0) fetch_pages(next);
-                    fetch(next);
+                    if ((next & 63) == 0) more_rows(next);
+                    fetch(pc, rows, next, free_stage);
                 }
                 if (step >= n_mine) continue;
             }
-            const uint32_t stage = (step % STAGES) * STAGEB;
-            const int32_t t0 = (tile0 + wt + step * WT) * kTreeTok;
-
-            // ---- scores ----
-            f32x16_t sacc;
+            const uint32_t stage = c_stage * STAGEB;
+            const int32_t t0 = (pc.tile0 + wt + step * WT) * kTreeTok;
+            // ---- every LDS read of the tile, issued together: the scores wait for those of K, those of V come meanwhile ----
+            bf16x8_t kw[NSL], va[2][NDB];
+            i32x2_t kw8[NSL], va8[2][NDB];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sacc[i] = 0.f;
-            if constexpr (KV8) {
-                i32x2_t kw[NSL];
-#pragma unroll
-                for (int s = 0; s < NSL; ++s) kw[s] = *lds_at<i32x2_t>(k_rd[s] + stage);
-#pragma unroll
-                for (int s = 0; s < NSL; ++s) sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(kw[s]), qb[s], sacc, 0, 0, 0);
-            } else {
-                bf16x8_t kw[NSL];
-#pragma unroll
-                for (int s = 0; s < NSL; ++s) kw[s] = *lds_at<bf16x8_t>(k_rd[s] + stage);
-#pragma unroll
-                for (int s = 0; s < NSL; ++s) sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kw[s], qb[s], sacc, 0, 0, 0);
+            for (int s = 0; s < NSL; ++s) {
+                if constexpr (KV8)
+                    kw8[s] = *lds_at<i32x2_t>((k_rd + stage) ^ (16 * s));
+                else
+                    kw[s] = *lds_at<bf16x8_t>((k_rd + stage) ^ (32 * s));
             }
-            bf16x8_t va[2][NDB];
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int nb = 0; nb < NDB; ++nb) {
                     if constexpr (KV8) {
-                        va[j][nb] = widen8(__builtin_amdgcn_ds_read_tr8_b64_v2i32(lds_at<i32x2_t>(v_rd[nb][0] + stage + j * 16 * ROWB)));
+                        va8[j][nb] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(lds_at<i32x2_t>(((v_rd + stage) ^ (32 * nb)) + j * 16 * ROWB));
                     } else {
-                        const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<i16x4_t>(v_rd[nb][0] + stage + j * 16 * ROWB)));
-                        const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<i16x4_t>(v_rd[nb][1] + stage + j * 16 * ROWB)));
+                        const uint32_t at_v = ((v_rd + stage) ^ (64 * nb)) + j * 16 * ROWB;
+                        const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<i16x4_t>(at_v)));
+                        const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<i16x4_t>(at_v + 8 * ROWB)));
                         va[j][nb] = __builtin_bit_cast(bf16x8_t, u32x4_t{x.x, x.y, y.x, y.y});
                     }
                 }
-            // Element r of a lane: token t0 + 8 (r / 4) + 4 hi + r % 4.
-            float sv[16];
+            __builtin_amdgcn_sched_barrier(0);
+
+            // ---- scores; element r of a lane: token t0 + 8 (r / 4) + 4 hi + r % 4 ----
+            f32x16_t sacc;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sv[r] = sacc[r] * s_mul;
+            for (int i = 0; i < 16; ++i) sacc[i] = 0.f;
+#pragma unroll
+            for (int s = 0; s < NSL; ++s) {
+                if constexpr (KV8) kw[s] = widen8(kw8[s]);
+                sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kw[s], qs.q[s], sacc, 0, 0, 0);
+            }
+            if constexpr (KV8) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int nb = 0; nb < NDB; ++nb) va[j][nb] = widen8(va8[j][nb]);
+            }
 
             // ---- what is not seen: rows of the draft, rows past the end, rows that the cache does not have ----
-            const uint32_t lacks = missing >> 2 * (step % STAGES) & 3;
+            const uint32_t lacks = missing >> 2 * c_stage & 3;
             const bool masked = t0 + kTreeTok > base || lacks != 0;
             uint32_t seen = ~0u;                      // bit 8 (r / 4) + r % 4
             if (masked) {
@@ -357,13 +492,14 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
                 if (lacks & 2) seen &= 0x0000ffffu;
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (!(seen >> (8 * (r / 4) + r % 4) & 1)) sv[r] = -INFINITY;
+                    if (!(seen >> (8 * (r / 4) + r % 4) & 1)) sacc[r] = -INFINITY;
             }
 
-            // ---- a reference maximum that is raised when some score is far above it ----
-            float mx = sv[0];
+            // ---- a reference maximum, in log2 units, that is raised when some score is far above it ----
+            float mx = sacc[0];
 #pragma unroll
-            for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sv[r]);
+            for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sacc[r]);
+            mx *= s_abs;
             if (__builtin_amdgcn_ballot_w64(mx > m_run + kBump) != 0) {
                 const float m_new = fmaxf(m_run, halves_max(mx));
                 const float alpha = m_new == m_run ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
@@ -376,14 +512,17 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
             }
             const float m_ref = m_run == -INFINITY ? 0.f : m_run;      // nothing seen yet: weights of 0
 
-            // ---- weights ----
-            uint32_t pw[8], rest[8];
+            // ---- weights, as PARTS bf16 numbers that add up to them ----
+            uint32_t pw[PARTS][8];
 #pragma unroll
             for (int r = 0; r < 16; r += 2) {
-                const float p0 = __builtin_amdgcn_exp2f(sv[r] - m_ref), p1 = __builtin_amdgcn_exp2f(sv[r + 1] - m_ref);
+                float p0 = __builtin_amdgcn_exp2f(fmaf(sacc[r], s_abs, -m_ref)), p1 = __builtin_amdgcn_exp2f(fmaf(sacc[r + 1], s_abs, -m_ref));
                 l_run += p0 + p1;
-                pw[r / 2] = pack_bf16(p0, p1);
-                if constexpr (FINE) rest[r / 2] = pack_bf16(p0 - bf16_lo(pw[r / 2]), p1 - bf16_hi(pw[r / 2]));
+#pragma unroll
+                for (int part = 0; part < PARTS; ++part) {
+                    pw[part][r / 2] = pack_bf16(p0, p1);
+                    p0 -= bf16_lo(pw[part][r / 2]), p1 -= bf16_hi(pw[part][r / 2]);      // exact
+                }
             }
 
             if (masked) {
@@ -449,124 +588,209 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
 
             // ---- O^T += V^T P ----
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, u32x4_t{pw[4 * j], pw[4 * j + 1], pw[4 * j + 2], pw[4 * j + 3]});
+            for (int part = 0; part < PARTS; ++part)
 #pragma unroll
-                for (int nb = 0; nb < NDB; ++nb) o[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[j][nb], pb, o[nb], 0, 0, 0);
-                if constexpr (FINE) {
-                    const bf16x8_t pr = __builtin_bit_cast(bf16x8_t, u32x4_t{rest[4 * j], rest[4 * j + 1], rest[4 * j + 2], rest[4 * j + 3]});
+                for (int j = 0; j < 2; ++j) {
+                    const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, u32x4_t{pw[part][4 * j], pw[part][4 * j + 1], pw[part][4 * j + 2], pw[part][4 * j + 3]});
 #pragma unroll
-                    for (int nb = 0; nb < NDB; ++nb) o[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[j][nb], pr, o[nb], 0, 0, 0);
+                    for (int nb = 0; nb < NDB; ++nb) o[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[j][nb], pb, o[nb], 0, 0, 0);
                 }
-            }
             if constexpr (WC == 1) {
                 const int next = step + kAhead;
                 if (next < n_mine) {
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                    if (a.rows.pages && (next & 63) == 0) fetch_pages(next);
-                    fetch(next);
+                    if ((next & 63) == 0) more_rows(next);
+                    fetch(pc, rows, next, free_stage);
                 }
             }
         }
 
-        // ---- the end of the piece ----
+        // ---- the end of the piece: the next one's first tiles and queries are requested, and come while this one's results are folded ----
         l_run = halves_sum(l_run);
-        if constexpr (WT > 1) {                       // the other groups' results to the first one, through the ring's memory
-            float *fold = reinterpret_cast<float *>(lds);
-            __syncthreads();
-            if (wt > 0) {
-                float *mine = fold + ((wt - 1) * CB + wc * kTreeCols + l32) * (FOLDROW + 2);
-#pragma unroll
-                for (int nb = 0; nb < NDB; ++nb)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) mine[32 * nb + 8 * i + 4 * hi + e] = o[nb][4 * i + e];
-                if (hi == 0) mine[D] = m_run, mine[D + 1] = l_run;
-            }
-            __syncthreads();
-            if (wt == 0) {
-                float f[WT], m_star = m_run;
-#pragma unroll
-                for (int w = 1; w < WT; ++w) m_star = fmaxf(m_star, fold[((w - 1) * CB + wc * kTreeCols + l32) * (FOLDROW + 2) + D]);
-                f[0] = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_star);
-                float l_star = l_run * f[0];
-#pragma unroll
-                for (int nb = 0; nb < NDB; ++nb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[nb][i] *= f[0];
-#pragma unroll
-                for (int w = 1; w < WT; ++w) {
-                    const float *theirs = fold + ((w - 1) * CB + wc * kTreeCols + l32) * (FOLDROW + 2);
-                    f[w] = theirs[D] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(theirs[D] - m_star);
-                    l_star = fmaf(theirs[D + 1], f[w], l_star);
-#pragma unroll
-                    for (int nb = 0; nb < NDB; ++nb)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[nb][i] = fmaf(theirs[32 * nb + 8 * (i / 4) + 4 * hi + i % 4], f[w], o[nb][i]);
-                }
-                m_run = m_star, l_run = l_star;
-            }
-            __syncthreads();                          // before the ring is filled again
-        } else if constexpr (WC > 1) {
-            __syncthreads();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if constexpr (WC > 1) __syncthreads();        // nobody reads the ring any more
+        const bool whole = pc.tile0 == 0 && pc.tile1 == pc.tiles, active = col < pc.nn * a.G;
+        if (more) {
+            rows = rows_of(ahead, 0, pages_ahead);
+            begin_ring(ahead, rows);
+            if (NW == 4 && whole) qs = fetch_queries(ahead);      // else behind the fold, or what follows a cut piece: there are not the registers
         }
-        if (wt == 0) {
-            if (whole) {
-                if (active) {
-                    const float v_mul = KV8 ? a.v_scale[sc] : 1.f;
-#pragma unroll
-                    for (int nb = 0; nb < NDB; ++nb)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            write_tree_out<D>(a, q_row, 32 * nb + 8 * i + 4 * hi, make_float4(o[nb][4 * i], o[nb][4 * i + 1], o[nb][4 * i + 2], o[nb][4 * i + 3]), m_run,
-                                              l_run, v_mul);
-                }
-            } else {
-                const size_t slot = (static_cast<size_t>(blockIdx.y) * a.n_slots + my_slot) * 2 + (tile0 == 0 ? 1 : 0);
-                const int c = wc * kTreeCols + l32;
-#pragma unroll
-                for (int nb = 0; nb < NDB; ++nb)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        *reinterpret_cast<float4 *>(a.part_o + ((slot * (D / 4) + 8 * nb + 2 * i + hi) * CB + c) * 4) =
-                            make_float4(o[nb][4 * i], o[nb][4 * i + 1], o[nb][4 * i + 2], o[nb][4 * i + 3]);
-                if (hi == 0) *reinterpret_cast<float2 *>(a.part_ml + (slot * CB + c) * 2) = make_float2(m_run, l_run);
-                if (tile0 == 0 && threadIdx.x == 0) {
-                    cut[0] = pair;
-                    cut[1] = static_cast<int32_t>((first + tiles - 1) / share - first / share + 1);
-                }
-            }
-        }
-    }
-}
 
-// Adds up the pieces of the pair whose first piece workgroup x of column block y had: the first is in the slot of the end of that
-// workgroup's share, the others in those of the beginnings of the next workgroups' shares.
-template <int D, int CB>
-__global__ __launch_bounds__(256) void fairkv_tree_merge_kernel(TreeArgs a)
-{
-    const size_t group = static_cast<size_t>(blockIdx.y) * a.n_slots + blockIdx.x;
-    const int pieces = a.cut[group * 2 + 1];
-    if (pieces == 0) return;
-    const int pair = a.cut[group * 2], b = pair / a.Hkv, h = pair - b * a.Hkv, live = tree_new(a, b) * a.G;
-    for (int idx = blockIdx.z * 256 + threadIdx.x; idx < CB * (D / 4); idx += gridDim.z * 256) {
-        const int c = idx % CB, d4 = idx / CB, col = blockIdx.y * CB + c;
-        if (col >= live) continue;
-        float m_star = -INFINITY, l_star = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int i = 0; i < pieces; ++i) {
-            const size_t slot = (group + i) * 2 + (i == 0 ? 1 : 0);
-            const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + (slot * CB + c) * 2);
-            const float4 o = *reinterpret_cast<const float4 *>(a.part_o + ((slot * (D / 4) + d4) * CB + c) * 4);
-            const float m_new = fmaxf(m_star, ml.x);
-            const float keep = m_star == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_star - m_new), f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m_new);
-            l_star = l_star * keep + ml.y * f;
-            acc.x = acc.x * keep + o.x * f, acc.y = acc.y * keep + o.y * f, acc.z = acc.z * keep + o.z * f, acc.w = acc.w * keep + o.w * f;
-            m_star = m_new;
+        const uint32_t out_row = column.row(a, pc.b, pc.h);
+        const int c = wc * kTreeCols + l32;
+        const float v_mul = KV8 ? a.v_scale[sc] : 1.f;
+        float m_star = m_run, l_star = l_run;
+        // What the workgroup's groups have found is added up through LDS: coordinates 32 nb .. + 31 by group nb % WT, as its block nb / WT.
+        constexpr int kOwn = NDB < WT ? 1 : NDB / WT;
+        const bool owns = wt < NDB;
+        f32x16_t res[kOwn];
+        if constexpr (WT > 1) {
+            if (hi == 0) st_ml[wt][c] = make_float2(m_run, l_run);
+            __syncthreads();
+            float2 ml[WT];
+#pragma unroll
+            for (int w = 0; w < WT; ++w) ml[w] = st_ml[w][c], m_star = fmaxf(m_star, ml[w].x);
+            l_star = 0.f;
+#pragma unroll
+            for (int w = 0; w < WT; ++w) l_star = fmaf(ml[w].y, ml[w].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[w].x - m_star), l_star);
+            const float f = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_star);
+#pragma unroll
+            for (int nb = 0; nb < NDB; ++nb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[nb][i] *= f;
+            // block j of a round, of the group u = 1 .. WT - 1 places behind the one that adds it up
+            auto place = [&](int j, int u) __attribute__((always_inline)) {
+                return reinterpret_cast<float4 *>(lds + RING + ((j * (WT - 1) + u - 1) * WC + wc) * kBlock) + hi * kTreeCols + l32;
+            };
+#pragma unroll
+            for (int r = 0; r < NDB; r += kRound) {
+                if (r > 0) __syncthreads();           // the round before has been read
+#pragma unroll
+                for (int j = 0; j < kRound; ++j) {
+                    const int nb = r + j, u = (wt + WT - nb % WT) % WT;
+                    if (u == 0) continue;
+                    float4 *to = place(j, u);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) to[2 * i * kTreeCols] = make_float4(o[nb][4 * i], o[nb][4 * i + 1], o[nb][4 * i + 2], o[nb][4 * i + 3]);
+                }
+                __syncthreads();
+#pragma unroll
+                for (int j = 0; j < kRound; ++j) {
+                    const int nb = r + j;
+                    if (nb % WT != wt) continue;
+#pragma unroll
+                    for (int u = 1; u < WT; ++u) {
+                        const float4 *from = place(j, u);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float4 x = from[2 * i * kTreeCols];
+                            o[nb][4 * i] += x.x, o[nb][4 * i + 1] += x.y, o[nb][4 * i + 2] += x.z, o[nb][4 * i + 3] += x.w;
+                        }
+                    }
+                    res[nb / WT] = o[nb];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int nb = 0; nb < NDB; ++nb) res[nb] = o[nb];
         }
-        const Column column(a, col);
-        write_tree_out<D>(a, column.row(a, b, h), d4 * 4, acc, m_star, l_star, a.v_scale[a.n_scales > 1 ? h : 0]);
+        auto four = [&](int q, int i) __attribute__((always_inline)) { return make_float4(res[q][4 * i], res[q][4 * i + 1], res[q][4 * i + 2], res[q][4 * i + 3]); };
+        auto first_of = [&](int q, int i) __attribute__((always_inline)) { return 32 * (q * WT + wt) + 8 * i + 4 * hi; };      // coordinate of four(q, i)
+        if (NW != 4 && more && whole) qs = fetch_queries(ahead);
+        bool finished = whole;
+        if (!whole) {
+            // ---- a piece of a pair that was cut: the last workgroup to come adds the pieces up, in their order, whichever it is ----
+            auto slot_of = [&](int64_t place) __attribute__((always_inline)) {
+                return static_cast<int>(small ? static_cast<uint32_t>(place) / static_cast<uint32_t>(share) : place / share);
+            };
+            const int from_slot = slot_of(pc.first), pieces = slot_of(pc.first + pc.tiles - 1) - from_slot + 1, me = my_slot - from_slot;
+            const size_t block = static_cast<size_t>(blockIdx.y) * a.n_slots;
+            auto part = [&](int piece) __attribute__((always_inline)) {      // where a piece's result is: the pair's first piece ends its workgroup's share
+                return (block + from_slot + piece) * 2 + (piece == 0 ? 1 : 0);
+            };
+            // Pieces first, first + apart, ... (n of them, this workgroup's the mine_th) into this workgroup's registers, if it is the last of them to come.
+            auto join = [&](int32_t *counter, int first, int apart, int n, int mine_th) __attribute__((always_inline)) {
+                __syncthreads();                      // `counted` has been read
+                // The others are there already: nothing need be written.  (They counted in behind their results' arrival.)
+                if (threadIdx.x == 0) counted = __hip_atomic_load(counter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                __syncthreads();
+                bool last = __builtin_amdgcn_readfirstlane(counted) == n - 1;
+                if (!last) {
+                    const size_t to = part(first + mine_th * apart);
+                    if (active && owns) {
+#pragma unroll
+                        for (int q = 0; q < kOwn; ++q)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) publish_f32x4(a.part_o + to * (D * CB), (first_of(q, i) / 4 * CB + c) * 16, four(q, i));
+                        if (wt == 0 && hi == 0) publish_f32x2(a.part_ml + to * (CB * 2), c * 8, m_star, l_star);
+                    }
+                    drain_vmem();
+                    __syncthreads();
+                    if (threadIdx.x == 0) counted = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    __syncthreads();
+                    last = __builtin_amdgcn_readfirstlane(counted) == n - 1;
+                }
+                if (!last) return false;
+                if (threadIdx.x == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                f2_t ml[kJoin];
+#pragma unroll
+                for (int i = 0; i < kJoin; ++i) {
+                    ml[i] = f2_t{-INFINITY, 0.f};
+                    if (i < n && i != mine_th)
+                        ml[i] = __builtin_bit_cast(f2_t, __builtin_amdgcn_raw_buffer_load_b64(parts_rsrc(a.part_ml + part(first + i * apart) * (CB * 2), CB * 8), c * 8, 0, kAgent));
+                }
+                float top = m_star, sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < kJoin; ++i) {
+                    if (i == mine_th) ml[i] = f2_t{m_star, l_star};
+                    top = fmaxf(top, ml[i][0]);
+                }
+#pragma unroll
+                for (int i = 0; i < kJoin; ++i) {
+                    ml[i][0] = ml[i][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[i][0] - top);
+                    sum = fmaf(ml[i][1], ml[i][0], sum);
+                }
+                auto weight = [&](int i) __attribute__((always_inline)) {
+                    float f = ml[0][0];
+#pragma unroll
+                    for (int j = 1; j < kJoin; ++j) f = i == j ? ml[j][0] : f;
+                    return f;
+                };
+                constexpr int kAtOnce = kOwn > 2 ? 1 : kOwn;      // of a wave's blocks of coordinates
+#pragma unroll
+                for (int q0 = 0; q0 < kOwn; q0 += kAtOnce) {
+                    float acc[kAtOnce][16] = {};
+#pragma clang loop unroll(disable)
+                    for (int i = 0; i < n; ++i) {
+                        const float f = weight(i);
+                        if (i == mine_th) {
+#pragma unroll
+                            for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) acc[u][e] = fmaf(res[q0 + u][e], f, acc[u][e]);
+                            continue;
+                        }
+                        const __amdgpu_buffer_rsrc_t from = parts_rsrc(a.part_o + part(first + i * apart) * (D * CB), D * CB * 4);
+                        f4_t x[kAtOnce][4];
+#pragma unroll
+                        for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)      // (where a group owns no block: past the end, and not used)
+                                x[u][e] = __builtin_bit_cast(f4_t, __builtin_amdgcn_raw_buffer_load_b128(from, (first_of(q0 + u, e) / 4 * CB + c) * 16, 0, kAgent));
+#pragma unroll
+                        for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) acc[u][e] = fmaf(x[u][e / 4][e % 4], f, acc[u][e]);
+                    }
+#pragma unroll
+                    for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) res[q0 + u][e] = acc[u][e];
+                }
+                m_star = top, l_star = sum;
+                return true;
+            };
+            // Up to kJoin pieces at once; more in groups of as many, whose sums are joined in groups in turn.  A group's counter lies by its level
+            // and the place of its first piece.
+            finished = true;
+            int unit = 1, at_level = me;
+            int32_t *level = a.arrivals + block * (2 * kLevels);
+#pragma clang loop unroll(disable)
+            for (int left = pieces; finished && left > 1; left = (left + kJoin - 1) / kJoin) {
+                const int group = at_level / kJoin, n = min(kJoin, left - group * kJoin), first = group * kJoin * unit;
+                if (n > 1) finished = join(level + (from_slot + first) * 2 + (first == 0 ? 1 : 0), first, unit, n, at_level % kJoin);
+                at_level = group, unit *= kJoin, level += 2 * a.n_slots;
+            }
+        }
+        if (finished && active && owns) {
+#pragma unroll
+            for (int q = 0; q < kOwn; ++q)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) write_tree_out<D>(a, out_row, first_of(q, i), four(q, i), m_star, l_star, v_mul);
+        }
+        if (!more) break;
+        if (!whole) qs = fetch_queries(ahead);
+        pc = ahead;
     }
 }
 

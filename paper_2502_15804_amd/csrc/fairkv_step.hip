@@ -8,6 +8,7 @@
 #include "append_rotated.h"
 #include "decode_tree.h"
 #include "fairkv.h"
+#include "zero_words.h"
 
 namespace {
 
@@ -135,41 +136,42 @@ TreeShape tree_shape(int32_t cols, int32_t n_slots)
     return s;
 }
 
+constexpr int32_t kTreeBlocks = 32;      // of 32 columns: 16 heads of 64 nodes
+
+// The counters come first and take what n_slots alone says, so that calls of different shapes may share a workspace.
 struct TreeSpace {
-    size_t cut, ml, o;
+    size_t counters, ml, o;
 };
-TreeSpace tree_space(const TreeShape &s, int32_t D)
+size_t tree_counters(int32_t n_slots) { return align256((static_cast<size_t>(n_slots) + kTreeBlocks) * 2 * kLevels * sizeof(int32_t)); }
+TreeSpace tree_space(const TreeShape &s, int32_t D, int32_t n_slots)
 {
-    const size_t groups = static_cast<size_t>(s.blocks) * s.slots, cols = 32 * static_cast<size_t>(s.waves);
-    return {align256(groups * 2 * sizeof(int32_t)), align256(groups * 2 * cols * 2 * sizeof(float)), align256(groups * 2 * cols * D * sizeof(float))};
+    const size_t groups = static_cast<size_t>(s.blocks) * s.slots, cols = 32 * static_cast<size_t>(s.waves);      // groups <= n_slots, or one a block
+    return {tree_counters(n_slots), align256(groups * 2 * cols * 2 * sizeof(float)), align256(groups * 2 * cols * D * sizeof(float))};
 }
 
 int check_tree(const fairkv_cache *c, int32_t Hq, int32_t q_len, int32_t n_slots)
 {
     if (const int rc = check_cache(c)) return rc;
     if (Hq < 1 || q_len < 1 || n_slots < 1 || Hq % c->Hkv != 0) return FAIRKV_EINVAL;
-    if (c->dtype == FAIRKV_F32 || q_len > FAIRKV_MAX_DRAFT || Hq / c->Hkv > 16 || n_slots > 65536) return FAIRKV_EUNSUPPORTED;
+    if (c->dtype == FAIRKV_F32 || q_len > FAIRKV_MAX_DRAFT || Hq / c->Hkv > 16 || n_slots > kTreeSlots) return FAIRKV_EUNSUPPORTED;
     return FAIRKV_OK;
 }
 
-template <int D, bool KV8, int WC, int WT, int STAGES, bool FINE>
+template <int D, bool KV8, int WC, int WT, int STAGES, int PARTS>
 void launch_tree_kernel(const TreeArgs &a, int32_t blocks, hipStream_t st)
 {
-    hipLaunchKernelGGL((fairkv_decode_tree_kernel<D, KV8, WC, WT, STAGES, FINE>), dim3(static_cast<unsigned>(a.n_slots), static_cast<unsigned>(blocks)),
+    hipLaunchKernelGGL((fairkv_decode_tree_kernel<D, KV8, WC, WT, STAGES, PARTS>), dim3(static_cast<unsigned>(a.n_slots), static_cast<unsigned>(blocks)),
                        dim3(WC * WT * 64), 0, st, a);
-    constexpr int CB = WC * kTreeCols;
-    hipLaunchKernelGGL((fairkv_tree_merge_kernel<D, CB>), dim3(static_cast<unsigned>(a.n_slots), static_cast<unsigned>(blocks), std::min(8, CB * D / 1024)),
-                       dim3(256), 0, st, a);
 }
 
 template <int D, bool KV8>
 void launch_tree(int waves, bool fine, const TreeArgs &a, int32_t blocks, hipStream_t st)
 {
     switch (waves) {
-    case 1: return launch_tree_kernel<D, KV8, 1, 4, 2, true>(a, blocks, st);
-    case 2: return launch_tree_kernel<D, KV8, 2, 4, 2, true>(a, blocks, st);
-    case 4: return fine ? launch_tree_kernel<D, KV8, 4, 2, 3, true>(a, blocks, st) : launch_tree_kernel<D, KV8, 4, 2, 3, false>(a, blocks, st);
-    default: return fine ? launch_tree_kernel<D, KV8, 8, 1, 4, true>(a, blocks, st) : launch_tree_kernel<D, KV8, 8, 1, 4, false>(a, blocks, st);
+    case 1: return fine ? launch_tree_kernel<D, KV8, 1, 4, 2, 3>(a, blocks, st) : launch_tree_kernel<D, KV8, 1, 4, 2, 2>(a, blocks, st);
+    case 2: return fine ? launch_tree_kernel<D, KV8, 2, 4, 2, 3>(a, blocks, st) : launch_tree_kernel<D, KV8, 2, 4, 2, 2>(a, blocks, st);
+    case 4: return fine ? launch_tree_kernel<D, KV8, 4, 2, 3, 3>(a, blocks, st) : launch_tree_kernel<D, KV8, 4, 2, 3, 1>(a, blocks, st);
+    default: return fine ? launch_tree_kernel<D, KV8, 8, 1, 4, 3>(a, blocks, st) : launch_tree_kernel<D, KV8, 8, 1, 4, 1>(a, blocks, st);
     }
 }
 
@@ -178,8 +180,19 @@ void launch_tree(int waves, bool fine, const TreeArgs &a, int32_t blocks, hipStr
 extern "C" size_t fairkv_tree_workspace_bytes(const fairkv_cache *c, int32_t Hq, int32_t q_len, int32_t n_slots)
 {
     if (check_tree(c, Hq, q_len, n_slots) != FAIRKV_OK) return 0;
-    const TreeSpace s = tree_space(tree_shape(Hq / c->Hkv * q_len, n_slots), c->D);
-    return s.cut + s.ml + s.o;
+    const TreeSpace s = tree_space(tree_shape(Hq / c->Hkv * q_len, n_slots), c->D, n_slots);
+    return s.counters + s.ml + s.o;
+}
+
+extern "C" size_t fairkv_tree_counter_bytes(int32_t n_slots) { return n_slots < 1 || n_slots > kTreeSlots ? 0 : tree_counters(n_slots); }
+
+extern "C" int fairkv_tree_workspace_reset(void *workspace, size_t workspace_bytes, int32_t n_slots, void *hip_stream)
+{
+    const size_t need = fairkv_tree_counter_bytes(n_slots);
+    if (!workspace || need == 0 || !aligned(workspace, 16)) return FAIRKV_EINVAL;
+    if (workspace_bytes < need) return FAIRKV_EWORKSPACE;
+    zero_words(workspace, need / sizeof(uint32_t), static_cast<hipStream_t>(hip_stream));
+    return launched();
 }
 
 extern "C" int fairkv_decode_attn_tree(const fairkv_cache *c, const void *q, const uint64_t *tree, const int32_t *n_new, const int32_t *len,
@@ -192,8 +205,8 @@ extern "C" int fairkv_decode_attn_tree(const fairkv_cache *c, const void *q, con
     if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16) || (tree && !aligned(tree, 8))) return FAIRKV_EINVAL;
     if (static_cast<int64_t>(c->B) * q_len * Hq * c->D > INT32_MAX) return FAIRKV_EINVAL;
     const TreeShape shape = tree_shape(Hq / c->Hkv * q_len, n_slots);
-    const TreeSpace space = tree_space(shape, c->D);
-    if (!workspace || workspace_bytes < space.cut + space.ml + space.o) return FAIRKV_EWORKSPACE;
+    const TreeSpace space = tree_space(shape, c->D, n_slots);
+    if (!workspace || workspace_bytes < space.counters + space.ml + space.o) return FAIRKV_EWORKSPACE;
 
     TreeArgs a{};
     a.q = q, a.k = c->k, a.v = c->v;
@@ -201,9 +214,9 @@ extern "C" int fairkv_decode_attn_tree(const fairkv_cache *c, const void *q, con
     a.len = len, a.n_new = n_new, a.tree = reinterpret_cast<const int64_t *>(tree);
     a.out = out, a.lse = lse;
     char *ws = static_cast<char *>(workspace);
-    a.cut = reinterpret_cast<int32_t *>(ws);
-    a.part_ml = reinterpret_cast<float *>(ws + space.cut);
-    a.part_o = reinterpret_cast<float *>(ws + space.cut + space.ml);
+    a.arrivals = reinterpret_cast<int32_t *>(ws);
+    a.part_ml = reinterpret_cast<float *>(ws + space.counters);
+    a.part_o = reinterpret_cast<float *>(ws + space.counters + space.ml);
     a.B = c->B, a.Hq = Hq, a.Hkv = c->Hkv, a.G = Hq / c->Hkv, a.q_len = q_len, a.cols = a.G * q_len;
     a.n_slots = shape.slots;
     // 2^31 - 2^16 tokens: what is added to a token's number inside a tile or a batch of pages does not wrap around

@@ -253,15 +253,27 @@ def test_accept(dtype, D, q_len, page):
 
 
 # ---- attention -------------------------------------------------------------------------------------------
+def _workspace(cache, Hq, q_len, n_slots=None):
+    """Counters of zero, NaN everywhere else."""
+    ws = torch.full((F.fairkv_tree_workspace_bytes(cache, Hq, q_len, n_slots),), 0xff, dtype=torch.uint8, device=DEV)
+    F.fairkv_tree_workspace_reset(ws, cache.n_slots if n_slots is None else n_slots)
+    return ws
+
+
 def _attend(s, Hq, q_len, out_dtype, tree=None, n_new=None, n_slots=None, seed=0, scale=None, q=None, stream=None, q_mul=1.0):
     scale = 1 / math.sqrt(s.D) if scale is None else scale
     if q is None:
         q = (torch.randn(s.B, q_len, Hq, s.D, generator=torch.Generator().manual_seed(seed + 1)) * q_mul).to(torch.bfloat16).to(DEV)
     out = torch.full(q.shape, 3.0, dtype=out_dtype, device=DEV)
     lse = torch.full(q.shape[:-1], 3.0, dtype=torch.float32, device=DEV)
-    ws = torch.full((F.fairkv_tree_workspace_bytes(s.cache, Hq, q_len, n_slots),), 0xff, dtype=torch.uint8, device=DEV)     # NaN, and no counts
+    ws = _workspace(s.cache, Hq, q_len, n_slots)
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())
     F.fairkv_decode_attn_tree(s.cache, s.lens, q, ws, out, lse, scale, tree=None if tree is None else torch.as_tensor(tree.view(np.int64), device=DEV),
                               n_new=None if n_new is None else I32(n_new), n_slots=n_slots, stream=stream)
+    if stream is None:
+        counters = ws[:F.fairkv_tree_counter_bytes(s.cache.n_slots if n_slots is None else n_slots)]
+        assert not counters.any()            # left as they were found
     return q, out, lse, scale
 
 
@@ -462,7 +474,7 @@ def test_another_stream_and_no_lse():
     side.synchronize()
     _compare(s, *got, None, None)
     q, out = got[0], torch.empty_like(got[1])
-    ws = torch.empty(F.fairkv_tree_workspace_bytes(s.cache, 8, 3), dtype=torch.uint8, device=DEV)
+    ws = _workspace(s.cache, 8, 3)
     F.fairkv_decode_attn_tree(s.cache, s.lens, q, ws, out, None, got[3])
     assert torch.equal(out, got[1])
 
@@ -508,7 +520,7 @@ def test_steps_captured_once_and_replayed_while_the_cache_grows(dtype, page):
     tree = torch.zeros(B, q_len, dtype=torch.int64, device=DEV)
     n_new, path, n_path = I32(np.zeros(B)), I32(np.zeros((B, q_len))), I32(np.zeros(B))
     q_out, bad = torch.zeros_like(q), I32([0])
-    ws = torch.full((F.fairkv_tree_workspace_bytes(s.cache, Hq, q_len),), 0xff, dtype=torch.uint8, device=DEV)
+    ws = _workspace(s.cache, Hq, q_len)
     outs = [(torch.zeros(q.shape, device=DEV), torch.zeros(q.shape[:-1], device=DEV)) for _ in range(2)]
     grown = torch.zeros_like(s.lens)
 

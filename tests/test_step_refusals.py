@@ -107,6 +107,15 @@ def test_tree_workspace():
         assert _tree(c, Hq=Hq, q_len=q_len, n_slots=n_slots, ws_bytes=need - 1) == F.FAIRKV_EWORKSPACE
 
 
+def test_tree_workspace_reset_and_its_counters():
+    L = F.lib()
+    assert [L.fairkv_tree_counter_bytes(n) for n in (0, -1, 65537)] == [0, 0, 0]
+    assert 0 < L.fairkv_tree_counter_bytes(1) <= L.fairkv_tree_counter_bytes(256) < L.fairkv_tree_workspace_bytes(ctypes.byref(_cache()), 8, 4, 256)
+    for args, code in (((None, 1 << 30, 256), F.FAIRKV_EINVAL), ((AT + 4, 1 << 30, 256), F.FAIRKV_EINVAL), ((AT, 1 << 30, 0), F.FAIRKV_EINVAL),
+                       ((AT, F.fairkv_tree_counter_bytes(256) - 1, 256), F.FAIRKV_EWORKSPACE)):
+        assert L.fairkv_tree_workspace_reset(*args, None) == code
+
+
 @pytest.mark.parametrize("kw,code", [
     (dict(path=None), F.FAIRKV_EINVAL), (dict(n_path=None), F.FAIRKV_EINVAL), (dict(len_=None), F.FAIRKV_EINVAL), (dict(len_out=None), F.FAIRKV_EINVAL),
     (dict(q_len=0), F.FAIRKV_EINVAL), (dict(q_len=65), F.FAIRKV_EUNSUPPORTED)])
