@@ -16,8 +16,9 @@
 // and are added up at its end.  K and V go from HBM to LDS directly.
 //
 // Schedule.  Lengths change from step to step and stay on the GPU, so that a captured launch may be replayed while the cache grows: every
-// workgroup adds up the lengths by itself and finds its share of the line of all pairs, each as long as its tiles and kTreeOverhead more.
-// The pieces of a pair that is cut leave partial results in the workspace, which a second small kernel adds up in the order of the pieces.
+// workgroup adds up the lengths by itself and finds its share of the line of all pairs, each as long as its tiles and what a
+// piece costs besides.  The pieces of a pair that is cut leave partial results in the workspace, and the workgroup that comes last adds them up,
+// in the order of the pieces.
 #pragma once
 #include "cache_rows.h"
 #include "decode_mfma.h"
@@ -33,6 +34,9 @@ constexpr int kTreeTok = 32;          // tokens of a tile
 constexpr int kTreeCols = 32;         // columns of a wave
 constexpr int kJoin = 8;              // pieces of a pair that are added up at once
 constexpr int kLevels = 6;            // of such sums, for pairs in up to 8^6 pieces
+// What a piece costs besides its tiles, in tiles: queries, fold, outputs.  A pair that one wave has alone has next to none of that.  Measured with
+// 6, 9 and 13 a piece: 128 columns, 16 x 8 pairs of 2000 rows in fp32 63, 59 and 56 us (one wave side by side), 56, 52 and 53 us (four).
+constexpr int kPieceCost = 10, kSoloCost = 2;
 constexpr int kTreeSlots = 65536;     // most workgroups of a block of columns
 static_assert(kTreeSlots <= 1 << 3 * kLevels && kJoin == 8, "levels");
 
@@ -133,6 +137,8 @@ __device__ __forceinline__ int64_t wave_upto(int64_t x)
 struct TreePiece {
     int pair, b, h;
     int32_t len, nn, tiles, tile0, tile1;
+    int from, apart;                  // this wave's tiles are tile0 + from, + apart, ...: its group's, or all of them
+    bool solo;                        // a short pair that one wave has alone
     int64_t off;                      // first row of a packed pair, -1 if its run does not fit the cache
     int64_t first;                    // place of the pair's first tile in the line
 };
@@ -153,14 +159,30 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
     constexpr int kAhead = WC == 1 ? STAGES : STAGES - 1;       // tiles on their way while one is waited for
     constexpr int RING = WT * STAGES * STAGEB;
     constexpr int kBlock = kTreeCols * 32 * 4;        // bytes of 32 coordinates of a wave's columns
-    constexpr int kOverhead = WC == 1 ? 3 : 5;        // what a pair costs a workgroup beside its tiles, in tiles
-    constexpr int kRound = WT == 1 ? 0 : WC == 1 ? (NDB < 2 ? NDB : 2) : 1;      // such blocks of a group that are folded at once
+    constexpr int kSolo = WC == 1 && WT == 4 ? 4 : 0; // a whole pair of at most so many tiles goes to one wave: no fold, four pairs side by side
+    auto overhead = [&](int tiles) __attribute__((always_inline)) { return tiles <= kSolo ? kSoloCost : kPieceCost; };
+    constexpr int kRound = WT == 1 ? 0 : WC == 1 ? NDB : NDB / 2;      // such blocks of a group that are folded at once
     constexpr int FOLD = (WT - 1) * WC * kRound * kBlock;
+    // The fold has memory of its own where that fits beside the ring, else the ring's last stage, which is empty then.
+    constexpr bool kFoldInRing = RING + FOLD > 158 * 1024;
+    constexpr int kFoldAt = kFoldInRing ? RING - WT * STAGEB : RING;
+    static_assert(!kFoldInRing || FOLD <= WT * STAGEB, "a stage of all groups");
+    // The queries of a piece come through LDS, whole rows at a time (straight into the registers a load would touch 32 rows): a wave's own 32 columns
+    // into its ring's last stage, which is empty then; with waves side by side, the workgroup's into memory of their own, or the fold's.
+    constexpr int QROWB = 2 * D, QBYTES = CB * QROWB;
+    constexpr bool kOwnQueries = WC == 1;
+    constexpr int kOwnMemory = RING + (kFoldInRing ? 0 : FOLD);
+    constexpr bool kQueriesInFold = !kOwnQueries && kOwnMemory + QBYTES > 156 * 1024;
+    static_assert(!kOwnQueries || QBYTES <= STAGEB, "a group's stage");
+    static_assert(!kQueriesInFold || (!kFoldInRing && FOLD >= QBYTES), "the fold's memory");
+    constexpr int kTail = (kFoldInRing ? 0 : FOLD) + (kOwnQueries || kQueriesInFold ? 0 : QBYTES);
+    constexpr int kQueriesAt = kOwnQueries ? RING - WT * STAGEB : kQueriesInFold ? kFoldAt : kOwnMemory;
     static_assert(LOADS * kAhead < 64, "vmcnt is a 6-bit counter");
     static_assert(WT == 1 || NDB % kRound == 0, "rounds");
 
     constexpr int kTable = NT * 16;                   // what a pair's piece needs to know, of up to NT pairs; before the first fold
-    __shared__ __attribute__((aligned(1024))) char lds[RING + (FOLD > kTable ? FOLD : kTable)];
+    __shared__ __attribute__((aligned(1024))) char lds[RING + (kTail > kTable ? kTail : kTable)];
+    __shared__ uint32_t q_byte[CB];                   // of every column: its query behind those of the pair's first column
     __shared__ float2 st_ml[WT][CB];
     __shared__ int64_t scan[NW + 2];                  // totals of the waves; the pair the workgroup starts with and where it ends
     __shared__ int32_t counted;
@@ -173,6 +195,10 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
 
     // ---- this workgroup's share of the line, which it walks from its end to its beginning: the piece at its end, whose pair goes on in the
     //      next workgroup, is done first, so that it is there when that one, having done the pair's other piece last, adds the two up ----
+    for (int c = threadIdx.x; c < CB; c += NT) {
+        const Column x(a, min(c0 + c, a.cols - 1));
+        q_byte[c] = static_cast<uint32_t>(x.node * a.Hq + x.head) * QROWB;
+    }
     int4 *const table = reinterpret_cast<int4 *>(lds + RING);
     const bool in_table = n_pairs <= NT;
     auto pair_entry = [&](int p) __attribute__((always_inline)) {      // length, new tokens, first row (-1: a run that does not fit the cache)
@@ -191,10 +217,10 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
             if (p0 < p1) {
                 const int4 e = pair_entry(p0);
                 table[p0] = e;
-                mine = kOverhead + tiles_of(e.x);
+                mine = tiles_of(e.x) + overhead(tiles_of(e.x));
             }
         } else {
-            for (int p = p0; p < p1; ++p) mine += kOverhead + tiles_of(tree_len(a, p));
+            for (int p = p0; p < p1; ++p) mine += tiles_of(tree_len(a, p)) + overhead(tiles_of(tree_len(a, p)));
         }
         const int64_t upto = wave_upto(mine);
         if (lane == 63) scan[wave] = upto;
@@ -218,12 +244,12 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
             int p = p0;
             if (!in_table)
                 for (; p < p1; ++p) {
-                    const int cost = kOverhead + tiles_of(tree_len(a, p));
+                    const int cost = tiles_of(tree_len(a, p)) + overhead(tiles_of(tree_len(a, p)));
                     if (target < before + cost) break;
                     before += cost;
                 }
             scan[NW] = p;
-            scan[NW + 1] = before + (in_table ? mine : kOverhead + tiles_of(tree_len(a, p)));
+            scan[NW + 1] = before + (in_table ? mine : tiles_of(tree_len(a, p)) + overhead(tiles_of(tree_len(a, p))));
         }
         __syncthreads();
         pair = __builtin_amdgcn_readfirstlane(static_cast<int>(scan[NW]));
@@ -234,7 +260,8 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
     // ---- what depends on the lane alone ----
     const int col = c0 + wc * kTreeCols + l32;
     const Column column(a, min(col, a.cols - 1));
-    const uint32_t ring = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(FAIRKV_LDS_PTR(lds))) + wt * (STAGES * STAGEB);
+    const uint32_t ring = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(FAIRKV_LDS_PTR(lds))) + wt * STAGEB;      // the group's stage 0
+    constexpr uint32_t kStage = WT * STAGEB;          // from one stage of a group to the next
     const int ld_row = lane / PPR, ld_col = lane % PPR;
     // Where the lane reads in stage 0: its row of K, and its share of the transposing reads of V.  Pieces further on in a row are a bit pattern
     // away, since swizzles are patterns too, rows further on whole rows: swizzles repeat every 8 (8-bit: 16) rows.
@@ -248,6 +275,7 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
     int held = pair;                                  // the pair of lane 0; lane i has the i-th before it
     int4 entry;
     entry = in_table ? table[max(pair - lane, 0)] : pair_entry(max(pair - lane, 0));
+    if constexpr (!kOwnQueries) __syncthreads();      // the table's memory is the queries'
     auto next_piece = [&](TreePiece &pc) __attribute__((always_inline)) {      // false: the share has no more
         while (pair >= 0) {
             if (held - pair >= 64) {
@@ -262,12 +290,21 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
                                           static_cast<uint32_t>(__builtin_amdgcn_readlane(entry.z, i)));
             pc.tiles = tiles_of(pc.len);
             pc.first = at - pc.tiles;
-            at = pc.first - kOverhead;
+            at = pc.first - overhead(pc.tiles);
             pair = at <= begin ? -1 : pair - 1;
             pc.tile0 = static_cast<int32_t>(max(begin - pc.first, static_cast<int64_t>(0)));
             pc.tile1 = static_cast<int32_t>(min(end - pc.first, static_cast<int64_t>(pc.tiles)));
             const bool empty = pc.tiles == 0 && begin < pc.first && pc.first <= end;      // a pair without rows belongs to one workgroup too
-            if ((pc.tile1 > pc.tile0 || empty) && c0 < pc.nn * a.G) return true;
+            if ((pc.tile1 <= pc.tile0 && !empty) || c0 >= pc.nn * a.G) continue;
+            pc.from = wt, pc.apart = WT, pc.solo = false;
+            if constexpr (kSolo > 0) {
+                pc.solo = pc.tile0 == 0 && pc.tile1 == pc.tiles && pc.tiles <= kSolo;
+                if (pc.solo) {
+                    pc.from = 0, pc.apart = 1;
+                    if ((pc.pair & 3) != wave) continue;      // another wave's
+                }
+            }
+            return true;
         }
         return false;
     };
@@ -284,7 +321,7 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
     auto fetch_pages = [&](const TreePiece &pc, int step) __attribute__((always_inline)) {      // page numbers of steps step .. step + 63, not waited for
         int2 ids = {0, 0};
         if (a.rows.pages && pc.len > 0) {
-            const int t = min((pc.tile0 + wt + (step + lane) * WT) * kTreeTok, pc.len - 1);
+            const int t = min((pc.tile0 + pc.from + (step + lane) * pc.apart) * kTreeTok, pc.len - 1);
             const int32_t *of_pair = a.rows.pages + static_cast<int64_t>(pc.pair) * a.rows.max_pages;
             ids = {of_pair[t >> a.rows.page_shift], of_pair[min(t + 16, pc.len - 1) >> a.rows.page_shift]};
         }
@@ -292,7 +329,7 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
     };
     auto rows_of = [&](const TreePiece &pc, int step, int2 ids) __attribute__((always_inline)) {
         Rows x;
-        const int t = min((pc.tile0 + wt + (step + lane) * WT) * kTreeTok, max(pc.len - 1, 0) & ~15);
+        const int t = min((pc.tile0 + pc.from + (step + lane) * pc.apart) * kTreeTok, max(pc.len - 1, 0) & ~15);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const int th = half ? min(t + 16, max(pc.len - 1, 0) & ~15) : t;
@@ -302,47 +339,51 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
         }
         return x;
     };
-    // This wave's share of a stage: with more than one wave side by side all of it K or all of it V.  Rows past the end of the pair are its last
-    // row again, rows that the cache does not have the cache's first one: their weights are 0.  `missing` says of every stage which of its two
-    // halves the cache does not have.
+    // This wave's share of a stage: with more than one wave side by side all of it K or all of it V.  Loads of whole rows go in runs that neither
+    // leave a half nor a wave's share.  Rows past the end of the pair are its last row again, rows that the cache does not have the cache's
+    // first one: their weights are 0.  `missing` says of every stage which of its two halves the cache does not have.
     static_assert(WC == 1 || LPT % LOADS == 0, "a wave loads K or V");
+    constexpr int kHalf = LPT / 2, kRun = kHalf < LOADS ? kHalf : LOADS;      // loads of a half, of a run
     const int load0 = wc * LOADS;                     // the wave's first load of a stage
+    const bool loads = 2 * LPT >= WC || load0 < 2 * LPT;
     auto is_v = [&](int x) __attribute__((always_inline)) { return WC == 1 ? x >= LPT : load0 >= LPT; };
     auto nth = [&](int x) __attribute__((always_inline)) { return WC == 1 ? x % LPT : load0 % LPT + x; };      // load of the tile of K or V
     auto swizzled = [&](int x) __attribute__((always_inline)) {      // byte of its row that the lane fetches in load x
         const int r = nth(x) * RPI + ld_row;
         return static_cast<uint32_t>((ld_col ^ (is_v(x) ? v_swizzle<ROWB, KV8>(r) : k_swizzle<ROWB>(r))) * 16);
     };
-    // The lane's offset in a load of whole rows, from the first row of the load: swizzles repeat every kTurns loads.
-    constexpr int kTurns = ROWB / 64 < LOADS ? ROWB / 64 : LOADS, kKinds = WC == 1 ? 2 : 1;
-    uint32_t full_offset[kKinds][kTurns];
+    constexpr int kKinds = WC == 1 ? 2 : 1;           // of a wave's runs: swizzles are the same from half to half
+    uint32_t run_offset[kKinds][kRun];
 #pragma unroll
     for (int kind = 0; kind < kKinds; ++kind)
 #pragma unroll
-        for (int x = 0; x < kTurns; ++x) {
-            full_offset[kind][x] = ld_row * ROWB + swizzled(kind * LPT + x);
-            asm volatile("" : "+v"(full_offset[kind][x]));
+        for (int x = 0; x < kRun; ++x) {
+            run_offset[kind][x] = ld_row * ROWB + swizzled(kind * LPT + x);      // 1024 x behind that is the load's own
+            asm volatile("" : "+v"(run_offset[kind][x]));
         }
     uint32_t missing = 0;
     auto fetch = [&](const TreePiece &pc, const Rows &rows, int step, int at_stage) __attribute__((always_inline)) {
-        const int last = pc.len - 1 - (pc.tile0 + wt + step * WT) * kTreeTok;
-        const uint32_t stage = ring + at_stage * STAGEB;
+        const int last = pc.len - 1 - (pc.tile0 + pc.from + step * pc.apart) * kTreeTok;
+        const uint32_t stage = ring + at_stage * kStage;
         const int64_t row0 = rows.get(0, step & 63), row1 = rows.get(1, step & 63);
         const bool full = last >= kTreeTok - 1 && (row0 | row1) >= 0;
         missing &= ~(3u << 2 * at_stage);
+        if (!loads) return;
         if (full) {
 #pragma unroll
-            for (int x = 0; x < LOADS; ++x) {
-                if (2 * LPT < WC && load0 >= 2 * LPT) break;
-                load16_to_lds((is_v(x) ? v_base : k_base) + ((nth(x) * RPI >= 16 ? row1 : row0) + nth(x) * RPI % 16) * ROWB,
-                              full_offset[WC == 1 && x >= LPT ? 1 : 0][x % kTurns], stage + (is_v(x) ? TILEB : 0) + nth(x) * 1024);
+            for (int x = 0; x < LOADS; x += kRun) {
+                const char *from = (is_v(x) ? v_base : k_base) + ((nth(x) >= kHalf ? row1 : row0) + nth(x) % kHalf * RPI) * ROWB;
+                const uint32_t to = stage + (is_v(x) ? TILEB : 0) + nth(x) * 1024;
+                if constexpr (kRun == 1)
+                    load16_to_lds(from, run_offset[WC == 1 && x >= LPT ? 1 : 0][0], to);
+                else
+                    load_tile_to_lds<kRun>(from, run_offset[WC == 1 && x >= LPT ? 1 : 0], to);
             }
         } else {
             missing |= ((row0 < 0 ? 1u : 0u) | (row1 < 0 ? 2u : 0u)) << 2 * at_stage;
 #pragma unroll
             for (int x = 0; x < LOADS; ++x) {
-                if (2 * LPT < WC && load0 >= 2 * LPT) break;
-                const bool upper = nth(x) * RPI >= 16;
+                const bool upper = nth(x) >= kHalf;
                 const int64_t row = upper ? row1 : row0;
                 const int behind = row < 0 ? 0 : min(nth(x) * RPI + ld_row, last) - (upper && last >= 16 ? 16 : 0);
                 load16_to_lds((is_v(x) ? v_base : k_base) + max(row, static_cast<int64_t>(0)) * ROWB, behind * ROWB + swizzled(x),
@@ -350,11 +391,11 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
             }
         }
     };
-    auto mine_of = [&](const TreePiece &pc) __attribute__((always_inline)) { return max(0, (pc.tile1 - pc.tile0 - wt + WT - 1) / WT); };
+    auto mine_of = [&](const TreePiece &pc) __attribute__((always_inline)) { return WT == 1 ? pc.tile1 - pc.tile0 : pc.solo ? pc.tiles : max(0, (pc.tile1 - pc.tile0 - wt + WT - 1) / WT); };
+    // A piece's first tile is requested with its queries, the others when both are there: all at once, and with them every workgroup's, the memory
+    // would answer in no fair order.
     auto begin_ring = [&](const TreePiece &pc, const Rows &rows) __attribute__((always_inline)) {
-        const int n = mine_of(pc);
-#pragma clang loop unroll(disable)                    // 20 KB of instructions less, which come from memory once per launch
-        for (int s = 0; s < min(n, kAhead); ++s) fetch(pc, rows, s, s);
+        if (mine_of(pc) > 0) fetch(pc, rows, 0, 0);
     };
     auto wait_stage = [&](int later) __attribute__((always_inline)) {      // all but the loads of `later` stages have landed
         if (later <= 0)
@@ -367,25 +408,41 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
             wait_vmcnt<3 * LOADS>();
     };
     static_assert(kAhead <= 4, "stages waited for");
-    // The lane's column of the queries, and what it sees of the draft.
-    struct Queries {
-        bf16x8_t q[NSL];
-        uint64_t sees;
-    };
-    auto fetch_queries = [&](const TreePiece &pc) __attribute__((always_inline)) {
-        Queries x;
-        const char *row = static_cast<const char *>(a.q) + static_cast<size_t>(column.row(a, pc.b, pc.h)) * (2 * D);
+    // The lane's column of the queries, and what it sees of the draft: requested, and read when they have come.
+    bf16x8_t qb[NSL];
+    uint64_t tree_word = 0;
+    auto request_queries = [&](const TreePiece &pc) __attribute__((always_inline)) {
+        constexpr int PPQ = QROWB / 16, RPQ = 64 / PPQ, QL = QBYTES / 1024, SHARE = kOwnQueries ? QL : (QL + NW - 1) / NW;      // loads, a wave's of them
+        const char *from = static_cast<const char *>(a.q) + (static_cast<size_t>(pc.b) * a.q_len * a.Hq + static_cast<size_t>(pc.h) * a.G) * QROWB;
+        const uint32_t to = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(FAIRKV_LDS_PTR(lds))) + kQueriesAt + (kOwnQueries ? wt * STAGEB : 0);
 #pragma unroll
-        for (int s = 0; s < NSL; ++s) x.q[s] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t *>(row + 32 * s + 16 * hi));
-        x.sees = a.tree ? static_cast<uint64_t>(a.tree[pc.b * a.q_len + column.node]) : ~0ull >> (63 - column.node);
-        return x;
+        for (int x = 0; x < SHARE; ++x) {
+            const int load = kOwnQueries ? x : wave * SHARE + x, r = load * RPQ + lane / PPQ;
+            if (QL % SHARE != 0 || QL < NW) {
+                if (load >= QL) break;
+            }
+            load16_to_lds_keep(from, q_byte[r] + ((lane % PPQ) ^ k_swizzle<QROWB>(r)) * 16, to + load * 1024);
+        }
+        tree_word = a.tree ? static_cast<uint64_t>(a.tree[pc.b * a.q_len + column.node]) : ~0ull >> (63 - column.node);
+    };
+    auto take_queries = [&]() __attribute__((always_inline)) {
+        asm volatile("" : "+v"(tree_word));           // waited for here: in the loop, every turn would wait for all tiles
+        drain_vmem();
+        if constexpr (!kOwnQueries) __syncthreads();
+        const uint32_t at_q = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(FAIRKV_LDS_PTR(lds))) + kQueriesAt + (kOwnQueries ? wt * STAGEB : wc * kTreeCols * QROWB) +
+                              l32 * QROWB + ((k_swizzle<QROWB>(l32) ^ hi) * 16);
+#pragma unroll
+        for (int s = 0; s < NSL; ++s) qb[s] = *lds_at<bf16x8_t>(at_q ^ (32 * s));
+#pragma unroll
+        for (int s = 0; s < NSL; ++s) asm volatile("" : "+v"(qb[s]));      // (and have left the LDS)
+        if constexpr (!kOwnQueries) __syncthreads();
     };
 
     TreePiece pc;
     if (!next_piece(pc)) return;
     Rows rows = rows_of(pc, 0, fetch_pages(pc, 0));
     begin_ring(pc, rows);
-    Queries qs = fetch_queries(pc);
+    request_queries(pc);
 
     for (;;) {
         TreePiece ahead;
@@ -394,7 +451,6 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
         if (more) pages_ahead = fetch_pages(ahead, 0);
 
         const int32_t base = pc.len - pc.nn;          // rows in front of the draft
-        const uint64_t sees = qs.sees & (pc.nn >= 64 ? ~0ull : (1ull << pc.nn) - 1);
         const int sc = a.n_scales > 1 ? pc.h : 0;
         // Scores to log2 units by a factor above 0 (a mask's -inf stays one; a factor of 0 is one under which every score is): the sign goes into q.
         const float s_mul = KV8 ? a.scale_log2 * a.k_scale[sc] : a.scale_log2, s_abs = fmaxf(fabsf(s_mul), 1e-37f);
@@ -410,14 +466,15 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
             rows = rows_of(pc, step, fetch_pages(pc, step));
             __builtin_amdgcn_s_waitcnt(0x0F70);       // said to the compiler, which would wait in every turn of the loop
         };
-        // The queries are here before the loop: waited for inside it, every turn would wait for all tiles.
-#pragma unroll
-        for (int s = 0; s < NSL; ++s) asm volatile("" : "+v"(qs.q[s]));
+        take_queries();
+        const uint64_t sees = tree_word & (pc.nn >= 64 ? ~0ull : (1ull << pc.nn) - 1);
         if (s_mul < 0.f) {
 #pragma unroll
-            for (int s = 0; s < NSL; ++s) qs.q[s] = __builtin_bit_cast(bf16x8_t, __builtin_bit_cast(u32x4_t, qs.q[s]) ^ 0x80008000u);
+            for (int s = 0; s < NSL; ++s) qb[s] = __builtin_bit_cast(bf16x8_t, __builtin_bit_cast(u32x4_t, qb[s]) ^ 0x80008000u);
         }
 
+#pragma clang loop unroll(disable)
+        for (int s = 1; s < min(n_mine, kAhead); ++s) fetch(pc, rows, s, s);
         int c_stage = 0, free_stage = WC == 1 ? 0 : STAGES - 1;      // the stage of this step, and the one that is filled in it
         auto turn = [&]() __attribute__((always_inline)) {
             c_stage = c_stage == STAGES - 1 ? 0 : c_stage + 1;
@@ -435,8 +492,8 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
                 }
                 if (step >= n_mine) continue;
             }
-            const uint32_t stage = c_stage * STAGEB;
-            const int32_t t0 = (pc.tile0 + wt + step * WT) * kTreeTok;
+            const uint32_t stage = c_stage * kStage;
+            const int32_t t0 = (pc.tile0 + pc.from + step * pc.apart) * kTreeTok;
             // ---- every LDS read of the tile, issued together: the scores wait for those of K, those of V come meanwhile ----
             bf16x8_t kw[NSL], va[2][NDB];
             i32x2_t kw8[NSL], va8[2][NDB];
@@ -469,7 +526,7 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
 #pragma unroll
             for (int s = 0; s < NSL; ++s) {
                 if constexpr (KV8) kw[s] = widen8(kw8[s]);
-                sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kw[s], qs.q[s], sacc, 0, 0, 0);
+                sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kw[s], qb[s], sacc, 0, 0, 0);
             }
             if constexpr (KV8) {
 #pragma unroll
@@ -613,13 +670,26 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
         if (more) {
             rows = rows_of(ahead, 0, pages_ahead);
             begin_ring(ahead, rows);
-            if (NW == 4 && whole) qs = fetch_queries(ahead);      // else behind the fold, or what follows a cut piece: there are not the registers
+            if (kSolo > 0 && pc.solo) request_queries(ahead);      // else behind the fold, whose memory it may be
         }
 
         const uint32_t out_row = column.row(a, pc.b, pc.h);
         const int c = wc * kTreeCols + l32;
         const float v_mul = KV8 ? a.v_scale[sc] : 1.f;
         float m_star = m_run, l_star = l_run;
+        if (kSolo > 0 && pc.solo) {                   // this wave has seen all of the pair
+            if (active) {
+#pragma unroll
+                for (int nb = 0; nb < NDB; ++nb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        write_tree_out<D>(a, out_row, 32 * nb + 8 * i + 4 * hi, make_float4(o[nb][4 * i], o[nb][4 * i + 1], o[nb][4 * i + 2], o[nb][4 * i + 3]), m_run,
+                                          l_run, v_mul);
+            }
+            if (!more) break;
+            pc = ahead;
+            continue;
+        }
         // What the workgroup's groups have found is added up through LDS: coordinates 32 nb .. + 31 by group nb % WT, as its block nb / WT.
         constexpr int kOwn = NDB < WT ? 1 : NDB / WT;
         const bool owns = wt < NDB;
@@ -640,7 +710,7 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
                 for (int i = 0; i < 16; ++i) o[nb][i] *= f;
             // block j of a round, of the group u = 1 .. WT - 1 places behind the one that adds it up
             auto place = [&](int j, int u) __attribute__((always_inline)) {
-                return reinterpret_cast<float4 *>(lds + RING + ((j * (WT - 1) + u - 1) * WC + wc) * kBlock) + hi * kTreeCols + l32;
+                return reinterpret_cast<float4 *>(lds + kFoldAt + ((j * (WT - 1) + u - 1) * WC + wc) * kBlock) + hi * kTreeCols + l32;
             };
 #pragma unroll
             for (int r = 0; r < NDB; r += kRound) {
@@ -674,9 +744,10 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
 #pragma unroll
             for (int nb = 0; nb < NDB; ++nb) res[nb] = o[nb];
         }
+        if constexpr (WT > 1 && (kFoldInRing || kQueriesInFold)) __syncthreads();      // the fold's memory is the ring's, or the queries', again
+        if (more) request_queries(ahead);
         auto four = [&](int q, int i) __attribute__((always_inline)) { return make_float4(res[q][4 * i], res[q][4 * i + 1], res[q][4 * i + 2], res[q][4 * i + 3]); };
         auto first_of = [&](int q, int i) __attribute__((always_inline)) { return 32 * (q * WT + wt) + 8 * i + 4 * hi; };      // coordinate of four(q, i)
-        if (NW != 4 && more && whole) qs = fetch_queries(ahead);
         bool finished = whole;
         if (!whole) {
             // ---- a piece of a pair that was cut: the last workgroup to come adds the pieces up, in their order, whichever it is ----
@@ -691,10 +762,15 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
             // Pieces first, first + apart, ... (n of them, this workgroup's the mine_th) into this workgroup's registers, if it is the last of them to come.
             auto join = [&](int32_t *counter, int first, int apart, int n, int mine_th) __attribute__((always_inline)) {
                 __syncthreads();                      // `counted` has been read
-                // The others are there already: nothing need be written.  (They counted in behind their results' arrival.)
-                if (threadIdx.x == 0) counted = __hip_atomic_load(counter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                __syncthreads();
-                bool last = __builtin_amdgcn_readfirstlane(counted) == n - 1;
+                // Where the others are there already, which the last piece's often are, nothing need be written.  (They counted in behind their
+                // results' arrival.)
+                bool last = false;
+                if (mine_th == n - 1) {
+                    if (threadIdx.x == 0) counted = __hip_atomic_load(counter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    __syncthreads();
+                    last = __builtin_amdgcn_readfirstlane(counted) == n - 1;
+                    __syncthreads();
+                }
                 if (!last) {
                     const size_t to = part(first + mine_th * apart);
                     if (active && owns) {
@@ -789,7 +865,6 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
                 for (int i = 0; i < 4; ++i) write_tree_out<D>(a, out_row, first_of(q, i), four(q, i), m_star, l_star, v_mul);
         }
         if (!more) break;
-        if (!whole) qs = fetch_queries(ahead);
         pc = ahead;
     }
 }

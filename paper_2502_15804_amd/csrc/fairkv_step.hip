@@ -127,12 +127,37 @@ namespace {
 struct TreeShape {
     int32_t waves, blocks, slots;
 };
-TreeShape tree_shape(int32_t cols, int32_t n_slots)
+// Rows that the pairs of a cache can have in all; what they do have is known on the device alone.
+int64_t cache_rows(const fairkv_cache *c)
 {
+    const int64_t rows = std::max<int64_t>(c->n_rows, 0);
+    return c->pages ? std::min(rows, static_cast<int64_t>(c->B) * c->Hkv * c->max_pages * c->page_rows) : rows;
+}
+// Waves side by side read a tile of K and V from LDS that came once for all of them; waves that take the tiles in turn cut a pair into fewer
+// pieces, and have fewer columns to hand over at the end of each.  So it is the work of a workgroup that decides, in tiles of 32 columns by 32
+// tokens, counted with full caches, a pair's own costs as 20.  Measured (bf16, D 128, 256 slots; us with 1, 2, 4, 8 waves side by side):
+//     192 columns, 1 x 8 pairs of 4000 rows, work 27           21   28   33   42
+//     128 columns, 2 x 8 pairs of 8000 rows, 67                34   36   39   52
+//     128 columns, 16 x 8 pairs of 512 rows, 72                22   19   28   28
+//     64 columns, 8 x 8 pairs of 4000 rows, 72                 36   41   46   55
+//     192 columns, 1 x 8 pairs of 16000 rows, 97               39   42   47   61
+//     192 columns, 4 x 8 pairs of 4000 rows, 109               41   40   40   47
+//     128 columns, 16 x 8 pairs of 2000 rows, 165              56   50   48   54   (8-bit: 43   36   40   58)
+//     64 columns, 32 x 8 pairs of 2000 rows, 165               65   63   67   82
+//     512 columns, 4 x 8 pairs of 4000 rows, 290               74   63   54   64
+//     128 columns, 16 x 8 pairs of 4000 rows, 290              96   78   72   90
+//     512 columns, 16 x 8 pairs of 4000 rows, 1160            294  244  167  160
+// More waves than columns need gain nothing at any size.  Slots come in eights where there are as many, so that the workgroups with the same
+// rows and other columns, n_slots further on, share an XCD and its cache (192 columns, 1 x 8 pairs of 16000 rows: 39 us, against 60 with 42 slots).
+TreeShape tree_shape(const fairkv_cache *c, int32_t Hq, int32_t q_len, int32_t n_slots)
+{
+    const int32_t cols = Hq / c->Hkv * q_len, blocks32 = (cols + 31) / 32;
+    const int64_t work = (cache_rows(c) / 32 + 20 * static_cast<int64_t>(c->B) * c->Hkv) * blocks32 / n_slots;
     TreeShape s{};
-    s.waves = cols <= 32 ? 1 : cols <= 64 ? 2 : cols <= 128 ? 4 : 8;
+    s.waves = std::min(work < 80 ? 1 : work < 200 ? 2 : work < 640 ? 4 : 8, blocks32 <= 2 ? blocks32 : blocks32 <= 4 ? 4 : 8);
     s.blocks = (cols + 32 * s.waves - 1) / (32 * s.waves);
     s.slots = std::max(1, n_slots / s.blocks);
+    if (s.slots > 8) s.slots &= ~7;
     return s;
 }
 
@@ -180,7 +205,7 @@ void launch_tree(int waves, bool fine, const TreeArgs &a, int32_t blocks, hipStr
 extern "C" size_t fairkv_tree_workspace_bytes(const fairkv_cache *c, int32_t Hq, int32_t q_len, int32_t n_slots)
 {
     if (check_tree(c, Hq, q_len, n_slots) != FAIRKV_OK) return 0;
-    const TreeSpace s = tree_space(tree_shape(Hq / c->Hkv * q_len, n_slots), c->D, n_slots);
+    const TreeSpace s = tree_space(tree_shape(c, Hq, q_len, n_slots), c->D, n_slots);
     return s.counters + s.ml + s.o;
 }
 
@@ -204,7 +229,7 @@ extern "C" int fairkv_decode_attn_tree(const fairkv_cache *c, const void *q, con
     if (out_dtype != FAIRKV_BF16 && out_dtype != FAIRKV_F32) return FAIRKV_EUNSUPPORTED;
     if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16) || (tree && !aligned(tree, 8))) return FAIRKV_EINVAL;
     if (static_cast<int64_t>(c->B) * q_len * Hq * c->D > INT32_MAX) return FAIRKV_EINVAL;
-    const TreeShape shape = tree_shape(Hq / c->Hkv * q_len, n_slots);
+    const TreeShape shape = tree_shape(c, Hq, q_len, n_slots);
     const TreeSpace space = tree_space(shape, c->D, n_slots);
     if (!workspace || workspace_bytes < space.counters + space.ml + space.o) return FAIRKV_EWORKSPACE;
 

@@ -331,6 +331,20 @@ def test_attention_of_a_tree(Hkv, G, q_len, dtype, D, page, out_dtype):
     _compare(s, *_attend(s, Hkv * G, q_len, out_dtype, tree), tree, None)
 
 
+@pytest.mark.parametrize("n_slots", [1, 2, 4, 8, 32])
+@pytest.mark.parametrize("dtype,D,page", [("bf16", 128, 16), ("bf16", 64, 0), ("kv8", 128, 0), ("kv8", 64, 32)])
+@pytest.mark.parametrize("G,q_len", [(4, 13), (8, 16), (8, 24), (4, 64)])
+def test_few_workgroups_with_many_columns_each(G, q_len, dtype, D, page, n_slots):
+    """The fewer workgroups, the more columns has one: 32 to 256 here."""
+    rng = np.random.default_rng(q_len)
+    lens = np.array([[400, 33], [0, 129], [31, 257]]) + q_len
+    s = Setup(lens, 1, D, dtype, page, seed=q_len + G, scales=True)
+    tree = _random_tree(3, q_len, rng)
+    n_new = np.array([q_len, q_len - 1, q_len // 2])
+    for out_dtype in (torch.float32, torch.bfloat16):
+        _compare(s, *_attend(s, 2 * G, q_len, out_dtype, tree, n_new, n_slots, scale=-0.1 if n_slots == 2 else None), tree, n_new)
+
+
 @pytest.mark.parametrize("q_len,G", [(1, 4), (4, 8), (16, 4), (40, 8)])
 def test_attention_of_a_chain_of_ragged_drafts_and_short_pairs(q_len, G):
     """Pairs without rows, shorter than their draft, drafts of no token, counts out of range: what is no node is left as it was."""
@@ -342,9 +356,10 @@ def test_attention_of_a_chain_of_ragged_drafts_and_short_pairs(q_len, G):
     _compare(s, *_attend(s, 2 * G, q_len, torch.float32, None, n_new), None, n_new)
 
 
+@pytest.mark.parametrize("n_slots", [None, 1, 4])
 @pytest.mark.parametrize("page", [0, 16])
 @pytest.mark.parametrize("G,q_len", [(2, 8), (8, 16), (8, 64)])
-def test_masks_that_leave_rows_empty(G, q_len, page):
+def test_masks_that_leave_rows_empty(G, q_len, page, n_slots):
     """Nodes that see nothing at all, nodes that see every draft row, bits behind the draft."""
     rng = np.random.default_rng(5)
     n_new = rng.integers(1, q_len + 1, 6)
@@ -352,12 +367,13 @@ def test_masks_that_leave_rows_empty(G, q_len, page):
     tree[:, 0], tree[1] = 0, ~np.uint64(0)
     lens = np.stack([n_new, n_new + 40], 1)                # the first head has nothing but the draft
     s = Setup(lens, 0, 128, page=page, seed=1)
-    _compare(s, *_attend(s, 2 * G, q_len, torch.float32, tree, n_new), tree, n_new)
+    _compare(s, *_attend(s, 2 * G, q_len, torch.float32, tree, n_new, n_slots), tree, n_new)
 
 
+@pytest.mark.parametrize("n_slots", [None, 1, 2, 8])
 @pytest.mark.parametrize("dtype", ["bf16", "kv8"])
 @pytest.mark.parametrize("G,q_len", [(4, 6), (8, 12), (8, 40)])
-def test_infinite_and_nan_rows_count_for_the_nodes_that_see_them(G, q_len, dtype):
+def test_infinite_and_nan_rows_count_for_the_nodes_that_see_them(G, q_len, dtype, n_slots):
     """Values of draft rows that some nodes do not see, rows behind the last one and rows of no pair."""
     rng = np.random.default_rng(11)
     lens = np.array([[50, 33], [q_len, 97]]) + np.array([[q_len], [0]])
@@ -376,12 +392,12 @@ def test_infinite_and_nan_rows_count_for_the_nodes_that_see_them(G, q_len, dtype
             cell = torch.tensor([value]).to(s.v.dtype).to(DEV)
             _bits(s.v[r])[(u * 7) * s.v.element_size():(u * 7 + 1) * s.v.element_size()] = _bits(cell)
     for out_dtype in (torch.float32, torch.bfloat16):
-        _compare(s, *_attend(s, 2 * G, q_len, out_dtype, tree), tree, None)
+        _compare(s, *_attend(s, 2 * G, q_len, out_dtype, tree, n_slots=n_slots), tree, None)
     # a NaN key of a row that only some see
     for p in range(4):
         poison(s.k, s.row(p, int(lens.reshape(-1)[p]) - 1), math.nan)
         poison(s.v, s.row(p, int(lens.reshape(-1)[p]) - 1), 1.0)
-    q, out, lse, scale = _attend(s, 2 * G, q_len, torch.float32, tree)
+    q, out, lse, scale = _attend(s, 2 * G, q_len, torch.float32, tree, n_slots=n_slots)
     seen = (tree >> np.uint64(q_len - 1) & np.uint64(1)).astype(bool)
     nan = np.isnan(out.cpu().numpy()).all(-1)
     assert nan[seen].all() and not np.isnan(lse.cpu().numpy())[~seen].any()
