@@ -56,18 +56,47 @@ struct TreeArgs {
     float k_scale[kCacheScales], v_scale[kCacheScales];
 };
 
-// log2 of how rows are swizzled: 16-byte piece c of row r lies at piece c ^ swz(r).  K is read a row per lane: consecutive rows that fill
-// the 256 bytes of all banks take different pieces.  V is read by the transposing instruction, 64 (8-bit: 32) bytes of each of 4 (8) rows.
+// Where a tile's rows lie in LDS.  A wave-wide load brings a chunk of 1 KB, kRows whole rows, and may put its 64 pieces of 16 bytes in any
+// order: groups of `group` pieces, in a group the rows, in a row's place the group's pieces in turn.  So the pieces that a lane reads of its row
+// are constants apart, which the instructions' immediate offsets hold.  K is read a row per lane: 16 rows (8-bit: twice as many, half a piece
+// of each) take all 64 banks when a row is 16 `group` bytes behind the last and the chunks 16 bytes further apart.  V is read by the
+// transposing instruction, 64 bytes of 4 rows or 32 bytes of 8 (8-bit; 0 .. 3 and 8 .. 11), which lie in one run of 256 bytes or two halves of it.
+template <int ROWB, bool KV8>
+struct TreeTile {
+    static constexpr int kRows = 1024 / ROWB, kChunks = kTreeTok / kRows;
+    static constexpr int kGroupK = ROWB == 256 ? 4 : ROWB == 128 ? 2 : 1, kGroupV = KV8 ? 2 : 4;
+    static constexpr int kPitchK = ROWB == 64 ? 1024 : 1040, kPitchV = ROWB == 128 && KV8 ? 1152 : 1024;      // bytes from chunk to chunk
+    static constexpr int kBytesK = kChunks * kPitchK, kStage = (kBytesK + kChunks * kPitchV + 255) / 256 * 256;
+    // place of V's row r in its chunk and the row of a place: 64-byte rows with 4 .. 7 and 8 .. 11 swapped
+    static __device__ __forceinline__ constexpr int place_v(int r) { return ROWB == 64 ? (r & 3) | (r >> 3 & 1) << 2 | (r >> 2 & 1) << 3 : r; }
+    static __device__ __forceinline__ constexpr int piece(int group, int p) { return (p / group * kRows * group + p % group) * 16; }      // byte of piece p of row 0
+};
+
+// N wave-wide loads of 1 KB that lie 1 KB apart in memory, PITCH bytes apart in LDS: the instruction's immediate offset moves both addresses,
+// so M0 is written once.  off[i] + PITCH i is the byte offset of load i from base.
+template <int N, int PITCH>
+__device__ __forceinline__ void load_chunks_to_lds(const void *base, const uint32_t (&off)[N], uint32_t lds_base)
+{
+    static_assert(N == 2 || N == 4, "loads of a run");
+    uint64_t from;
+    if constexpr (N == 2)
+        asm volatile("s_mov_b32 m0, %4\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %1, %0 nt\n\t"
+                     "global_load_lds_dwordx4 %2, %0 offset:%5 nt"
+                     : "=&s"(from) : "v"(off[0]), "v"(off[1]), "s"(base), "s"(lds_base), "n"(PITCH) : "memory", "m0");
+    else
+        asm volatile("s_mov_b32 m0, %6\n\ts_mov_b64 %0, %5\n\tglobal_load_lds_dwordx4 %1, %0 nt\n\t"
+                     "global_load_lds_dwordx4 %2, %0 offset:%7 nt\n\t"
+                     "global_load_lds_dwordx4 %3, %0 offset:%8 nt\n\t"
+                     "global_load_lds_dwordx4 %4, %0 offset:%9 nt"
+                     : "=&s"(from) : "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base), "s"(lds_base), "n"(PITCH), "n"(2 * PITCH), "n"(3 * PITCH)
+                     : "memory", "m0");
+}
+
+// Piece c of row r of the queries lies at piece c ^ query_swizzle(r): rows that fill the 256 bytes of all banks take different ones.
 template <int ROWB>
-__device__ __forceinline__ constexpr int k_swizzle(int r)
+__device__ __forceinline__ constexpr int query_swizzle(int r)
 {
     return r / (256 / ROWB) % (ROWB / 16);
-}
-template <int ROWB, bool KV8>
-__device__ __forceinline__ constexpr int v_swizzle(int r)
-{
-    if (!KV8) return ROWB == 256 ? 4 * (r & 3) : 4 * (r >> 1 & 1);
-    return ROWB == 128 ? 2 * ((r >> 1 & 1) | (r >> 3 & 1) << 1) : 2 * (r >> 3 & 1);
 }
 
 __device__ __forceinline__ float halves_max(float x)
@@ -151,9 +180,9 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
 {
     constexpr int NW = WC * WT, NT = NW * 64, CB = WC * kTreeCols;
     constexpr int ROWB = KV8 ? D : 2 * D;             // bytes of a row of K or V
-    constexpr int PPR = ROWB / 16, RPI = 64 / PPR;    // 16-byte pieces of a row, rows of a wave-wide load
-    constexpr int LPT = kTreeTok / RPI;               // wave-wide loads of a tile of K
-    constexpr int TILEB = kTreeTok * ROWB, STAGEB = 2 * TILEB;
+    using Tile = TreeTile<ROWB, KV8>;
+    constexpr int RPI = Tile::kRows, LPT = Tile::kChunks;      // rows of a wave-wide load, loads of a tile of K
+    constexpr int STAGEB = Tile::kStage;
     constexpr int LOADS = 2 * LPT >= WC ? 2 * LPT / WC : 1;     // a wave's share of the loads of a stage
     constexpr int NSL = D / 16, NDB = D / 32;
     constexpr int kAhead = WC == 1 ? STAGES : STAGES - 1;       // tiles on their way while one is waited for
@@ -262,13 +291,12 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
     const Column column(a, min(col, a.cols - 1));
     const uint32_t ring = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(FAIRKV_LDS_PTR(lds))) + wt * STAGEB;      // the group's stage 0
     constexpr uint32_t kStage = WT * STAGEB;          // from one stage of a group to the next
-    const int ld_row = lane / PPR, ld_col = lane % PPR;
-    // Where the lane reads in stage 0: its row of K, and its share of the transposing reads of V.  Pieces further on in a row are a bit pattern
-    // away, since swizzles are patterns too, rows further on whole rows: swizzles repeat every 8 (8-bit: 16) rows.
-    const uint32_t k_rd = (ring + l32 * ROWB + k_swizzle<ROWB>(l32) * 16 + (KV8 ? hi * 8 : 0)) ^ (KV8 ? 0 : hi * 16);
+    // Where the lane reads in stage 0: its row of K, and its share of the transposing reads of V.
     const int x16 = lane & 15, dq = lane >> 4 & 1;
     const int v_row = KV8 ? (x16 < 8 ? x16 >> 1 : (x16 >> 1) + 4) + 4 * hi : 4 * hi + (x16 >> 2);
-    const uint32_t v_rd = ring + TILEB + v_row * ROWB + ((KV8 ? dq : 2 * dq + ((x16 & 3) >> 1)) ^ v_swizzle<ROWB, KV8>(v_row)) * 16 + (x16 & 1) * 8;
+    const uint32_t k_rd = ring + l32 / RPI * Tile::kPitchK + l32 % RPI * Tile::kGroupK * 16 + (KV8 ? hi * 8 : hi * 16);
+    const uint32_t v_rd = ring + Tile::kBytesK + v_row / RPI * Tile::kPitchV + Tile::place_v(v_row % RPI) * Tile::kGroupV * 16 +
+                          (KV8 ? dq : 2 * dq + ((x16 & 3) >> 1)) * 16 + (x16 & 1) * 8;
     const char *const k_base = static_cast<const char *>(a.k), *const v_base = static_cast<const char *>(a.v);
 
     // ---- the pieces of the share: what 64 pairs' pieces need to know is held in lanes ----
@@ -348,20 +376,26 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
     const bool loads = 2 * LPT >= WC || load0 < 2 * LPT;
     auto is_v = [&](int x) __attribute__((always_inline)) { return WC == 1 ? x >= LPT : load0 >= LPT; };
     auto nth = [&](int x) __attribute__((always_inline)) { return WC == 1 ? x % LPT : load0 % LPT + x; };      // load of the tile of K or V
-    auto swizzled = [&](int x) __attribute__((always_inline)) {      // byte of its row that the lane fetches in load x
-        const int r = nth(x) * RPI + ld_row;
-        return static_cast<uint32_t>((ld_col ^ (is_v(x) ? v_swizzle<ROWB, KV8>(r) : k_swizzle<ROWB>(r))) * 16);
-    };
-    constexpr int kKinds = WC == 1 ? 2 : 1;           // of a wave's runs: swizzles are the same from half to half
-    uint32_t run_offset[kKinds][kRun];
+    // The row of its chunk that the lane fetches of K and of V, and the byte of that row.
+    constexpr int kKinds = WC == 1 ? 2 : 1;           // of a wave's loads
+    int ld_row[kKinds];
+    uint32_t ld_byte[kKinds], run_offset[kKinds][kRun];
+    constexpr int kBehind = 512;                      // runs start so many bytes early: from load to load more is added to both addresses than to the global one
 #pragma unroll
-    for (int kind = 0; kind < kKinds; ++kind)
+    for (int kind = 0; kind < kKinds; ++kind) {
+        const bool v = is_v(kind * LPT);
+        const int group = v ? Tile::kGroupV : Tile::kGroupK, at_row = lane / group % RPI;
+        ld_row[kind] = v ? Tile::place_v(at_row) : at_row;
+        ld_byte[kind] = (lane / (RPI * group) * group + lane % group) * 16;
 #pragma unroll
         for (int x = 0; x < kRun; ++x) {
-            run_offset[kind][x] = ld_row * ROWB + swizzled(kind * LPT + x);      // 1024 x behind that is the load's own
+            run_offset[kind][x] = kBehind + ld_row[kind] * ROWB + ld_byte[kind] - x * ((v ? Tile::kPitchV : Tile::kPitchK) - 1024);
             asm volatile("" : "+v"(run_offset[kind][x]));
         }
+    }
+    static_assert((kRun - 1) * (Tile::kPitchV - 1024) <= kBehind && (kRun - 1) * (Tile::kPitchK - 1024) <= kBehind, "offsets are not negative");
     uint32_t missing = 0;
+    auto place_of = [&](uint32_t stage, int x) __attribute__((always_inline)) { return stage + (is_v(x) ? Tile::kBytesK + nth(x) * Tile::kPitchV : nth(x) * Tile::kPitchK); };
     auto fetch = [&](const TreePiece &pc, const Rows &rows, int step, int at_stage) __attribute__((always_inline)) {
         const int last = pc.len - 1 - (pc.tile0 + pc.from + step * pc.apart) * kTreeTok;
         const uint32_t stage = ring + at_stage * kStage;
@@ -372,22 +406,24 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
         if (full) {
 #pragma unroll
             for (int x = 0; x < LOADS; x += kRun) {
-                const char *from = (is_v(x) ? v_base : k_base) + ((nth(x) >= kHalf ? row1 : row0) + nth(x) % kHalf * RPI) * ROWB;
-                const uint32_t to = stage + (is_v(x) ? TILEB : 0) + nth(x) * 1024;
+                const char *from = (is_v(x) ? v_base : k_base) + ((nth(x) >= kHalf ? row1 : row0) + nth(x) % kHalf * RPI) * ROWB - kBehind;
+                const uint32_t (&offsets)[kRun] = run_offset[WC == 1 && x >= LPT ? 1 : 0];
                 if constexpr (kRun == 1)
-                    load16_to_lds(from, run_offset[WC == 1 && x >= LPT ? 1 : 0][0], to);
+                    load16_to_lds(from, offsets[0], place_of(stage, x));
+                else if (is_v(x))
+                    load_chunks_to_lds<kRun, Tile::kPitchV>(from, offsets, place_of(stage, x));
                 else
-                    load_tile_to_lds<kRun>(from, run_offset[WC == 1 && x >= LPT ? 1 : 0], to);
+                    load_chunks_to_lds<kRun, Tile::kPitchK>(from, offsets, place_of(stage, x));
             }
         } else {
             missing |= ((row0 < 0 ? 1u : 0u) | (row1 < 0 ? 2u : 0u)) << 2 * at_stage;
 #pragma unroll
             for (int x = 0; x < LOADS; ++x) {
+                const int kind = WC == 1 && x >= LPT ? 1 : 0;
                 const bool upper = nth(x) >= kHalf;
                 const int64_t row = upper ? row1 : row0;
-                const int behind = row < 0 ? 0 : min(nth(x) * RPI + ld_row, last) - (upper && last >= 16 ? 16 : 0);
-                load16_to_lds((is_v(x) ? v_base : k_base) + max(row, static_cast<int64_t>(0)) * ROWB, behind * ROWB + swizzled(x),
-                              stage + (is_v(x) ? TILEB : 0) + nth(x) * 1024);
+                const int behind = row < 0 ? 0 : min(nth(x) * RPI + ld_row[kind], last) - (upper && last >= 16 ? 16 : 0);
+                load16_to_lds((is_v(x) ? v_base : k_base) + max(row, static_cast<int64_t>(0)) * ROWB, behind * ROWB + ld_byte[kind], place_of(stage, x));
             }
         }
     };
@@ -421,7 +457,7 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
             if (QL % SHARE != 0 || QL < NW) {
                 if (load >= QL) break;
             }
-            load16_to_lds_keep(from, q_byte[r] + ((lane % PPQ) ^ k_swizzle<QROWB>(r)) * 16, to + load * 1024);
+            load16_to_lds_keep(from, q_byte[r] + ((lane % PPQ) ^ query_swizzle<QROWB>(r)) * 16, to + load * 1024);
         }
         tree_word = a.tree ? static_cast<uint64_t>(a.tree[pc.b * a.q_len + column.node]) : ~0ull >> (63 - column.node);
     };
@@ -430,7 +466,7 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
         drain_vmem();
         if constexpr (!kOwnQueries) __syncthreads();
         const uint32_t at_q = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(FAIRKV_LDS_PTR(lds))) + kQueriesAt + (kOwnQueries ? wt * STAGEB : wc * kTreeCols * QROWB) +
-                              l32 * QROWB + ((k_swizzle<QROWB>(l32) ^ hi) * 16);
+                              l32 * QROWB + ((query_swizzle<QROWB>(l32) ^ hi) * 16);
 #pragma unroll
         for (int s = 0; s < NSL; ++s) qb[s] = *lds_at<bf16x8_t>(at_q ^ (32 * s));
 #pragma unroll
@@ -500,20 +536,21 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
 #pragma unroll
             for (int s = 0; s < NSL; ++s) {
                 if constexpr (KV8)
-                    kw8[s] = *lds_at<i32x2_t>((k_rd + stage) ^ (16 * s));
+                    kw8[s] = *lds_at<i32x2_t>(k_rd + stage + Tile::piece(Tile::kGroupK, s));
                 else
-                    kw[s] = *lds_at<bf16x8_t>((k_rd + stage) ^ (32 * s));
+                    kw[s] = *lds_at<bf16x8_t>(k_rd + stage + Tile::piece(Tile::kGroupK, 2 * s));
             }
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int nb = 0; nb < NDB; ++nb) {
                     if constexpr (KV8) {
-                        va8[j][nb] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(lds_at<i32x2_t>(((v_rd + stage) ^ (32 * nb)) + j * 16 * ROWB));
+                        const uint32_t at_v = v_rd + stage + Tile::piece(Tile::kGroupV, 2 * nb) + j * (16 / RPI) * Tile::kPitchV;
+                        va8[j][nb] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(lds_at<i32x2_t>(at_v));
                     } else {
-                        const uint32_t at_v = ((v_rd + stage) ^ (64 * nb)) + j * 16 * ROWB;
+                        const uint32_t at_v = v_rd + stage + Tile::piece(Tile::kGroupV, 4 * nb) + j * (16 / RPI) * Tile::kPitchV;
                         const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<i16x4_t>(at_v)));
-                        const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<i16x4_t>(at_v + 8 * ROWB)));
+                        const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<i16x4_t>(at_v + 8 / RPI * Tile::kPitchV)));
                         va[j][nb] = __builtin_bit_cast(bf16x8_t, u32x4_t{x.x, x.y, y.x, y.y});
                     }
                 }
