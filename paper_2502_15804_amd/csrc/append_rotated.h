@@ -24,7 +24,7 @@ struct RotateArgs {
     RowMap rows;
     int64_t q_stride, k_stride, v_stride;
     int32_t B, Hq, Hkv, q_len, n_pos, rot, pairs;
-    int32_t q_groups, head_slots;         // workgroups for the queries; rows of one token that a pass of a workgroup covers
+    int32_t q_groups, head_slots, passes; // workgroups for the queries; rows of one token that a pass of a workgroup covers; its passes
     int32_t n_scales;
     float eps;
     float k_scale[kCacheScales], v_scale[kCacheScales];      // reciprocals
@@ -118,6 +118,25 @@ __device__ __forceinline__ Turn turn_of(const RotateArgs &a, int32_t pos, int pi
     return t;
 }
 
+// x of another lane of the same 16, by the wave's own data paths.
+template <int kCtrl>
+__device__ __forceinline__ float from_lane(float x)
+{
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), kCtrl, 0xf, 0xf, false));
+}
+constexpr int kXor1 = 0xb1, kXor2 = 0x4e, kQuadMirror = 0x1b, kHalfMirror = 0x141, kMirror = 0x140, kRotate8 = 0x128;
+
+// The sum over a row's L lanes, in each of them.
+template <int L>
+__device__ __forceinline__ float row_sum(float x)
+{
+    static_assert(L == 8 || L == 16, "lanes of a row");
+    x += from_lane<kXor1>(x);
+    x += from_lane<kXor2>(x);
+    x += from_lane<kHalfMirror>(x);        // quads are uniform by now, and so are halves
+    return L == 16 ? x + from_lane<kMirror>(x) : x;
+}
+
 // Norm and rotation of a row whose D / 8 lanes sit side by side in a wave; all of them are here.
 template <int D>
 __device__ __forceinline__ void norm_and_turn(const RotateArgs &a, float (&x)[kRow8], bool norm, const float (&weight)[kRow8], const Turn &t, int piece)
@@ -126,9 +145,7 @@ __device__ __forceinline__ void norm_and_turn(const RotateArgs &a, float (&x)[kR
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < kRow8; ++i) sum = fmaf(x[i], x[i], sum);
-#pragma unroll
-        for (int o = 1; o < D / kRow8; o *= 2) sum += __shfl_xor(sum, o, 64);
-        const float inv = 1.f / sqrtf(sum * (1.f / D) + a.eps);
+        const float inv = rsqrtf(row_sum<D / kRow8>(sum) * (1.f / D) + a.eps);
 #pragma unroll
         for (int i = 0; i < kRow8; ++i) x[i] = x[i] * inv * weight[i];
     }
@@ -137,6 +154,9 @@ __device__ __forceinline__ void norm_and_turn(const RotateArgs &a, float (&x)[kR
     if (a.pairs) {
 #pragma unroll
         for (int i = 0; i < kRow8; ++i) y[i] = x[i ^ 1];
+    } else if (a.rot == D) {               // half the row's lanes away
+#pragma unroll
+        for (int i = 0; i < kRow8; ++i) y[i] = D == 128 ? from_lane<kRotate8>(x[i]) : from_lane<kQuadMirror>(from_lane<kHalfMirror>(x[i]));
     } else {
         const int apart = a.rot / (2 * kRow8), lane = threadIdx.x & 63;
         const int from = piece < apart ? lane + apart : piece < 2 * apart ? lane - apart : lane;
@@ -154,9 +174,12 @@ __device__ __forceinline__ int32_t new_tokens(const int32_t *n_new, int b, int q
 }
 __device__ __forceinline__ bool in_table(const RotateArgs &a, int32_t pos) { return !a.table || (pos >= 0 && pos < a.n_pos); }
 
-// T: element type of q, k_new and v_new; C: of the cache.  Workgroups 0 .. q_groups - 1 turn queries: one has kThreads / (D / 8) rows in
-// hand at a time, head_slots heads of each of several tokens, so that a lane's cosines and sines serve all the heads it meets.  The others have
-// whole pairs: all the new rows of a pair are one workgroup's, which has read the pair's length before it writes it.
+// T: element type of q, k_new and v_new; C: of the cache.  Workgroups 0 .. q_groups - 1 turn queries: a pass of one has 256 / (D / 8) rows in hand,
+// head_slots heads of each of several tokens, so that a lane's cosines and sines serve all the heads it meets; it makes `passes` of them, and
+// the next rows are requested before the ones in hand are turned.  The others have whole pairs: all the new rows of a pair are one
+// workgroup's, which has read the pair's length before it writes it.
+// Bound by memory, at 5.1 TB/s with all tokens there (128 x 64 tokens, 64 + 16 heads of 128, 336 MB in 66 us; without norms and rotation
+// 5.8 TB/s: the arithmetic shows through); a step of one sequence is 4 us, three dependent reads after a launch.
 template <typename T, typename C, int D>
 __global__ __launch_bounds__(256) void fairkv_append_rotated_kernel(RotateArgs a)
 {
@@ -170,32 +193,61 @@ __global__ __launch_bounds__(256) void fairkv_append_rotated_kernel(RotateArgs a
     for (int i = 0; i < kRow8; ++i) weight[i] = norm ? norm[piece * kRow8 + i] : 1.f;
 
     if (static_cast<int>(blockIdx.x) < a.q_groups) {
-        const int64_t token = static_cast<int64_t>(blockIdx.x) * (kSlots / a.head_slots) + slot / a.head_slots;
-        if (token >= static_cast<int64_t>(a.B) * a.q_len) return;          // whole rows: the lanes of the others stay
-        const int b = static_cast<int>(token / a.q_len), i = static_cast<int>(token % a.q_len);
-        const int32_t pos = a.table ? a.pos[token] : 0;
-        if (i >= new_tokens(a.n_new, b, a.q_len)) return;
-        if (!in_table(a, pos)) {
-            if (slot % a.head_slots == 0 && piece == 0 && a.bad) atomicAdd(a.bad, 1);
-            return;
-        }
-        const Turn t = turn_of(a, pos, piece);
-        const char *src = a.q + (token * a.q_stride + piece * kRow8) * EB;
-        char *dst = a.q_out + (token * a.Hq * D + piece * kRow8) * EB;
+        // lane j of every wave looks after token j of the workgroup's: whether there is anything to do, and at which position
+        const int each = kSlots / a.head_slots, n_tokens = a.B * a.q_len, lane = threadIdx.x & 63;
+        const int token0 = static_cast<int>(blockIdx.x) * each * a.passes;      // (tokens fit 31 bits, and 64 more)
+        const int looked = min(token0 + lane, n_tokens - 1), of_b = looked / a.q_len;
+        const bool live = lane < each * a.passes && token0 + lane < n_tokens && looked - of_b * a.q_len < new_tokens(a.n_new, of_b, a.q_len);
+        const int32_t held_pos = a.table ? a.pos[looked] : 0;
+        const bool ok = live && in_table(a, held_pos);
+        if (live && !ok && threadIdx.x < 64 && a.bad) atomicAdd(a.bad, 1);
+        const uint64_t todo = __builtin_amdgcn_ballot_w64(ok);
+        if (todo == 0) return;
+        const int of_pass = slot / a.head_slots, h_slot = slot % a.head_slots;
         constexpr int kAhead = 4;
-        for (int h0 = slot % a.head_slots; h0 < a.Hq; h0 += kAhead * a.head_slots) {
+        struct Rows {
             typename Eight<T>::raw_t raw[kAhead];
+            Turn t;
+            int32_t token, h0;             // token < 0: nothing
+        };
+        int pass = 0, h_next = 0;          // of the rows to be requested next
+        auto request = [&](Rows &x) __attribute__((always_inline)) {      // false: no more
+            while (pass < a.passes && (todo >> (pass * each) & (~0ull >> (64 - each))) == 0) ++pass;
+            if (pass >= a.passes) return false;
+            const int j = pass * each + of_pass;
+            const int32_t pos = __shfl(held_pos, j, 64);
+            x.token = todo >> j & 1 ? token0 + j : -1, x.h0 = h_next + h_slot;
+            if (x.token >= 0) {
+                const char *src = a.q + (x.token * a.q_stride + piece * kRow8) * EB;
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) raw[u] = Eight<T>::load(src + static_cast<int64_t>(min(h0 + u * a.head_slots, a.Hq - 1)) * D * EB);
+                for (int u = 0; u < kAhead; ++u) x.raw[u] = Eight<T>::load(src + static_cast<int64_t>(min(x.h0 + u * a.head_slots, a.Hq - 1)) * D * EB);
+                x.t = turn_of(a, pos, piece);
+            }
+            h_next += kAhead * a.head_slots;
+            if (h_next >= a.Hq) h_next = 0, ++pass;
+            return true;
+        };
+        auto turn = [&](const Rows &x) __attribute__((always_inline)) {
+            if (x.token < 0) return;       // whole rows: the lanes of the others stay
+            char *dst = a.q_out + (static_cast<int64_t>(x.token) * a.Hq * D + piece * kRow8) * EB;
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const int h = h0 + u * a.head_slots;
+                const int h = x.h0 + u * a.head_slots;
                 if (h >= a.Hq) break;
-                float x[kRow8];
-                Eight<T>::floats(raw[u], x);
-                norm_and_turn<D>(a, x, norm != nullptr, weight, t, piece);
-                Eight<T>::store(dst + static_cast<int64_t>(h) * D * EB, x);
+                float y[kRow8];
+                Eight<T>::floats(x.raw[u], y);
+                norm_and_turn<D>(a, y, norm != nullptr, weight, x.t, piece);
+                Eight<T>::store(dst + static_cast<int64_t>(h) * D * EB, y);
             }
+        };
+        Rows one, other;
+        bool more = request(one);
+        while (more) {
+            more = request(other);
+            turn(one);
+            if (!more) break;
+            more = request(one);
+            turn(other);
         }
         return;
     }
@@ -240,8 +292,7 @@ __global__ __launch_bounds__(256) void fairkv_append_rotated_kernel(RotateArgs a
         float x[kRow8], y[kRow8];
         Eight<T>::floats(k_raw[u], x);
         Eight<T>::floats(v_raw[u], y);
-        const Turn t = turn_of(a, pos[u], piece);
-        norm_and_turn<D>(a, x, norm != nullptr, weight, t, piece);
+        norm_and_turn<D>(a, x, norm != nullptr, weight, turn_of(a, pos[u], piece), piece);
         if constexpr (CB == 1) {
             const int sc = a.n_scales > 1 ? h : 0;
 #pragma unroll
