@@ -34,9 +34,11 @@ constexpr int kTreeTok = 32;          // tokens of a tile
 constexpr int kTreeCols = 32;         // columns of a wave
 constexpr int kJoin = 8;              // pieces of a pair that are added up at once
 constexpr int kLevels = 6;            // of such sums, for pairs in up to 8^6 pieces
-// What a piece costs besides its tiles, in tiles: queries, fold, outputs.  A pair that one wave has alone has next to none of that.  Measured with
-// 6, 9 and 13 a piece: 128 columns, 16 x 8 pairs of 2000 rows in fp32 63, 59 and 56 us (one wave side by side), 56, 52 and 53 us (four).
-constexpr int kPieceCost = 10, kSoloCost = 2;
+// What a piece costs besides its tiles, in tiles: queries, fold, outputs; a short pair that one wave has alone has no fold.  Measured with 6, 9
+// and 13 a piece: 128 columns, 16 x 8 pairs of 2000 rows in fp32 63, 59 and 56 us (one wave side by side), 56, 52 and 53 us (four).  Short pairs
+// of up to 4 or 8 tiles at 2 or 4: 32 x 8 heavy-tailed pairs of 32 columns 40.2 and 39.0, 43.6 and 41.8 us; 128 x 8 of 8 columns 34.4 and 33.2,
+// 31.4 and 31.6 us.
+constexpr int kPieceCost = 10, kSoloCost = 4;
 constexpr int kTreeSlots = 65536;     // most workgroups of a block of columns
 static_assert(kTreeSlots <= 1 << 3 * kLevels && kJoin == 8, "levels");
 
