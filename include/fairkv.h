@@ -413,7 +413,7 @@ typedef struct {
     int32_t B, Hkv, D;       /* D 64 or 128 */
     int32_t dtype;           /* FAIRKV_BF16, FAIRKV_E4M3 or (append, accept) FAIRKV_F32 */
     int32_t n_scales;        /* E4M3: 1, or Hkv (at most FAIRKV_CACHE_SCALES): a stored byte of head h stands for byte * k_scale[h]; else 0 */
-    float k_scale[FAIRKV_CACHE_SCALES], v_scale[FAIRKV_CACHE_SCALES];   /* finite, not 0 */
+    float k_scale[FAIRKV_CACHE_SCALES], v_scale[FAIRKV_CACHE_SCALES];   /* finite, not 0, their reciprocals finite */
 } fairkv_cache;              /* a host struct; 336 bytes */
 
 /* What is done to the heads of new queries and keys before they are used, all of it in fp32, rounded once at the end:
@@ -462,7 +462,8 @@ int fairkv_append_rotated(const fairkv_cache *cache, const fairkv_rotation *r, c
  * n_slots    workgroups to balance over: the GPU's compute units
  * out        device [B][q_len][Hq][D] of out_dtype (FAIRKV_F32 or FAIRKV_BF16); lse device float [B][q_len][Hq] or NULL
  * Lengths below 0 count as 0, those beyond the cache's rows (paged: max_pages * page_rows) as that many.
- * Enqueues one kernel; no synchronisation.  FAIRKV_EUNSUPPORTED: q_len > FAIRKV_MAX_DRAFT, an F32 cache, D, Hq / Hkv > 16. */
+ * Enqueues one kernel; no synchronisation.  FAIRKV_EUNSUPPORTED: q_len > FAIRKV_MAX_DRAFT, an F32 cache, D, Hq / Hkv > 16.  FAIRKV_EINVAL also:
+ * more than 2^31 - 1 elements of q, a scale (times a k_scale) that is not finite in log2 units. */
 size_t fairkv_tree_counter_bytes(int32_t n_slots);
 size_t fairkv_tree_workspace_bytes(const fairkv_cache *cache, int32_t Hq, int32_t q_len, int32_t n_slots);
 int fairkv_tree_workspace_reset(void *workspace, size_t workspace_bytes, int32_t n_slots, void *hip_stream);

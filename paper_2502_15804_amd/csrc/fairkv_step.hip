@@ -30,8 +30,9 @@ int check_cache(const fairkv_cache *c)
     if (c->dtype != FAIRKV_E4M3) return c->n_scales == 0 ? FAIRKV_OK : FAIRKV_EINVAL;
     if (c->n_scales > FAIRKV_CACHE_SCALES) return FAIRKV_EUNSUPPORTED;
     if (c->n_scales != 1 && c->n_scales != c->Hkv) return FAIRKV_EINVAL;
+    auto usable = [](float scale) { return std::isfinite(scale) && scale != 0.f && std::isfinite(1.f / scale); };      // rows are multiplied by the reciprocal
     for (int32_t h = 0; h < c->n_scales; ++h)
-        if (!std::isfinite(c->k_scale[h]) || !std::isfinite(c->v_scale[h]) || c->k_scale[h] == 0.f || c->v_scale[h] == 0.f) return FAIRKV_EINVAL;
+        if (!usable(c->k_scale[h]) || !usable(c->v_scale[h])) return FAIRKV_EINVAL;
     return FAIRKV_OK;
 }
 
@@ -135,8 +136,9 @@ struct TreeShape {
 // Rows that the pairs of a cache can have in all; what they do have is known on the device alone.
 int64_t cache_rows(const fairkv_cache *c)
 {
-    const int64_t rows = std::max<int64_t>(c->n_rows, 0);
-    return c->pages ? std::min(rows, static_cast<int64_t>(c->B) * c->Hkv * c->max_pages * c->page_rows) : rows;
+    const int64_t rows = std::min<int64_t>(c->n_rows, int64_t(1) << 48), pairs = static_cast<int64_t>(c->B) * c->Hkv;      // no product below leaves 64 bits
+    const int64_t each = c->pages ? static_cast<int64_t>(c->max_pages) * c->page_rows : rows;
+    return each > rows / pairs ? rows : each * pairs;
 }
 // Waves side by side read a tile of K and V from LDS that came once for all of them; waves that take the tiles in turn cut a pair into fewer
 // pieces, and have fewer columns to hand over at the end of each.  So it is the work of a workgroup that decides, in tiles of 32 columns by 32
@@ -234,6 +236,8 @@ extern "C" int fairkv_decode_attn_tree(const fairkv_cache *c, const void *q, con
     if (out_dtype != FAIRKV_BF16 && out_dtype != FAIRKV_F32) return FAIRKV_EUNSUPPORTED;
     if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16) || (tree && !aligned(tree, 8))) return FAIRKV_EINVAL;
     if (static_cast<int64_t>(c->B) * q_len * Hq * c->D > INT32_MAX) return FAIRKV_EINVAL;
+    for (int32_t h = 0; h < std::max(c->n_scales, 1); ++h)      // a score's factor that is no number would make scores of 0 NaN
+        if (!std::isfinite(scale * kLog2e * (c->n_scales > 0 ? c->k_scale[h] : 1.f))) return FAIRKV_EINVAL;
     const TreeShape shape = tree_shape(c, Hq, q_len, n_slots);
     const TreeSpace space = tree_space(shape, c->D, n_slots);
     if (!workspace || workspace_bytes < space.counters + space.ml + space.o) return FAIRKV_EWORKSPACE;

@@ -269,6 +269,7 @@ def _attend(s, Hq, q_len, out_dtype, tree=None, n_new=None, n_slots=None, seed=0
     ws = _workspace(s.cache, Hq, q_len, n_slots)
     if stream is not None:
         stream.wait_stream(torch.cuda.current_stream())
+        ws.record_stream(stream)
     F.fairkv_decode_attn_tree(s.cache, s.lens, q, ws, out, lse, scale, tree=None if tree is None else torch.as_tensor(tree.view(np.int64), device=DEV),
                               n_new=None if n_new is None else I32(n_new), n_slots=n_slots, stream=stream)
     if stream is None:
@@ -589,3 +590,74 @@ def test_steps_captured_once_and_replayed_while_the_cache_grows(dtype, page):
             assert torch.equal(ref, _bits(y))
             x.copy_(y)
         assert s.lens.cpu().numpy().tolist() == (lens_before + kept[:, None]).tolist()
+
+
+@pytest.mark.parametrize("page", [0, 64])
+def test_rows_behind_4_gib_are_those_that_are_meant(page):
+    """The same steps near the front of a cache and behind byte 2^32 of it: the same bits."""
+    B, Hkv, G, q_len, D, each = 2, 2, 4, 5, 128, 320
+    n_rows = (1 << 24) + 4096
+    k, v = (torch.empty(n_rows, D, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    lens = np.array([[200, 31], [300, 0]])
+    firsts = (64, (1 << 24) + 64)            # of B * Hkv runs of `each` rows
+    old = [torch.randn(B * Hkv * each, D, generator=torch.Generator().manual_seed(i)).to(torch.bfloat16).to(DEV) for i in range(2)]
+    q, k_new, v_new = (torch.randn(B, q_len, h, D, generator=torch.Generator().manual_seed(h)).to(torch.bfloat16).to(DEV) for h in (Hkv * G, Hkv, Hkv))
+    path, n_path = I32([[4, 1, 2, 0, 0], [3, 4, 0, 0, 0]]), I32([3, 2])
+    results = []
+    for first in firsts:
+        at = slice(first, first + B * Hkv * each)
+        k[at], v[at] = old[0], old[1]
+        where = dict(off=torch.arange(B * Hkv, device=DEV).view(B, Hkv) * each + first) if not page else \
+            dict(pages=I32((first + np.arange(B * Hkv * each).reshape(B * Hkv, -1)[:, ::page]) // page), page_rows=page)
+        cache = F.Cache(k, v, I32(np.full((B, Hkv), each)), **where)
+        t, q_out, out, lse = I32(lens), torch.empty_like(q), torch.empty(q.shape, device=DEV), torch.empty(q.shape[:-1], device=DEV)
+        F.fairkv_append_rotated(cache, t, q, k_new, v_new, q_out, q_norm=torch.ones(D, device=DEV))
+        F.fairkv_decode_attn_tree(cache, t, q_out, _workspace(cache, Hkv * G, q_len), out, lse, 0.1)
+        F.fairkv_accept(cache, t, path, n_path)
+        results.append((t, q_out, out, lse, k[at].clone(), v[at].clone()))
+    assert not torch.equal(results[0][4], old[0])
+    for near, far in zip(*results):
+        assert torch.equal(near, far)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,B,q_len", [(80, 1, 128, 48, 64), (5, 1, 128, 160, 64), (1, 1, 64, 1100, 64), (16, 2, 128, 3000, 1)])
+def test_many_tokens_in_a_workgroup_give_what_few_give(Hq, Hkv, D, B, q_len):
+    """So many tokens that workgroups of the queries make several passes, against calls of a few sequences each."""
+    rng = np.random.default_rng(Hq)
+    n_new = rng.integers(0, q_len + 1, B)
+    n_new[B // 2: B // 2 + 3] = 0
+    lens = rng.integers(0, 9, (B, Hkv))
+    s = Setup(lens, q_len, D, seed=Hq)
+    q, k_new, v_new = _new(s, q_len, Hq, 1, True)
+    pos = rng.integers(0, 32, (B, q_len))
+    pos[rng.integers(0, B, 20), rng.integers(0, q_len, 20)] = 32      # outside the table
+    kw = dict(table=_table(32, 32, 0), q_norm=torch.rand(D, device=DEV), k_norm=torch.rand(D, device=DEV))
+    k0, v0 = s.k.clone(), s.v.clone()
+
+    def run(per_call):
+        s.k.copy_(k0), s.v.copy_(v0)
+        q_out, bad, grown = torch.full((B, q_len, Hq, D), 3.0, dtype=torch.bfloat16, device=DEV), I32([0]), I32(np.full((B, Hkv), -1))
+        for b in range(0, B, per_call):
+            at = slice(b, min(b + per_call, B))
+            cache = F.Cache(s.k, s.v, I32(s.cap_h[at]), off=torch.as_tensor(s.off.reshape(B, Hkv)[at].copy(), device=DEV))
+            F.fairkv_append_rotated(cache, I32(lens[at]), q[at], k_new[at], v_new[at], q_out[at], pos=I32(pos[at]), n_new=I32(n_new[at]),
+                                    lens_out=grown[at], bad=bad, **kw)
+        return q_out, bad, grown, s.k.clone(), s.v.clone()
+
+    for many, few in zip(run(B), run(16 if q_len > 1 else 500)):
+        assert torch.equal(many, few)
+
+
+def test_two_streams_at_once_with_a_workspace_each():
+    s = Setup(np.random.default_rng(3).integers(0, 900, (6, 4)), 0, 128, seed=21)
+    q, out, lse, scale = _attend(s, 32, 12, torch.float32)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    spaces = [_workspace(s.cache, 32, 12) for _ in streams]
+    got = [[(torch.empty_like(out), torch.empty_like(lse)) for _ in range(4)] for _ in streams]
+    torch.cuda.synchronize()
+    for i in range(4):
+        for stream, ws, results in zip(streams, spaces, got):
+            F.fairkv_decode_attn_tree(s.cache, s.lens, q, ws, *results[i], scale, stream=stream)
+    torch.cuda.synchronize()
+    for x in got[0] + got[1]:
+        assert torch.equal(x[0], out) and torch.equal(x[1], lse)

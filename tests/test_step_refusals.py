@@ -99,6 +99,28 @@ def test_tree_refuses_more_than_it_can_address_and_an_fp32_cache():
     assert _tree(_cache(dtype=F.FAIRKV_F32)) == F.FAIRKV_EUNSUPPORTED
 
 
+@pytest.mark.parametrize("scale,k_scale", [(3e38, 1.0), (1.0, 3e38), (-1e30, 1e30)])
+def test_tree_refuses_factors_that_are_no_numbers(scale, k_scale):
+    assert _tree(_cache(dtype=F.FAIRKV_E4M3, n_scales=2, scales=[1.0, k_scale]), scale=scale) == F.FAIRKV_EINVAL
+    if k_scale == 1.0:
+        assert _tree(_cache(), scale=scale) == F.FAIRKV_EINVAL
+
+
+def test_a_scale_without_a_reciprocal_is_refused():
+    c = _cache(dtype=F.FAIRKV_E4M3, n_scales=1, scales=[1e-45])
+    assert [call(c) for call in (_append, _tree, _accept)] == [F.FAIRKV_EINVAL] * 3
+
+
+def test_tree_workspace_of_caches_of_any_size():
+    """Rows, pages and pairs whose products leave 64 bits: what a cache of so many rows takes, whatever its pages."""
+    L, n = F.lib(), 1 << 62
+    packed = L.fairkv_tree_workspace_bytes(ctypes.byref(_cache(n_rows=n, B=1 << 12, Hkv=8)), 64, 64, 256)
+    paged = _cache(n_rows=n, off=None, pages=AT, max_pages=(1 << 31) - 1, page_rows=1 << 30, B=1 << 12, Hkv=8)
+    assert 0 < L.fairkv_tree_workspace_bytes(ctypes.byref(paged), 64, 64, 256) == packed
+    few = _cache(n_rows=n, off=None, pages=AT, max_pages=1, page_rows=16, B=1, Hkv=8)
+    assert 0 < L.fairkv_tree_workspace_bytes(ctypes.byref(few), 64, 8, 256) < packed
+
+
 def test_tree_workspace():
     L, c = F.lib(), _cache()
     for Hq, q_len, n_slots in ((8, 4, 256), (2, 1, 1), (32, 64, 256), (6, 33, 7)):
