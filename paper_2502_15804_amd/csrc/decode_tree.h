@@ -190,7 +190,10 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
     constexpr int kAhead = WC == 1 ? STAGES : STAGES - 1;       // tiles on their way while one is waited for
     constexpr int RING = WT * STAGES * STAGEB;
     constexpr int kBlock = kTreeCols * 32 * 4;        // bytes of 32 coordinates of a wave's columns
-    constexpr int kSolo = WC == 1 && WT == 4 ? 4 : 0; // a whole pair of at most so many tiles goes to one wave: no fold, four pairs side by side
+    // A whole pair of at most so many tiles goes to one wave: no fold, four pairs side by side; of at most twice as many if the share has three of
+    // those.  (128 x 8 pairs of 130 rows: 17.8 us, 31 without the longer ones, with rows of all lengths around that 31 and 36; 256 x 4 in 32
+    // columns 48 and 60.  Always: 32 x 8 heavy-tailed pairs 42 us instead of 39, the other waves wait for the one.)
+    constexpr int kSolo = WC == 1 && WT == 4 ? 4 : 0, kSoloMany = 2 * kSolo;
     auto overhead = [&](int tiles) __attribute__((always_inline)) { return tiles <= kSolo ? kSoloCost : kPieceCost; };
     constexpr int kRound = WT == 1 ? 0 : WC == 1 ? NDB : NDB / 2;      // such blocks of a group that are folded at once
     constexpr int FOLD = (WT - 1) * WC * kRound * kBlock;
@@ -306,6 +309,13 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
     int4 entry;
     entry = in_table ? table[max(pair - lane, 0)] : pair_entry(max(pair - lane, 0));
     if constexpr (!kOwnQueries) __syncthreads();      // the table's memory is the queries'
+    int solo_most = kSolo;                            // tiles of a pair that one wave has alone
+    if constexpr (kSolo > 0) {
+        const int tiles = tiles_of(entry.x);
+        const int64_t first = at - wave_upto(tiles + overhead(tiles)) + overhead(tiles);      // place of the lane's pair
+        const bool fits = lane <= pair && tiles <= kSoloMany && first - overhead(tiles) >= begin && first + tiles <= end;
+        if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(fits)) >= 3) solo_most = kSoloMany;
+    }
     auto next_piece = [&](TreePiece &pc) __attribute__((always_inline)) {      // false: the share has no more
         while (pair >= 0) {
             if (held - pair >= 64) {
@@ -328,7 +338,7 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
             if ((pc.tile1 <= pc.tile0 && !empty) || c0 >= pc.nn * a.G) continue;
             pc.from = wt, pc.apart = WT, pc.solo = false;
             if constexpr (kSolo > 0) {
-                pc.solo = pc.tile0 == 0 && pc.tile1 == pc.tiles && pc.tiles <= kSolo;
+                pc.solo = pc.tile0 == 0 && pc.tile1 == pc.tiles && pc.tiles <= solo_most;
                 if (pc.solo) {
                     pc.from = 0, pc.apart = 1;
                     if ((pc.pair & 3) != wave) continue;      // another wave's

@@ -346,6 +346,19 @@ def test_few_workgroups_with_many_columns_each(G, q_len, dtype, D, page, n_slots
         _compare(s, *_attend(s, 2 * G, q_len, out_dtype, tree, n_new, n_slots, scale=-0.1 if n_slots == 2 else None), tree, n_new)
 
 
+@pytest.mark.parametrize("n_slots", [2, 5, 9, 24])
+@pytest.mark.parametrize("dtype,page", [("bf16", 0), ("kv8", 16)])
+@pytest.mark.parametrize("longest", [130, 256, 400])
+def test_many_short_pairs_in_a_share(longest, dtype, page, n_slots):
+    """Pairs of up to 4 and up to 8 tiles that one wave takes alone, between longer ones and empty ones."""
+    rng = np.random.default_rng(longest + n_slots)
+    lens = rng.integers(longest // 3, longest + 1, (20, 2))
+    lens[3], lens[7, 1], lens[11] = 0, 900, 3
+    s = Setup(lens, 0, 128, dtype, page, seed=longest, scales=True)
+    n_new = rng.integers(0, 4, 20)
+    _compare(s, *_attend(s, 8, 3, torch.float32, None, n_new, n_slots), None, n_new)
+
+
 @pytest.mark.parametrize("q_len,G", [(1, 4), (4, 8), (16, 4), (40, 8)])
 def test_attention_of_a_chain_of_ragged_drafts_and_short_pairs(q_len, G):
     """Pairs without rows, shorter than their draft, drafts of no token, counts out of range: what is no node is left as it was."""
