@@ -417,7 +417,7 @@ def test_infinite_and_nan_rows_count_for_the_nodes_that_see_them(G, q_len, dtype
     assert nan[seen].all() and not np.isnan(lse.cpu().numpy())[~seen].any()
 
 
-@pytest.mark.parametrize("n_slots", [1, 2, 7, 64, 256])
+@pytest.mark.parametrize("n_slots", [1, 2, 7, 64, 256, 1024, 20000])
 @pytest.mark.parametrize("G,q_len", [(1, 1), (8, 5), (8, 12), (4, 64)])
 def test_long_pairs_cut_into_many_pieces(G, q_len, n_slots):
     s = Setup([[3000], [70], [9]], 1, 64, page=64, seed=3)
@@ -439,6 +439,14 @@ def test_a_pages_list_longer_than_a_batch_of_64_tiles(q_len):
     """One workgroup alone: 64 tiles of each of its groups of waves are more than one batch of page numbers."""
     s = Setup([[9000 + q_len]], 1, 64, page=16, seed=5)
     _compare(s, *_attend(s, 8, q_len, torch.float32, n_slots=1), None, None)
+
+
+@pytest.mark.parametrize("dtype,page", [("bf16", 16), ("kv8", 0)])
+def test_one_long_pair_in_more_than_512_pieces(dtype, page):
+    """Sums of sums of sums."""
+    s = Setup([[20000, 40]], 1, 64, dtype, page, seed=31)
+    tree = _random_tree(1, 8, np.random.default_rng(6))
+    _compare(s, *_attend(s, 8, 8, torch.float32, tree, n_slots=1500), tree, None)
 
 
 @pytest.mark.parametrize("page", [0, 16])
