@@ -70,7 +70,7 @@ class fairkv_cache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_rows", ctypes.c_int64), ("off", ctypes.c_void_p),
                 ("pages", ctypes.c_void_p), ("cap", ctypes.c_void_p)] + [
         (n, ctypes.c_int32) for n in ("max_pages", "page_rows", "B", "Hkv", "D", "dtype", "n_scales")] + [
-        (n, ctypes.c_float * FAIRKV_CACHE_SCALES) for n in ("k_scale", "v_scale")]
+        (n, ctypes.c_float * FAIRKV_CACHE_SCALES) for n in ("k_scale", "v_scale")] + [("expected_rows", ctypes.c_int64)]
 
 
 class fairkv_rotation(ctypes.Structure):
@@ -417,11 +417,12 @@ class Cache:
 
     k, v [n_rows, D] bfloat16, float32 or 8-bit floats (torch.float8_e4m3fn, or uint8 holding the same bytes); cap int32 [B, Hkv]: the
     tokens a pair may hold.  Packed: off int64 [B, Hkv].  Paged: pages int32 [B, Hkv, max_pages] (or [B * Hkv, max_pages]) and page_rows.
-    k_scale, v_scale: of an 8-bit cache, a number or one per KV head (1).  All tensors are on one GPU and contiguous; the cache keeps them
+    k_scale, v_scale: of an 8-bit cache, a number or one per KV head (1).  expected_rows: rows that all pairs together are expected to have
+    (None: as many as there are), for the attention's speed only.  All tensors are on one GPU and contiguous; the cache keeps them
     and reads what is in them at every call, so pages may be entered into `pages` as sequences grow.
     """
 
-    def __init__(self, k, v, cap, off=None, pages=None, page_rows=None, k_scale=None, v_scale=None):
+    def __init__(self, k, v, cap, off=None, pages=None, page_rows=None, k_scale=None, v_scale=None, expected_rows=None):
         torch = _torch()[0]
         codes = {torch.bfloat16: FAIRKV_BF16, torch.float32: FAIRKV_F32, torch.float8_e4m3fn: FAIRKV_E4M3, torch.uint8: FAIRKV_E4M3}
         if k.dtype not in codes or v.dtype != k.dtype:
@@ -440,7 +441,7 @@ class Cache:
             raise ValueError("the tensors of a cache must be on one device")
         c = fairkv_cache(k=_ptr(k), v=_ptr(v), n_rows=k.shape[0], off=_ptr(off), pages=_ptr(pages), cap=_ptr(cap),
                          max_pages=pages.shape[-1] if pages is not None else 0, page_rows=int(page_rows or 0), B=B, Hkv=Hkv, D=k.shape[1],
-                         dtype=codes[k.dtype])
+                         dtype=codes[k.dtype], expected_rows=int(expected_rows or 0))
         if c.dtype == FAIRKV_E4M3:
             c.n_scales = Hkv if np.ndim(k_scale) or np.ndim(v_scale) else 1
             if c.n_scales > FAIRKV_CACHE_SCALES:

@@ -23,6 +23,7 @@ int check_cache(const fairkv_cache *c)
     if (!c || !c->k || !c->v || !c->cap || (c->off == nullptr) == (c->pages == nullptr)) return FAIRKV_EINVAL;
     if (c->B < 1 || c->Hkv < 1 || c->D < 1 || c->n_rows < 0 || !aligned(c->k, 16) || !aligned(c->v, 16)) return FAIRKV_EINVAL;
     if (static_cast<int64_t>(c->B) * c->Hkv > INT32_MAX / 2) return FAIRKV_EINVAL;
+    if (c->expected_rows < 0) return FAIRKV_EINVAL;
     if (c->pages && (c->max_pages < 1 || c->page_rows < 16 || (c->page_rows & (c->page_rows - 1)) != 0 || c->page_rows > (1 << 30))) return FAIRKV_EINVAL;
     if (c->off && (c->max_pages != 0 || c->page_rows != 0)) return FAIRKV_EINVAL;
     if (c->dtype != FAIRKV_BF16 && c->dtype != FAIRKV_F32 && c->dtype != FAIRKV_E4M3) return FAIRKV_EUNSUPPORTED;
@@ -133,16 +134,17 @@ namespace {
 struct TreeShape {
     int32_t waves, blocks, slots;
 };
-// Rows that the pairs of a cache can have in all; what they do have is known on the device alone.
+// Rows that the pairs of a cache are expected to have in all, or can have; what they do have is known on the device alone.
 int64_t cache_rows(const fairkv_cache *c)
 {
     const int64_t rows = std::min<int64_t>(c->n_rows, int64_t(1) << 48), pairs = static_cast<int64_t>(c->B) * c->Hkv;      // no product below leaves 64 bits
     const int64_t each = c->pages ? static_cast<int64_t>(c->max_pages) * c->page_rows : rows;
-    return each > rows / pairs ? rows : each * pairs;
+    const int64_t most = each > rows / pairs ? rows : each * pairs;
+    return c->expected_rows > 0 ? std::min(c->expected_rows, most) : most;
 }
 // Waves side by side read a tile of K and V from LDS that came once for all of them; waves that take the tiles in turn cut a pair into fewer
 // pieces, and have fewer columns to hand over at the end of each.  So it is the work of a workgroup that decides, in tiles of 32 columns by 32
-// tokens, counted with full caches, a pair's own costs as 20.  Measured (bf16, D 128, 256 slots; us with 1, 2, 4, 8 waves side by side):
+// tokens, counted with the expected rows or full caches, a pair's own costs as 20.  Measured (bf16, D 128, 256 slots; us with 1, 2, 4, 8 waves side by side):
 //     192 columns, 1 x 8 pairs of 4000 rows, work 27           21   28   33   42
 //     128 columns, 2 x 8 pairs of 8000 rows, 67                34   36   39   52
 //     128 columns, 16 x 8 pairs of 512 rows, 72                22   19   28   28

@@ -449,6 +449,16 @@ def test_one_long_pair_in_more_than_512_pieces(dtype, page):
     _compare(s, *_attend(s, 8, 8, torch.float32, tree, n_slots=1500), tree, None)
 
 
+@pytest.mark.parametrize("expected", [1, 3000, 1 << 40])
+def test_a_cache_for_more_rows_than_there_are(expected):
+    """However many rows are expected, the results are those of the rows that are there."""
+    s = Setup(np.random.default_rng(9).integers(0, 500, (4, 2)), 60000, 64, seed=9)
+    where = dict(off=torch.as_tensor(s.off.reshape(4, 2), device=DEV))
+    s.cache = F.Cache(s.k, s.v, I32(s.cap_h), expected_rows=expected, **where)
+    tree = _random_tree(4, 32, np.random.default_rng(7))
+    _compare(s, *_attend(s, 16, 32, torch.float32, tree, n_slots=64), tree, None)
+
+
 @pytest.mark.parametrize("page", [0, 16])
 @pytest.mark.parametrize("q_len", [2, 20])
 def test_rows_that_the_cache_does_not_have_are_not_attended_to(page, q_len):

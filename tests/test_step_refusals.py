@@ -41,7 +41,7 @@ BAD_CACHES = [
     (dict(pages=AT), F.FAIRKV_EINVAL), (dict(off=None, pages=AT), F.FAIRKV_EINVAL), (dict(off=None, pages=AT, max_pages=4, page_rows=8), F.FAIRKV_EINVAL),
     (dict(off=None, pages=AT, max_pages=4, page_rows=48), F.FAIRKV_EINVAL), (dict(off=None, pages=AT, max_pages=0, page_rows=16), F.FAIRKV_EINVAL),
     (dict(max_pages=4), F.FAIRKV_EINVAL), (dict(page_rows=16), F.FAIRKV_EINVAL), (dict(k=AT + 8), F.FAIRKV_EINVAL), (dict(v=AT + 2), F.FAIRKV_EINVAL),
-    (dict(n_rows=-1), F.FAIRKV_EINVAL), (dict(B=0), F.FAIRKV_EINVAL), (dict(Hkv=0), F.FAIRKV_EINVAL), (dict(B=1 << 20, Hkv=1 << 11), F.FAIRKV_EINVAL),
+    (dict(n_rows=-1), F.FAIRKV_EINVAL), (dict(expected_rows=-1), F.FAIRKV_EINVAL), (dict(B=0), F.FAIRKV_EINVAL), (dict(Hkv=0), F.FAIRKV_EINVAL), (dict(B=1 << 20, Hkv=1 << 11), F.FAIRKV_EINVAL),
     (dict(D=96), F.FAIRKV_EUNSUPPORTED), (dict(dtype=F.FAIRKV_BF16_VALU), F.FAIRKV_EUNSUPPORTED), (dict(n_scales=1, scales=[1.0]), F.FAIRKV_EINVAL),
     (dict(dtype=F.FAIRKV_E4M3), F.FAIRKV_EINVAL), (dict(dtype=F.FAIRKV_E4M3, n_scales=3, scales=[1.0] * 3), F.FAIRKV_EINVAL),
     (dict(dtype=F.FAIRKV_E4M3, n_scales=33, Hkv=33), F.FAIRKV_EUNSUPPORTED), (dict(dtype=F.FAIRKV_E4M3, n_scales=1, scales=[0.0]), F.FAIRKV_EINVAL),
@@ -119,6 +119,13 @@ def test_tree_workspace_of_caches_of_any_size():
     assert 0 < L.fairkv_tree_workspace_bytes(ctypes.byref(paged), 64, 64, 256) == packed
     few = _cache(n_rows=n, off=None, pages=AT, max_pages=1, page_rows=16, B=1, Hkv=8)
     assert 0 < L.fairkv_tree_workspace_bytes(ctypes.byref(few), 64, 8, 256) < packed
+
+
+def test_expected_rows_decide_how_columns_are_dealt_and_never_beyond_the_cache():
+    L, size = F.lib(), lambda **kw: F.lib().fairkv_tree_workspace_bytes(ctypes.byref(_cache(B=4, Hkv=8, **kw)), 64, 24, 256)
+    assert size(n_rows=1 << 24, expected_rows=20000) == size(n_rows=20000) < size(n_rows=1 << 24)
+    assert size(n_rows=20000, expected_rows=1 << 40) == size(n_rows=20000)
+    assert ctypes.sizeof(F.fairkv_cache) == 344
 
 
 def test_tree_workspace():
