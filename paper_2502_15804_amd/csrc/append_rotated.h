@@ -25,6 +25,7 @@ struct RotateArgs {
     int64_t q_stride, k_stride, v_stride;
     int32_t B, Hq, Hkv, q_len, n_pos, rot, pairs;
     int32_t q_groups, head_slots, passes; // workgroups for the queries; rows of one token that a pass of a workgroup covers; its passes
+    int32_t apart;                        // how many passes' tokens further on, but for the workgroups' number of them, its next pass's lie
     int32_t n_scales;
     float eps;
     float k_scale[kCacheScales], v_scale[kCacheScales];      // reciprocals
@@ -193,11 +194,14 @@ __global__ __launch_bounds__(256) void fairkv_append_rotated_kernel(RotateArgs a
     for (int i = 0; i < kRow8; ++i) weight[i] = norm ? norm[piece * kRow8 + i] : 1.f;
 
     if (static_cast<int>(blockIdx.x) < a.q_groups) {
-        // lane j of every wave looks after token j of the workgroup's: whether there is anything to do, and at which position
+        // Lane j of every wave looks after token j of the workgroup's: whether there is anything to do, and at which position.  A pass's tokens follow
+        // one another; from pass to pass they lie all over the batch, and further on in their sequences, so that ragged drafts, whose last tokens
+        // are none, leave every workgroup about as much to do (256 drafts of up to 64 tokens: 78 us instead of 95).
         const int each = kSlots / a.head_slots, n_tokens = a.B * a.q_len, lane = threadIdx.x & 63;
-        const int token0 = static_cast<int>(blockIdx.x) * each * a.passes;      // (tokens fit 31 bits, and 64 more)
-        const int looked = min(token0 + lane, n_tokens - 1), of_b = looked / a.q_len;
-        const bool live = lane < each * a.passes && token0 + lane < n_tokens && looked - of_b * a.q_len < new_tokens(a.n_new, of_b, a.q_len);
+        const int of_lane = min(lane / each, a.passes - 1);
+        const int token = (of_lane * a.q_groups + (static_cast<int>(blockIdx.x) + of_lane * a.apart) % a.q_groups) * each + lane % each;      // (fits 31 bits, and 256 more)
+        const int looked = min(token, n_tokens - 1), of_b = looked / a.q_len;
+        const bool live = lane < each * a.passes && token < n_tokens && looked - of_b * a.q_len < new_tokens(a.n_new, of_b, a.q_len);
         const int32_t held_pos = a.table ? a.pos[looked] : 0;
         const bool ok = live && in_table(a, held_pos);
         if (live && !ok && threadIdx.x < 64 && a.bad) atomicAdd(a.bad, 1);
@@ -215,8 +219,8 @@ __global__ __launch_bounds__(256) void fairkv_append_rotated_kernel(RotateArgs a
             while (pass < a.passes && (todo >> (pass * each) & (~0ull >> (64 - each))) == 0) ++pass;
             if (pass >= a.passes) return false;
             const int j = pass * each + of_pass;
-            const int32_t pos = __shfl(held_pos, j, 64);
-            x.token = todo >> j & 1 ? token0 + j : -1, x.h0 = h_next + h_slot;
+            const int32_t pos = __shfl(held_pos, j, 64), at = __shfl(token, j, 64);
+            x.token = todo >> j & 1 ? at : -1, x.h0 = h_next + h_slot;
             if (x.token >= 0) {
                 const char *src = a.q + (x.token * a.q_stride + piece * kRow8) * EB;
 #pragma unroll

@@ -70,7 +70,7 @@ extern "C" int fairkv_append_rotated(const fairkv_cache *c, const fairkv_rotatio
     if (!aligned(q, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(q_out, 16)) return FAIRKV_EINVAL;
     if ((r->q_norm || r->k_norm) && !(r->eps >= 0.f && std::isfinite(r->eps))) return FAIRKV_EINVAL;
     if (r->table && (!r->pos || r->n_pos < 1 || r->rot < 16 || r->rot % 16 != 0 || r->rot > c->D || !aligned(r->table, 16))) return FAIRKV_EINVAL;
-    if (tokens > INT32_MAX - 64 || q_out == k_new || q_out == v_new) return FAIRKV_EINVAL;
+    if (tokens > INT32_MAX - 256 || q_out == k_new || q_out == v_new) return FAIRKV_EINVAL;
     if (q_out == q && q_stride != static_cast<int64_t>(Hq) * c->D) return FAIRKV_EINVAL;
 
     RotateArgs a{};
@@ -89,11 +89,12 @@ extern "C" int fairkv_append_rotated(const fairkv_cache *c, const fairkv_rotatio
     while (a.head_slots * 2 <= std::min(Hq, slots)) a.head_slots *= 2;
     // As many passes as leave a thousand workgroups, what the card has at a time, and at most the 64 tokens that a wave's lanes look after.
     // 128 sequences x 64 tokens, 64 + 16 heads: 66 us, 68 and 72 with two and four thousand workgroups, 81 with one of every token;
-    // 256 x 64 of which half are none: 95, 99, 104 and 126.
+    // 256 x 64 of which half are none: 95, 99, 104 and 126 with a workgroup's tokens one behind the other, 78 as they lie.
     const int64_t groups = (tokens + slots / a.head_slots - 1) / (slots / a.head_slots);
     a.passes = static_cast<int32_t>(std::clamp<int64_t>(groups / 1024, 1, 64 / (slots / a.head_slots)));
     const int64_t tokens_each = slots / a.head_slots * a.passes, pairs_each = std::max(1, slots / q_len);
     a.q_groups = static_cast<int32_t>((tokens + tokens_each - 1) / tokens_each);
+    a.apart = static_cast<int32_t>(std::max<int64_t>(1, q_len / tokens_each));      // the passes of a workgroup go once through a sequence
     const int64_t grid = a.q_groups + (static_cast<int64_t>(c->B) * c->Hkv + pairs_each - 1) / pairs_each;
     if (grid > INT32_MAX) return FAIRKV_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
