@@ -420,6 +420,7 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
         const int64_t row0 = rows.get(0, step & 63), row1 = rows.get(1, step & 63);
         const bool full = last >= kTreeTok - 1 && (row0 | row1) >= 0;
         missing &= ~(3u << 2 * at_stage);
+        if (!full) missing |= ((row0 < 0 ? 1u : 0u) | (row1 < 0 ? 2u : 0u)) << 2 * at_stage;      // a wave that loads nothing masks too
         if (!loads) return;
         if (full) {
 #pragma unroll
@@ -434,7 +435,6 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
                     load_chunks_to_lds<kRun, Tile::kPitchK>(from, offsets, place_of(stage, x));
             }
         } else {
-            missing |= ((row0 < 0 ? 1u : 0u) | (row1 < 0 ? 2u : 0u)) << 2 * at_stage;
 #pragma unroll
             for (int x = 0; x < LOADS; ++x) {
                 const int kind = WC == 1 && x >= LPT ? 1 : 0;
