@@ -456,7 +456,9 @@ int fairkv_append_rotated(const fairkv_cache *cache, const fairkv_rotation *r, c
  * them there); node i < n of sequence b sees every row in front of them and draft row j < n iff bit j of tree[b][i] is set: its ancestors'
  * bits and, as a rule, its own.  tree == NULL: nodes 0 .. i, a chain; q_len = 1 is a plain decode step.
  * out = softmax(scale * q . K^T) V over the rows that are seen, in fp32, and lse = log sum exp of the scaled scores; a node that sees
- * nothing gets out = 0 and lse = -inf.  An infinite or NaN row counts for the nodes that see it only.  Nodes i >= n are left as they are.
+ * nothing gets out = 0 and lse = -inf.  An infinite or NaN row counts for the nodes that see it only: an
+ * infinite value gives an infinite output as long as its weight, next to the largest, is one of fp32's normal numbers (2^-126), below that an
+ * infinite one or NaN, as 0 times infinity.  Nodes i >= n are left as they are.
  * q          device bf16 [B][q_len][Hq][D], 16-byte aligned; Hq a multiple of Hkv, any Hq / Hkv up to 16
  * tree       device uint64 [B][q_len], or NULL
  * workspace  device, fairkv_tree_workspace_bytes(cache, Hq, q_len, n_slots) bytes, 16-byte aligned.  Its first fairkv_tree_counter_bytes(n_slots)

@@ -180,9 +180,9 @@ struct TreePiece {
     int64_t first;                    // place of the pair's first tile in the line
 };
 
-// PARTS: a weight enters the second product as so many bf16 numbers, each the rounding of what those before leave, in as many times the
-// instructions.  Three keep an fp32 output's accuracy; one is off by 2^-8 of a weight, which adds 0.4 times to the error that a bf16 output's own
-// rounding makes.
+// PARTS: a weight enters the second product as so many bf16 numbers, in as many times the instructions.  Three are all 24 bits of it and keep an
+// fp32 output's accuracy, two are off by 2^-16 of a weight; one, rounded, is off by 2^-8, which adds 0.4 times to the error that a bf16 output's
+// own rounding makes.
 template <int D, bool KV8, int WC, int WT, int STAGES, int PARTS>
 __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(TreeArgs a)
 {
@@ -624,16 +624,23 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
             }
             const float m_ref = m_run == -INFINITY ? 0.f : m_run;      // nothing seen yet: weights of 0
 
-            // ---- weights, as PARTS bf16 numbers that add up to them ----
-            uint32_t pw[PARTS][8];
+            // ---- weights, as PARTS bf16 numbers that add up to them: the upper half, that of what it leaves, and the last rounded.  All of them
+            //      are positive if the weight is, so an infinite V stays one: of a part that would be 0 the smallest number of bf16, 2^-133, is
+            //      left (0 for a weight of 0).  The largest weight is at least 1, and one below 2^-126 is 0, as fp32 has it.  8-bit rows have no infinity. ----
+            uint32_t pw[PARTS][8], ones = 0x00010001u;
+            asm("" : "+s"(ones));                     // a minimum with a known 1 becomes two compares and two selects
 #pragma unroll
             for (int r = 0; r < 16; r += 2) {
                 float p0 = __builtin_amdgcn_exp2f(fmaf(sacc[r], s_abs, -m_ref)), p1 = __builtin_amdgcn_exp2f(fmaf(sacc[r + 1], s_abs, -m_ref));
                 l_run += p0 + p1;
+                u16x2_t least{};
 #pragma unroll
                 for (int part = 0; part < PARTS; ++part) {
-                    pw[part][r / 2] = pack_bf16(p0, p1);
-                    p0 -= bf16_lo(pw[part][r / 2]), p1 -= bf16_hi(pw[part][r / 2]);      // exact
+                    uint32_t w = part == PARTS - 1 ? pack_bf16(p0, p1) : __builtin_amdgcn_perm(__float_as_uint(p1), __float_as_uint(p0), 0x07060302u);
+                    p0 -= bf16_hi(__float_as_uint(p0)), p1 -= bf16_hi(__float_as_uint(p1));      // exact
+                    if (!KV8 && part == 0) least = __builtin_elementwise_min(__builtin_bit_cast(u16x2_t, w), __builtin_bit_cast(u16x2_t, ones));
+                    if (!KV8 && part > 0) w = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, w), least));
+                    pw[part][r / 2] = w;
                 }
             }
 

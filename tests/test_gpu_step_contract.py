@@ -32,3 +32,39 @@ def test_rows_that_the_cache_does_not_have_at_every_width(page, dtype, D, q_len,
     s.make()
     for out_dtype in (torch.float32, torch.bfloat16):
         _compare(s, *_attend(s, 16, q_len, out_dtype, n_slots=n_slots), None, None)
+
+
+@pytest.mark.parametrize("n_slots", [None, 1, 16])
+@pytest.mark.parametrize("G,q_len", [(1, 1)] + [(8, n) for n in WIDTHS])
+@pytest.mark.parametrize("D,page", [(64, 16), (128, 0)])
+def test_infinite_values_in_front_of_the_draft(D, page, G, q_len, n_slots):
+    """Every node sees them: the output is that infinity, whatever the weight's bits, the width and the type of the output."""
+    s = Setup(np.array([[333, 70], [45, 700]]) + q_len, 1, D, "bf16", page, seed=3)
+    for p in range(4):
+        for i, t in enumerate((0, 5, 31, 40)):                       # before a draft of pair 2, which has 45 rows in front of it
+            s.v[s.row(p, t), 3 * i + p] = math.inf if i % 2 else -math.inf
+    tree = _random_tree(2, q_len, np.random.default_rng(4))
+    for out_dtype in (torch.float32, torch.bfloat16):
+        _compare(s, *_attend(s, 2 * G, q_len, out_dtype, tree, n_slots=n_slots), tree, None)
+
+
+@pytest.mark.parametrize("n_slots", [1, 8])
+@pytest.mark.parametrize("q_len", [1] + WIDTHS)
+@pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16])
+def test_an_infinite_value_under_small_weights(out_dtype, q_len, n_slots):
+    """Row 0 of each pair has the largest score, all others lie `gap` log2 units below it; rows 1 and 40 have an infinite V.  Weights of 2**-gap
+    that are bf16 numbers themselves, and some that are not."""
+    gaps = [1, 7, 60, 100.5, 110, 111, 111.5, 112, 112.5, 113, 118, 120.5, 125]
+    B = len(gaps)
+    s = Setup(np.full((B, 1), 96 + q_len), 0, 128, seed=5)
+    s.k.zero_(), s.v.fill_(1.0)
+    for p, gap in enumerate(gaps):
+        rows = [s.row(p, t) for t in range(96 + q_len)]
+        s.k[rows[1:], 0] = -gap
+        s.v[rows[1], 5], s.v[rows[40], 9] = math.inf, -math.inf
+    q = torch.zeros((B, q_len, 8, 128), dtype=torch.bfloat16, device=DEV)
+    q[..., 0] = 1
+    out = _attend(s, 8, q_len, out_dtype, n_slots=n_slots, q=q, scale=math.log(2.0))[1].double().cpu().numpy()
+    assert np.isposinf(out[..., 5]).all() and np.isneginf(out[..., 9]).all()
+    # out is a mean of ones: 2^-16 of each weight at most are lost, 136 fp32 sums 2^-24 each; a bf16 number next to 1 is 2^-8 away
+    assert np.abs(np.delete(out, [5, 9], axis=-1) - 1).max() <= (2.0 ** -8 if out_dtype == torch.bfloat16 else 2.0 ** -16 + 136 * 2.0 ** -24)
