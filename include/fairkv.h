@@ -458,7 +458,8 @@ int fairkv_append_rotated(const fairkv_cache *cache, const fairkv_rotation *r, c
  * out = softmax(scale * q . K^T) V over the rows that are seen, in fp32, and lse = log sum exp of the scaled scores; a node that sees
  * nothing gets out = 0 and lse = -inf.  An infinite or NaN row counts for the nodes that see it only: an
  * infinite value gives an infinite output as long as its weight, next to the largest, is one of fp32's normal numbers (2^-126), below that an
- * infinite one or NaN, as 0 times infinity.  Nodes i >= n are left as they are.
+ * infinite one or NaN, as 0 times infinity.  Softmax weights have all 24 bits for an fp32
+ * output, 2^-16 of them are lost for a bf16 one.  Nodes i >= n are left as they are.
  * q          device bf16 [B][q_len][Hq][D], 16-byte aligned; Hq a multiple of Hkv, any Hq / Hkv up to 16
  * tree       device uint64 [B][q_len], or NULL
  * workspace  device, fairkv_tree_workspace_bytes(cache, Hq, q_len, n_slots) bytes, 16-byte aligned.  Its first fairkv_tree_counter_bytes(n_slots)

@@ -181,8 +181,8 @@ struct TreePiece {
 };
 
 // PARTS: a weight enters the second product as so many bf16 numbers, in as many times the instructions.  Three are all 24 bits of it and keep an
-// fp32 output's accuracy, two are off by 2^-16 of a weight; one, rounded, is off by 2^-8, which adds 0.4 times to the error that a bf16 output's
-// own rounding makes.
+// fp32 output's accuracy; two are off by 2^-16 of a weight, which a bf16 output's own rounding, 2^-8, hides.  (One would be off by 2^-8 and make
+// a bf16 output's error 1.4 times as large: 64 x 8 pairs of 4096 rows and 512 columns 670 us instead of 852.)
 template <int D, bool KV8, int WC, int WT, int STAGES, int PARTS>
 __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(TreeArgs a)
 {

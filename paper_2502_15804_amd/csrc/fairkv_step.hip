@@ -145,18 +145,24 @@ int64_t cache_rows(const fairkv_cache *c)
 }
 // Waves side by side read a tile of K and V from LDS that came once for all of them; waves that take the tiles in turn cut a pair into fewer
 // pieces, and have fewer columns to hand over at the end of each.  So it is the work of a workgroup that decides, in tiles of 32 columns by 32
-// tokens, counted with the expected rows or full caches, a pair's own costs as 20.  Measured (bf16, D 128, 256 slots; us with 1, 2, 4, 8 waves side by side):
-//     192 columns, 1 x 8 pairs of 4000 rows, work 27           21   28   33   42
-//     128 columns, 2 x 8 pairs of 8000 rows, 67                34   36   39   52
-//     128 columns, 16 x 8 pairs of 512 rows, 72                22   19   28   28
-//     64 columns, 8 x 8 pairs of 4000 rows, 72                 36   41   46   55
-//     192 columns, 1 x 8 pairs of 16000 rows, 97               39   42   47   61
-//     192 columns, 4 x 8 pairs of 4000 rows, 109               41   40   40   47
-//     128 columns, 16 x 8 pairs of 2000 rows, 165              56   50   48   54   (8-bit: 43   36   40   58)
-//     64 columns, 32 x 8 pairs of 2000 rows, 165               65   63   67   82
-//     512 columns, 4 x 8 pairs of 4000 rows, 290               74   63   54   64
-//     128 columns, 16 x 8 pairs of 4000 rows, 290              96   78   72   90
-//     512 columns, 16 x 8 pairs of 4000 rows, 1160            294  244  167  160
+// tokens, counted with the expected rows or full caches, a pair's own costs as 20.  Measured (bf16 outputs, D 128, 256 slots; us with 1, 2, 4, 8 waves
+// side by side; * what the rule takes):
+//     192 columns, 1 x 8 pairs of 4000 rows, work 27           21*  27   33   44
+//     64 columns, 4 x 8 pairs of 8000 rows, 69                 37*  42   55   79
+//     128 columns, 2 x 8 pairs of 8000 rows, 68                31*  36   42   55
+//     64 columns, 8 x 8 pairs of 4000 rows, 73                 40*  39   45   67
+//     128 columns, 16 x 8 pairs of 512 rows, 76                22*  18   27   32
+//     192 columns, 1 x 8 pairs of 16000 rows, 98               39   41*  54   67
+//     192 columns, 4 x 8 pairs of 4000 rows, 110               40   38*  47   61
+//     128 columns, 16 x 8 pairs of 2000 rows, 169              57   45*  49   66   (8-bit: 43   37   47   68)
+//     64 columns, 32 x 8 pairs of 2000 rows, 169               64   59*  67  103
+//     512 columns, 4 x 8 pairs of 4000 rows, 294               76   64   69*  78
+//     128 columns, 16 x 8 pairs of 4000 rows, 294              98   76   77* 115   (rows of all lengths around that: 101   84   74  113)
+//     512 columns, 8 x 8 pairs of 4000 rows, 588              153  126  114* 120
+//     128 columns, 32 x 8 pairs of 4000 rows, 588             202  151  131* 202
+//     512 columns, 10 x 8 pairs of 4000 rows, 735             189  160  145  141*
+//     512 columns, 16 x 8 pairs of 4000 rows, 1176            293  246  222  210*
+// Next to a border the other side is as good or up to a fifth better: one number for columns, pairs and rows does not order all of them.
 // More waves than columns need gain nothing at any size.  Slots come in eights where there are as many, so that the workgroups with the same
 // rows and other columns, n_slots further on, share an XCD and its cache (192 columns, 1 x 8 pairs of 16000 rows: 39 us, against 60 with 42 slots).
 TreeShape tree_shape(const fairkv_cache *c, int32_t Hq, int32_t q_len, int32_t n_slots)
@@ -202,11 +208,12 @@ void launch_tree_kernel(const TreeArgs &a, int32_t blocks, hipStream_t st)
 template <int D, bool KV8>
 void launch_tree(int waves, bool fine, const TreeArgs &a, int32_t blocks, hipStream_t st)
 {
+    // What a weight is rounded to goes by the output's type alone: the width is a matter of speed, which hints and the size of a pool decide.
     switch (waves) {
     case 1: return fine ? launch_tree_kernel<D, KV8, 1, 4, 2, 3>(a, blocks, st) : launch_tree_kernel<D, KV8, 1, 4, 2, 2>(a, blocks, st);
     case 2: return fine ? launch_tree_kernel<D, KV8, 2, 4, 2, 3>(a, blocks, st) : launch_tree_kernel<D, KV8, 2, 4, 2, 2>(a, blocks, st);
-    case 4: return fine ? launch_tree_kernel<D, KV8, 4, 2, 3, 3>(a, blocks, st) : launch_tree_kernel<D, KV8, 4, 2, 3, 1>(a, blocks, st);
-    default: return fine ? launch_tree_kernel<D, KV8, 8, 1, 4, 3>(a, blocks, st) : launch_tree_kernel<D, KV8, 8, 1, 4, 1>(a, blocks, st);
+    case 4: return fine ? launch_tree_kernel<D, KV8, 4, 2, 3, 3>(a, blocks, st) : launch_tree_kernel<D, KV8, 4, 2, 3, 2>(a, blocks, st);
+    default: return fine ? launch_tree_kernel<D, KV8, 8, 1, 4, 3>(a, blocks, st) : launch_tree_kernel<D, KV8, 8, 1, 4, 2>(a, blocks, st);
     }
 }
 

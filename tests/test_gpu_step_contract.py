@@ -68,3 +68,22 @@ def test_an_infinite_value_under_small_weights(out_dtype, q_len, n_slots):
     assert np.isposinf(out[..., 5]).all() and np.isneginf(out[..., 9]).all()
     # out is a mean of ones: 2^-16 of each weight at most are lost, 136 fp32 sums 2^-24 each; a bf16 number next to 1 is 2^-8 away
     assert np.abs(np.delete(out, [5, 9], axis=-1) - 1).max() <= (2.0 ** -8 if out_dtype == torch.bfloat16 else 2.0 ** -16 + 136 * 2.0 ** -24)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "kv8"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("expected", [1, 20000, 60000, 1 << 40])
+def test_rows_that_are_expected_cost_no_bits_of_a_bf16_output(expected, D, dtype):
+    """256 columns in one, two, four and eight waves side by side: a weight is off by 2^-16 of itself in all of them."""
+    s = Setup(np.random.default_rng(9).integers(20, 60, (4, 2)) + 32, 20000, D, dtype, seed=9, scales=True)
+    kw = dict(k_scale=s.ks.tolist(), v_scale=s.vs.tolist()) if dtype == "kv8" else {}
+    s.cache = F.Cache(s.k, s.v, I32(s.cap_h), expected_rows=expected, off=torch.as_tensor(s.off.reshape(4, 2), device=DEV), **kw)
+    q, out, lse, scale = _attend(s, 16, 32, torch.bfloat16, n_slots=64)
+    _compare(s, q, out, lse, scale, None, None)
+    q_h = q.float().cpu().numpy().astype(np.float64).reshape(4, 32, 2, 8, D) * s.ks[None, None, :, None, None]
+    vs = np.repeat(s.vs, 8)[None, None, :]
+    ref, _, v_top, s_top = S.attend(q_h.reshape(4, 32, 16, D), *s.numbers(), s.lens_h, [32] * 4, lambda b, i, j: j <= i, scale, 2, s.row)
+    ref, v_top = ref * vs[..., None], v_top * vs
+    # scores: D products in fp32, twice for the sum; the weights' bits; 92 fp32 sums; the output's own rounding
+    tol = (2 * (s_top * D * 2.0 ** -24 + 2.0 ** -22) + 2.0 ** -16 + 92 * 2.0 ** -24) * v_top
+    assert (np.abs(out.double().cpu().numpy() - ref) <= tol[..., None] + 2.0 ** -8 * (np.abs(ref) + tol[..., None])).all()
