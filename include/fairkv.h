@@ -446,7 +446,7 @@ typedef struct {
  * bad               device counter or NULL: plus one for every pair that is left alone (its length kept, none of its rows written), because
  *                   it has no room for all n, a row of them lies outside the cache or a position outside the table, and for every token whose
  *                   queries are left alone because its position lies outside the table.
- * An E4M3 cache takes x / scale rounded to nearest even, what is beyond +-448 as +-448.
+ * An E4M3 cache takes x / scale, the quotient of two fp32 numbers, rounded to nearest even, what is beyond +-448 as +-448.
  * Enqueues one kernel; no synchronisation.  FAIRKV_EUNSUPPORTED: q_len > FAIRKV_MAX_DRAFT, types, D. */
 int fairkv_append_rotated(const fairkv_cache *cache, const fairkv_rotation *r, const void *q, int64_t q_stride, const void *k_new,
                           int64_t k_stride, const void *v_new, int64_t v_stride, void *q_out, int32_t q_len, int32_t Hq, int32_t dtype,

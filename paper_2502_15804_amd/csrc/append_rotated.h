@@ -28,7 +28,7 @@ struct RotateArgs {
     int32_t apart;                        // how many passes' tokens further on, but for the workgroups' number of them, its next pass's lie
     int32_t n_scales;
     float eps;
-    float k_scale[kCacheScales], v_scale[kCacheScales];      // reciprocals
+    float k_scale[kCacheScales], v_scale[kCacheScales];
 };
 
 constexpr int kRow8 = 8;                  // elements of a row that a lane has
@@ -298,9 +298,9 @@ __global__ __launch_bounds__(256) void fairkv_append_rotated_kernel(RotateArgs a
         Eight<T>::floats(v_raw[u], y);
         norm_and_turn<D>(a, x, norm != nullptr, weight, turn_of(a, pos[u], piece), piece);
         if constexpr (CB == 1) {
-            const int sc = a.n_scales > 1 ? h : 0;
+            const int sc = a.n_scales > 1 ? h : 0;        // a rounded reciprocal would put one value in a thousand into the next step of the format
 #pragma unroll
-            for (int i = 0; i < kRow8; ++i) x[i] *= a.k_scale[sc], y[i] *= a.v_scale[sc];
+            for (int i = 0; i < kRow8; ++i) x[i] /= a.k_scale[sc], y[i] /= a.v_scale[sc];
         }
         Eight<C>::store(a.k + (row[u] * D + piece * kRow8) * CB, x);
         Eight<C>::store(a.v + (row[u] * D + piece * kRow8) * CB, y);

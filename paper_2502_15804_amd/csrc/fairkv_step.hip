@@ -31,7 +31,7 @@ int check_cache(const fairkv_cache *c)
     if (c->dtype != FAIRKV_E4M3) return c->n_scales == 0 ? FAIRKV_OK : FAIRKV_EINVAL;
     if (c->n_scales > FAIRKV_CACHE_SCALES) return FAIRKV_EUNSUPPORTED;
     if (c->n_scales != 1 && c->n_scales != c->Hkv) return FAIRKV_EINVAL;
-    auto usable = [](float scale) { return std::isfinite(scale) && scale != 0.f && std::isfinite(1.f / scale); };      // rows are multiplied by the reciprocal
+    auto usable = [](float scale) { return std::isfinite(scale) && scale != 0.f && std::isfinite(1.f / scale); };      // smaller ones have few bits of their own left
     for (int32_t h = 0; h < c->n_scales; ++h)
         if (!usable(c->k_scale[h]) || !usable(c->v_scale[h])) return FAIRKV_EINVAL;
     return FAIRKV_OK;
@@ -83,7 +83,7 @@ extern "C" int fairkv_append_rotated(const fairkv_cache *c, const fairkv_rotatio
     a.B = c->B, a.Hq = Hq, a.Hkv = c->Hkv, a.q_len = q_len, a.n_pos = r->n_pos, a.rot = r->table ? r->rot : 0, a.pairs = r->pairs;
     a.eps = r->eps;
     a.n_scales = c->n_scales;
-    for (int32_t h = 0; h < c->n_scales; ++h) a.k_scale[h] = 1.f / c->k_scale[h], a.v_scale[h] = 1.f / c->v_scale[h];
+    for (int32_t h = 0; h < c->n_scales; ++h) a.k_scale[h] = c->k_scale[h], a.v_scale[h] = c->v_scale[h];
     const int slots = 256 / (c->D / kRow8);
     a.head_slots = 1;
     while (a.head_slots * 2 <= std::min(Hq, slots)) a.head_slots *= 2;

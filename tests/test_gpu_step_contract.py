@@ -87,3 +87,23 @@ def test_rows_that_are_expected_cost_no_bits_of_a_bf16_output(expected, D, dtype
     # scores: D products in fp32, twice for the sum; the weights' bits; 92 fp32 sums; the output's own rounding
     tol = (2 * (s_top * D * 2.0 ** -24 + 2.0 ** -22) + 2.0 ** -16 + 92 * 2.0 ** -24) * v_top
     assert (np.abs(out.double().cpu().numpy() - ref) <= tol[..., None] + 2.0 ** -8 * (np.abs(ref) + tol[..., None])).all()
+
+
+@pytest.mark.parametrize("scales", [7.0, 0.02, 0.3, [1.0, 0.033], [448.0, 3e-3]])
+def test_8_bit_rows_are_the_quotient_rounded_to_nearest_even(scales):
+    """Every bf16 number as a value: the bytes of x / scale in fp32, rounded to E4M3, beyond +-448 as +-448."""
+    H = np.size(scales)
+    every = torch.arange(1 << 16, dtype=torch.int32).to(torch.uint16).view(torch.bfloat16).view(8, 64, 1, 128)
+    v_new = every.expand(8, 64, H, 128).contiguous()
+    n_rows = 8 * H * 64
+    k, v = (torch.zeros(n_rows, 128, dtype=torch.uint8, device=DEV) for _ in range(2))
+    off = torch.arange(8 * H, device=DEV).view(8, H) * 64
+    cache = F.Cache(k, v, I32(np.full((8, H), 64)), off=off, k_scale=scales, v_scale=scales)
+    q = torch.zeros(8, 64, H, 128, dtype=torch.bfloat16, device=DEV)
+    F.fairkv_append_rotated(cache, I32(np.zeros((8, H))), q, v_new.to(DEV), v_new.to(DEV), torch.empty_like(q))
+    x = v_new.float() / torch.tensor(scales, dtype=torch.float32).reshape(-1, 1)
+    want = torch.where(x.isnan(), x, x.clamp(-448, 448)).to(torch.float8_e4m3fn).transpose(1, 2).reshape(n_rows, 128)
+    nan = want.float().isnan()
+    for got in (k.cpu(), v.cpu()):
+        assert torch.equal(got.view(torch.float8_e4m3fn).float().isnan(), nan)
+        assert torch.equal(got[~nan], want.view(torch.uint8)[~nan])
