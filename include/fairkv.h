@@ -464,7 +464,8 @@ int fairkv_append_rotated(const fairkv_cache *cache, const fairkv_rotation *r, c
  * tree       device uint64 [B][q_len], or NULL
  * workspace  device, fairkv_tree_workspace_bytes(cache, Hq, q_len, n_slots) bytes, 16-byte aligned.  Its first fairkv_tree_counter_bytes(n_slots)
  *            bytes must be zero before the first use (fairkv_tree_workspace_reset); every completed call leaves them zero, and nothing else
- *            in it is kept from call to call, so calls of any shapes with one n_slots that are ordered on one stream may share it.
+ *            in it is kept from call to call, so calls of any shapes with one n_slots that are ordered on one stream may share it.  What
+ *            it takes does not fall with q_len, Hq or expected_rows: a workspace for a cache's longest draft is one for all shorter ones.
  * n_slots    workgroups to balance over: the GPU's compute units
  * out        device [B][q_len][Hq][D] of out_dtype (FAIRKV_F32 or FAIRKV_BF16); lse device float [B][q_len][Hq] or NULL
  * Lengths below 0 count as 0, those beyond the cache's rows (paged: max_pages * page_rows) as that many.

@@ -179,14 +179,16 @@ TreeShape tree_shape(const fairkv_cache *c, int32_t Hq, int32_t q_len, int32_t n
 
 constexpr int32_t kTreeBlocks = 32;      // of 32 columns: 16 heads of 64 nodes
 
-// The counters come first and take what n_slots alone says, so that calls of different shapes may share a workspace.
+// The counters come first and take what n_slots alone says, so that calls of different shapes may share a workspace.  The partials take what the
+// widest workgroups that a shape up to this one could have would leave in all slots, so that a workspace for the longest draft is one for every
+// shorter one: waves do not fall with the columns, and blocks * waves, the columns' blocks rounded up, does not either.
 struct TreeSpace {
     size_t counters, ml, o;
 };
 size_t tree_counters(int32_t n_slots) { return align256((static_cast<size_t>(n_slots) + kTreeBlocks) * 2 * kLevels * sizeof(int32_t)); }
 TreeSpace tree_space(const TreeShape &s, int32_t D, int32_t n_slots)
 {
-    const size_t groups = static_cast<size_t>(s.blocks) * s.slots, cols = 32 * static_cast<size_t>(s.waves);      // groups <= n_slots, or one a block
+    const size_t groups = static_cast<size_t>(std::max(n_slots, s.blocks)), cols = 32 * static_cast<size_t>(s.waves);      // at least blocks * slots
     return {tree_counters(n_slots), align256(groups * 2 * cols * 2 * sizeof(float)), align256(groups * 2 * cols * D * sizeof(float))};
 }
 
