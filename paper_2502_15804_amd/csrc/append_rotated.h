@@ -343,8 +343,8 @@ __global__ __launch_bounds__(256) void fairkv_accept_kernel(AcceptArgs a)
         to[u] = -1;
         if (own >= per_group || pair >= n_pairs) continue;
         const int b = pair / a.Hkv;
-        const int32_t nn = new_tokens(a.n_new, b, a.q_len), kept = a.n_path[b], base = a.len[pair] - nn;
-        bool ok = kept >= 0 && kept <= nn && base >= 0;
+        const int32_t nn = new_tokens(a.n_new, b, a.q_len), kept = a.n_path[b], length = a.len[pair], base = max(length, nn) - nn;
+        bool ok = kept >= 0 && kept <= nn && length >= nn;
         if (ok && i < kept) {
             const int32_t from = a.path[static_cast<int64_t>(b) * a.q_len + i];
             ok = from >= 0 && from < nn;

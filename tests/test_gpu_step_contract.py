@@ -107,3 +107,14 @@ def test_8_bit_rows_are_the_quotient_rounded_to_nearest_even(scales):
     for got in (k.cpu(), v.cpu()):
         assert torch.equal(got.view(torch.float8_e4m3fn).float().isnan(), nan)
         assert torch.equal(got[~nan], want.view(torch.uint8)[~nan])
+
+
+@pytest.mark.parametrize("page", [0, 16])
+def test_accept_of_nothing_leaves_the_smallest_lengths_alone(page):
+    """The draft's rows cannot be taken from a length of -2^31: the difference is no number of 32 bits."""
+    s = Setup([[20, 9]], 2, 64, page=page, seed=7)
+    s.lens_h = np.array([[-2 ** 31, 9]])
+    s.make()
+    bad = I32([0])
+    F.fairkv_accept(s.cache, s.lens, I32(np.zeros((1, 6))), I32([0]), bad=bad)
+    assert s.lens.cpu().tolist() == [[-2 ** 31, 3]] and int(bad) == 1
