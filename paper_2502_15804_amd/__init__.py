@@ -481,7 +481,8 @@ def fairkv_tree_counter_bytes(n_slots: int) -> int:
 def fairkv_tree_workspace_reset(workspace, n_slots, stream=None):
     """Enqueue the kernel that zeroes the counter bytes of a device workspace (see the header)."""
     _check_dev(workspace=workspace)
-    rc = lib().fairkv_tree_workspace_reset(_ptr(workspace), workspace.numel() * workspace.element_size(), int(n_slots), _stream(stream, workspace))
+    with _torch()[0].cuda.device(workspace.get_device()):      # whichever is the current one
+        rc = lib().fairkv_tree_workspace_reset(_ptr(workspace), workspace.numel() * workspace.element_size(), int(n_slots), _stream(stream, workspace))
     if rc != FAIRKV_OK:
         raise FairKVError(rc, "fairkv_tree_workspace_reset")
 
