@@ -436,6 +436,9 @@ class Cache:
             raise ValueError("cap must be int32 [B, Hkv], off int64 of its size")
         if pages is not None and (pages.dtype != torch.int32 or pages.dim() not in (2, 3) or pages.shape[:-1].numel() != cap.numel()):
             raise ValueError("pages must be int32 [B, Hkv, max_pages]")
+        for name, n, bits in (("page_rows", page_rows, 31), ("expected_rows", expected_rows, 63)):      # a ctypes field would take the low bits
+            if n is not None and int(n) >> bits != 0:
+                raise ValueError(f"{name} must be a number of {bits} bits")
         _check_dev(k=k, v=v, cap=cap, off=off, pages=pages)
         if any(t is not None and t.device != k.device for t in (v, cap, off, pages)):
             raise ValueError("the tensors of a cache must be on one device")

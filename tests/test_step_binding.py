@@ -37,3 +37,11 @@ def test_a_workspace_is_reset_on_its_own_device(monkeypatch):
     monkeypatch.setattr(F, "lib", lambda: Library)
     F.fairkv_tree_workspace_reset(Workspace(), 256, stream=Stream)
     assert seen == [(1, 77)] and current == [0]
+
+
+@pytest.mark.parametrize("kw", [dict(page_rows=(1 << 32) + 16), dict(page_rows=1 << 31), dict(page_rows=-16), dict(expected_rows=1 << 63), dict(expected_rows=(1 << 64) + 5),
+                                dict(expected_rows=-1)])
+def test_a_cache_refuses_numbers_that_its_fields_do_not_hold(kw):
+    k, cap, pages = torch.zeros(16, 64, dtype=torch.bfloat16), torch.ones(1, 1, dtype=torch.int32), torch.zeros(1, 1, dtype=torch.int32)
+    with pytest.raises(ValueError, match="bits"):
+        F.Cache(k, k, cap, pages=pages, **{**dict(page_rows=16), **kw})
