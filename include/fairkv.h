@@ -447,7 +447,8 @@ typedef struct {
  *                   it has no room for all n, a row of them lies outside the cache or a position outside the table, and for every token whose
  *                   queries are left alone because its position lies outside the table.
  * An E4M3 cache takes x / scale, the quotient of two fp32 numbers, rounded to nearest even, what is beyond +-448 as +-448.
- * Enqueues one kernel; no synchronisation.  FAIRKV_EUNSUPPORTED: q_len > FAIRKV_MAX_DRAFT, types, D. */
+ * Enqueues one kernel; no synchronisation.  FAIRKV_EUNSUPPORTED: q_len > FAIRKV_MAX_DRAFT, types, D.  FAIRKV_EINVAL also: more than 2^24 - 1
+ * workgroups, of 64 tokens' queries each and of one pair or more each. */
 int fairkv_append_rotated(const fairkv_cache *cache, const fairkv_rotation *r, const void *q, int64_t q_stride, const void *k_new,
                           int64_t k_stride, const void *v_new, int64_t v_stride, void *q_out, int32_t q_len, int32_t Hq, int32_t dtype,
                           const int32_t *n_new, const int32_t *len, int32_t *len_out, int32_t *bad, void *hip_stream);
@@ -481,7 +482,8 @@ int fairkv_decode_attn_tree(const fairkv_cache *cache, const void *q, const uint
 /* Keeps n_path[b] of the n = n_new[b] draft rows at the end of every pair: draft row path[b][i] becomes draft row i for i < n_path[b], and
  * len_out[p] = len[p] - n + n_path[b].  path: device int32 [B][q_len], in any order, what is behind n_path[b] is not read; n_path device [B].
  * A pair is left alone (its length kept) and counted in *bad if n_path[b] is not in 0 .. n, an entry not in 0 .. n - 1, its length below n,
- * or a row outside the cache.  len_out may be len; bad may be NULL.  Enqueues one kernel; no synchronisation. */
+ * or a row outside the cache.  len_out may be len; bad may be NULL.  Enqueues one kernel; no synchronisation.  FAIRKV_EINVAL also: more
+ * than 2^24 - 1 workgroups, of one pair or more each. */
 int fairkv_accept(const fairkv_cache *cache, const int32_t *path, const int32_t *n_path, const int32_t *n_new, const int32_t *len,
                   int32_t *len_out, int32_t q_len, int32_t *bad, void *hip_stream);
 

@@ -16,6 +16,7 @@ using namespace fairkv;
 
 bool aligned(const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+constexpr int64_t kMaxGroups = UINT32_MAX / 256;      // a grid's threads are counted in 32 bits
 int launched() { return hipGetLastError() == hipSuccess ? FAIRKV_OK : FAIRKV_EHIP; }
 
 int check_cache(const fairkv_cache *c)
@@ -96,7 +97,7 @@ extern "C" int fairkv_append_rotated(const fairkv_cache *c, const fairkv_rotatio
     a.q_groups = static_cast<int32_t>((tokens + tokens_each - 1) / tokens_each);
     a.apart = static_cast<int32_t>(std::max<int64_t>(1, q_len / tokens_each));      // the passes of a workgroup go once through a sequence
     const int64_t grid = a.q_groups + (static_cast<int64_t>(c->B) * c->Hkv + pairs_each - 1) / pairs_each;
-    if (grid > INT32_MAX) return FAIRKV_EINVAL;
+    if (grid > kMaxGroups) return FAIRKV_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (dtype == FAIRKV_F32)
         launch_rotated<float, float>(c->D, static_cast<unsigned>(grid), st, a);
@@ -115,7 +116,9 @@ extern "C" int fairkv_accept(const fairkv_cache *c, const int32_t *path, const i
     if (q_len > FAIRKV_MAX_DRAFT) return FAIRKV_EUNSUPPORTED;
     const AcceptArgs a{static_cast<char *>(c->k), static_cast<char *>(c->v), path, n_path, n_new, len, len_out, bad, row_map(c), c->B, c->Hkv, q_len};
     const int rb = c->D * (c->dtype == FAIRKV_E4M3 ? 1 : c->dtype == FAIRKV_BF16 ? 2 : 4), slots = 256 / (rb / 16), each = std::max(1, slots / q_len);
-    const dim3 grid(static_cast<unsigned>((c->B * c->Hkv + each - 1) / each));
+    const int64_t groups = (static_cast<int64_t>(c->B) * c->Hkv + each - 1) / each;
+    if (groups > kMaxGroups) return FAIRKV_EINVAL;
+    const dim3 grid(static_cast<unsigned>(groups));
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (rb == 64)
         hipLaunchKernelGGL(fairkv_accept_kernel<64>, grid, dim3(256), 0, st, a);
