@@ -397,8 +397,9 @@ int fairkv_plan_grow(fairkv_item *items, int32_t n_items, int32_t B, int32_t Hkv
  *   packed (off given, pages null)   row off[p] + t
  *   paged (pages given, off null)    row pages[p * max_pages + t / page_rows] * page_rows + t % page_rows
  * A pair may hold cap[p] tokens (paged: and max_pages * page_rows).  Rows of different pairs must not overlap; pages that no
- * token lies in are not looked at.  A pair whose off, or a token whose page, lies outside the n_rows rows has no such row:
- * such tokens are not attended to, and nothing is appended or moved there. */
+ * token lies in are not looked at.  A token whose page or row lies outside the n_rows rows has no such row:
+ * it is not attended to, and nothing is appended or moved there.  A packed pair whose run of len rows does not lie inside the cache as a whole is
+ * not attended to at all (its nodes see nothing); append and accept look at the rows that they read and write. */
 enum { FAIRKV_MAX_DRAFT = 64,     /* most new tokens of a sequence in one call */
        FAIRKV_CACHE_SCALES = 32 };
 
@@ -457,7 +458,7 @@ int fairkv_append_rotated(const fairkv_cache *cache, const fairkv_rotation *r, c
  * them there); node i < n of sequence b sees every row in front of them and draft row j < n iff bit j of tree[b][i] is set: its ancestors'
  * bits and, as a rule, its own.  tree == NULL: nodes 0 .. i, a chain; q_len = 1 is a plain decode step.
  * out = softmax(scale * q . K^T) V over the rows that are seen, in fp32, and lse = log sum exp of the scaled scores; a node that sees
- * nothing gets out = 0 and lse = -inf.  An infinite or NaN row counts for the nodes that see it only: an
+ * nothing, or only rows whose scores are -inf, gets out = 0 and lse = -inf.  An infinite or NaN row counts for the nodes that see it only: an
  * infinite value gives an infinite output as long as its weight, next to the largest, is one of fp32's normal numbers (2^-126), below that an
  * infinite one or NaN, as 0 times infinity.  Softmax weights have all 24 bits for an fp32
  * output, 2^-16 of them are lost for a bf16 one.  Nodes i >= n are left as they are.

@@ -118,3 +118,44 @@ def test_accept_of_nothing_leaves_the_smallest_lengths_alone(page):
     bad = I32([0])
     F.fairkv_accept(s.cache, s.lens, I32(np.zeros((1, 6))), I32([0]), bad=bad)
     assert s.lens.cpu().tolist() == [[-2 ** 31, 3]] and int(bad) == 1
+
+
+@pytest.mark.parametrize("q_len", WIDTHS)
+def test_scores_of_minus_infinity_count_as_rows_that_are_not_seen(q_len):
+    s = Setup([[70, 70, 2], [300, 300, 300]], q_len, 64, seed=11)
+    s.lens_h = s.lens_h + q_len
+    s.make()
+    q = torch.randn(2, q_len, 24, 64, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).to(DEV)
+    q[..., 0] = 1
+    for p in range(6):
+        rows = [s.row(p, t) for t in range(int(s.lens_h.reshape(-1)[p]))]
+        s.k[rows if p != 1 else rows[1:], 0] = -math.inf         # pair 1: but for its first row
+    got, lse = (x.cpu() for x in _attend(s, 24, q_len, torch.float32, n_slots=16, q=q)[1:3])
+    first = s.v[s.row(1, 0)].float().cpu().expand(q_len, 8, 64)
+    # a weight p next to 1 in three parts, (p v) (1 / p): three sums of the parts' products, a quotient and a product, 2^-24 each
+    assert ((got[0, :, 8:16] - first).abs() <= 2.0 ** -21 * first.abs()).all() and lse[0, :, 8:16].isfinite().all()
+    got[0, :, 8:16], lse[0, :, 8:16] = 0, -math.inf
+    assert not got.any() and (lse == -math.inf).all()
+
+
+def test_a_packed_run_that_sticks_out_of_the_cache():
+    """It is not attended to; what accept moves lies inside, and so does not move where it would not; an append behind it is left alone."""
+    s = Setup([[40, 40]], 8, 64, seed=12)
+    s.off[0] = s.n_rows - 38                                     # tokens 38 and 39 have no row
+    s.make()
+    q, out, lse, _ = _attend(s, 2, 4, torch.float32, n_slots=4)
+    assert not out[:, :, 0].any() and (lse[:, :, 0] == -math.inf).all() and lse[:, :, 1].isfinite().all()
+    k0, v0 = s.k.clone(), s.v.clone()
+    for path, moved in (([3, 1, 0, 0], False), ([1, 0, 0, 0], True)):
+        s.k.copy_(k0), s.v.copy_(v0)
+        bad, lens = I32([0]), torch.zeros_like(s.lens)
+        F.fairkv_accept(s.cache, s.lens, I32([path]), I32([2]), lens_out=lens, bad=bad)
+        assert lens.cpu().tolist() == [[38 if moved else 40, 38]] and int(bad) == (0 if moved else 1)
+        ref_k, ref_v = k0.clone(), v0.clone()
+        for p in range(0 if moved else 1, 2):
+            at = [s.row(p, 36 + i) for i in range(2)], [s.row(p, 36 + i) for i in path[:2]]
+            ref_k[at[0]], ref_v[at[0]] = k0[at[1]], v0[at[1]]
+        assert torch.equal(s.k, ref_k) and torch.equal(s.v, ref_v)
+    bad, rows = I32([0]), torch.ones(1, 1, 2, 64, dtype=torch.bfloat16, device=DEV)
+    F.fairkv_append_rotated(s.cache, s.lens, rows, rows, rows, torch.empty_like(rows), bad=bad)
+    assert s.lens.cpu().tolist() == [[40, 41]] and int(bad) == 1
