@@ -415,9 +415,9 @@ typedef struct {
     int32_t dtype;           /* FAIRKV_BF16, FAIRKV_E4M3 or (append, accept) FAIRKV_F32 */
     int32_t n_scales;        /* E4M3: 1, or Hkv (at most FAIRKV_CACHE_SCALES): a stored byte of head h stands for byte * k_scale[h]; else 0 */
     float k_scale[FAIRKV_CACHE_SCALES], v_scale[FAIRKV_CACHE_SCALES];   /* finite, not 0, their reciprocals finite */
-    int64_t expected_rows;   /* rows that all pairs together are expected to have, 0: as many as there are.  Only what is fast depends on it: the
-                              * attention deals its columns for so much work (and takes a workspace for that).  Worth giving where the cache is made
-                              * for far more rows than the sequences have. */
+    int64_t expected_rows;   /* rows that all pairs together are expected to have, 0: as many as there are.  Only what is fast, and the order of sums,
+                              * depends on it: the attention deals its columns for so much work (and takes a workspace for that).  Worth giving where
+                              * the cache is made for far more rows than the sequences have. */
 } fairkv_cache;              /* a host struct; 344 bytes */
 
 /* What is done to the heads of new queries and keys before they are used, all of it in fp32, rounded once at the end:

@@ -21,10 +21,10 @@
 // in the order of the pieces.
 //
 // What bounds it (MI355X, D 128, 8 KV heads, G 8; times of a launch in a row of them).  Long pairs with few columns: memory, 32 x 8 heavy-tailed
-// pairs of 32 columns 166 MB in 38 us (4.3 TB/s).  Many columns: power, 64 x 8 pairs of 4096 rows and 512 columns 653 us (855 TFLOP/s; matrix
-// cores busy in 37 % of the cycles while the clock falls from 2.4 to 1.7 GHz, so cycles that overlapping saves come back as a lower clock).  In
-// between, the fixed parts: 5 us until the first tile is there (lengths, shares, first rows), 5 to 8 for a piece's queries, fold and join.  16 x 8
-// pairs of 1024 rows, 128 columns: 34 us, 31 from an 8-bit cache; one sequence with 24 nodes: 15 us.
+// pairs of 32 columns 166 MB in 39 us (4.3 TB/s).  Many columns: power, 64 x 8 pairs of 4096 rows and 512 columns 852 us (655 TFLOP/s, 980 with the
+// weights' second halves; matrix cores busy in 46 % of the cycles while the clock falls from 2.3 to 1.6 GHz, so cycles that overlapping saves come
+// back as a lower clock).  In between, the fixed parts: 5 us until the first tile is there (lengths, shares, first rows), 5 to 8 for a piece's
+// queries, fold and join.  16 x 8 pairs of 1024 rows, 128 columns: 35 us, 32 from an 8-bit cache; one sequence with 24 nodes: 15 us.
 #pragma once
 #include "cache_rows.h"
 #include "decode_mfma.h"
