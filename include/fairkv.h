@@ -440,7 +440,8 @@ typedef struct {
  * q, k_new, v_new   device, of type dtype (BF16, or F32 with an F32 cache): token (b, i) at element (b * q_len + i) * stride, its Hq (Hkv)
  *                   heads one behind the other; strides in elements, at least Hq * D (Hkv * D), so that all three may lie in one
  *                   projection's output.  16-byte aligned, strides multiples of 16 bytes.
- * q_out             device [B][q_len][Hq][D] of type dtype; may be q where q's tokens follow one another
+ * q_out             device [B][q_len][Hq][D] of type dtype; may be q where q's tokens follow one another, else it must not meet what lies from
+ *                   the first to the last token of q, k_new or v_new
  * n_new             device [B]: how many of the q_len tokens a sequence has (taken into 0 .. q_len), or NULL: all.  What is behind them is not
  *                   read, and the queries there are left as they are.
  * len_out           device [B][Hkv]; may be len

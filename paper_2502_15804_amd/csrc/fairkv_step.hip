@@ -67,12 +67,20 @@ extern "C" int fairkv_append_rotated(const fairkv_cache *c, const fairkv_rotatio
     const int64_t elem = dtype == FAIRKV_BF16 ? 2 : 4, tokens = static_cast<int64_t>(c->B) * q_len;
     if (q_stride < static_cast<int64_t>(Hq) * c->D || k_stride < static_cast<int64_t>(c->Hkv) * c->D || v_stride < static_cast<int64_t>(c->Hkv) * c->D)
         return FAIRKV_EINVAL;
-    if (q_stride * elem % 16 != 0 || k_stride * elem % 16 != 0 || v_stride * elem % 16 != 0) return FAIRKV_EINVAL;
+    if (q_stride % (16 / elem) != 0 || k_stride % (16 / elem) != 0 || v_stride % (16 / elem) != 0) return FAIRKV_EINVAL;
     if (!aligned(q, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(q_out, 16)) return FAIRKV_EINVAL;
     if ((r->q_norm || r->k_norm) && !(r->eps >= 0.f && std::isfinite(r->eps))) return FAIRKV_EINVAL;
     if (r->table && (!r->pos || r->n_pos < 1 || r->rot < 16 || r->rot % 16 != 0 || r->rot > c->D || !aligned(r->table, 16))) return FAIRKV_EINVAL;
-    if (tokens > INT32_MAX - 256 || q_out == k_new || q_out == v_new) return FAIRKV_EINVAL;
-    if (q_out == q && q_stride != static_cast<int64_t>(Hq) * c->D) return FAIRKV_EINVAL;
+    if (tokens > INT32_MAX - 256) return FAIRKV_EINVAL;
+    // Queries are written while others are read: q_out is q itself, token by token, or apart from all that is read.
+    const int64_t q_row = static_cast<int64_t>(Hq) * c->D, kv_row = static_cast<int64_t>(c->Hkv) * c->D;
+    auto meets = [&](const void *from, int64_t stride, int64_t row) {
+        const auto read = reinterpret_cast<uintptr_t>(from), written = reinterpret_cast<uintptr_t>(q_out);
+        const auto end = static_cast<unsigned __int128>(read) + (static_cast<unsigned __int128>(tokens - 1) * stride + row) * elem;
+        return written < end && read < static_cast<unsigned __int128>(written) + static_cast<unsigned __int128>(tokens) * q_row * elem;
+    };
+    if (meets(k_new, k_stride, kv_row) || meets(v_new, v_stride, kv_row)) return FAIRKV_EINVAL;
+    if (!(q_out == q && q_stride == q_row) && meets(q, q_stride, q_row)) return FAIRKV_EINVAL;
 
     RotateArgs a{};
     a.q = static_cast<const char *>(q), a.k_new = static_cast<const char *>(k_new), a.v_new = static_cast<const char *>(v_new);

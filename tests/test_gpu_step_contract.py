@@ -159,3 +159,28 @@ def test_a_packed_run_that_sticks_out_of_the_cache():
     bad, rows = I32([0]), torch.ones(1, 1, 2, 64, dtype=torch.bfloat16, device=DEV)
     F.fairkv_append_rotated(s.cache, s.lens, rows, rows, rows, torch.empty_like(rows), bad=bad)
     assert s.lens.cpu().tolist() == [[40, 41]] and int(bad) == 1
+
+
+@pytest.mark.parametrize("dtype,page", [("bf16", 0), ("kv8", 16)])
+def test_one_token_without_its_dimension_and_words_without_a_sign(dtype, page):
+    """[B, H, D] is [B, 1, H, D], pages [B * Hkv, n] are [B, Hkv, n], a uint64 word is an int64 one: the same bits."""
+    s = Setup([[70, 9], [300, 0]], 4, 128, dtype, page, seed=14, scales=True)
+    q, k_new, v_new = (torch.randn(2, 1, h, 128, generator=torch.Generator().manual_seed(h)).to(torch.bfloat16).to(DEV) for h in (16, 2, 3))
+    v_new = v_new[:, :, 1:]
+    k0, v0, results = s.k.clone(), s.v.clone(), []
+    for flat in (False, True):
+        s.k.copy_(k0), s.v.copy_(v0)
+        pages = {} if not page else dict(pages=I32(s.pages.reshape(2, 2, -1) if flat else s.pages), page_rows=page)
+        kw = dict(k_scale=s.ks.tolist(), v_scale=s.vs.tolist()) if dtype == "kv8" else {}
+        cache = F.Cache(s.k, s.v, I32(s.cap_h), **kw, **(pages or dict(off=torch.as_tensor(s.off if flat else s.off.reshape(2, 2), device=DEV))))
+        x = [t[:, 0] if flat else t for t in (q, k_new, v_new)]
+        lens, q_out, lse = I32(s.lens_h), torch.empty_like(x[0]), torch.empty(x[0].shape[:-1], device=DEV)
+        out = torch.empty(q_out.shape, device=DEV)
+        F.fairkv_append_rotated(cache, lens, *x, q_out, q_norm=torch.ones(128, device=DEV))
+        tree = torch.full((2, 1), 1, dtype=torch.uint64 if flat else torch.int64, device=DEV)
+        F.fairkv_decode_attn_tree(cache, lens, q_out, torch.zeros(F.fairkv_tree_workspace_bytes(cache, 16, 1), dtype=torch.uint8, device=DEV), out, lse, 0.1, tree=tree)
+        F.fairkv_accept(cache, lens, I32([[0], [0]]), I32([1, 0]))
+        results.append([t.flatten() for t in (lens, q_out, out, lse, s.k.view(torch.uint8), s.v.view(torch.uint8))])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+    assert results[0][0].tolist() == [71, 10, 300, 0] and results[0][2].isfinite().all()
