@@ -489,6 +489,72 @@ int fairkv_decode_attn_tree(const fairkv_cache *cache, const void *q, const uint
 int fairkv_accept(const fairkv_cache *cache, const int32_t *path, const int32_t *n_path, const int32_t *n_new, const int32_t *len,
                   int32_t *len_out, int32_t q_len, int32_t *bad, void *hip_stream);
 
+/* ---- compression of a growing cache: which rows matter, which stay, and away with the others ---------
+ *
+ * What makes a cache one that is compressed per head (the setting above) and keeps it one while it grows.  Three calls, which read lengths and lists
+ * on the GPU and may be captured:
+ *
+ *     fairkv_attn_weights    the attention weight that the last tokens' queries give every row, added to what it had
+ *     fairkv_select          which rows of every pair stay, under a budget of the pair or of the sequence
+ *     fairkv_evict           these rows move to the front of their pair, or into another cache
+ *
+ * Weights lie as the rows do: weights[row] belongs to row `row` of the cache, whichever pair and token that is. */
+
+/* For every token t of every pair, over the q_len queries of a sequence (its last n = n_new[b] tokens, whose rows are in the cache already):
+ *     weights_out[row] = decay * weights[row] + sum over the nodes i < n that see t, and the heads g of the group, of exp(scale * q . k_t - lse)
+ * in fp32; a row of the last n themselves starts from 0 instead of from decay * weights[row], and with decay 0 weights are not read.  Who sees what
+ * is as in fairkv_decode_attn_tree, whose lse of the same queries it takes.
+ * q            device bf16 [B][q_len][Hq][D], 16-byte aligned; Hq a multiple of Hkv, any Hq / Hkv up to 16
+ * tree, n_new  as in fairkv_decode_attn_tree; queries and lse of nodes i >= n are not read
+ * lse          device float [B][q_len][Hq]; -inf for a node that sees nothing, which gives no weight
+ * weights      device float [n_rows]; weights_out may be weights, or must not meet it
+ * n_slots      the GPU's compute units
+ * Rows of no token are left as they are, and so are those of a packed pair whose run sticks out of the cache.  The sums are the same from call to
+ * call.  A NaN or infinite row counts for the nodes that see it, in its own weight only.
+ * Enqueues one kernel; no synchronisation, no workspace.  FAIRKV_EUNSUPPORTED: q_len > FAIRKV_MAX_DRAFT, an F32 cache, D, Hq / Hkv > 16.
+ * FAIRKV_EINVAL also: more than 2^31 - 1 elements of q, a decay, or a scale (times a k_scale) in log2 units, that is not finite. */
+int fairkv_attn_weights(const fairkv_cache *cache, const void *q, const uint64_t *tree, const int32_t *n_new, const int32_t *len,
+                        const float *lse, const float *weights, float *weights_out, float decay, int32_t n_slots, int32_t q_len,
+                        int32_t Hq, float scale, void *hip_stream);
+
+typedef struct {
+    const int32_t *budget;   /* device [B][Hkv]: rows that a pair may keep; shared: [B], rows that the pairs of a sequence may keep together */
+    int32_t shared;          /* 0 or 1 */
+    int32_t pool;            /* odd, 1 .. 63 */
+    int32_t sink, recent;    /* >= 0 */
+} fairkv_selection;
+
+/* The first `sink` and the last `recent` tokens of a pair are protected and stay, whatever the budget.  Of the others, the candidates, each has the value
+ * max weights[row of u] over the candidates u of its pair with |u - t| <= pool / 2, and the largest values of a pair (shared: of a sequence) stay, as many
+ * as the budget leaves room for behind the protected tokens.  Of equal values that of the lower head stays, then that of the lower token; -0 is
+ * 0, and a NaN is as low as -inf.  A token that has no row in the cache does not stay and takes no part.
+ * weights    device float [n_rows]
+ * keep       device [B][Hkv][max_keep], out: the tokens that stay, ascending; what is behind them is left as it is
+ * n_keep     device [B][Hkv], out: their number; -1, and the pair counted in *bad, for a pair with more than max_keep of them, whose list then says nothing
+ * bad        device counter or NULL
+ * workspace  device, fairkv_select_workspace_bytes(cache, shared, n_slots) bytes, 16-byte aligned, all of it zero before the first use; every completed
+ *            call leaves it so, so calls of any shapes that are ordered on one stream may share a workspace that is large enough for each
+ * n_slots    the GPU's compute units
+ * No synchronisation.  FAIRKV_EUNSUPPORTED: pool > 63. */
+size_t fairkv_select_workspace_bytes(const fairkv_cache *cache, int32_t shared, int32_t n_slots);
+int fairkv_select(const fairkv_cache *cache, const fairkv_selection *s, const float *weights, const int32_t *len, int32_t *keep,
+                  int32_t max_keep, int32_t *n_keep, int32_t *bad, void *workspace, size_t workspace_bytes, int32_t n_slots,
+                  void *hip_stream);
+
+/* Row keep[p][i] of every pair becomes its row i for i < n_keep[p], K, V and, if given, its weight; len_out[p] = n_keep[p].
+ * into         NULL: in place, a list has to ascend.  Else another cache of the same B, Hkv, D, type and scales, whose rows of these pairs are none that
+ *              this one's tokens have (its pages may be of the same pool): lists may be in any order and name a token twice.
+ * keep         device [B][Hkv][max_keep], n_keep device [B][Hkv], as fairkv_select leaves them
+ * len_out      device [B][Hkv]; may be len, must not meet n_keep
+ * weights      device float [n_rows] and weights_out device float [n_rows of into], or both NULL; in place the same
+ * A pair is left alone and counted in *bad, its length kept (into another cache: 0, and what is in its rows there says nothing), if n_keep[p] is not in
+ * 0 .. max_keep (in place: or its length; else: or its room there), an entry not in 0 .. len - 1, not ascending (in place), or a row outside its cache.
+ * Pages behind ceil(len_out / page_rows) hold no token of a pair any more.  Packed rows stay where the pair's run begins.
+ * Enqueues two kernels; no synchronisation. */
+int fairkv_evict(const fairkv_cache *cache, const fairkv_cache *into, const int32_t *keep, int32_t max_keep, const int32_t *n_keep,
+                 const int32_t *len, int32_t *len_out, const float *weights, float *weights_out, int32_t *bad, int32_t n_slots,
+                 void *hip_stream);
+
 /* The measurement aids (the decode kernel with wall-clock stamps, the reader that only streams) are declared in
  * fairkv_measure.h: they are in the library for the benchmark, not for callers of the method. */
 

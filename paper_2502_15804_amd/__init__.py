@@ -34,6 +34,7 @@ EXPORTS = ("fairkv_default_params", "fairkv_plan", "fairkv_workspace_bytes", "fa
            "fairkv_decode_attn_static", "fairkv_decode_attn_trace",
            "fairkv_place", "fairkv_pack", "fairkv_append", "fairkv_plan_grow", "fairkv_stream_probe", "fairkv_stream_probe_shape", "fairkv_workspace_reset",
            "fairkv_append_rotated", "fairkv_decode_attn_tree", "fairkv_tree_workspace_bytes", "fairkv_tree_counter_bytes", "fairkv_tree_workspace_reset", "fairkv_accept",
+           "fairkv_attn_weights", "fairkv_select", "fairkv_select_workspace_bytes", "fairkv_evict",
            "fairkv_strerror", "fairkv_version")
 
 
@@ -76,6 +77,10 @@ class fairkv_cache(ctypes.Structure):
 class fairkv_rotation(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("q_norm", "k_norm", "table", "pos")] + [("eps", ctypes.c_float)] + [
         (n, ctypes.c_int32) for n in ("n_pos", "rot", "pairs")]
+
+
+class fairkv_selection(ctypes.Structure):
+    _fields_ = [("budget", ctypes.c_void_p)] + [(n, ctypes.c_int32) for n in ("shared", "pool", "sink", "recent")]
 
 
 SHARE_DTYPE = np.dtype([(n, np.int32) for n, _ in fairkv_share._fields_])
@@ -168,6 +173,14 @@ def lib() -> ctypes.CDLL:
         L.fairkv_decode_attn_tree.argtypes = [cache_p, vp, vp, vp, vp, vp, ctypes.c_size_t, i32, vp, vp, i32, i32, i32, ctypes.c_float, vp]
         L.fairkv_accept.restype = ctypes.c_int
         L.fairkv_accept.argtypes = [cache_p, vp, vp, vp, vp, vp, i32, vp, vp]
+        L.fairkv_attn_weights.restype = ctypes.c_int
+        L.fairkv_attn_weights.argtypes = [cache_p, vp, vp, vp, vp, vp, vp, vp, ctypes.c_float, i32, i32, i32, ctypes.c_float, vp]
+        L.fairkv_select_workspace_bytes.restype = ctypes.c_size_t
+        L.fairkv_select_workspace_bytes.argtypes = [cache_p, i32, i32]
+        L.fairkv_select.restype = ctypes.c_int
+        L.fairkv_select.argtypes = [cache_p, ctypes.POINTER(fairkv_selection), vp, vp, vp, i32, vp, vp, vp, ctypes.c_size_t, i32, vp]
+        L.fairkv_evict.restype = ctypes.c_int
+        L.fairkv_evict.argtypes = [cache_p, cache_p, vp, i32, vp, vp, vp, vp, vp, vp, i32, vp]
         L.fairkv_strerror.restype = ctypes.c_char_p
         L.fairkv_strerror.argtypes = [ctypes.c_int]
         L.fairkv_version.restype = ctypes.c_int
@@ -319,7 +332,7 @@ def _native():
         m.init(ITEM_DTYPE, *(ctypes.cast(f, ctypes.c_void_p).value for f in (
             L.fairkv_decode_attn_multi, L.fairkv_decode_attn_static, L.fairkv_decode_attn_trace, L.fairkv_decode_attn_kv8,
             L.fairkv_decode_attn_kv8_per_head, L.fairkv_pack, L.fairkv_append, L.fairkv_append_rotated, L.fairkv_decode_attn_tree,
-            L.fairkv_accept)))
+            L.fairkv_accept, L.fairkv_attn_weights, L.fairkv_select, L.fairkv_evict)))
         _native_module = m
     return _native_module
 
@@ -510,6 +523,48 @@ def fairkv_accept(cache, lens, path, n_path, n_new=None, lens_out=None, bad=None
     rc = (_native_module or _native()).accept((_pt or _torch())[1], cache.address, cache.device, lens, path, n_path, n_new, lens_out, bad, stream)
     if rc != FAIRKV_OK:
         raise FairKVError(rc, "fairkv_accept")
+
+
+def fairkv_attn_weights(cache, lens, q, lse, weights, scale, tree=None, n_new=None, decay=0.0, weights_out=None, n_slots=None, stream=None):
+    """Enqueue the sum of the attention weights that the last tokens' queries give every row of the cache (see the header).
+
+    q bfloat16 [B, q_len, Hq, D] (or [B, Hq, D]), lse float32 [B, q_len, Hq], tree and n_new as in fairkv_decode_attn_tree, which leaves that lse; lens int32
+    [B, Hkv]; weights float32 [n_rows], one to a row of the cache: what it holds counts `decay` times, 0: it is not read.  weights_out=None: in
+    place.  Nothing is allocated or synchronised here."""
+    rc = (_native_module or _native()).attn_weights((_pt or _torch())[1], cache.address, cache.device, lens, q, lse, weights, weights_out, scale, tree, n_new,
+                                                    decay, cache.n_slots if n_slots is None else n_slots, stream)
+    if rc != FAIRKV_OK:
+        raise FairKVError(rc, "fairkv_attn_weights")
+
+
+def fairkv_select_workspace_bytes(cache, shared: bool, n_slots=None) -> int:
+    """Bytes of the workspace of fairkv_select, which has to be zero-filled before its first use; shared: the heads of a sequence share a budget."""
+    return int(lib().fairkv_select_workspace_bytes(ctypes.byref(cache.struct), int(shared), cache.n_slots if n_slots is None else int(n_slots)))
+
+
+def fairkv_select(cache, lens, weights, budget, keep, n_keep, workspace, pool=1, sink=0, recent=0, bad=None, n_slots=None, stream=None):
+    """Enqueue the choice of the rows that stay (see the header).
+
+    weights float32 [n_rows]; budget int32 [B, Hkv] (a pair's own) or [B] (shared by the heads of a sequence); keep int32 [B, Hkv, max_keep] and n_keep
+    int32 [B, Hkv] are written: the tokens that stay, ascending, and their number; workspace uint8 of fairkv_select_workspace_bytes, zero-filled
+    before its first use; bad int32 [1].  The first `sink` and the last `recent` tokens of a pair always stay."""
+    rc = (_native_module or _native()).select((_pt or _torch())[1], cache.address, cache.device, lens, weights, budget, keep, n_keep, workspace, pool, sink,
+                                              recent, bad, cache.n_slots if n_slots is None else n_slots, stream)
+    if rc != FAIRKV_OK:
+        raise FairKVError(rc, "fairkv_select")
+
+
+def fairkv_evict(cache, lens, keep, n_keep, into=None, lens_out=None, weights=None, weights_out=None, bad=None, n_slots=None, stream=None):
+    """Enqueue the move of the rows that stay to the front of their pair (see the header).
+
+    keep int32 [B, Hkv, max_keep], n_keep int32 [B, Hkv] as fairkv_select leaves them.  into=None: in place; lens_out=None: lens is written over.  into: a
+    Cache of the same B, Hkv, D, type and scales that the rows go to, lens_out its lengths.  weights float32 [n_rows] move with their rows, into
+    weights_out float32 [into's n_rows] (in place: None); bad int32 [1]."""
+    rc = (_native_module or _native()).evict((_pt or _torch())[1], cache.address, cache.device, lens, keep, n_keep, None if into is None else into.address,
+                                             cache.device if into is None else into.device, lens_out, weights, weights_out, bad,
+                                             cache.n_slots if n_slots is None else n_slots, stream)
+    if rc != FAIRKV_OK:
+        raise FairKVError(rc, "fairkv_evict")
 
 
 def fairkv_workspace_reset(workspace, n_pairs, stream=None):

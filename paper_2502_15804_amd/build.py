@@ -14,9 +14,9 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfairkv.so")
 BINDING = os.path.join(HERE, "_binding.so")
 BINDING_SOURCE = os.path.join(CSRC, "binding.cpp")
-SOURCES = [os.path.join(CSRC, "fairkv_api.hip"), os.path.join(CSRC, "fairkv_step.hip"), os.path.join(CSRC, "fairkv_plan.cpp"),
+SOURCES = [os.path.join(CSRC, "fairkv_api.hip"), os.path.join(CSRC, "fairkv_step.hip"), os.path.join(CSRC, "fairkv_compress.hip"), os.path.join(CSRC, "fairkv_plan.cpp"),
            os.path.join(CSRC, "fairkv_place.cpp")]
-HEADERS = [os.path.join(ROOT, "include", "fairkv.h"), os.path.join(ROOT, "include", "fairkv_measure.h")] + [os.path.join(CSRC, h) for h in ("append_rotated.h", "cache_rows.h", "common.h", "decode_f32.h", "decode_mfma.h", "decode_tree.h", "decode_valu.h", "pack.h", "plan_check.h", "rows.h", "stream_probe.h", "zero_words.h")]
+HEADERS = [os.path.join(ROOT, "include", "fairkv.h"), os.path.join(ROOT, "include", "fairkv_measure.h")] + [os.path.join(CSRC, h) for h in ("append_rotated.h", "attn_weights.h", "cache_check.h", "cache_rows.h", "common.h", "decode_f32.h", "decode_mfma.h", "decode_tree.h", "decode_valu.h", "evict.h", "line.h", "pack.h", "plan_check.h", "rows.h", "select.h", "stream_probe.h", "zero_words.h")]
 
 
 def _hipcc() -> str:

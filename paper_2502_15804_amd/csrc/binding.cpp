@@ -30,6 +30,9 @@ decltype(&fairkv_append) append_rows;
 decltype(&fairkv_append_rotated) append_rotated_rows;
 decltype(&fairkv_decode_attn_tree) decode_tree_attn;
 decltype(&fairkv_accept) accept_rows;
+decltype(&fairkv_attn_weights) attn_weights_rows;
+decltype(&fairkv_select) select_rows;
+decltype(&fairkv_evict) evict_rows;
 PyArray_Descr *item_descr;      // of the plan's item array
 
 struct Refused {};              // a Python exception is set
@@ -477,12 +480,103 @@ PyObject *accept(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---- compression of a growing cache ----
+// (current, cache, device, lens, q, lse, weights, weights_out, scale, tree, n_new, decay, n_slots, stream)
+PyObject *attn_weights(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 14, [&]() -> int {
+        const CacheArg cache(a[1], a[2]);
+        const fairkv_cache *c = cache.c;
+        const at::Tensor &q = cache.here(a[4], "q");
+        on_device(q, "q");
+        const bool multi = q.dim() == 4;
+        if (!multi && q.dim() != 3) refuse(PyExc_ValueError, "q must be [B, Hq, D] or [B, q_len, Hq, D]");
+        if (q.size(0) != c->B || q.size(-1) != c->D) refuse(PyExc_ValueError, "shape mismatch");
+        if (!is(q, at::kBFloat16)) refuse(PyExc_TypeError, "q must be bf16");
+        const int64_t q_len = multi ? q.size(1) : 1, Hq = q.size(-2);
+        if (q_len > INT32_MAX || Hq > INT32_MAX) refuse(PyExc_ValueError, "shape mismatch");
+        const at::Tensor &lens = cache.flat(a[3], "lens", at::kInt, cache.pairs()), &lse = cache.flat(a[5], "lse", at::kFloat, c->B * q_len * Hq),
+                         &weights = cache.flat(a[6], "weights", at::kFloat, c->n_rows), &out = cache.flat(a[7], "weights_out", at::kFloat, c->n_rows, true),
+                         &tree = cache.here(a[9], "tree", true), &count = cache.flat(a[10], "n_new", at::kInt, c->B, true);
+        if (tree.defined()) {
+            on_device(tree, "tree");
+            if ((!is(tree, at::kLong) && !is(tree, at::kUInt64)) || tree.numel() != c->B * q_len)
+                refuse(PyExc_ValueError, "tree must have a 64-bit word for every new token");
+        }
+        const float scale = float_of(a[8]), decay = float_of(a[11]);
+        const int32_t n_slots = index_of(a[12]);
+        void *st = stream_of(a[13], a[0], q);
+        const c10::DeviceGuard guard = cache.guard();
+        return unlocked([&] {
+            return attn_weights_rows(c, q.data_ptr(), data<const uint64_t>(tree), data<const int32_t>(count), data<const int32_t>(lens), data<const float>(lse),
+                                     data<const float>(weights), data<float>(out.defined() ? out : weights), decay, n_slots, static_cast<int32_t>(q_len),
+                                     static_cast<int32_t>(Hq), scale, st);
+        });
+    });
+}
+
+// Lists of a cache's pairs: [B, Hkv, max_keep].
+int32_t most_kept(const CacheArg &cache, const at::Tensor &keep)
+{
+    if (keep.dim() != 3 || keep.size(0) != cache.c->B || keep.size(1) != cache.c->Hkv || keep.size(2) > INT32_MAX) refuse(PyExc_ValueError, "keep must be [B, Hkv, max_keep]");
+    return static_cast<int32_t>(keep.size(2));
+}
+
+// (current, cache, device, lens, weights, budget, keep, n_keep, workspace, pool, sink, recent, bad, n_slots, stream)
+PyObject *select(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 15, [&]() -> int {
+        const CacheArg cache(a[1], a[2]);
+        const fairkv_cache *c = cache.c;
+        const at::Tensor &lens = cache.flat(a[3], "lens", at::kInt, cache.pairs()), &weights = cache.flat(a[4], "weights", at::kFloat, c->n_rows),
+                         &budget = cache.flat(a[5], "budget", at::kInt, -1), &keep = cache.flat(a[6], "keep", at::kInt, -1),
+                         &n_keep = cache.flat(a[7], "n_keep", at::kInt, cache.pairs()), &workspace = cache.here(a[8], "workspace"),
+                         &bad = cache.flat(a[12], "bad", at::kInt, 1, true);
+        on_device(workspace, "workspace");
+        const bool own = budget.numel() == cache.pairs();
+        if (!own && budget.numel() != c->B) refuse(PyExc_ValueError, "budget must be [B, Hkv] or [B]");
+        const int32_t most = most_kept(cache, keep);
+        const fairkv_selection s{data<const int32_t>(budget), own ? 0 : 1, index_of(a[9]), index_of(a[10]), index_of(a[11])};
+        const int32_t n_slots = index_of(a[13]);
+        void *st = stream_of(a[14], a[0], weights);
+        const c10::DeviceGuard guard = cache.guard();
+        return unlocked([&] {
+            return select_rows(c, &s, data<const float>(weights), data<const int32_t>(lens), data<int32_t>(keep), most, data<int32_t>(n_keep),
+                               data<int32_t>(bad), workspace.data_ptr(), workspace.nbytes(), n_slots, st);
+        });
+    });
+}
+
+// (current, cache, device, lens, keep, n_keep, into or 0, its device, lens_out, weights, weights_out, bad, n_slots, stream)
+PyObject *evict(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 14, [&]() -> int {
+        const CacheArg cache(a[1], a[2]);
+        const bool in_place = a[6] == Py_None;
+        const CacheArg into = in_place ? cache : CacheArg(a[6], a[7]);
+        if (into.device != cache.device) refuse(PyExc_ValueError, "into must be on the cache's device");
+        const at::Tensor &lens = cache.flat(a[3], "lens", at::kInt, cache.pairs()), &keep = cache.flat(a[4], "keep", at::kInt, -1),
+                         &n_keep = cache.flat(a[5], "n_keep", at::kInt, cache.pairs()), &lens_out = cache.flat(a[8], "lens_out", at::kInt, cache.pairs(), true),
+                         &weights = cache.flat(a[9], "weights", at::kFloat, cache.c->n_rows, true),
+                         &weights_out = cache.flat(a[10], "weights_out", at::kFloat, into.c->n_rows, true), &bad = cache.flat(a[11], "bad", at::kInt, 1, true);
+        const int32_t most = most_kept(cache, keep), n_slots = index_of(a[12]);
+        if (!in_place && !lens_out.defined()) refuse(PyExc_ValueError, "lens_out is the other cache's lengths");
+        void *st = stream_of(a[13], a[0], keep);
+        const c10::DeviceGuard guard = cache.guard();
+        return unlocked([&] {
+            return evict_rows(cache.c, in_place ? nullptr : into.c, data<const int32_t>(keep), most, data<const int32_t>(n_keep), data<const int32_t>(lens),
+                              data<int32_t>(lens_out.defined() ? lens_out : lens), data<const float>(weights),
+                              data<float>(in_place && !weights_out.defined() ? weights : weights_out), data<int32_t>(bad), n_slots, st);
+        });
+    });
+}
+
 // (dtype of the plan's items, addresses of the library's functions in the order of the pointers above)
 PyObject *init(PyObject *, PyObject *args)
 {
     PyObject *dtype;
-    unsigned long long f[10];
-    if (!PyArg_ParseTuple(args, "OKKKKKKKKKK", &dtype, f, f + 1, f + 2, f + 3, f + 4, f + 5, f + 6, f + 7, f + 8, f + 9)) return nullptr;
+    unsigned long long f[13];
+    if (!PyArg_ParseTuple(args, "OKKKKKKKKKKKKK", &dtype, f, f + 1, f + 2, f + 3, f + 4, f + 5, f + 6, f + 7, f + 8, f + 9, f + 10, f + 11, f + 12)) return nullptr;
     if (!PyArray_DescrCheck(dtype)) return PyErr_Format(PyExc_TypeError, "a numpy dtype is expected");
     Py_INCREF(dtype);
     Py_XDECREF(reinterpret_cast<PyObject *>(item_descr));
@@ -490,6 +584,7 @@ PyObject *init(PyObject *, PyObject *args)
     auto set = [&](auto &fn, int i) { fn = reinterpret_cast<std::decay_t<decltype(fn)>>(static_cast<uintptr_t>(f[i])); };
     set(decode_multi, 0), set(decode_static, 1), set(decode_trace, 2), set(decode_kv8, 3), set(decode_kv8_per_head, 4);
     set(pack_rows, 5), set(append_rows, 6), set(append_rotated_rows, 7), set(decode_tree_attn, 8), set(accept_rows, 9);
+    set(attn_weights_rows, 10), set(select_rows, 11), set(evict_rows, 12);
     Py_RETURN_NONE;
 }
 
@@ -505,6 +600,9 @@ PyMethodDef methods[] = {
     {"append_rotated", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(append_rotated)), METH_FASTCALL, nullptr},
     {"decode_tree", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(decode_tree)), METH_FASTCALL, nullptr},
     {"accept", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(accept)), METH_FASTCALL, nullptr},
+    {"attn_weights", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(attn_weights)), METH_FASTCALL, nullptr},
+    {"select", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(select)), METH_FASTCALL, nullptr},
+    {"evict", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(evict)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

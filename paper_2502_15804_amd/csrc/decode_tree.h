@@ -28,8 +28,7 @@
 #pragma once
 #include "cache_rows.h"
 #include "decode_mfma.h"
-
-#include <type_traits>
+#include "line.h"
 
 namespace fairkv {
 
@@ -150,25 +149,6 @@ __device__ __forceinline__ int32_t tree_new(const TreeArgs &a, int b)
 // Tokens of a pair as far as a length can be one, and its place in the line.
 __device__ __forceinline__ int32_t tree_len(const TreeArgs &a, int pair) { return min(max(a.len[pair], 0), a.max_len); }
 __device__ __forceinline__ int32_t tiles_of(int32_t len) { return (len + kTreeTok - 1) / kTreeTok; }
-
-// x plus those of the lanes below, by steps of the wave's own data paths.
-__device__ __forceinline__ int64_t wave_upto(int64_t x)
-{
-    auto step = [&](auto ctrl, auto rows, auto banks) __attribute__((always_inline)) {
-        const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(x), ctrl(), rows(), banks(), false);
-        const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(x >> 32), ctrl(), rows(), banks(), false);
-        x += static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
-    };
-#define FAIRKV_N(n) std::integral_constant<int, n>{}
-    step(FAIRKV_N(0x111), FAIRKV_N(0xf), FAIRKV_N(0xf));      // from 1, 2, 4, 8 lanes below in the row of 16
-    step(FAIRKV_N(0x112), FAIRKV_N(0xf), FAIRKV_N(0xf));
-    step(FAIRKV_N(0x114), FAIRKV_N(0xf), FAIRKV_N(0xf));
-    step(FAIRKV_N(0x118), FAIRKV_N(0xf), FAIRKV_N(0xf));
-    step(FAIRKV_N(0x142), FAIRKV_N(0xa), FAIRKV_N(0xf));      // from the end of the row below, of both rows below
-    step(FAIRKV_N(0x143), FAIRKV_N(0xc), FAIRKV_N(0xf));
-#undef FAIRKV_N
-    return x;
-}
 
 // A run of tiles of one pair.
 struct TreePiece {

@@ -1,0 +1,148 @@
+// C ABI of the compression of a growing cache: argument checks, kernel selection and launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "attn_weights.h"
+#include "cache_check.h"
+#include "evict.h"
+#include "fairkv.h"
+#include "select.h"
+
+namespace {
+
+using namespace fairkv;
+
+constexpr int32_t kMaxSlots = 65536;
+constexpr int32_t kMaxPool = 63;
+
+// Tokens that a length can count: 2^31 - 2^16, so that what is added to a token's number does not wrap around.
+int32_t max_len(const fairkv_cache *c)
+{
+    const int64_t rows = c->n_rows < 1 ? 0 : c->pages ? static_cast<int64_t>(c->max_pages) * c->page_rows : c->n_rows;
+    return static_cast<int32_t>(std::min<int64_t>(rows, INT32_MAX - 65535));
+}
+// Whether two runs of bytes share one.
+bool meet(const void *x, size_t nx, const void *y, size_t ny)
+{
+    const auto a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y);
+    return a < static_cast<unsigned __int128>(b) + ny && b < static_cast<unsigned __int128>(a) + nx;
+}
+
+template <int D, bool KV8>
+void launch_weights(const WeightsArgs &a, unsigned grid, hipStream_t st)
+{
+    hipLaunchKernelGGL((fairkv_attn_weights_kernel<D, KV8, 1>), dim3(grid), dim3(kWeightWaves * 64), 0, st, a);
+}
+
+}  // namespace
+
+extern "C" int fairkv_attn_weights(const fairkv_cache *c, const void *q, const uint64_t *tree, const int32_t *n_new, const int32_t *len,
+                                   const float *lse, const float *weights, float *weights_out, float decay, int32_t n_slots, int32_t q_len,
+                                   int32_t Hq, float scale, void *hip_stream)
+{
+    if (const int rc = check_cache(c)) return rc;
+    if (!q || !len || !lse || !weights || !weights_out || Hq < 1 || q_len < 1 || n_slots < 1 || Hq % c->Hkv != 0) return FAIRKV_EINVAL;
+    if (c->dtype == FAIRKV_F32 || q_len > FAIRKV_MAX_DRAFT || Hq / c->Hkv > 16 || n_slots > kMaxSlots) return FAIRKV_EUNSUPPORTED;
+    if (!std::isfinite(scale) || !std::isfinite(decay)) return FAIRKV_EINVAL;
+    if (!aligned(q, 16) || !aligned(lse, 4) || !aligned(weights, 4) || !aligned(weights_out, 4) || (tree && !aligned(tree, 8))) return FAIRKV_EINVAL;
+    if (static_cast<int64_t>(c->B) * q_len * Hq * c->D > INT32_MAX) return FAIRKV_EINVAL;
+    if (weights_out != weights && meet(weights, sizeof(float) * c->n_rows, weights_out, sizeof(float) * c->n_rows)) return FAIRKV_EINVAL;
+    for (int32_t h = 0; h < std::max(c->n_scales, 1); ++h)
+        if (!std::isfinite(scale * kLog2e * (c->n_scales > 0 ? c->k_scale[h] : 1.f))) return FAIRKV_EINVAL;
+    WeightsArgs a{};
+    a.q = static_cast<const char *>(q), a.k = static_cast<const char *>(c->k);
+    a.rows = row_map(c);
+    a.len = len, a.n_new = n_new, a.tree = reinterpret_cast<const int64_t *>(tree), a.lse = lse;
+    a.weights = weights, a.out = weights_out;
+    a.B = c->B, a.Hq = Hq, a.Hkv = c->Hkv, a.G = Hq / c->Hkv, a.q_len = q_len, a.max_len = max_len(c), a.n_scales = c->n_scales;
+    a.scale_log2 = scale * kLog2e, a.decay = decay;
+    for (int h = 0; h < kCacheScales; ++h) a.k_scale[h] = h < c->n_scales ? c->k_scale[h] : 1.f;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const unsigned grid = static_cast<unsigned>(n_slots) * 3;
+    if (c->dtype == FAIRKV_E4M3)
+        c->D == 128 ? launch_weights<128, true>(a, grid, st) : launch_weights<64, true>(a, grid, st);
+    else
+        c->D == 128 ? launch_weights<128, false>(a, grid, st) : launch_weights<64, false>(a, grid, st);
+    return launched();
+}
+
+extern "C" size_t fairkv_select_workspace_bytes(const fairkv_cache *c, int32_t shared, int32_t n_slots)
+{
+    if (check_cache(c) != FAIRKV_OK || n_slots < 1 || n_slots > kMaxSlots || shared < 0 || shared > 1) return 0;
+    return 256;
+}
+
+extern "C" int fairkv_select(const fairkv_cache *c, const fairkv_selection *s, const float *weights, const int32_t *len, int32_t *keep,
+                             int32_t max_keep, int32_t *n_keep, int32_t *bad, void *workspace, size_t workspace_bytes, int32_t n_slots,
+                             void *hip_stream)
+{
+    if (const int rc = check_cache(c)) return rc;
+    if (!s || !s->budget || !weights || !len || !keep || !n_keep || max_keep < 1 || n_slots < 1) return FAIRKV_EINVAL;
+    if (s->shared < 0 || s->shared > 1 || s->sink < 0 || s->recent < 0 || s->pool < 1 || s->pool % 2 == 0) return FAIRKV_EINVAL;
+    if (s->pool > kMaxPool || n_slots > kMaxSlots) return FAIRKV_EUNSUPPORTED;
+    if (!aligned(weights, 4) || !aligned(workspace, 16)) return FAIRKV_EINVAL;
+    const int64_t pairs = static_cast<int64_t>(c->B) * c->Hkv, groups = s->shared ? c->B : pairs;
+    if (groups > UINT32_MAX / kSelectThreads) return FAIRKV_EINVAL;
+    if (!workspace || workspace_bytes < fairkv_select_workspace_bytes(c, s->shared, n_slots)) return FAIRKV_EWORKSPACE;
+    SelectArgs a{};
+    a.rows = row_map(c);
+    a.weights = weights, a.len = len, a.budget = s->budget, a.keep = keep, a.n_keep = n_keep, a.bad = bad;
+    a.B = c->B, a.Hkv = c->Hkv, a.max_len = max_len(c), a.max_keep = max_keep, a.half = s->pool / 2, a.sink = s->sink, a.recent = s->recent;
+    a.per_group = s->shared ? c->Hkv : 1;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    hipLaunchKernelGGL(fairkv_select_kernel, dim3(static_cast<unsigned>(groups)), dim3(kSelectThreads), 0, st, a);
+    return launched();
+}
+
+extern "C" int fairkv_evict(const fairkv_cache *c, const fairkv_cache *into, const int32_t *keep, int32_t max_keep, const int32_t *n_keep,
+                            const int32_t *len, int32_t *len_out, const float *weights, float *weights_out, int32_t *bad, int32_t n_slots,
+                            void *hip_stream)
+{
+    if (const int rc = check_cache(c)) return rc;
+    if (into) {
+        if (const int rc = check_cache(into)) return rc;
+        if (into->B != c->B || into->Hkv != c->Hkv || into->D != c->D || into->dtype != c->dtype || into->n_scales != c->n_scales) return FAIRKV_EINVAL;
+        for (int32_t h = 0; h < c->n_scales; ++h)      // bytes move as they are
+            if (into->k_scale[h] != c->k_scale[h] || into->v_scale[h] != c->v_scale[h]) return FAIRKV_EINVAL;
+    }
+    if (!keep || !n_keep || !len || !len_out || max_keep < 1 || n_slots < 1 || (weights == nullptr) != (weights_out == nullptr)) return FAIRKV_EINVAL;
+    if (n_slots > kMaxSlots) return FAIRKV_EUNSUPPORTED;
+    if (!aligned(weights, 4) || !aligned(weights_out, 4) || (!into && weights_out != weights)) return FAIRKV_EINVAL;
+    const int64_t pairs = static_cast<int64_t>(c->B) * c->Hkv;
+    if (pairs > UINT32_MAX / 1024) return FAIRKV_EINVAL;
+    if (meet(len_out, sizeof(int32_t) * pairs, n_keep, sizeof(int32_t) * pairs) || (len_out != len && meet(len_out, sizeof(int32_t) * pairs, len, sizeof(int32_t) * pairs)))
+        return FAIRKV_EINVAL;
+    EvictArgs a{};
+    const fairkv_cache *to = into ? into : c;
+    a.k = static_cast<const char *>(c->k), a.v = static_cast<const char *>(c->v);
+    a.k_to = static_cast<char *>(to->k), a.v_to = static_cast<char *>(to->v);
+    a.w = weights, a.w_to = weights_out;
+    a.from = row_map(c), a.to = row_map(to);
+    a.cap_to = into ? into->cap : nullptr;
+    a.keep = keep, a.n_keep = n_keep, a.len = len, a.len_out = len_out, a.bad = bad;
+    a.n_pairs = static_cast<int32_t>(pairs), a.max_keep = max_keep;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const int rb = c->D * (c->dtype == FAIRKV_E4M3 ? 1 : c->dtype == FAIRKV_BF16 ? 2 : 4);
+    auto move = [&](auto row_bytes) {
+        constexpr int ROWB = decltype(row_bytes)::value;
+        if (into)
+            hipLaunchKernelGGL(fairkv_evict_into_kernel<ROWB>, dim3(static_cast<unsigned>(n_slots) * 8), dim3(256), 0, st, a);
+        else
+            hipLaunchKernelGGL(fairkv_evict_kernel<ROWB>, dim3(static_cast<unsigned>(pairs)), dim3(1024), 0, st, a);
+    };
+    if (rb == 64)
+        move(std::integral_constant<int, 64>{});
+    else if (rb == 128)
+        move(std::integral_constant<int, 128>{});
+    else if (rb == 256)
+        move(std::integral_constant<int, 256>{});
+    else
+        move(std::integral_constant<int, 512>{});
+    if (const int rc = launched()) return rc;
+    // Lengths change behind all that reads them: they may be written over the old ones.
+    hipLaunchKernelGGL(fairkv_evict_lengths_kernel, dim3(static_cast<unsigned>(pairs)), dim3(256), 0, st, a);
+    return launched();
+}
