@@ -63,10 +63,10 @@ __global__ __launch_bounds__(kWeightWaves * 64) void fairkv_attn_weights_kernel(
     const LineShare share = line_share<NT>(n_pairs, gridDim.x, blockIdx.x, [&](int p) { return blocks_of(len_of(p)); });
     int pair = share.pair, in_lds = -1, chunk_in_lds = 0;
     int64_t block = share.begin;
+    int32_t len = share.left > 0 ? len_of(pair) : 0;
     for (int64_t left = share.left; left > 0; --left, ++block) {
-        int32_t len = len_of(pair);
-        while (block >= blocks_of(len)) {
-            ++pair, block = 0;
+        if (block >= blocks_of(len)) {
+            pair = next_pair(pair, n_pairs, [&](int p) { return blocks_of(len_of(p)); }), block = 0;
             len = len_of(pair);
         }
         const int b = pair / a.Hkv, h = pair - b * a.Hkv;

@@ -78,10 +78,10 @@ __global__ __launch_bounds__(256) void fairkv_evict_into_kernel(EvictArgs a)
     const LineShare share = line_share<256>(a.n_pairs, gridDim.x, blockIdx.x, [&](int p) { return blocks_of(count(p)); });
     int pair = share.pair;
     int64_t block = share.begin;
+    int32_t n = share.left > 0 ? count(pair) : 0;
     for (int64_t left = share.left; left > 0; --left, ++block) {
-        int32_t n = count(pair);
-        while (block >= blocks_of(n)) {
-            ++pair, block = 0;
+        if (block >= blocks_of(n)) {
+            pair = next_pair(pair, a.n_pairs, count), block = 0;
             n = count(pair);
         }
         const int32_t len = a.len[pair], i0 = static_cast<int32_t>(block) * kBlock;

@@ -16,7 +16,8 @@ namespace {
 using namespace fairkv;
 
 constexpr int32_t kMaxSlots = 65536;
-constexpr int32_t kMaxPool = 63;
+constexpr int32_t kSmallCap = 8192, kLargeCap = 16384;      // rows of a group in a workgroup's registers
+static_assert(kSmallCap % kBlockRows == 0 && kLargeCap % kBlockRows == 0, "a larger group has more blocks than that");
 
 // Tokens that a length can count: 2^31 - 2^16, so that what is added to a token's number does not wrap around.
 int32_t max_len(const fairkv_cache *c)
@@ -69,10 +70,45 @@ extern "C" int fairkv_attn_weights(const fairkv_cache *c, const void *q, const u
     return launched();
 }
 
+// ---- selection: which kernels a call takes --------------------------------------------------------
+namespace {
+
+struct SelectShape {
+    int32_t cap, min_blocks;      // rows of a group that one workgroup has; blocks that a larger one has at least
+    int64_t max_blocks;           // of all larger groups, 0: there can be none
+    int64_t slots;
+};
+SelectShape select_shape(const fairkv_cache *c, int32_t shared, int32_t n_slots)
+{
+    const int64_t pairs = static_cast<int64_t>(c->B) * c->Hkv, per_group = shared ? c->Hkv : 1, groups = pairs / per_group;
+    const int64_t each = max_len(c), most = std::min(std::max<int64_t>(c->n_rows, 0), each * pairs), group_most = std::min(most, each * per_group);
+    SelectShape s{};
+    s.cap = group_most <= kSmallCap || (group_most > kLargeCap && groups > n_slots) ? kSmallCap : kLargeCap;
+    if (group_most <= s.cap && per_group <= kMaxPairs) return s;
+    s.min_blocks = per_group > kMaxPairs ? kMaxPairs : s.cap / kBlockRows;
+    // every pair of a large group has a block that is not full
+    const int64_t large_pairs = per_group > kMaxPairs ? pairs : std::min(pairs, most / s.cap * per_group);
+    s.max_blocks = most / kBlockRows + large_pairs;
+    s.slots = s.max_blocks / s.min_blocks + 1;
+    return s;
+}
+size_t select_bytes(const SelectShape &s) { return 256 + sizeof(SelectSlot) * s.slots + sizeof(int2) * s.max_blocks; }
+
+template <int NT, int KPT>
+void launch_select(const SelectArgs &a, unsigned groups, hipStream_t st)
+{
+    if (a.half > 0)
+        hipLaunchKernelGGL((fairkv_select_kernel<NT, KPT, true>), dim3(groups), dim3(NT), 0, st, a);
+    else
+        hipLaunchKernelGGL((fairkv_select_kernel<NT, KPT, false>), dim3(groups), dim3(NT), 0, st, a);
+}
+
+}  // namespace
+
 extern "C" size_t fairkv_select_workspace_bytes(const fairkv_cache *c, int32_t shared, int32_t n_slots)
 {
     if (check_cache(c) != FAIRKV_OK || n_slots < 1 || n_slots > kMaxSlots || shared < 0 || shared > 1) return 0;
-    return 256;
+    return select_bytes(select_shape(c, shared, n_slots));
 }
 
 extern "C" int fairkv_select(const fairkv_cache *c, const fairkv_selection *s, const float *weights, const int32_t *len, int32_t *keep,
@@ -82,18 +118,35 @@ extern "C" int fairkv_select(const fairkv_cache *c, const fairkv_selection *s, c
     if (const int rc = check_cache(c)) return rc;
     if (!s || !s->budget || !weights || !len || !keep || !n_keep || max_keep < 1 || n_slots < 1) return FAIRKV_EINVAL;
     if (s->shared < 0 || s->shared > 1 || s->sink < 0 || s->recent < 0 || s->pool < 1 || s->pool % 2 == 0) return FAIRKV_EINVAL;
-    if (s->pool > kMaxPool || n_slots > kMaxSlots) return FAIRKV_EUNSUPPORTED;
+    if (s->pool > 2 * kMostHalf + 1 || n_slots > kMaxSlots) return FAIRKV_EUNSUPPORTED;
     if (!aligned(weights, 4) || !aligned(workspace, 16)) return FAIRKV_EINVAL;
     const int64_t pairs = static_cast<int64_t>(c->B) * c->Hkv, groups = s->shared ? c->B : pairs;
-    if (groups > UINT32_MAX / kSelectThreads) return FAIRKV_EINVAL;
-    if (!workspace || workspace_bytes < fairkv_select_workspace_bytes(c, s->shared, n_slots)) return FAIRKV_EWORKSPACE;
+    if (groups > UINT32_MAX / 1024) return FAIRKV_EINVAL;
+    const SelectShape shape = select_shape(c, s->shared, n_slots);
+    if (!workspace || workspace_bytes < select_bytes(shape)) return FAIRKV_EWORKSPACE;
     SelectArgs a{};
     a.rows = row_map(c);
     a.weights = weights, a.len = len, a.budget = s->budget, a.keep = keep, a.n_keep = n_keep, a.bad = bad;
-    a.B = c->B, a.Hkv = c->Hkv, a.max_len = max_len(c), a.max_keep = max_keep, a.half = s->pool / 2, a.sink = s->sink, a.recent = s->recent;
-    a.per_group = s->shared ? c->Hkv : 1;
+    a.n_pairs = static_cast<int32_t>(pairs), a.max_len = max_len(c), a.max_keep = max_keep;
+    a.half = s->pool / 2, a.sink = s->sink, a.recent = s->recent, a.per_group = s->shared ? c->Hkv : 1;
+    a.cap = shape.cap, a.min_blocks = shape.min_blocks, a.max_blocks = shape.max_blocks;
+    if (shape.max_blocks > 0) {
+        a.slots = static_cast<SelectSlot *>(workspace);
+        a.blocks = reinterpret_cast<int2 *>(static_cast<char *>(workspace) + sizeof(SelectSlot) * shape.slots);
+    }
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    hipLaunchKernelGGL(fairkv_select_kernel, dim3(static_cast<unsigned>(groups)), dim3(kSelectThreads), 0, st, a);
+    if (shape.cap == kSmallCap)
+        launch_select<512, kSmallCap / 512>(a, static_cast<unsigned>(groups), st);
+    else
+        launch_select<1024, kLargeCap / 1024>(a, static_cast<unsigned>(groups), st);
+    if (shape.max_blocks > 0) {
+        const dim3 grid(static_cast<unsigned>(std::min<int64_t>(shape.max_blocks, 4 * static_cast<int64_t>(n_slots))));
+        hipLaunchKernelGGL(fairkv_select_large_kernel<0>, grid, dim3(256), 0, st, a);
+        hipLaunchKernelGGL(fairkv_select_large_kernel<1>, grid, dim3(256), 0, st, a);
+        hipLaunchKernelGGL(fairkv_select_large_kernel<2>, grid, dim3(256), 0, st, a);
+        hipLaunchKernelGGL(fairkv_select_large_kernel<3>, grid, dim3(256), 0, st, a);
+        hipLaunchKernelGGL(fairkv_select_large_kernel<4>, grid, dim3(256), 0, st, a);
+    }
     return launched();
 }
 

@@ -31,6 +31,7 @@ __device__ __forceinline__ int64_t wave_upto(int64_t x)
 struct LineShare {
     int pair;
     int64_t begin, left;
+    int64_t at, total;                // the share's place in the line, and the whole line's length
 };
 template <int NT, class Units>
 __device__ __forceinline__ LineShare line_share(int n_pairs, int n_slots, int slot, Units units)
@@ -44,7 +45,7 @@ __device__ __forceinline__ LineShare line_share(int n_pairs, int n_slots, int sl
     for (int p = p0; p < p1; ++p) mine += units(p);
     const int64_t upto = wave_upto(mine);
     if (lane == 63) totals[wave] = upto;
-    if (threadIdx.x == 0) found = LineShare{n_pairs, 0, 0};
+    if (threadIdx.x == 0) found = LineShare{n_pairs, 0, 0, 0, 0};
     __syncthreads();
     int64_t before = upto - mine, total = 0;
 #pragma unroll
@@ -62,10 +63,24 @@ __device__ __forceinline__ LineShare line_share(int n_pairs, int n_slots, int sl
             if (begin < before + u) break;
             before += u;
         }
-        found = LineShare{p, begin - before, left};
+        found = LineShare{p, begin - before, left, begin, total};
     }
     __syncthreads();
-    return found;
+    LineShare r = found;
+    r.total = total;
+    return r;
+}
+
+// The first pair behind `pair` that has units, n_pairs if none has: 64 are looked at at once.
+template <class Units>
+__device__ __forceinline__ int next_pair(int pair, int n_pairs, Units units)
+{
+    const int lane = threadIdx.x & 63;
+    for (int p = pair + 1; p < n_pairs; p += 64) {
+        const uint64_t some = __builtin_amdgcn_ballot_w64(p + lane < n_pairs && units(min(p + lane, n_pairs - 1)) > 0);
+        if (some) return p + __builtin_ctzll(some);
+    }
+    return n_pairs;
 }
 
 }  // namespace fairkv

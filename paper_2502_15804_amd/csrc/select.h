@@ -6,163 +6,517 @@
 // for behind the protected rows; of equal values the one of the lower head, then of the lower token.
 //
 // Values are compared as 32-bit whole numbers in the order of the floats.  The least one that stays is found digit by digit from the top, by
-// counting how many candidates have which digit among those that share the digits found so far; then the rows are listed in their order.
+// counting how many candidates have which digit among those that share the digits found so far: 11, 11 and 10 bits.  Where all candidates that
+// share some digits stay, the others need not be looked at.
+//
+// A group of up to CAP rows is one workgroup's, which reads its weights once and holds its values in registers.  Rows of larger groups are dealt
+// to the whole GPU in blocks: three kernels count a digit each, one counts what stays of every block, one lists it.
 #pragma once
 #include "cache_rows.h"
+#include "line.h"
 
 namespace fairkv {
 
+constexpr int kDigits = 3;
+constexpr int kDigitShift[kDigits] = {21, 10, 0}, kBins = 2048;      // bins of a digit, the last digit's half as many
+constexpr int kBlockRows = 4096;          // of a large group
+constexpr int kMaxPairs = 256;            // of a group that one workgroup has
+constexpr int kMostHalf = 31;             // of the window
+
+// What the kernels of a large group hand on.  Slots are of groups: a group has at least min_blocks blocks, so the place of its first block in the
+// line, divided by min_blocks, is no other's.  A step's workgroups read what the step before left, in `found` of its own, and clear what nobody
+// reads any more.
+struct SelectFound {
+    int64_t need;                         // how many stay of the candidates that share the digits found so far
+    uint32_t least;                       // these digits, the rest 0; with `done`: what is larger stays
+    int32_t done;                         // no more digits need be looked at
+};
+struct SelectSlot {
+    int32_t bins[kDigits][kBins];         // 0 between calls
+    unsigned long long protected_rows;    // with a row in the cache; 0 between calls
+    SelectFound found[kDigits];           // 0 between calls
+    int64_t listed;                       // blocks whose list is written; 0 between calls
+};
 struct SelectArgs {
     RowMap rows;
     const float *weights;                 // [n_rows]
     const int32_t *len, *budget;          // [B * Hkv]; [groups]
     int32_t *keep, *n_keep, *bad;         // [B * Hkv][max_keep], [B * Hkv], [1] or null
-    int32_t B, Hkv, max_len, max_keep, half, sink, recent, per_group;      // per_group: pairs of a group, 1 or Hkv
+    SelectSlot *slots;                    // null: no group can be large
+    int2 *blocks;                         // [max_blocks]: rows of a block that stay whatever ties do, and ties; 0 between calls
+    int64_t max_blocks;
+    int32_t n_pairs, n_groups, max_len, max_keep, half, sink, recent, per_group, cap, min_blocks;      // per_group: pairs of a group
 };
 
-constexpr int kSelectThreads = 1024;
+// Not a candidate and does not stay; protected.  All candidates lie in between, from that of -inf to that of +inf.
+constexpr uint32_t kNone = 0, kProtected = 0xffffffffu;
 
-// The float's place in the order of floats.  -0 is +0, and a NaN is below all numbers (fmaxf has left it out).
+// The float's place in the order of floats.  -0 is +0; no float's is kNone or kProtected, NaN aside.
 __device__ __forceinline__ uint32_t order_of(float x)
 {
     const uint32_t u = __float_as_uint(x + 0.f);
     return u ^ (u & 0x80000000u ? 0xffffffffu : 0x80000000u);
 }
 
-struct Candidates {                       // of a pair: its length, and the candidates' first token and the one behind the last
-    int32_t len, first, end;
-    __device__ __forceinline__ Candidates(const SelectArgs &a, int pair)
-    {
-        len = min(max(a.len[pair], 0), a.max_len);
-        first = min(a.sink, len);
-        end = max(first, len - min(a.recent, len));
-    }
+__device__ __forceinline__ int32_t select_len(const SelectArgs &a, int pair) { return min(max(a.len[pair], 0), a.max_len); }
+struct Candidates {                       // of a pair: the first token that is one, and the one behind the last
+    int32_t first, end;
+    __device__ __forceinline__ Candidates(const SelectArgs &a, int32_t len) : first(min(a.sink, len)), end(max(first, len - min(a.recent, len))) {}
+    __device__ __forceinline__ bool has(int32_t t) const { return t >= first && t < end; }
 };
 
-__device__ __forceinline__ uint32_t value_of(const SelectArgs &a, int pair, const Candidates &c, int32_t t)
+// The bin, from the top, in which the need-th candidate lies (need >= 1 and at most the sum of all bins), how many are needed of that bin, and how
+// many it has.  Called by all NT threads, the bins complete; ends with a barrier behind the last look at them.
+struct BinFound {
+    int32_t bin, in_bin;
+    int64_t need;
+};
+template <int NT, class At>
+__device__ __forceinline__ BinFound find_bin(int64_t need, At bin_at)
 {
-    float x = -INFINITY;
-    for (int32_t u = max(c.first, t - a.half); u <= min(c.end - 1, t + a.half); ++u) {
-        const int64_t row = a.rows.row(pair, u);
-        if (row >= 0) x = fmaxf(x, a.weights[row]);
+    constexpr int PER = kBins / NT, NW = NT / 64;
+    static_assert(kBins % NT == 0, "bins of a thread");
+    __shared__ int64_t totals[NW];
+    __shared__ BinFound found;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, top = kBins - 1 - static_cast<int>(threadIdx.x) * PER;
+    int32_t n[PER];
+    int64_t mine = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) n[i] = bin_at(top - i), mine += n[i];
+    const int64_t upto = wave_upto(mine);
+    if (lane == 63) totals[wave] = upto;
+    if (threadIdx.x == 0) found = BinFound{0, 0, 0};
+    __syncthreads();
+    int64_t before = upto - mine;
+    for (int w = 0; w < wave; ++w) before += totals[w];
+    if (before < need && need <= before + mine) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            if (before < need && need <= before + n[i]) found = BinFound{top - i, n[i], need - before};
+            before += n[i];
+        }
     }
-    return order_of(x);
+    __syncthreads();
+    return found;
 }
 
-// Sum over the workgroup of what the threads before this one have, and of all.
-struct Before {
-    int32_t before, total;
-};
-template <int NT>
-__device__ __forceinline__ Before count_before(bool x, int32_t *of_waves /* LDS [NT / 64] */)
+// Adds one to the bin of every lane whose `counts` is set.  Bins lie in LDS.
+__device__ __forceinline__ void count_digit(int32_t *bins, uint32_t key, int digit, uint32_t least, bool counts)
 {
+    const int shift = kDigitShift[digit];
+    // all digits in front are the ones found
+    if (counts && (digit == 0 || (key ^ least) >> kDigitShift[digit > 0 ? digit - 1 : 0] == 0)) atomicAdd(&bins[key >> shift & (kBins - 1) & (digit == 2 ? 1023 : ~0)], 1);
+}
+
+// Rows i NT + threadIdx.x, i < KPT, of which bit i of a thread's x says whether it is one of some: how many of them are in front of a row.
+// count_rows is called by all threads and ends with a barrier; another one stands between the last rows_before and the next count_rows.
+template <int NT, int KPT>
+__device__ __forceinline__ void count_rows(int32_t (&counts)[KPT][NT / 64], uint32_t x)
+{
+    constexpr int NW = NT / 64, PER = KPT * NW / 64;
+    static_assert(KPT * NW % 64 == 0, "sums of a lane");
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint64_t here = __builtin_amdgcn_ballot_w64(x);
-    __syncthreads();
-    if (lane == 0) of_waves[wave] = __builtin_popcountll(here);
-    __syncthreads();
-    Before r{__builtin_popcountll(here & ((1ull << lane) - 1)), 0};
-    for (int w = 0; w < NT / 64; ++w) {
-        if (w < wave) r.before += of_waves[w];
-        r.total += of_waves[w];
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+        const int32_t n = __builtin_popcountll(__builtin_amdgcn_ballot_w64((x >> i & 1) != 0));
+        if (lane == 0) counts[i][wave] = n;
     }
-    return r;
+    __syncthreads();
+    if (wave == 0) {
+        int32_t n[PER], all = 0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) n[j] = (&counts[0][0])[lane * PER + j], all += n[j];
+        int32_t before = static_cast<int32_t>(wave_upto(all)) - all;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            (&counts[0][0])[lane * PER + j] = before;
+            before += n[j];
+        }
+    }
+    __syncthreads();
+}
+template <int NT, int KPT>
+__device__ __forceinline__ int32_t rows_before(const int32_t (&counts)[KPT][NT / 64], uint32_t x, int i)
+{
+    return counts[i][threadIdx.x >> 6] + __builtin_popcountll(__builtin_amdgcn_ballot_w64((x >> i & 1) != 0) & ((1ull << (threadIdx.x & 63)) - 1));
 }
 
-// One workgroup per group.
-__global__ __launch_bounds__(kSelectThreads) void fairkv_select_kernel(SelectArgs a)
+// ---- a group that one workgroup has: keys of rows threadIdx.x + i NT of the group's, one pair's behind the other's ----
+template <int NT, int KPT, bool POOL>
+__global__ __launch_bounds__(NT) void fairkv_select_kernel(SelectArgs a)
 {
-    constexpr int NT = kSelectThreads;
-    __shared__ int32_t bins[256], of_waves[NT / 64], of_waves2[NT / 64];
-    __shared__ int64_t room_left;
-    __shared__ uint32_t digit_found;
-    const int group = blockIdx.x, first_pair = group * a.per_group;
-    auto has_row = [&](int pair, int32_t t) { return a.rows.row(pair, t) >= 0; };
-
-    // ---- how many candidates stay: what the budget leaves behind the protected rows ----
-    int64_t room = 0, candidates = 0;
-    {
-        int32_t mine = 0, also = 0;
-        for (int p = first_pair; p < first_pair + a.per_group; ++p) {
-            const Candidates c(a, p);
-            for (int32_t t = threadIdx.x; t < c.len; t += NT)
-                if (has_row(p, t)) {
-                    if (t < c.first || t >= c.end)
-                        ++mine;
-                    else
-                        ++also;
-                }
+    constexpr int CAP = NT * KPT, NW = NT / 64;
+    __shared__ int32_t start[kMaxPairs + 1], stays_from[kMaxPairs], stays_to[kMaxPairs];
+    __shared__ int32_t bins[kBins];
+    __shared__ float raw[POOL ? CAP : 1];
+    __shared__ int32_t counts[KPT][NW];
+    __shared__ int32_t protected_rows, candidate_rows;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = blockIdx.x, p0 = group * a.per_group;
+    const int n_pairs = a.per_group;
+    auto refuse = [&]() {
+        for (int p = threadIdx.x; p < n_pairs; p += NT) {
+            a.n_keep[p0 + p] = -1;
+            if (a.bad) atomicAdd(a.bad, 1);
         }
-        __shared__ unsigned long long total[2];
-        if (threadIdx.x < 2) total[threadIdx.x] = 0;
-        __syncthreads();
-        atomicAdd(&total[0], static_cast<unsigned long long>(mine));
-        atomicAdd(&total[1], static_cast<unsigned long long>(also));
-        __syncthreads();
-        room = max(static_cast<int64_t>(a.budget[group]) - static_cast<int64_t>(total[0]), static_cast<int64_t>(0));
-        candidates = static_cast<int64_t>(total[1]);
+    };
+    if (n_pairs > kMaxPairs) {
+        if (!a.slots) refuse();
+        return;
     }
-    uint32_t least = 0;                   // the least value that stays, and how many of those that have it
+    // ---- where the pairs begin ----
+    if (wave == 0) {
+        int64_t before = 0;
+        for (int q = 0; q < n_pairs; q += 64) {
+            const int p = q + lane;
+            const int32_t len = p < n_pairs ? select_len(a, p0 + p) : 0;
+            const int64_t upto = wave_upto(len);
+            if (p < n_pairs) start[p] = static_cast<int32_t>(min(before + upto - len, static_cast<int64_t>(INT32_MAX)));
+            before += __shfl(upto, 63);
+        }
+        if (lane == 0) start[n_pairs] = static_cast<int32_t>(min(before, static_cast<int64_t>(INT32_MAX))), protected_rows = candidate_rows = 0;
+    }
+    __syncthreads();
+    const int32_t total = start[n_pairs];
+    if (total > a.cap) {                  // a.cap is CAP or less
+        if (!a.slots) refuse();
+        return;
+    }
+    // ---- values ----
+    uint32_t key[KPT];
+    auto pair_of = [&](int32_t f) __attribute__((always_inline)) {      // the last pair that begins at f or before and is not empty there
+        int lo = 0, hi = n_pairs - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (start[mid] <= f)
+                lo = mid;
+            else
+                hi = mid - 1;
+        }
+        return lo;
+    };
+    float value[KPT];
+    int32_t mine = 0, also = 0;
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+        const int32_t f = i * NT + static_cast<int32_t>(threadIdx.x);
+        key[i] = kNone;
+        value[i] = -INFINITY;
+        if (f >= total) continue;
+        const int p = pair_of(f);
+        const int32_t t = f - start[p];
+        const Candidates c(a, start[p + 1] - start[p]);
+        const int64_t row = a.rows.row(p0 + p, t);
+        if (row < 0) continue;
+        key[i] = c.has(t) ? 1 : kProtected;
+        if (c.has(t)) value[i] = a.weights[row];
+    }
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+        value[i] = fmaxf(value[i], -INFINITY);      // a NaN is as low
+        if (key[i] == kProtected) ++mine;
+        if (key[i] == 1) ++also;
+        if constexpr (POOL) {
+            if (i * NT + static_cast<int32_t>(threadIdx.x) < total) raw[i * NT + threadIdx.x] = value[i];
+        }
+    }
+    if (mine) atomicAdd(&protected_rows, mine);
+    if (also) atomicAdd(&candidate_rows, also);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+        if (key[i] != 1) continue;
+        if constexpr (POOL) {             // rows that are no candidates have -inf there; the window ends where the pair does
+            const int32_t f = i * NT + static_cast<int32_t>(threadIdx.x);
+            const int p = pair_of(f);
+            for (int32_t u = max(start[p], f - a.half); u <= min(start[p + 1] - 1, f + a.half); ++u) value[i] = fmaxf(value[i], raw[u]);
+        }
+        key[i] = order_of(value[i]);
+    }
+
+    // ---- the least that stays, and how many of those that are equal to it ----
+    const int64_t room = max(static_cast<int64_t>(a.budget[group]) - protected_rows, static_cast<int64_t>(0));
+    uint32_t least = 0;                   // what is larger stays
     int64_t ties = 0;
-    if (room > 0 && room < candidates) {
-        int64_t left = room;
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int i = threadIdx.x; i < 256; i += NT) bins[i] = 0;
+    if (room == 0) {
+        least = kProtected - 1;
+    } else if (room < candidate_rows) {
+        int64_t need = room;
+#pragma unroll
+        for (int digit = 0; digit < kDigits; ++digit) {
+            for (int i = threadIdx.x; i < kBins; i += NT) bins[i] = 0;
             __syncthreads();
-            for (int p = first_pair; p < first_pair + a.per_group; ++p) {
-                const Candidates c(a, p);
-                for (int32_t t = c.first + threadIdx.x; t < c.end; t += NT) {
-                    if (!has_row(p, t)) continue;
-                    const uint32_t x = value_of(a, p, c, t);
-                    if (shift == 24 || x >> (shift + 8) == least >> (shift + 8)) atomicAdd(&bins[x >> shift & 255], 1);
-                }
+#pragma unroll
+            for (int i = 0; i < KPT; ++i)
+                if (i * NT < total) count_digit(bins, key[i], digit, least, key[i] != kNone && key[i] != kProtected);
+            __syncthreads();
+            const BinFound b = find_bin<NT>(need, [&](int x) { return bins[x]; });
+            need = b.need;
+            least |= static_cast<uint32_t>(b.bin) << kDigitShift[digit];
+            if (need == b.in_bin) {       // all of them stay, whatever their other digits are
+                least -= 1;
+                need = 0;
+                break;
             }
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                int d = 255;
-                int64_t n = left;
-                for (; d > 0 && n > bins[d]; --d) n -= bins[d];
-                room_left = n, digit_found = static_cast<uint32_t>(d);
-            }
-            __syncthreads();
-            left = room_left, least |= digit_found << shift;
         }
-        ties = left;
-    } else if (room == 0) {
-        least = 0xffffffffu;              // no value is as large: a float's order is at most that of a NaN, and those are none
-    } else {
-        ties = INT64_MAX;
+        ties = need;
     }
 
-    // ---- the lists, in the order of the tokens ----
-    int64_t ties_before = 0;
-    for (int p = first_pair; p < first_pair + a.per_group; ++p) {
-        const Candidates c(a, p);
-        int32_t kept = 0;
-        int32_t *to = a.keep + static_cast<int64_t>(p) * a.max_keep;
-        for (int32_t t0 = 0; t0 < c.len; t0 += NT) {
-            const int32_t t = t0 + threadIdx.x;
-            bool stays = false, tie = false;
-            if (t < c.len && has_row(p, t)) {
-                if (t < c.first || t >= c.end) {
-                    stays = true;
+    // ---- the lists: how many stay in front of a row, in the order of the rows ----
+    uint32_t stays = 0;                   // bit i
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) stays |= (key[i] > least ? 1u : 0u) << i;
+    if (ties > 0) {
+        uint32_t equal = 0;
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) equal |= (key[i] == least ? 1u : 0u) << i;
+        count_rows<NT, KPT>(counts, equal);
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) {
+            const int32_t n = rows_before<NT, KPT>(counts, equal, i);
+            if ((equal >> i & 1) && n < ties) stays |= 1u << i;
+        }
+        __syncthreads();
+    }
+    count_rows<NT, KPT>(counts, stays);
+    for (int p = threadIdx.x; p < n_pairs; p += NT)
+        if (start[p] == start[p + 1]) stays_from[p] = stays_to[p] = 0;
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+        const int32_t f = i * NT + static_cast<int32_t>(threadIdx.x), n = rows_before<NT, KPT>(counts, stays, i);
+        if (f >= total) continue;
+        const int p = pair_of(f);
+        if (f == start[p]) stays_from[p] = n;
+        if (f == start[p + 1] - 1) stays_to[p] = n + static_cast<int32_t>(stays >> i & 1);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+        const int32_t f = i * NT + static_cast<int32_t>(threadIdx.x), n = rows_before<NT, KPT>(counts, stays, i);
+        if (!(stays >> i & 1)) continue;
+        const int p = pair_of(f);
+        if (n - stays_from[p] < a.max_keep) a.keep[static_cast<int64_t>(p0 + p) * a.max_keep + n - stays_from[p]] = f - start[p];
+    }
+    for (int p = threadIdx.x; p < n_pairs; p += NT) {
+        const int32_t n = stays_to[p] - stays_from[p];
+        a.n_keep[p0 + p] = n <= a.max_keep ? n : -1;
+        if (n > a.max_keep && a.bad) atomicAdd(a.bad, 1);
+    }
+}
+
+// ---- large groups: the line of their blocks ----
+struct LargeGroups {
+    const SelectArgs &a;
+    int known = -1;                       // the group that was looked at last, and whether it is a large one
+    bool large = false;
+    __device__ __forceinline__ explicit LargeGroups(const SelectArgs &args) : a(args) {}
+    __device__ __forceinline__ int64_t operator()(int pair)
+    {
+        const int group = pair / a.per_group;
+        if (group != known) {
+            known = group;
+            large = a.per_group > kMaxPairs;
+            int64_t rows = 0;
+            for (int p = group * a.per_group; !large && p < (group + 1) * a.per_group; ++p) rows += select_len(a, p), large = rows > a.cap;
+        }
+        return large ? max(1, (select_len(a, pair) + kBlockRows - 1) / kBlockRows) : 0;      // one of an empty pair too: its list is one
+    }
+};
+
+// STEP 0 .. 2: a digit is counted; 3: what stays of every block; 4: the lists.
+template <int STEP>
+__global__ __launch_bounds__(256, 3) void fairkv_select_large_kernel(SelectArgs a)
+{
+    constexpr int NT = 256, NW = NT / 64, KPT = kBlockRows / NT;
+    constexpr bool kCounts = STEP < kDigits;
+    __shared__ float raw[kBlockRows + 2 * kMostHalf];
+    __shared__ int32_t bins[kCounts ? kBins : 1];
+    __shared__ int32_t counts[KPT][NW];
+    __shared__ unsigned long long sums[5];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    LargeGroups blocks_of(a);
+    const LineShare share = line_share<NT>(a.n_pairs, gridDim.x, blockIdx.x, [&](int p) { return blocks_of(p); });
+    if (share.total > a.max_blocks) {     // runs of rows that overlap: so many blocks no cache has
+        if (STEP == kDigits + 1 && blockIdx.x == 0)
+            for (int p = threadIdx.x; p < a.n_pairs; p += NT)
+                if (blocks_of(p) > 0) {
+                    a.n_keep[p] = -1;
+                    if (a.bad) atomicAdd(a.bad, 1);
+                }
+        return;
+    }
+    int pair = share.pair, group = -1;
+    int64_t block = share.begin, at = share.at, group_at = 0;      // group_at: the place of the group's first block
+    SelectSlot *slot = nullptr;
+    SelectFound f{0, 0, 0};
+    int32_t protected_rows = 0, blocks_here = 0;
+
+    auto end_group = [&]() __attribute__((always_inline)) {
+        if constexpr (kCounts) {
+            __syncthreads();
+            for (int i = threadIdx.x; i < kBins; i += NT)
+                if (bins[i]) atomicAdd(&slot->bins[STEP][i], bins[i]);
+            if (STEP == 0 && protected_rows) atomicAdd(&slot->protected_rows, static_cast<unsigned long long>(protected_rows));
+            __syncthreads();
+        }
+        if constexpr (STEP == kDigits + 1) {      // who comes last leaves all of the group's as it was found
+            int64_t n = 0;
+            for (int p = group * a.per_group; p < (group + 1) * a.per_group; ++p) n += blocks_of(p);
+            __syncthreads();
+            if (threadIdx.x == 0) sums[0] = atomicAdd(reinterpret_cast<unsigned long long *>(&slot->listed), static_cast<unsigned long long>(blocks_here)) + blocks_here;
+            __syncthreads();
+            if (static_cast<int64_t>(sums[0]) == n) {
+                for (int64_t x = threadIdx.x; x < n; x += NT) a.blocks[group_at + x] = make_int2(0, 0);
+                for (int i = threadIdx.x; i < kBins; i += NT) slot->bins[kDigits - 1][i] = 0;
+                if (threadIdx.x < kDigits) slot->found[threadIdx.x] = SelectFound{0, 0, 0};
+                if (threadIdx.x == 0) slot->listed = 0;
+            }
+            blocks_here = 0;
+        }
+    };
+    auto begin_group = [&]() __attribute__((always_inline)) {
+        group = pair / a.per_group, group_at = at - block;
+        for (int p = group * a.per_group; p < pair; ++p) group_at -= blocks_of(p);
+        slot = a.slots + group_at / a.min_blocks;
+        if constexpr (STEP == 1) {
+            f = {max(static_cast<int64_t>(a.budget[group]) - static_cast<int64_t>(slot->protected_rows), static_cast<int64_t>(0)), 0, 0};
+            if (f.need == 0) f = {0, kProtected - 1, 1};
+        }
+        if constexpr (STEP > 1) f = slot->found[STEP == kDigits + 1 ? kDigits - 1 : STEP - 2];
+        if constexpr (STEP >= 1 && STEP <= kDigits) {
+            if (!f.done) {
+                const BinFound b = find_bin<NT>(f.need, [&](int x) { return slot->bins[STEP - 1][x]; });
+                if (b.need == 0) {        // there are no so many candidates: all of them stay
+                    f = {0, 0, 1};
                 } else {
-                    const uint32_t x = value_of(a, p, c, t);
-                    stays = x > least, tie = x == least;
+                    f.need = b.need, f.least |= static_cast<uint32_t>(b.bin) << kDigitShift[STEP - 1];
+                    if (f.need == b.in_bin) f = {0, f.least - 1, 1};      // all that share these digits stay
                 }
             }
-            const Before equal = count_before<NT>(tie, of_waves2);
-            if (tie && ties_before + equal.before < ties) stays = true;
-            ties_before += equal.total;
-            const Before n = count_before<NT>(stays, of_waves);
-            if (stays && kept + n.before < a.max_keep) to[kept + n.before] = t;
-            kept += n.total;
         }
-        if (threadIdx.x == 0) {
-            a.n_keep[p] = kept <= a.max_keep ? kept : -1;
-            if (kept > a.max_keep && a.bad) atomicAdd(a.bad, 1);
+        if (at == group_at) {             // this workgroup has the group's first block
+            if (STEP >= 1 && STEP <= kDigits && threadIdx.x == 0) slot->found[STEP - 1] = f;
+            if (STEP == 2 && threadIdx.x == 0) slot->protected_rows = 0;
+            if constexpr (STEP == 2 || STEP == 3)
+                for (int i = threadIdx.x; i < kBins; i += NT) slot->bins[STEP - 2][i] = 0;
+        }
+        if constexpr (kCounts) {
+            for (int i = threadIdx.x; i < kBins; i += NT) bins[i] = 0;
+            protected_rows = 0;
+            __syncthreads();
+        }
+    };
+
+    for (int64_t left = share.left; left > 0; --left, ++block, ++at) {
+        if (block >= blocks_of(pair)) pair = next_pair(pair, a.n_pairs, [&](int p) { return blocks_of(p); }), block = 0;
+        if (pair / a.per_group != group) {
+            if (group >= 0) end_group();
+            begin_group();
+        }
+        ++blocks_here;
+        if ((STEP == 1 || STEP == 2) && f.done) continue;
+        // ---- values ----
+        const int32_t len = select_len(a, pair), t0 = static_cast<int32_t>(block) * kBlockRows;
+        const Candidates c(a, len);
+        uint32_t key[KPT];
+        float value[KPT];
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) {
+            const int32_t t = t0 + i * NT + static_cast<int32_t>(threadIdx.x);
+            const int64_t row = t < len ? a.rows.row(pair, t) : -1;
+            key[i] = row < 0 ? kNone : c.has(t) ? 1 : kProtected;
+            value[i] = key[i] == 1 ? a.weights[row] : -INFINITY;
+        }
+        float edge = -INFINITY;           // rows beside the block that its windows reach
+        const int e = static_cast<int>(threadIdx.x);
+        if (e < 2 * a.half) {
+            const int32_t t = e < a.half ? t0 - a.half + e : t0 + kBlockRows + e - a.half;
+            const int64_t row = c.has(t) ? a.rows.row(pair, t) : -1;
+            if (row >= 0) edge = a.weights[row];
+        }
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) value[i] = fmaxf(value[i], -INFINITY);      // a NaN is as low
+        if (a.half > 0) {
+            __syncthreads();              // the windows of the block before have been looked at
+#pragma unroll
+            for (int i = 0; i < KPT; ++i) raw[a.half + i * NT + threadIdx.x] = value[i];
+            if (e < 2 * a.half) raw[e < a.half ? e : kBlockRows + e] = fmaxf(edge, -INFINITY);
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < KPT; ++i) {
+                const int32_t u0 = i * NT + static_cast<int32_t>(threadIdx.x);
+                if (key[i] == 1)
+                    for (int32_t u = u0; u <= u0 + 2 * a.half; ++u) value[i] = fmaxf(value[i], raw[u]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) {
+            if (key[i] == kProtected) ++protected_rows;
+            if (key[i] == 1) key[i] = order_of(value[i]);
+        }
+        // ---- counts ----
+        if constexpr (kCounts) {
+#pragma unroll
+            for (int i = 0; i < KPT; ++i) count_digit(bins, key[i], STEP, f.least, key[i] != kNone && key[i] != kProtected);
+            continue;
+        }
+        uint32_t stays = 0, equal = 0;
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) {
+            stays |= (key[i] > f.least ? 1u : 0u) << i;
+            equal |= (f.need > 0 && key[i] == f.least ? 1u : 0u) << i;
+        }
+        if constexpr (STEP == kDigits) {
+            __syncthreads();
+            if (threadIdx.x < 2) sums[threadIdx.x] = 0;
+            __syncthreads();
+            atomicAdd(&sums[0], static_cast<unsigned long long>(__builtin_popcount(stays)));
+            atomicAdd(&sums[1], static_cast<unsigned long long>(__builtin_popcount(equal)));
+            __syncthreads();
+            if (threadIdx.x == 0) a.blocks[at] = make_int2(static_cast<int>(sums[0]), static_cast<int>(sums[1]));
+        }
+        if constexpr (STEP == kDigits + 1) {
+            // ties in front of the pair, and of the block; rows in front of the block that stay anyhow; both of the whole pair
+            const int64_t pair_at = at - block, pair_end = pair_at + blocks_of(pair);
+            __syncthreads();
+            if (threadIdx.x < 5) sums[threadIdx.x] = 0;
+            __syncthreads();
+            unsigned long long s[5] = {0, 0, 0, 0, 0};
+            for (int64_t x = (f.need > 0 ? group_at : pair_at) + threadIdx.x; x < (block == 0 ? pair_end : at); x += NT) {
+                const int2 n = a.blocks[x];
+                if (x < pair_at) s[0] += n.y;
+                if (x < at) s[1] += n.y;
+                if (x >= pair_at && x < at) s[2] += n.x;
+                if (x >= pair_at) s[3] += n.y, s[4] += n.x;
+            }
+            for (int i = 0; i < 5; ++i)
+                if (s[i]) atomicAdd(&sums[i], s[i]);
+            __syncthreads();
+            const int64_t ties_pair = sums[0], ties_block = sums[1];
+            const int64_t from = static_cast<int64_t>(sums[2]) + min(f.need, ties_block) - min(f.need, ties_pair);
+            if (block == 0 && threadIdx.x == 0) {
+                const int64_t n = static_cast<int64_t>(sums[4]) + min(f.need, ties_pair + static_cast<int64_t>(sums[3])) - min(f.need, ties_pair);
+                a.n_keep[pair] = n <= a.max_keep ? static_cast<int32_t>(n) : -1;
+                if (n > a.max_keep && a.bad) atomicAdd(a.bad, 1);
+            }
+            if (f.need > 0) {
+                count_rows<NT, KPT>(counts, equal);
+#pragma unroll
+                for (int i = 0; i < KPT; ++i) {
+                    const int32_t n = rows_before<NT, KPT>(counts, equal, i);
+                    if ((equal >> i & 1) && ties_block + n < f.need) stays |= 1u << i;
+                }
+                __syncthreads();
+            }
+            count_rows<NT, KPT>(counts, stays);
+#pragma unroll
+            for (int i = 0; i < KPT; ++i) {
+                const int64_t n = from + rows_before<NT, KPT>(counts, stays, i);
+                if ((stays >> i & 1) && n < a.max_keep) a.keep[static_cast<int64_t>(pair) * a.max_keep + n] = t0 + i * NT + static_cast<int32_t>(threadIdx.x);
+            }
         }
     }
+    if (group >= 0) end_group();
+    (void)lane, (void)wave;
 }
 
 }  // namespace fairkv
