@@ -16,8 +16,7 @@ namespace {
 using namespace fairkv;
 
 constexpr int32_t kMaxSlots = 65536;
-constexpr int32_t kSmallCap = 8192, kLargeCap = 16384;      // rows of a group in a workgroup's registers
-static_assert(kSmallCap % kBlockRows == 0 && kLargeCap % kBlockRows == 0, "a larger group has more blocks than that");
+constexpr int32_t kSmallCap = 128, kLargeCap = 256;      // units of a group in a workgroup's registers
 
 // Tokens that a length can count: 2^31 - 2^16, so that what is added to a token's number does not wrap around.
 int32_t max_len(const fairkv_cache *c)
@@ -74,7 +73,7 @@ extern "C" int fairkv_attn_weights(const fairkv_cache *c, const void *q, const u
 namespace {
 
 struct SelectShape {
-    int32_t cap, min_blocks;      // rows of a group that one workgroup has; blocks that a larger one has at least
+    int32_t cap, min_blocks;      // units of 64 rows of a group that one workgroup has; blocks that a larger one has at least
     int64_t max_blocks;           // of all larger groups, 0: there can be none
     int64_t slots;
 };
@@ -83,24 +82,26 @@ SelectShape select_shape(const fairkv_cache *c, int32_t shared, int32_t n_slots)
     const int64_t pairs = static_cast<int64_t>(c->B) * c->Hkv, per_group = shared ? c->Hkv : 1, groups = pairs / per_group;
     const int64_t each = max_len(c), most = std::min(std::max<int64_t>(c->n_rows, 0), each * pairs), group_most = std::min(most, each * per_group);
     SelectShape s{};
-    s.cap = group_most <= kSmallCap || (group_most > kLargeCap && groups > n_slots) ? kSmallCap : kLargeCap;
-    if (group_most <= s.cap && per_group <= kMaxPairs) return s;
-    s.min_blocks = per_group > kMaxPairs ? kMaxPairs : s.cap / kBlockRows;
-    // every pair of a large group has a block that is not full
-    const int64_t large_pairs = per_group > kMaxPairs ? pairs : std::min(pairs, most / s.cap * per_group);
+    auto fits = [&](int32_t cap) { return per_group <= kMaxPairs && (group_most + 63 * per_group) / 64 <= cap; };      // pairs' last units are not full
+    s.cap = fits(kSmallCap) || (!fits(kLargeCap) && groups > n_slots) ? kSmallCap : kLargeCap;
+    if (fits(s.cap)) return s;
+    // A block of a pair has at most 64 units, so a large group has more than cap / 64 blocks; its rows are more than 64 cap - 63 per_group.
+    s.min_blocks = per_group > kMaxPairs ? kMaxPairs : s.cap / (kBlockRows / 64);
+    const int64_t least_rows = std::max<int64_t>(1, 64 * static_cast<int64_t>(s.cap) - 63 * per_group);
+    const int64_t large_pairs = per_group > kMaxPairs ? pairs : std::min(pairs, most / least_rows * per_group);      // each has a block that is not full
     s.max_blocks = most / kBlockRows + large_pairs;
     s.slots = s.max_blocks / s.min_blocks + 1;
     return s;
 }
 size_t select_bytes(const SelectShape &s) { return 256 + sizeof(SelectSlot) * s.slots + sizeof(int2) * s.max_blocks; }
 
-template <int NT, int KPT>
+template <int NT, int UNITS>
 void launch_select(const SelectArgs &a, unsigned groups, hipStream_t st)
 {
     if (a.half > 0)
-        hipLaunchKernelGGL((fairkv_select_kernel<NT, KPT, true>), dim3(groups), dim3(NT), 0, st, a);
+        hipLaunchKernelGGL((fairkv_select_kernel<NT, UNITS, true>), dim3(groups), dim3(NT), 0, st, a);
     else
-        hipLaunchKernelGGL((fairkv_select_kernel<NT, KPT, false>), dim3(groups), dim3(NT), 0, st, a);
+        hipLaunchKernelGGL((fairkv_select_kernel<NT, UNITS, false>), dim3(groups), dim3(NT), 0, st, a);
 }
 
 }  // namespace
@@ -136,16 +137,16 @@ extern "C" int fairkv_select(const fairkv_cache *c, const fairkv_selection *s, c
     }
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (shape.cap == kSmallCap)
-        launch_select<512, kSmallCap / 512>(a, static_cast<unsigned>(groups), st);
+        launch_select<512, kSmallCap>(a, static_cast<unsigned>(groups), st);
     else
-        launch_select<1024, kLargeCap / 1024>(a, static_cast<unsigned>(groups), st);
+        launch_select<1024, kLargeCap>(a, static_cast<unsigned>(groups), st);
     if (shape.max_blocks > 0) {
         const dim3 grid(static_cast<unsigned>(std::min<int64_t>(shape.max_blocks, 4 * static_cast<int64_t>(n_slots))));
-        hipLaunchKernelGGL(fairkv_select_large_kernel<0>, grid, dim3(256), 0, st, a);
-        hipLaunchKernelGGL(fairkv_select_large_kernel<1>, grid, dim3(256), 0, st, a);
-        hipLaunchKernelGGL(fairkv_select_large_kernel<2>, grid, dim3(256), 0, st, a);
-        hipLaunchKernelGGL(fairkv_select_large_kernel<3>, grid, dim3(256), 0, st, a);
-        hipLaunchKernelGGL(fairkv_select_large_kernel<4>, grid, dim3(256), 0, st, a);
+        hipLaunchKernelGGL(fairkv_select_large_kernel<0>, grid, dim3(512), 0, st, a);
+        hipLaunchKernelGGL(fairkv_select_large_kernel<1>, grid, dim3(512), 0, st, a);
+        hipLaunchKernelGGL(fairkv_select_large_kernel<2>, grid, dim3(512), 0, st, a);
+        hipLaunchKernelGGL(fairkv_select_large_kernel<3>, grid, dim3(512), 0, st, a);
+        hipLaunchKernelGGL(fairkv_select_large_kernel<4>, grid, dim3(512), 0, st, a);
     }
     return launched();
 }

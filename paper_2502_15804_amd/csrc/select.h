@@ -9,7 +9,7 @@
 // counting how many candidates have which digit among those that share the digits found so far: 11, 11 and 10 bits.  Where all candidates that
 // share some digits stay, the others need not be looked at.
 //
-// A group of up to CAP rows is one workgroup's, which reads its weights once and holds its values in registers.  Rows of larger groups are dealt
+// A group of up to `cap` units of 64 rows is one workgroup's, which reads its weights once and holds its values in registers.  Rows of larger groups are dealt
 // to the whole GPU in blocks: three kernels count a digit each, one counts what stays of every block, one lists it.
 #pragma once
 #include "cache_rows.h"
@@ -20,7 +20,7 @@ namespace fairkv {
 constexpr int kDigits = 3;
 constexpr int kDigitShift[kDigits] = {21, 10, 0}, kBins = 2048;      // bins of a digit, the last digit's half as many
 constexpr int kBlockRows = 4096;          // of a large group
-constexpr int kMaxPairs = 256;            // of a group that one workgroup has
+constexpr int kMaxPairs = 64;             // of a group that one workgroup has
 constexpr int kMostHalf = 31;             // of the window
 
 // What the kernels of a large group hand on.  Slots are of groups: a group has at least min_blocks blocks, so the place of its first block in the
@@ -108,10 +108,48 @@ __device__ __forceinline__ void count_digit(int32_t *bins, uint32_t key, int dig
     if (counts && (digit == 0 || (key ^ least) >> kDigitShift[digit > 0 ? digit - 1 : 0] == 0)) atomicAdd(&bins[key >> shift & (kBins - 1) & (digit == 2 ? 1023 : ~0)], 1);
 }
 
+// Weights of a thread's KPT rows, all on their way at once: first the pages' numbers, then the weights, with addresses that are always some of the
+// array's.  state: kNone where the cache has no such row (or `place` says so), 1 for a candidate, kProtected.
+template <int KPT, class Place>
+__device__ __forceinline__ void load_values(const SelectArgs &a, int pair, uint32_t (&state)[KPT], float (&value)[KPT], Place place)
+{
+    int32_t t[KPT];
+    int64_t row[KPT];
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) state[i] = place(i, t[i]);
+    if (a.rows.pages) {
+        int32_t id[KPT];
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) id[i] = a.rows.pages[static_cast<int64_t>(pair) * a.rows.max_pages + min(t[i] >> a.rows.page_shift, a.rows.max_pages - 1)];
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) row[i] = a.rows.row_of_page(id[i], t[i]);
+    } else {
+        const int64_t first = a.rows.off[pair];
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) row[i] = first >= 0 && static_cast<uint64_t>(first) + static_cast<uint32_t>(t[i]) < static_cast<uint64_t>(a.rows.n_rows) ? first + t[i] : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) value[i] = a.weights[max(row[i], static_cast<int64_t>(0))];
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+        if (row[i] < 0) state[i] = kNone;
+        value[i] = state[i] == 1 ? fmaxf(value[i], -INFINITY) : -INFINITY;      // a NaN is as low
+    }
+}
+// How many of the workgroup's lanes' bits are set in all, added to *sum in LDS.
+template <int KPT, class Is>
+__device__ __forceinline__ void add_rows(int32_t *sum, Is is)
+{
+    int32_t n = 0;
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) n += __builtin_popcountll(__builtin_amdgcn_ballot_w64(is(i)));
+    if ((threadIdx.x & 63) == 0 && n) atomicAdd(sum, n);
+}
+
 // Rows i NT + threadIdx.x, i < KPT, of which bit i of a thread's x says whether it is one of some: how many of them are in front of a row.
 // count_rows is called by all threads and ends with a barrier; another one stands between the last rows_before and the next count_rows.
 template <int NT, int KPT>
-__device__ __forceinline__ void count_rows(int32_t (&counts)[KPT][NT / 64], uint32_t x)
+__device__ __forceinline__ void count_rows(int32_t (&counts)[KPT][NT / 64], uint32_t x, int32_t *total /* LDS */)
 {
     constexpr int NW = NT / 64, PER = KPT * NW / 64;
     static_assert(KPT * NW % 64 == 0, "sums of a lane");
@@ -127,6 +165,7 @@ __device__ __forceinline__ void count_rows(int32_t (&counts)[KPT][NT / 64], uint
 #pragma unroll
         for (int j = 0; j < PER; ++j) n[j] = (&counts[0][0])[lane * PER + j], all += n[j];
         int32_t before = static_cast<int32_t>(wave_upto(all)) - all;
+        if (lane == 63) *total = before + all;
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
             (&counts[0][0])[lane * PER + j] = before;
@@ -141,165 +180,167 @@ __device__ __forceinline__ int32_t rows_before(const int32_t (&counts)[KPT][NT /
     return counts[i][threadIdx.x >> 6] + __builtin_popcountll(__builtin_amdgcn_ballot_w64((x >> i & 1) != 0) & ((1ull << (threadIdx.x & 63)) - 1));
 }
 
-// ---- a group that one workgroup has: keys of rows threadIdx.x + i NT of the group's, one pair's behind the other's ----
-template <int NT, int KPT, bool POOL>
+// ---- a group that one workgroup has ----
+// Its rows in units of 64, a pair's last one not full, so that all lanes of a wave are in one pair; wave w has units w, w + NW, ...  What a pair's
+// rows need to know is held in lanes: lane p has pair p.  Keys lie in LDS.
+template <int NT, int UNITS, bool POOL>
 __global__ __launch_bounds__(NT) void fairkv_select_kernel(SelectArgs a)
 {
-    constexpr int CAP = NT * KPT, NW = NT / 64;
-    __shared__ int32_t start[kMaxPairs + 1], stays_from[kMaxPairs], stays_to[kMaxPairs];
+    constexpr int NW = NT / 64, kBatch = 4, PER = UNITS / 64;
+    __shared__ uint32_t keys[UNITS * 64];             // first: kNone, 1 for a candidate, kProtected
+    __shared__ float raw[POOL ? UNITS * 64 : 1];
     __shared__ int32_t bins[kBins];
-    __shared__ float raw[POOL ? CAP : 1];
-    __shared__ int32_t counts[KPT][NW];
-    __shared__ int32_t protected_rows, candidate_rows;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = blockIdx.x, p0 = group * a.per_group;
+    __shared__ int32_t counts[UNITS];
+    __shared__ int32_t total, protected_rows, candidate_rows;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = blockIdx.x, p0 = group * a.per_group;
     const int n_pairs = a.per_group;
-    auto refuse = [&]() {
-        for (int p = threadIdx.x; p < n_pairs; p += NT) {
+    const uint64_t below = (1ull << lane) - 1;
+    // ---- where the pairs begin, in units ----
+    const bool one = lane < n_pairs;
+    const int32_t budget = a.budget[group];
+    const int32_t len = one ? select_len(a, p0 + lane) : 0;
+    const int64_t off = one && !a.rows.pages ? a.rows.off[p0 + lane] : 0;
+    const int64_t upto = wave_upto((static_cast<int64_t>(len) + 63) / 64), units64 = __shfl(upto, 63);
+    if (n_pairs > kMaxPairs || units64 > a.cap) {     // a.cap is UNITS or less: a larger group's other kernels do it, if there can be one
+        for (int p = threadIdx.x; p < n_pairs && !a.slots; p += NT) {
             a.n_keep[p0 + p] = -1;
             if (a.bad) atomicAdd(a.bad, 1);
         }
-    };
-    if (n_pairs > kMaxPairs) {
-        if (!a.slots) refuse();
         return;
     }
-    // ---- where the pairs begin ----
-    if (wave == 0) {
-        int64_t before = 0;
-        for (int q = 0; q < n_pairs; q += 64) {
-            const int p = q + lane;
-            const int32_t len = p < n_pairs ? select_len(a, p0 + p) : 0;
-            const int64_t upto = wave_upto(len);
-            if (p < n_pairs) start[p] = static_cast<int32_t>(min(before + upto - len, static_cast<int64_t>(INT32_MAX)));
-            before += __shfl(upto, 63);
-        }
-        if (lane == 0) start[n_pairs] = static_cast<int32_t>(min(before, static_cast<int64_t>(INT32_MAX))), protected_rows = candidate_rows = 0;
-    }
+    const int32_t units = __builtin_amdgcn_readfirstlane(static_cast<int>(units64));
+    const int32_t ends = static_cast<int32_t>(upto), begins = ends - (len + 63) / 64;      // of the lane's pair
+    auto pair_of = [&](int32_t unit) __attribute__((always_inline)) { return __builtin_popcountll(__builtin_amdgcn_ballot_w64(one && ends <= unit)); };
+    for (int i = threadIdx.x; i < kBins; i += NT) bins[i] = 0;
+    if (threadIdx.x == 0) protected_rows = candidate_rows = 0;
     __syncthreads();
-    const int32_t total = start[n_pairs];
-    if (total > a.cap) {                  // a.cap is CAP or less
-        if (!a.slots) refuse();
-        return;
-    }
-    // ---- values ----
-    uint32_t key[KPT];
-    auto pair_of = [&](int32_t f) __attribute__((always_inline)) {      // the last pair that begins at f or before and is not empty there
-        int lo = 0, hi = n_pairs - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (start[mid] <= f)
-                lo = mid;
-            else
-                hi = mid - 1;
+
+    // ---- values: a batch's page numbers, then its weights, on their way together, from addresses that are always some of the array's ----
+    int32_t is_protected = 0, is_candidate = 0;
+    for (int32_t u0 = wave; u0 < units; u0 += kBatch * NW) {
+        int32_t t[kBatch], n[kBatch], id[kBatch];
+        int64_t row[kBatch];
+        float value[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int32_t unit = min(u0 + i * NW, units - 1);
+            const int p = pair_of(unit);
+            t[i] = (unit - __builtin_amdgcn_readlane(begins, p)) * 64 + lane, n[i] = __builtin_amdgcn_readlane(len, p);
+            if (a.rows.pages) {
+                id[i] = a.rows.pages[static_cast<int64_t>(p0 + p) * a.rows.max_pages + min(min(t[i], n[i] - 1) >> a.rows.page_shift, a.rows.max_pages - 1)];
+            } else {
+                const int64_t first = static_cast<int64_t>((static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(off >> 32), p))) << 32) |
+                                                           static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(off), p)));
+                row[i] = first >= 0 && static_cast<uint64_t>(first) + static_cast<uint32_t>(t[i]) < static_cast<uint64_t>(a.rows.n_rows) ? first + t[i] : -1;
+            }
         }
-        return lo;
-    };
-    float value[KPT];
-    int32_t mine = 0, also = 0;
+        if (a.rows.pages) {
 #pragma unroll
-    for (int i = 0; i < KPT; ++i) {
-        const int32_t f = i * NT + static_cast<int32_t>(threadIdx.x);
-        key[i] = kNone;
-        value[i] = -INFINITY;
-        if (f >= total) continue;
-        const int p = pair_of(f);
-        const int32_t t = f - start[p];
-        const Candidates c(a, start[p + 1] - start[p]);
-        const int64_t row = a.rows.row(p0 + p, t);
-        if (row < 0) continue;
-        key[i] = c.has(t) ? 1 : kProtected;
-        if (c.has(t)) value[i] = a.weights[row];
-    }
+            for (int i = 0; i < kBatch; ++i) row[i] = a.rows.row_of_page(id[i], t[i]);
+        }
 #pragma unroll
-    for (int i = 0; i < KPT; ++i) {
-        value[i] = fmaxf(value[i], -INFINITY);      // a NaN is as low
-        if (key[i] == kProtected) ++mine;
-        if (key[i] == 1) ++also;
-        if constexpr (POOL) {
-            if (i * NT + static_cast<int32_t>(threadIdx.x) < total) raw[i * NT + threadIdx.x] = value[i];
+        for (int i = 0; i < kBatch; ++i) value[i] = a.weights[max(row[i], static_cast<int64_t>(0))];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            if (u0 + i * NW >= units) continue;
+            const int32_t at = (u0 + i * NW) * 64 + lane;
+            const bool candidate = Candidates(a, n[i]).has(t[i]) && row[i] >= 0, stays = t[i] < n[i] && row[i] >= 0 && !candidate;
+            value[i] = fmaxf(candidate ? value[i] : -INFINITY, -INFINITY);      // a NaN is as low
+            is_candidate += __builtin_popcountll(__builtin_amdgcn_ballot_w64(candidate));
+            is_protected += __builtin_popcountll(__builtin_amdgcn_ballot_w64(stays));
+            if constexpr (POOL) raw[at] = value[i];
+            keys[at] = stays ? kProtected : !candidate ? kNone : POOL ? 1u : order_of(value[i]);
+            if (!POOL && candidate) atomicAdd(&bins[order_of(value[i]) >> kDigitShift[0]], 1);
         }
     }
-    if (mine) atomicAdd(&protected_rows, mine);
-    if (also) atomicAdd(&candidate_rows, also);
+    if (lane == 0) atomicAdd(&candidate_rows, is_candidate), atomicAdd(&protected_rows, is_protected);
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < KPT; ++i) {
-        if (key[i] != 1) continue;
-        if constexpr (POOL) {             // rows that are no candidates have -inf there; the window ends where the pair does
-            const int32_t f = i * NT + static_cast<int32_t>(threadIdx.x);
-            const int p = pair_of(f);
-            for (int32_t u = max(start[p], f - a.half); u <= min(start[p + 1] - 1, f + a.half); ++u) value[i] = fmaxf(value[i], raw[u]);
+    if constexpr (POOL) {                             // rows that are no candidates have -inf there; the window ends where the pair does
+        for (int32_t unit = wave; unit < units; unit += NW) {
+            const int p = pair_of(unit);
+            const int32_t at = unit * 64 + lane, lo = __builtin_amdgcn_readlane(begins, p) * 64, hi = __builtin_amdgcn_readlane(ends, p) * 64 - 1;
+            float x = raw[at];
+#pragma unroll 4
+            for (int32_t d = 1; d <= a.half; ++d) x = fmaxf(x, fmaxf(raw[max(lo, at - d)], raw[min(hi, at + d)]));
+            if (keys[at] == 1) {
+                keys[at] = order_of(x);
+                atomicAdd(&bins[order_of(x) >> kDigitShift[0]], 1);
+            }
         }
-        key[i] = order_of(value[i]);
+        __syncthreads();
     }
 
     // ---- the least that stays, and how many of those that are equal to it ----
-    const int64_t room = max(static_cast<int64_t>(a.budget[group]) - protected_rows, static_cast<int64_t>(0));
-    uint32_t least = 0;                   // what is larger stays
+    const int64_t room = max(static_cast<int64_t>(budget) - protected_rows, static_cast<int64_t>(0));
+    uint32_t least = 0;                               // what is larger stays
     int64_t ties = 0;
     if (room == 0) {
         least = kProtected - 1;
     } else if (room < candidate_rows) {
-        int64_t need = room;
-#pragma unroll
+        ties = room;
         for (int digit = 0; digit < kDigits; ++digit) {
-            for (int i = threadIdx.x; i < kBins; i += NT) bins[i] = 0;
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < KPT; ++i)
-                if (i * NT < total) count_digit(bins, key[i], digit, least, key[i] != kNone && key[i] != kProtected);
-            __syncthreads();
-            const BinFound b = find_bin<NT>(need, [&](int x) { return bins[x]; });
-            need = b.need;
+            if (digit > 0) {
+                for (int i = threadIdx.x; i < kBins; i += NT) bins[i] = 0;
+                __syncthreads();
+                for (int32_t unit = wave; unit < units; unit += NW) {
+                    const uint32_t key = keys[unit * 64 + lane];
+                    count_digit(bins, key, digit, least, key != kNone && key != kProtected);
+                }
+                __syncthreads();
+            }
+            const BinFound b = find_bin<NT>(ties, [&](int x) { return bins[x]; });
+            ties = b.need;
             least |= static_cast<uint32_t>(b.bin) << kDigitShift[digit];
-            if (need == b.in_bin) {       // all of them stay, whatever their other digits are
+            if (ties == b.in_bin) {                   // all of them stay, whatever their other digits are
                 least -= 1;
-                need = 0;
+                ties = 0;
                 break;
             }
         }
-        ties = need;
     }
 
-    // ---- the lists: how many stay in front of a row, in the order of the rows ----
-    uint32_t stays = 0;                   // bit i
+    // ---- the lists: counts in front of every unit, in the order of the rows, of the ties and then of what stays ----
+    auto count = [&](auto is) __attribute__((always_inline)) {
+        for (int32_t unit = wave; unit < units; unit += NW) {
+            const int32_t n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(is(unit)));
+            if (lane == 0) counts[unit] = n;
+        }
+        __syncthreads();
+        if (wave == 0) {
+            int32_t n[PER], all = 0;
 #pragma unroll
-    for (int i = 0; i < KPT; ++i) stays |= (key[i] > least ? 1u : 0u) << i;
+            for (int i = 0; i < PER; ++i) n[i] = lane * PER + i < units ? counts[lane * PER + i] : 0, all += n[i];
+            int32_t before = static_cast<int32_t>(wave_upto(all)) - all;
+            if (lane == 63) total = before + all;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                if (lane * PER + i < units) counts[lane * PER + i] = before;
+                before += n[i];
+            }
+        }
+        __syncthreads();
+    };
     if (ties > 0) {
-        uint32_t equal = 0;
-#pragma unroll
-        for (int i = 0; i < KPT; ++i) equal |= (key[i] == least ? 1u : 0u) << i;
-        count_rows<NT, KPT>(counts, equal);
-#pragma unroll
-        for (int i = 0; i < KPT; ++i) {
-            const int32_t n = rows_before<NT, KPT>(counts, equal, i);
-            if ((equal >> i & 1) && n < ties) stays |= 1u << i;
+        auto equal = [&](int32_t unit) { return keys[unit * 64 + lane] == least; };
+        count(equal);
+        for (int32_t unit = wave; unit < units; unit += NW) {
+            const uint64_t here = __builtin_amdgcn_ballot_w64(equal(unit));
+            if (equal(unit) && counts[unit] + __builtin_popcountll(here & below) < ties) keys[unit * 64 + lane] = kProtected;
         }
         __syncthreads();
     }
-    count_rows<NT, KPT>(counts, stays);
-    for (int p = threadIdx.x; p < n_pairs; p += NT)
-        if (start[p] == start[p + 1]) stays_from[p] = stays_to[p] = 0;
-#pragma unroll
-    for (int i = 0; i < KPT; ++i) {
-        const int32_t f = i * NT + static_cast<int32_t>(threadIdx.x), n = rows_before<NT, KPT>(counts, stays, i);
-        if (f >= total) continue;
-        const int p = pair_of(f);
-        if (f == start[p]) stays_from[p] = n;
-        if (f == start[p + 1] - 1) stays_to[p] = n + static_cast<int32_t>(stays >> i & 1);
+    auto stays = [&](int32_t unit) { return keys[unit * 64 + lane] > least; };
+    count(stays);
+    const int32_t from = begins < units ? counts[begins] : total, to = ends < units ? counts[ends] : total;      // of the lane's pair: how many stay in front of it, and up to its end
+    for (int32_t unit = wave; unit < units; unit += NW) {
+        const int p = pair_of(unit);
+        const bool here = stays(unit);
+        const int32_t n = counts[unit] + __builtin_popcountll(__builtin_amdgcn_ballot_w64(here) & below) - __builtin_amdgcn_readlane(from, p);
+        if (here && n < a.max_keep) a.keep[static_cast<int64_t>(p0 + p) * a.max_keep + n] = (unit - __builtin_amdgcn_readlane(begins, p)) * 64 + lane;
     }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < KPT; ++i) {
-        const int32_t f = i * NT + static_cast<int32_t>(threadIdx.x), n = rows_before<NT, KPT>(counts, stays, i);
-        if (!(stays >> i & 1)) continue;
-        const int p = pair_of(f);
-        if (n - stays_from[p] < a.max_keep) a.keep[static_cast<int64_t>(p0 + p) * a.max_keep + n - stays_from[p]] = f - start[p];
-    }
-    for (int p = threadIdx.x; p < n_pairs; p += NT) {
-        const int32_t n = stays_to[p] - stays_from[p];
-        a.n_keep[p0 + p] = n <= a.max_keep ? n : -1;
-        if (n > a.max_keep && a.bad) atomicAdd(a.bad, 1);
+    if (wave == 0 && one) {
+        a.n_keep[p0 + lane] = to - from <= a.max_keep ? to - from : -1;
+        if (to - from > a.max_keep && a.bad) atomicAdd(a.bad, 1);
     }
 }
 
@@ -315,8 +356,12 @@ struct LargeGroups {
         if (group != known) {
             known = group;
             large = a.per_group > kMaxPairs;
-            int64_t rows = 0;
-            for (int p = group * a.per_group; !large && p < (group + 1) * a.per_group; ++p) rows += select_len(a, p), large = rows > a.cap;
+            if (!large) {
+                int64_t units = 0;
+#pragma unroll 8
+                for (int p = group * a.per_group; p < (group + 1) * a.per_group; ++p) units += (select_len(a, p) + 63) / 64;
+                large = units > a.cap;
+            }
         }
         return large ? max(1, (select_len(a, pair) + kBlockRows - 1) / kBlockRows) : 0;      // one of an empty pair too: its list is one
     }
@@ -324,15 +369,16 @@ struct LargeGroups {
 
 // STEP 0 .. 2: a digit is counted; 3: what stays of every block; 4: the lists.
 template <int STEP>
-__global__ __launch_bounds__(256, 3) void fairkv_select_large_kernel(SelectArgs a)
+__global__ __launch_bounds__(512) void fairkv_select_large_kernel(SelectArgs a)
 {
-    constexpr int NT = 256, NW = NT / 64, KPT = kBlockRows / NT;
+    constexpr int NT = 512, NW = NT / 64, KPT = kBlockRows / NT;
     constexpr bool kCounts = STEP < kDigits;
     __shared__ float raw[kBlockRows + 2 * kMostHalf];
     __shared__ int32_t bins[kCounts ? kBins : 1];
     __shared__ int32_t counts[KPT][NW];
     __shared__ unsigned long long sums[5];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ int32_t total;
+    const int lane = threadIdx.x & 63;
     LargeGroups blocks_of(a);
     const LineShare share = line_share<NT>(a.n_pairs, gridDim.x, blockIdx.x, [&](int p) { return blocks_of(p); });
     if (share.total > a.max_blocks) {     // runs of rows that overlap: so many blocks no cache has
@@ -355,7 +401,10 @@ __global__ __launch_bounds__(256, 3) void fairkv_select_large_kernel(SelectArgs 
             __syncthreads();
             for (int i = threadIdx.x; i < kBins; i += NT)
                 if (bins[i]) atomicAdd(&slot->bins[STEP][i], bins[i]);
-            if (STEP == 0 && protected_rows) atomicAdd(&slot->protected_rows, static_cast<unsigned long long>(protected_rows));
+            if constexpr (STEP == 0) {
+                const int64_t n = wave_upto(protected_rows);
+                if (lane == 63 && n) atomicAdd(&slot->protected_rows, static_cast<unsigned long long>(n));
+            }
             __syncthreads();
         }
         if constexpr (STEP == kDigits + 1) {      // who comes last leaves all of the group's as it was found
@@ -375,6 +424,7 @@ __global__ __launch_bounds__(256, 3) void fairkv_select_large_kernel(SelectArgs 
     };
     auto begin_group = [&]() __attribute__((always_inline)) {
         group = pair / a.per_group, group_at = at - block;
+#pragma unroll 8
         for (int p = group * a.per_group; p < pair; ++p) group_at -= blocks_of(p);
         slot = a.slots + group_at / a.min_blocks;
         if constexpr (STEP == 1) {
@@ -408,44 +458,44 @@ __global__ __launch_bounds__(256, 3) void fairkv_select_large_kernel(SelectArgs 
 
     for (int64_t left = share.left; left > 0; --left, ++block, ++at) {
         if (block >= blocks_of(pair)) pair = next_pair(pair, a.n_pairs, [&](int p) { return blocks_of(p); }), block = 0;
+        // ---- values, on their way while the group's state is found ----
+        const int32_t len = select_len(a, pair), t0 = static_cast<int32_t>(block) * kBlockRows;
+        const Candidates c(a, len);
+        uint32_t key[KPT];
+        float value[KPT], edge[1];        // edge: rows beside the block that its windows reach
+        uint32_t edge_state[1];
+        const int e = static_cast<int>(threadIdx.x);
+        if (len == 0) {                   // of a cache without rows, maybe: nothing is read
+#pragma unroll
+            for (int i = 0; i < KPT; ++i) key[i] = kNone, value[i] = -INFINITY;
+            edge[0] = -INFINITY;
+        } else if ((STEP == 0 || STEP > 2) || pair / a.per_group != group || !f.done) {
+            load_values<KPT>(a, pair, key, value, [&](int i, int32_t &t) {
+                t = min(t0 + i * NT + e, max(len - 1, 0));
+                return t0 + i * NT + e >= len ? kNone : c.has(t) ? 1u : kProtected;
+            });
+            if (a.half > 0)
+                load_values<1>(a, pair, edge_state, edge, [&](int, int32_t &t) {
+                    const int32_t at_edge = e < a.half ? t0 - a.half + e : t0 + kBlockRows + e - a.half;
+                    t = min(max(at_edge, 0), max(len - 1, 0));
+                    return e < 2 * a.half && c.has(at_edge) ? 1u : kNone;
+                });
+        }
         if (pair / a.per_group != group) {
             if (group >= 0) end_group();
             begin_group();
         }
         ++blocks_here;
         if ((STEP == 1 || STEP == 2) && f.done) continue;
-        // ---- values ----
-        const int32_t len = select_len(a, pair), t0 = static_cast<int32_t>(block) * kBlockRows;
-        const Candidates c(a, len);
-        uint32_t key[KPT];
-        float value[KPT];
-#pragma unroll
-        for (int i = 0; i < KPT; ++i) {
-            const int32_t t = t0 + i * NT + static_cast<int32_t>(threadIdx.x);
-            const int64_t row = t < len ? a.rows.row(pair, t) : -1;
-            key[i] = row < 0 ? kNone : c.has(t) ? 1 : kProtected;
-            value[i] = key[i] == 1 ? a.weights[row] : -INFINITY;
-        }
-        float edge = -INFINITY;           // rows beside the block that its windows reach
-        const int e = static_cast<int>(threadIdx.x);
-        if (e < 2 * a.half) {
-            const int32_t t = e < a.half ? t0 - a.half + e : t0 + kBlockRows + e - a.half;
-            const int64_t row = c.has(t) ? a.rows.row(pair, t) : -1;
-            if (row >= 0) edge = a.weights[row];
-        }
-#pragma unroll
-        for (int i = 0; i < KPT; ++i) value[i] = fmaxf(value[i], -INFINITY);      // a NaN is as low
         if (a.half > 0) {
             __syncthreads();              // the windows of the block before have been looked at
 #pragma unroll
-            for (int i = 0; i < KPT; ++i) raw[a.half + i * NT + threadIdx.x] = value[i];
-            if (e < 2 * a.half) raw[e < a.half ? e : kBlockRows + e] = fmaxf(edge, -INFINITY);
+            for (int i = 0; i < KPT; ++i) raw[a.half + i * NT + e] = value[i];
+            if (e < 2 * a.half) raw[e < a.half ? e : kBlockRows + e] = edge[0];
             __syncthreads();
+            for (int d = 0; d <= 2 * a.half; ++d) {
 #pragma unroll
-            for (int i = 0; i < KPT; ++i) {
-                const int32_t u0 = i * NT + static_cast<int32_t>(threadIdx.x);
-                if (key[i] == 1)
-                    for (int32_t u = u0; u <= u0 + 2 * a.half; ++u) value[i] = fmaxf(value[i], raw[u]);
+                for (int i = 0; i < KPT; ++i) value[i] = fmaxf(value[i], raw[i * NT + e + d]);
             }
         }
 #pragma unroll
@@ -469,8 +519,8 @@ __global__ __launch_bounds__(256, 3) void fairkv_select_large_kernel(SelectArgs 
             __syncthreads();
             if (threadIdx.x < 2) sums[threadIdx.x] = 0;
             __syncthreads();
-            atomicAdd(&sums[0], static_cast<unsigned long long>(__builtin_popcount(stays)));
-            atomicAdd(&sums[1], static_cast<unsigned long long>(__builtin_popcount(equal)));
+            add_rows<KPT>(reinterpret_cast<int32_t *>(&sums[0]), [&](int i) { return (stays >> i & 1) != 0; });      // low halves
+            add_rows<KPT>(reinterpret_cast<int32_t *>(&sums[1]), [&](int i) { return (equal >> i & 1) != 0; });
             __syncthreads();
             if (threadIdx.x == 0) a.blocks[at] = make_int2(static_cast<int>(sums[0]), static_cast<int>(sums[1]));
         }
@@ -488,8 +538,11 @@ __global__ __launch_bounds__(256, 3) void fairkv_select_large_kernel(SelectArgs 
                 if (x >= pair_at && x < at) s[2] += n.x;
                 if (x >= pair_at) s[3] += n.y, s[4] += n.x;
             }
-            for (int i = 0; i < 5; ++i)
-                if (s[i]) atomicAdd(&sums[i], s[i]);
+#pragma unroll
+            for (int i = 0; i < 5; ++i) {
+                const int64_t n = wave_upto(static_cast<int64_t>(s[i]));
+                if (lane == 63 && n) atomicAdd(&sums[i], static_cast<unsigned long long>(n));
+            }
             __syncthreads();
             const int64_t ties_pair = sums[0], ties_block = sums[1];
             const int64_t from = static_cast<int64_t>(sums[2]) + min(f.need, ties_block) - min(f.need, ties_pair);
@@ -499,7 +552,7 @@ __global__ __launch_bounds__(256, 3) void fairkv_select_large_kernel(SelectArgs 
                 if (n > a.max_keep && a.bad) atomicAdd(a.bad, 1);
             }
             if (f.need > 0) {
-                count_rows<NT, KPT>(counts, equal);
+                count_rows<NT, KPT>(counts, equal, &total);
 #pragma unroll
                 for (int i = 0; i < KPT; ++i) {
                     const int32_t n = rows_before<NT, KPT>(counts, equal, i);
@@ -507,7 +560,7 @@ __global__ __launch_bounds__(256, 3) void fairkv_select_large_kernel(SelectArgs 
                 }
                 __syncthreads();
             }
-            count_rows<NT, KPT>(counts, stays);
+            count_rows<NT, KPT>(counts, stays, &total);
 #pragma unroll
             for (int i = 0; i < KPT; ++i) {
                 const int64_t n = from + rows_before<NT, KPT>(counts, stays, i);
@@ -516,7 +569,7 @@ __global__ __launch_bounds__(256, 3) void fairkv_select_large_kernel(SelectArgs 
         }
     }
     if (group >= 0) end_group();
-    (void)lane, (void)wave;
+    (void)lane;
 }
 
 }  // namespace fairkv
