@@ -16,7 +16,8 @@ namespace {
 using namespace fairkv;
 
 constexpr int32_t kMaxSlots = 65536;
-constexpr int32_t kSmallCap = 128, kLargeCap = 256;      // units of a group in a workgroup's registers
+// Units of a group whose keys lie in a workgroup's LDS: four such workgroups of 512 threads share a CU's 160 KB, and two of 1024.
+constexpr int32_t kSmallCap = 120, kLargeCap = 256;
 
 // Tokens that a length can count: 2^31 - 2^16, so that what is added to a token's number does not wrap around.
 int32_t max_len(const fairkv_cache *c)
@@ -75,25 +76,26 @@ namespace {
 struct SelectShape {
     int32_t cap, min_blocks;      // units of 64 rows of a group that one workgroup has; blocks that a larger one has at least
     int64_t max_blocks;           // of all larger groups, 0: there can be none
-    int64_t slots;
+    int64_t slots, shares;        // of the large groups' kernels: groups, workgroups
 };
 SelectShape select_shape(const fairkv_cache *c, int32_t shared, int32_t n_slots)
 {
-    const int64_t pairs = static_cast<int64_t>(c->B) * c->Hkv, per_group = shared ? c->Hkv : 1, groups = pairs / per_group;
+    const int64_t pairs = static_cast<int64_t>(c->B) * c->Hkv, per_group = shared ? c->Hkv : 1;
     const int64_t each = max_len(c), most = std::min(std::max<int64_t>(c->n_rows, 0), each * pairs), group_most = std::min(most, each * per_group);
     SelectShape s{};
     auto fits = [&](int32_t cap) { return per_group <= kMaxPairs && (group_most + 63 * per_group) / 64 <= cap; };      // pairs' last units are not full
-    s.cap = fits(kSmallCap) || (!fits(kLargeCap) && groups > n_slots) ? kSmallCap : kLargeCap;
+    s.cap = fits(kSmallCap) || !fits(kLargeCap) ? kSmallCap : kLargeCap;
     if (fits(s.cap)) return s;
     // A block of a pair has at most 64 units, so a large group has more than cap / 64 blocks; its rows are more than 64 cap - 63 per_group.
-    s.min_blocks = per_group > kMaxPairs ? kMaxPairs : s.cap / (kBlockRows / 64);
+    s.min_blocks = per_group > kMaxPairs ? kMaxPairs : s.cap / (kBlockRows / 64) + 1;
     const int64_t least_rows = std::max<int64_t>(1, 64 * static_cast<int64_t>(s.cap) - 63 * per_group);
     const int64_t large_pairs = per_group > kMaxPairs ? pairs : std::min(pairs, most / least_rows * per_group);      // each has a block that is not full
     s.max_blocks = most / kBlockRows + large_pairs;
     s.slots = s.max_blocks / s.min_blocks + 1;
+    s.shares = std::min<int64_t>(s.max_blocks, 4 * static_cast<int64_t>(n_slots));
     return s;
 }
-size_t select_bytes(const SelectShape &s) { return 256 + sizeof(SelectSlot) * s.slots + sizeof(int2) * s.max_blocks; }
+size_t select_bytes(const SelectShape &s) { return 256 + sizeof(SelectSlot) * s.slots + sizeof(SelectShare) * s.shares + sizeof(int2) * s.max_blocks; }
 
 template <int NT, int UNITS>
 void launch_select(const SelectArgs &a, unsigned groups, hipStream_t st)
@@ -122,32 +124,36 @@ extern "C" int fairkv_select(const fairkv_cache *c, const fairkv_selection *s, c
     if (s->pool > 2 * kMostHalf + 1 || n_slots > kMaxSlots) return FAIRKV_EUNSUPPORTED;
     if (!aligned(weights, 4) || !aligned(workspace, 16)) return FAIRKV_EINVAL;
     const int64_t pairs = static_cast<int64_t>(c->B) * c->Hkv, groups = s->shared ? c->B : pairs;
-    if (groups > UINT32_MAX / 1024) return FAIRKV_EINVAL;
+    if (groups > UINT32_MAX / 1024 - 4 * kMaxSlots) return FAIRKV_EINVAL;
     const SelectShape shape = select_shape(c, s->shared, n_slots);
     if (!workspace || workspace_bytes < select_bytes(shape)) return FAIRKV_EWORKSPACE;
     SelectArgs a{};
     a.rows = row_map(c);
     a.weights = weights, a.len = len, a.budget = s->budget, a.keep = keep, a.n_keep = n_keep, a.bad = bad;
-    a.n_pairs = static_cast<int32_t>(pairs), a.max_len = max_len(c), a.max_keep = max_keep;
+    a.n_pairs = static_cast<int32_t>(pairs), a.n_groups = static_cast<int32_t>(groups), a.max_len = max_len(c), a.max_keep = max_keep;
     a.half = s->pool / 2, a.sink = s->sink, a.recent = s->recent, a.per_group = s->shared ? c->Hkv : 1;
     a.cap = shape.cap, a.min_blocks = shape.min_blocks, a.max_blocks = shape.max_blocks;
-    if (shape.max_blocks > 0) {
-        a.slots = static_cast<SelectSlot *>(workspace);
-        a.blocks = reinterpret_cast<int2 *>(static_cast<char *>(workspace) + sizeof(SelectSlot) * shape.slots);
-    }
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (shape.cap == kSmallCap)
-        launch_select<512, kSmallCap>(a, static_cast<unsigned>(groups), st);
-    else
-        launch_select<1024, kLargeCap>(a, static_cast<unsigned>(groups), st);
-    if (shape.max_blocks > 0) {
-        const dim3 grid(static_cast<unsigned>(std::min<int64_t>(shape.max_blocks, 4 * static_cast<int64_t>(n_slots))));
-        hipLaunchKernelGGL(fairkv_select_large_kernel<0>, grid, dim3(512), 0, st, a);
-        hipLaunchKernelGGL(fairkv_select_large_kernel<1>, grid, dim3(512), 0, st, a);
-        hipLaunchKernelGGL(fairkv_select_large_kernel<2>, grid, dim3(512), 0, st, a);
-        hipLaunchKernelGGL(fairkv_select_large_kernel<3>, grid, dim3(512), 0, st, a);
-        hipLaunchKernelGGL(fairkv_select_large_kernel<4>, grid, dim3(512), 0, st, a);
+    if (shape.max_blocks == 0) {
+        if (shape.cap == kLargeCap || groups <= n_slots)      // few: the wider workgroup is the faster one (8 pairs of 1024 rows in one group 12.5 us with 512 threads)
+            shape.cap == kLargeCap ? launch_select<1024, kLargeCap>(a, static_cast<unsigned>(groups), st) : launch_select<1024, kSmallCap>(a, static_cast<unsigned>(groups), st);
+        else
+            launch_select<512, kSmallCap>(a, static_cast<unsigned>(groups), st);
+        return launched();
     }
+    char *ws = static_cast<char *>(workspace);
+    a.slots = reinterpret_cast<SelectSlot *>(ws);
+    a.shares = reinterpret_cast<SelectShare *>(ws + sizeof(SelectSlot) * shape.slots);
+    a.blocks = reinterpret_cast<int2 *>(ws + sizeof(SelectSlot) * shape.slots + sizeof(SelectShare) * shape.shares);
+    const dim3 grid(static_cast<unsigned>(shape.shares)), first(static_cast<unsigned>(groups + shape.shares)), threads(kLargeThreads);
+    if (a.half > 0)
+        hipLaunchKernelGGL((fairkv_select_first_kernel<kSmallCap, true>), first, threads, 0, st, a);
+    else
+        hipLaunchKernelGGL((fairkv_select_first_kernel<kSmallCap, false>), first, threads, 0, st, a);
+    hipLaunchKernelGGL(fairkv_select_large_kernel<1>, grid, threads, 0, st, a);
+    hipLaunchKernelGGL(fairkv_select_large_kernel<2>, grid, threads, 0, st, a);
+    hipLaunchKernelGGL(fairkv_select_large_kernel<3>, grid, threads, 0, st, a);
+    hipLaunchKernelGGL(fairkv_select_large_kernel<4>, grid, threads, 0, st, a);
     return launched();
 }
 

@@ -37,6 +37,10 @@ struct SelectSlot {
     SelectFound found[kDigits];           // 0 between calls
     int64_t listed;                       // blocks whose list is written; 0 between calls
 };
+struct SelectShare {                      // of a workgroup: its blocks in the line, and of the group that the first of them is in its first block and their number
+    int64_t left, block, at, group_at, group_blocks;      // left: how many; block: the first one's number in its pair
+    int64_t pair;
+};
 struct SelectArgs {
     RowMap rows;
     const float *weights;                 // [n_rows]
@@ -44,6 +48,7 @@ struct SelectArgs {
     int32_t *keep, *n_keep, *bad;         // [B * Hkv][max_keep], [B * Hkv], [1] or null
     SelectSlot *slots;                    // null: no group can be large
     int2 *blocks;                         // [max_blocks]: rows of a block that stay whatever ties do, and ties; 0 between calls
+    SelectShare *shares;                  // of the large groups' workgroups; 0 between calls
     int64_t max_blocks;
     int32_t n_pairs, n_groups, max_len, max_keep, half, sink, recent, per_group, cap, min_blocks;      // per_group: pairs of a group
 };
@@ -183,16 +188,24 @@ __device__ __forceinline__ int32_t rows_before(const int32_t (&counts)[KPT][NT /
 // ---- a group that one workgroup has ----
 // Its rows in units of 64, a pair's last one not full, so that all lanes of a wave are in one pair; wave w has units w, w + NW, ...  What a pair's
 // rows need to know is held in lanes: lane p has pair p.  Keys lie in LDS.
+template <int UNITS, bool POOL>
+struct GroupSpace {
+    uint32_t keys[UNITS * 64];                        // first: kNone, 1 for a candidate, kProtected
+    float raw[POOL ? UNITS * 64 : 1];
+    int32_t bins[kBins];
+    int32_t counts[UNITS];
+    int32_t total, protected_rows, candidate_rows;
+};
 template <int NT, int UNITS, bool POOL>
-__global__ __launch_bounds__(NT) void fairkv_select_kernel(SelectArgs a)
+__device__ __forceinline__ void select_group(const SelectArgs &a, int group, GroupSpace<UNITS, POOL> &m)
 {
-    constexpr int NW = NT / 64, kBatch = 4, PER = UNITS / 64;
-    __shared__ uint32_t keys[UNITS * 64];             // first: kNone, 1 for a candidate, kProtected
-    __shared__ float raw[POOL ? UNITS * 64 : 1];
-    __shared__ int32_t bins[kBins];
-    __shared__ int32_t counts[UNITS];
-    __shared__ int32_t total, protected_rows, candidate_rows;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = blockIdx.x, p0 = group * a.per_group;
+    constexpr int NW = NT / 64, kBatch = 4, PER = (UNITS + 63) / 64;
+    auto &keys = m.keys;
+    auto &raw = m.raw;
+    auto &bins = m.bins;
+    auto &counts = m.counts;
+    int32_t &total = m.total, &protected_rows = m.protected_rows, &candidate_rows = m.candidate_rows;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), p0 = group * a.per_group;
     const int n_pairs = a.per_group;
     const uint64_t below = (1ull << lane) - 1;
     // ---- where the pairs begin, in units ----
@@ -344,6 +357,13 @@ __global__ __launch_bounds__(NT) void fairkv_select_kernel(SelectArgs a)
     }
 }
 
+template <int NT, int UNITS, bool POOL>
+__global__ __launch_bounds__(NT) void fairkv_select_kernel(SelectArgs a)
+{
+    __shared__ GroupSpace<UNITS, POOL> m;
+    select_group<NT>(a, blockIdx.x, m);
+}
+
 // ---- large groups: the line of their blocks ----
 struct LargeGroups {
     const SelectArgs &a;
@@ -365,33 +385,65 @@ struct LargeGroups {
         }
         return large ? max(1, (select_len(a, pair) + kBlockRows - 1) / kBlockRows) : 0;      // one of an empty pair too: its list is one
     }
+    // Where the group of a share's pair begins, and how many blocks it has.
+    __device__ __forceinline__ void group_of(SelectShare &s)
+    {
+        const int first = static_cast<int>(s.pair) / a.per_group * a.per_group;
+        s.group_at = s.at - s.block, s.group_blocks = 0;
+#pragma unroll 8
+        for (int p = first; p < first + a.per_group; ++p) {
+            const int32_t n = max(1, (select_len(a, p) + kBlockRows - 1) / kBlockRows);
+            s.group_blocks += n;
+            if (p < s.pair) s.group_at -= n;
+        }
+    }
 };
 
-// STEP 0 .. 2: a digit is counted; 3: what stays of every block; 4: the lists.
+struct LargeSpace {
+    float raw[kBlockRows + 2 * kMostHalf];
+    int32_t bins[kBins];
+    int32_t counts[kBlockRows / 64];
+    unsigned long long sums[5];
+    int32_t total;
+};
+constexpr int kLargeThreads = 512;
+
+// Workgroup `slot_index` of n: STEP 0 .. 2: a digit is counted; 3: what stays of every block; 4: the lists.  The first step finds the workgroup's share of
+// the line, the others have it from there.
 template <int STEP>
-__global__ __launch_bounds__(512) void fairkv_select_large_kernel(SelectArgs a)
+__device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index, int n_slots, LargeSpace &m)
 {
-    constexpr int NT = 512, NW = NT / 64, KPT = kBlockRows / NT;
+    constexpr int NT = kLargeThreads, KPT = kBlockRows / NT;
     constexpr bool kCounts = STEP < kDigits;
-    __shared__ float raw[kBlockRows + 2 * kMostHalf];
-    __shared__ int32_t bins[kCounts ? kBins : 1];
-    __shared__ int32_t counts[KPT][NW];
-    __shared__ unsigned long long sums[5];
-    __shared__ int32_t total;
+    auto &raw = m.raw;
+    auto &bins = m.bins;
+    auto &counts = reinterpret_cast<int32_t (&)[KPT][NT / 64]>(m.counts);
+    auto &sums = m.sums;
+    int32_t &total = m.total;
     const int lane = threadIdx.x & 63;
     LargeGroups blocks_of(a);
-    const LineShare share = line_share<NT>(a.n_pairs, gridDim.x, blockIdx.x, [&](int p) { return blocks_of(p); });
-    if (share.total > a.max_blocks) {     // runs of rows that overlap: so many blocks no cache has
-        if (STEP == kDigits + 1 && blockIdx.x == 0)
-            for (int p = threadIdx.x; p < a.n_pairs; p += NT)
-                if (blocks_of(p) > 0) {
-                    a.n_keep[p] = -1;
-                    if (a.bad) atomicAdd(a.bad, 1);
-                }
-        return;
+    SelectShare share;
+    if constexpr (STEP == 0) {
+        const LineShare l = line_share<NT>(a.n_pairs, n_slots, slot_index, [&](int p) { return blocks_of(p); });
+        share = {l.total > a.max_blocks ? -1 : l.left, l.begin, l.at, 0, 0, l.pair};      // runs of rows that overlap: so many blocks no cache has
+        if (share.left > 0) blocks_of.group_of(share);
+        if (threadIdx.x == 0) a.shares[slot_index] = share;
+    } else {
+        share = a.shares[slot_index];
+        if (STEP == kDigits + 1) {
+            __syncthreads();
+            if (threadIdx.x == 0) a.shares[slot_index] = SelectShare{0, 0, 0, 0, 0, 0};
+        }
     }
-    int pair = share.pair, group = -1;
-    int64_t block = share.begin, at = share.at, group_at = 0;      // group_at: the place of the group's first block
+    if (share.left < 0 && STEP == kDigits + 1 && slot_index == 0)
+        for (int p = threadIdx.x; p < a.n_pairs; p += NT)
+            if (blocks_of(p) > 0) {
+                a.n_keep[p] = -1;
+                if (a.bad) atomicAdd(a.bad, 1);
+            }
+    if (share.left <= 0) return;
+    int pair = static_cast<int>(share.pair), group = -1;
+    int64_t block = share.block, at = share.at, group_at = share.group_at;      // group_at: the place of the group's first block
     SelectSlot *slot = nullptr;
     SelectFound f{0, 0, 0};
     int32_t protected_rows = 0, blocks_here = 0;
@@ -408,8 +460,7 @@ __global__ __launch_bounds__(512) void fairkv_select_large_kernel(SelectArgs a)
             __syncthreads();
         }
         if constexpr (STEP == kDigits + 1) {      // who comes last leaves all of the group's as it was found
-            int64_t n = 0;
-            for (int p = group * a.per_group; p < (group + 1) * a.per_group; ++p) n += blocks_of(p);
+            const int64_t n = share.group_blocks;
             __syncthreads();
             if (threadIdx.x == 0) sums[0] = atomicAdd(reinterpret_cast<unsigned long long *>(&slot->listed), static_cast<unsigned long long>(blocks_here)) + blocks_here;
             __syncthreads();
@@ -423,9 +474,12 @@ __global__ __launch_bounds__(512) void fairkv_select_large_kernel(SelectArgs a)
         }
     };
     auto begin_group = [&]() __attribute__((always_inline)) {
-        group = pair / a.per_group, group_at = at - block;
-#pragma unroll 8
-        for (int p = group * a.per_group; p < pair; ++p) group_at -= blocks_of(p);
+        if (group >= 0) {
+            share.at = at, share.block = block, share.pair = pair;
+            blocks_of.group_of(share);
+            group_at = share.group_at;
+        }
+        group = pair / a.per_group;
         slot = a.slots + group_at / a.min_blocks;
         if constexpr (STEP == 1) {
             f = {max(static_cast<int64_t>(a.budget[group]) - static_cast<int64_t>(slot->protected_rows), static_cast<int64_t>(0)), 0, 0};
@@ -456,10 +510,15 @@ __global__ __launch_bounds__(512) void fairkv_select_large_kernel(SelectArgs a)
         }
     };
 
+    auto blocks_of_large = [&](int32_t len) __attribute__((always_inline)) { return max(1, (len + kBlockRows - 1) / kBlockRows); };
+    int32_t len = select_len(a, pair);
     for (int64_t left = share.left; left > 0; --left, ++block, ++at) {
-        if (block >= blocks_of(pair)) pair = next_pair(pair, a.n_pairs, [&](int p) { return blocks_of(p); }), block = 0;
+        if (block >= blocks_of_large(len)) {
+            pair = next_pair(pair, a.n_pairs, [&](int p) { return blocks_of(p); }), block = 0;
+            len = select_len(a, pair);
+        }
         // ---- values, on their way while the group's state is found ----
-        const int32_t len = select_len(a, pair), t0 = static_cast<int32_t>(block) * kBlockRows;
+        const int32_t t0 = static_cast<int32_t>(block) * kBlockRows;
         const Candidates c(a, len);
         uint32_t key[KPT];
         float value[KPT], edge[1];        // edge: rows beside the block that its windows reach
@@ -526,7 +585,7 @@ __global__ __launch_bounds__(512) void fairkv_select_large_kernel(SelectArgs a)
         }
         if constexpr (STEP == kDigits + 1) {
             // ties in front of the pair, and of the block; rows in front of the block that stay anyhow; both of the whole pair
-            const int64_t pair_at = at - block, pair_end = pair_at + blocks_of(pair);
+            const int64_t pair_at = at - block, pair_end = pair_at + blocks_of_large(len);
             __syncthreads();
             if (threadIdx.x < 5) sums[threadIdx.x] = 0;
             __syncthreads();
@@ -568,8 +627,29 @@ __global__ __launch_bounds__(512) void fairkv_select_large_kernel(SelectArgs a)
             }
         }
     }
-    if (group >= 0) end_group();
+    end_group();
     (void)lane;
+}
+
+// The first step of the large groups, and beside it the groups that one workgroup has.
+template <int UNITS, bool POOL>
+__global__ __launch_bounds__(kLargeThreads) void fairkv_select_first_kernel(SelectArgs a)
+{
+    __shared__ union Space {
+        GroupSpace<UNITS, POOL> group;
+        LargeSpace large;
+        __device__ Space() {}
+    } m;
+    if (static_cast<int>(blockIdx.x) < a.n_groups)
+        select_group<kLargeThreads>(a, blockIdx.x, m.group);
+    else
+        select_large<0>(a, blockIdx.x - a.n_groups, gridDim.x - a.n_groups, m.large);
+}
+template <int STEP>
+__global__ __launch_bounds__(kLargeThreads) void fairkv_select_large_kernel(SelectArgs a)
+{
+    __shared__ LargeSpace m;
+    select_large<STEP>(a, blockIdx.x, gridDim.x, m);
 }
 
 }  // namespace fairkv
