@@ -15,7 +15,7 @@ namespace {
 
 using namespace fairkv;
 
-constexpr int32_t kMaxSlots = 65536;
+constexpr int32_t kMaxSlots = 65536;      // most compute units that a caller may name
 // Units of a group whose keys lie in a workgroup's LDS: four such workgroups of 512 threads share a CU's 160 KB, and two of 1024.
 constexpr int32_t kSmallCap = 120, kLargeCap = 256;
 
@@ -32,10 +32,19 @@ bool meet(const void *x, size_t nx, const void *y, size_t ny)
     return a < static_cast<unsigned __int128>(b) + ny && b < static_cast<unsigned __int128>(a) + nx;
 }
 
-template <int D, bool KV8>
-void launch_weights(const WeightsArgs &a, unsigned grid, hipStream_t st)
+template <int D, bool KV8, int T, int NW, int CC, int MIN>
+void launch_weights_kernel(const WeightsArgs &a, int64_t grid, hipStream_t st)
 {
-    hipLaunchKernelGGL((fairkv_attn_weights_kernel<D, KV8, 1>), dim3(grid), dim3(kWeightWaves * 64), 0, st, a);
+    hipLaunchKernelGGL((fairkv_attn_weights_kernel<D, KV8, T, NW, CC, MIN>), dim3(static_cast<unsigned>(grid)), dim3(NW * 64), 0, st, a);
+}
+template <int D, bool KV8>
+void launch_weights(const WeightsArgs &a, int32_t n_slots, hipStream_t st)
+{
+    const int cols = a.G * a.q_len;
+    if (cols <= 64)
+        launch_weights_kernel<D, KV8, 1, 4, 64, 4>(a, 4 * static_cast<int64_t>(n_slots), st);
+    else
+        launch_weights_kernel<D, KV8, 2, 12, D == 128 ? 512 : 1024, 3>(a, n_slots, st);
 }
 
 }  // namespace
@@ -62,11 +71,10 @@ extern "C" int fairkv_attn_weights(const fairkv_cache *c, const void *q, const u
     a.scale_log2 = scale * kLog2e, a.decay = decay;
     for (int h = 0; h < kCacheScales; ++h) a.k_scale[h] = h < c->n_scales ? c->k_scale[h] : 1.f;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const unsigned grid = static_cast<unsigned>(n_slots) * 3;
     if (c->dtype == FAIRKV_E4M3)
-        c->D == 128 ? launch_weights<128, true>(a, grid, st) : launch_weights<64, true>(a, grid, st);
+        c->D == 128 ? launch_weights<128, true>(a, n_slots, st) : launch_weights<64, true>(a, n_slots, st);
     else
-        c->D == 128 ? launch_weights<128, false>(a, grid, st) : launch_weights<64, false>(a, grid, st);
+        c->D == 128 ? launch_weights<128, false>(a, n_slots, st) : launch_weights<64, false>(a, n_slots, st);
     return launched();
 }
 

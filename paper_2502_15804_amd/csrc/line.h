@@ -7,13 +7,18 @@
 
 namespace fairkv {
 
-// x plus those of the lanes below, by steps of the wave's own data paths.
-__device__ __forceinline__ int64_t wave_upto(int64_t x)
+// x plus those of the lanes below, by steps of the wave's own data paths; 32 or 64 bits.
+template <class T>
+__device__ __forceinline__ T wave_upto(T x)
 {
     auto step = [&](auto ctrl, auto rows, auto banks) __attribute__((always_inline)) {
         const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(x), ctrl(), rows(), banks(), false);
-        const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(x >> 32), ctrl(), rows(), banks(), false);
-        x += static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
+        if constexpr (sizeof(T) == 8) {
+            const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(x >> 32), ctrl(), rows(), banks(), false);
+            x += static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
+        } else {
+            x += static_cast<T>(lo);
+        }
     };
 #define FAIRKV_N(n) std::integral_constant<int, n>{}
     step(FAIRKV_N(0x111), FAIRKV_N(0xf), FAIRKV_N(0xf));      // from 1, 2, 4, 8 lanes below in the row of 16
