@@ -5,7 +5,7 @@
 //     w[t] = decay w_old[t] [t < len - n] + sum over columns c = (node i < n, head g of the group) that see t of exp(s_ct - lse_c),
 // the sums in fp32.  No maximum runs along: lse is at least every score that it is of.
 //
-// Tiles.  A wave has T x 32 tokens, whose rows of K it holds in registers as an operand of 32x32x16 matrix instructions, and goes through the
+// Tiles.  A wave has 32 tokens, whose rows of K it holds in registers as an operand of 32x32x16 matrix instructions, and goes through the
 // columns 32 at a time:
 //     S[column][token] = q K^T         D / 16 instructions a tile of 32
 // A lane has one token (lane % 32) and 16 of the 32 columns, so a weight is added where it was computed; two lanes share a token.  Queries lie
@@ -33,11 +33,11 @@ struct WeightsArgs {
     float k_scale[kCacheScales];
 };
 
-// NW waves, CC columns in LDS.
-template <int D, bool KV8, int T, int NW, int CC, int MIN>
-__global__ __launch_bounds__(NW * 64, MIN) void fairkv_attn_weights_kernel(WeightsArgs a)
+// NW waves, CC columns in LDS, four waves of a SIMD.
+template <int D, bool KV8, int NW, int CC>
+__global__ __launch_bounds__(NW * 64, 4) void fairkv_attn_weights_kernel(WeightsArgs a)
 {
-    constexpr int NT = NW * 64, TOK = T * 32;
+    constexpr int NT = NW * 64, TOK = 32;
     constexpr int ROWB = KV8 ? D : 2 * D, QROWB = 2 * D;      // bytes of a row of K, of a query
     constexpr int NP = ROWB / 32, NSL = D / 16, PPQ = QROWB / 16;
     typedef __attribute__((ext_vector_type(4))) uint32_t u4;
@@ -78,22 +78,15 @@ __global__ __launch_bounds__(NW * 64, MIN) void fairkv_attn_weights_kernel(Weigh
             const int tile = tile0 + turn * NW + wave;
             const bool mine = turn * NW + wave < n_tiles;
             const int32_t t0 = tile * TOK;
-            // ---- rows of K, requested before the queries ----
-            int64_t row[T];
-            u4 raw[T][NP];
-            float old[T], sum[T][4];
+            // ---- rows of K, requested before the queries; where there is none the cache's first row stands in: what comes of it is not stored ----
+            const int32_t t = t0 + l32;
+            const int64_t row = mine && t < len ? a.rows.row(pair, t) : -1;
+            const char *from = a.k + max(row, static_cast<int64_t>(0)) * ROWB + hi * 16;
+            u4 raw[NP];
 #pragma unroll
-            for (int i = 0; i < T; ++i) {
-                const int32_t t = t0 + i * 32 + l32;
-                row[i] = mine && t < len ? a.rows.row(pair, t) : -1;
-                // where there is none the cache's first row stands in: what comes of it is not stored
-                const char *from = a.k + max(row[i], static_cast<int64_t>(0)) * ROWB + hi * 16;
-#pragma unroll
-                for (int p = 0; p < NP; ++p) raw[i][p] = *reinterpret_cast<const u4 *>(from + p * 32);
-                old[i] = a.decay != 0.f && row[i] >= 0 && t < base ? a.weights[row[i]] * a.decay : 0.f;
-#pragma unroll
-                for (int x = 0; x < 4; ++x) sum[i][x] = 0.f;
-            }
+            for (int p = 0; p < NP; ++p) raw[p] = *reinterpret_cast<const u4 *>(from + p * 32);
+            const float old = a.decay != 0.f && row >= 0 && t < base ? a.weights[row] * a.decay : 0.f;
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
             for (int chunk = 0; chunk == 0 || chunk * CC < cols; ++chunk) {
                 const int n = min(CC, cols - chunk * CC);
                 if (turn == 0 || cols > CC) {
@@ -112,64 +105,58 @@ __global__ __launch_bounds__(NW * 64, MIN) void fairkv_attn_weights_kernel(Weigh
                     __syncthreads();
                 }
                 if (!mine) continue;
-                bf16x8_t k[T][NSL];
+                bf16x8_t k[NSL];
 #pragma unroll
-                for (int i = 0; i < T; ++i)
-#pragma unroll
-                    for (int p = 0; p < NP; ++p) {
-                        if constexpr (KV8) {
-                            k[i][2 * p] = widen8(i32x2_t{static_cast<int>(raw[i][p][0]), static_cast<int>(raw[i][p][1])});
-                            k[i][2 * p + 1] = widen8(i32x2_t{static_cast<int>(raw[i][p][2]), static_cast<int>(raw[i][p][3])});
-                        } else {
-                            k[i][p] = __builtin_bit_cast(bf16x8_t, raw[i][p]);
-                        }
+                for (int p = 0; p < NP; ++p) {
+                    if constexpr (KV8) {
+                        k[2 * p] = widen8(i32x2_t{static_cast<int>(raw[p][0]), static_cast<int>(raw[p][1])});
+                        k[2 * p + 1] = widen8(i32x2_t{static_cast<int>(raw[p][2]), static_cast<int>(raw[p][3])});
+                    } else {
+                        k[p] = __builtin_bit_cast(bf16x8_t, raw[p]);
                     }
-                // 32 columns from c0; masked: some of them are past the last one, or do not see all of the tile's tokens
-                auto columns = [&](int c0, auto masked) __attribute__((always_inline)) {
-                    constexpr bool kMasked = decltype(masked)::value;
-                    const int c = kMasked ? min(c0 + l32, n - 1) : c0 + l32;      // past the last one: that one again, and it does not count
+                }
+                // 32 columns from c0.  some: not all of them are there; draft: some of the tile's tokens are the queries' own, and not seen by all
+                auto columns = [&](int c0, auto some, auto draft) __attribute__((always_inline)) {
+                    constexpr bool kSome = decltype(some)::value, kDraft = decltype(draft)::value;
+                    const int c = kSome ? min(c0 + l32, n - 1) : c0 + l32;      // past the last one: that one again, and it does not count
                     bf16x8_t q[NSL];
 #pragma unroll
                     for (int s = 0; s < NSL; ++s) {
                         const int p = KV8 ? (s & ~1) * 2 + 2 * hi + (s & 1) : 2 * s + hi;      // the order in which the lanes hold K
-                        q[s] = *reinterpret_cast<const bf16x8_t *>(qs + c * QROWB + ((p ^ swizzle(kMasked ? c : l32)) * 16));
+                        q[s] = *reinterpret_cast<const bf16x8_t *>(qs + c * QROWB + ((p ^ swizzle(kSome ? c : l32)) * 16));
                     }
-                    f32x16_t z[T];
+                    f32x16_t z;
 #pragma unroll
-                    for (int i = 0; i < T; ++i) {
+                    for (int r = 0; r < 16; ++r) z[r] = 0.f;
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) z[i][r] = 0.f;
-#pragma unroll
-                        for (int s = 0; s < NSL; ++s) z[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q[s], k[i][s], z[i], 0, 0, 0);
-                    }
+                    for (int s = 0; s < NSL; ++s) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q[s], k[s], z, 0, 0, 0);
+                    const int32_t j = t0 + l32 - base;                          // of the queries' own tokens, below 0 in front of them
+                    const uint32_t *words = reinterpret_cast<const uint32_t *>(sees) + (j >= 32 ? 1 : 0);
 #pragma unroll
                     for (int r4 = 0; r4 < 4; ++r4) {
+                        if (kSome && c0 + 8 * r4 >= n) break;
                         const float4 ml4 = *reinterpret_cast<const float4 *>(minus_lse + c0 + 8 * r4 + 4 * hi);
                         const float ml[4] = {ml4.x, ml4.y, ml4.z, ml4.w};
 #pragma unroll
                         for (int x = 0; x < 4; ++x) {
                             const int cr = c0 + 8 * r4 + 4 * hi + x;
-#pragma unroll
-                            for (int i = 0; i < T; ++i) {
-                                float e = __builtin_amdgcn_exp2f(fmaf(z[i][4 * r4 + x], s_mul, ml[x]));
-                                if constexpr (kMasked) {
-                                    const int32_t j = t0 + i * 32 + l32 - base;
-                                    if (cr >= n || (j >= 0 && !(sees[min(cr, n - 1)] >> min(j, 63) & 1))) e = 0.f;
-                                }
-                                sum[i][x] += e;
-                            }
+                            float e = __builtin_amdgcn_exp2f(fmaf(z[4 * r4 + x], s_mul, ml[x]));
+                            bool counts = true;
+                            if constexpr (kSome) counts = cr < n;
+                            if constexpr (kDraft) counts = counts && (j < 0 || (words[2 * min(cr, n - 1)] >> (j & 31) & 1) != 0);
+                            sum[x] += counts ? e : 0.f;
                         }
                     }
                 };
-                const int whole = t0 + TOK > base ? 0 : n / 32 * 32;
-                for (int c0 = 0; c0 < whole; c0 += 32) columns(c0, std::false_type{});
-                for (int c0 = whole; c0 < n; c0 += 32) columns(c0, std::true_type{});
+                if (t0 + TOK > base) {
+                    for (int c0 = 0; c0 < n; c0 += 32) columns(c0, std::true_type{}, std::true_type{});
+                } else {
+                    for (int c0 = 0; c0 + 32 <= n; c0 += 32) columns(c0, std::false_type{}, std::false_type{});
+                    if (n % 32 != 0) columns(n / 32 * 32, std::true_type{}, std::false_type{});
+                }
             }
-#pragma unroll
-            for (int i = 0; i < T; ++i) {
-                const float w = (sum[i][0] + sum[i][1]) + (sum[i][2] + sum[i][3]), both = w + __shfl_xor(w, 32);
-                if (hi == 0 && row[i] >= 0) a.out[row[i]] = old[i] + both;
-            }
+            const float w = (sum[0] + sum[1]) + (sum[2] + sum[3]), both = w + __shfl_xor(w, 32);
+            if (hi == 0 && row >= 0) a.out[row] = old + both;
         }
         left -= n_tiles, first += n_tiles;
     }
