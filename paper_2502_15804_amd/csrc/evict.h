@@ -19,7 +19,7 @@ struct EvictArgs {
     const int32_t *cap_to;                // of another cache, null in place
     const int32_t *keep, *n_keep, *len;   // [pairs][max_keep], [pairs], [pairs]
     int32_t *len_out, *bad;               // len_out null: not written by this kernel
-    int32_t n_pairs, max_keep;
+    int32_t n_pairs, max_keep, movers;    // movers: workgroups that move, of a launch into another cache
 };
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_row_t;
@@ -37,95 +37,160 @@ __device__ __forceinline__ bool list_ok(const EvictArgs &a, int pair, int32_t le
     return len >= 0 && n >= 0 && n <= a.max_keep && (!a.cap_to || n <= a.cap_to[pair]) && (a.cap_to || n <= len);
 }
 
-// Lengths of all pairs, by whole lists: a pair whose list is not right keeps its length (into another cache: has none there) and is counted.
+// Whether a pair's whole list is right, and its first entry that moves.  Called by all NT threads.
+struct ListFound {
+    int32_t ok, first;
+};
 template <int NT>
-__device__ __forceinline__ bool whole_list_ok(const EvictArgs &a, int pair, int32_t len, int32_t n, int32_t *flag /* LDS */)
+__device__ __forceinline__ ListFound whole_list(const EvictArgs &a, int pair, int32_t len, int32_t n, ListFound *found /* LDS */)
 {
-    if (threadIdx.x == 0) *flag = list_ok(a, pair, len, n);
+    if (threadIdx.x == 0) *found = ListFound{list_ok(a, pair, len, n), n};
     __syncthreads();
-    if (*flag) {
+    if (found->ok) {
         const int32_t *keep = a.keep + static_cast<int64_t>(pair) * a.max_keep;
         bool ok = true;
-        for (int32_t i = threadIdx.x; i < n; i += NT) ok = ok && entry_ok(a, pair, len, keep, i);
-        if (!ok) *flag = 0;
+        int32_t first = n;
+        for (int32_t i = threadIdx.x; i < n; i += NT) {
+            ok = ok && entry_ok(a, pair, len, keep, i);
+            if (keep[i] != i) first = min(first, i);
+        }
+        if (!ok) found->ok = 0;
+        if (first < n) atomicMin(&found->first, first);
     }
     __syncthreads();
-    return *flag != 0;
+    return *found;
 }
-__global__ __launch_bounds__(256) void fairkv_evict_lengths_kernel(EvictArgs a)
+// The lengths: a pair whose list is not right keeps its own (into another cache: has none there) and is counted.
+__device__ __forceinline__ void set_length(const EvictArgs &a, int pair)
 {
-    __shared__ int32_t flag;
-    const int pair = blockIdx.x;
+    __shared__ ListFound found;
     const int32_t len = a.len[pair], n = a.n_keep[pair];
-    const bool ok = whole_list_ok<256>(a, pair, len, n, &flag);
+    const bool ok = whole_list<256>(a, pair, len, n, &found).ok != 0;
     if (threadIdx.x == 0) {
         a.len_out[pair] = ok ? n : a.cap_to ? 0 : len;
         if (!ok && a.bad) atomicAdd(a.bad, 1);
     }
 }
+__global__ __launch_bounds__(256) void fairkv_evict_lengths_kernel(EvictArgs a) { set_length(a, blockIdx.x); }
 
-// Into another cache: the line of all lists, in blocks of so many entries.
+// Into another cache: the line of all lists, in blocks of 64 entries, one to a lane of a wave; behind the workgroups that move are those that set a pair's
+// length, where lengths are not written over those that are read.
 template <int ROWB>
 __global__ __launch_bounds__(256) void fairkv_evict_into_kernel(EvictArgs a)
 {
-    constexpr int PPR = ROWB / 16, kSlots = 256 / PPR, kBlock = 64;
-    const int piece = threadIdx.x % PPR, slot = threadIdx.x / PPR;
+    constexpr int PPR = ROWB / 16, RPW = 64 / PPR, PASSES = 64 / RPW, U = PASSES < 4 ? PASSES : 4;      // pieces of a row, rows of a wave-wide move, moves of a block, at once
+    if (static_cast<int>(blockIdx.x) >= a.movers) return set_length(a, blockIdx.x - a.movers);
+    const int lane = threadIdx.x & 63, piece = lane % PPR, slot = lane / PPR;
     auto count = [&](int p) __attribute__((always_inline)) {
         const int32_t n = a.n_keep[p];
         return list_ok(a, p, a.len[p], n) ? n : 0;
     };
-    auto blocks_of = [](int32_t n) __attribute__((always_inline)) { return (static_cast<int64_t>(n) + kBlock - 1) / kBlock; };
-    const LineShare share = line_share<256>(a.n_pairs, gridDim.x, blockIdx.x, [&](int p) { return blocks_of(count(p)); });
+    auto blocks_of = [](int32_t n) __attribute__((always_inline)) { return (static_cast<int64_t>(n) + 63) / 64; };
+    const LineShare share = line_share<256>(a.n_pairs, a.movers, blockIdx.x, [&](int p) { return blocks_of(count(p)); });
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int pair = share.pair;
-    int64_t block = share.begin;
-    int32_t n = share.left > 0 ? count(pair) : 0;
-    for (int64_t left = share.left; left > 0; --left, ++block) {
-        if (block >= blocks_of(n)) {
-            pair = next_pair(pair, a.n_pairs, count), block = 0;
-            n = count(pair);
+    int64_t first = share.begin, left = share.left;
+    int32_t n = left > 0 ? count(pair) : 0;
+    while (left > 0) {
+      if (first >= blocks_of(n)) {
+          pair = next_pair(pair, a.n_pairs, count), first = 0;
+          n = count(pair);
+      }
+      const int64_t end = min(first + left, blocks_of(n));
+      const int32_t len = a.len[pair];
+      for (int64_t block = first + wave; block < end; block += 4) {
+        // the lane's entry: a row that is none stays where it is
+        const int32_t i = static_cast<int32_t>(block) * 64 + lane;
+        const int32_t t = i < n ? a.keep[static_cast<int64_t>(pair) * a.max_keep + i] : -1;
+        int64_t from = t >= 0 && t < len ? a.from.row(pair, t) : -1;
+        const int64_t to = from >= 0 ? a.to.row(pair, i) : -1;
+        if (to < 0) from = -1;
+        if (a.w && from >= 0) a.w_to[to] = a.w[from];
+#pragma unroll 1
+        for (int p0 = 0; p0 < PASSES; p0 += U) {
+            if (static_cast<int32_t>(block) * 64 + p0 * RPW >= n) break;
+            int64_t at[U], out[U];
+            u32x4_row_t kk[U], vv[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                at[u] = __shfl(from, (p0 + u) * RPW + slot), out[u] = __shfl(to, (p0 + u) * RPW + slot);
+                const int64_t byte = max(at[u], static_cast<int64_t>(0)) * ROWB + piece * 16;
+                if (at[u] >= 0) {
+                    kk[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_row_t *>(a.k + byte));
+                    vv[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_row_t *>(a.v + byte));
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (at[u] >= 0) {
+                    const int64_t byte = out[u] * ROWB + piece * 16;
+                    *reinterpret_cast<u32x4_row_t *>(a.k_to + byte) = kk[u];
+                    *reinterpret_cast<u32x4_row_t *>(a.v_to + byte) = vv[u];
+                }
         }
-        const int32_t len = a.len[pair], i0 = static_cast<int32_t>(block) * kBlock;
-        const int32_t *keep = a.keep + static_cast<int64_t>(pair) * a.max_keep;
-        for (int32_t i = i0 + slot; i < min(n, i0 + kBlock); i += kSlots) {
-            if (!entry_ok(a, pair, len, keep, i)) continue;
-            const int64_t from = a.from.row(pair, keep[i]), to = a.to.row(pair, i);
-            const auto kk = *reinterpret_cast<const u32x4_row_t *>(a.k + from * ROWB + piece * 16), vv = *reinterpret_cast<const u32x4_row_t *>(a.v + from * ROWB + piece * 16);
-            *reinterpret_cast<u32x4_row_t *>(a.k_to + to * ROWB + piece * 16) = kk;
-            *reinterpret_cast<u32x4_row_t *>(a.v_to + to * ROWB + piece * 16) = vv;
-            if (a.w && piece == 0) a.w_to[to] = a.w[from];
-        }
+      }
+      left -= end - first, first = end;
     }
 }
 
-// In place: a workgroup per pair.
-template <int ROWB>
-__global__ __launch_bounds__(1024) void fairkv_evict_kernel(EvictArgs a)
+// In place.  A workgroup has so many bytes, WIDTH, of a pair's rows of K or of V: those of different workgroups have nothing to do with one another.  Rows are
+// moved in runs; a run's are in registers before one is written, and the next run's are on their way by then.
+template <int ROWB, int WIDTH>
+__global__ __launch_bounds__(256) void fairkv_evict_kernel(EvictArgs a)
 {
-    constexpr int PPR = ROWB / 16, kSlots = 1024 / PPR;
-    __shared__ int32_t flag;
-    const int pair = blockIdx.x, piece = threadIdx.x % PPR, slot = threadIdx.x / PPR;
+    constexpr int PPR = WIDTH / 16, SLICES = 2 * (ROWB / WIDTH), ROWS = 256 / PPR, U = 4, RUN = ROWS * U;
+    __shared__ ListFound found;
+    const int blocks = a.n_pairs * SLICES;
+    if (static_cast<int>(blockIdx.x) >= blocks) return set_length(a, blockIdx.x - blocks);
+    const int pair = blockIdx.x / SLICES, slice = blockIdx.x % SLICES, piece = threadIdx.x % PPR, slot = threadIdx.x / PPR;
     const int32_t len = a.len[pair], n = a.n_keep[pair];
-    if (!whole_list_ok<1024>(a, pair, len, n, &flag)) return;
+    const ListFound list = whole_list<256>(a, pair, len, n, &found);
+    if (!list.ok || list.first >= n) return;
     const int32_t *keep = a.keep + static_cast<int64_t>(pair) * a.max_keep;
-    for (int32_t i0 = 0; i0 < n; i0 += kSlots) {
-        const int32_t i = i0 + slot;
-        const int32_t t = i < n ? keep[i] : i;
-        u32x4_row_t kk, vv;
-        float w = 0.f;
-        if (t != i) {
-            const int64_t from = a.from.row(pair, t);
-            kk = *reinterpret_cast<const u32x4_row_t *>(a.k + from * ROWB + piece * 16);
-            vv = *reinterpret_cast<const u32x4_row_t *>(a.v + from * ROWB + piece * 16);
-            if (a.w && piece == 0) w = a.w[from];
+    const char *const from = (slice & 1 ? a.v : a.k) + slice / 2 * WIDTH + piece * 16;
+    char *const to = (slice & 1 ? a.v_to : a.k_to) + slice / 2 * WIDTH + piece * 16;
+    const bool weights = a.w && slice == 0 && piece == 0;
+    u32x4_row_t x[U], x_ahead[U];
+    float w[U], w_ahead[U];
+    int32_t t[U];                             // entries of the run behind
+    bool moves[U], moves_ahead[U];
+    auto entries = [&](int32_t i0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) t[u] = keep[min(i0 + u * ROWS + slot, n - 1)];
+    };
+    auto request = [&](int32_t i0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t i = i0 + u * ROWS + slot;
+            const int64_t row = a.from.row(pair, t[u]);
+            moves_ahead[u] = i < n && t[u] != i;
+            x_ahead[u] = *reinterpret_cast<const u32x4_row_t *>(from + row * ROWB);
+            w_ahead[u] = weights ? a.w[row] : 0.f;
         }
-        drain_vmem();                     // what another wave is about to write has been read
-        __syncthreads();
-        if (t != i) {
-            const int64_t to = a.to.row(pair, i);
-            *reinterpret_cast<u32x4_row_t *>(a.k_to + to * ROWB + piece * 16) = kk;
-            *reinterpret_cast<u32x4_row_t *>(a.v_to + to * ROWB + piece * 16) = vv;
-            if (a.w && piece == 0) a.w_to[to] = w;
+    };
+    int32_t i0 = list.first / RUN * RUN;
+    entries(i0);
+    request(i0);
+    entries(i0 + RUN);
+    for (; i0 < n; i0 += RUN) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = x_ahead[u], w[u] = w_ahead[u], moves[u] = moves_ahead[u];
+        int64_t row[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) row[u] = a.to.row(pair, min(i0 + u * ROWS + slot, n - 1));
+#pragma unroll
+        for (int u = 0; u < U; ++u) asm volatile("" : "+v"(x[u]), "+v"(w[u]));      // have come
+        __syncthreads();                      // ... to all waves: what another one is about to write has been read
+        if (i0 + RUN < n) {
+            request(i0 + RUN);
+            entries(i0 + 2 * RUN);
         }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (moves[u]) {
+                *reinterpret_cast<u32x4_row_t *>(to + row[u] * ROWB) = x[u];
+                if (weights) a.w_to[row[u]] = w[u];
+            }
     }
 }
 

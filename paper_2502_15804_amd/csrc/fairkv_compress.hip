@@ -15,6 +15,7 @@ namespace {
 
 using namespace fairkv;
 
+constexpr int32_t kMovers = 8;            // workgroups of a compute unit that move rows into another cache
 constexpr int32_t kMaxSlots = 65536;      // most compute units that a caller may name
 // Units of a group whose keys lie in a workgroup's LDS: four such workgroups of 512 threads share a CU's 160 KB, and two of 1024.
 constexpr int32_t kSmallCap = 120, kLargeCap = 256;
@@ -202,12 +203,18 @@ extern "C" int fairkv_evict(const fairkv_cache *c, const fairkv_cache *into, con
     a.n_pairs = static_cast<int32_t>(pairs), a.max_keep = max_keep;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const int rb = c->D * (c->dtype == FAIRKV_E4M3 ? 1 : c->dtype == FAIRKV_BF16 ? 2 : 4);
+    // Lengths that are written over those that the move reads are set behind it, by a kernel of their own.
+    const bool over = len_out == len;
+    const unsigned setters = over ? 0 : static_cast<unsigned>(pairs);
+    a.movers = n_slots * kMovers;
     auto move = [&](auto row_bytes) {
-        constexpr int ROWB = decltype(row_bytes)::value;
+        constexpr int ROWB = decltype(row_bytes)::value, kNarrow = ROWB > 64 ? 64 : ROWB;
         if (into)
-            hipLaunchKernelGGL(fairkv_evict_into_kernel<ROWB>, dim3(static_cast<unsigned>(n_slots) * 8), dim3(256), 0, st, a);
+            hipLaunchKernelGGL(fairkv_evict_into_kernel<ROWB>, dim3(static_cast<unsigned>(a.movers) + setters), dim3(256), 0, st, a);
+        else if (pairs >= 2 * static_cast<int64_t>(n_slots))
+            hipLaunchKernelGGL((fairkv_evict_kernel<ROWB, ROWB>), dim3(static_cast<unsigned>(pairs) * 2 + setters), dim3(256), 0, st, a);
         else
-            hipLaunchKernelGGL(fairkv_evict_kernel<ROWB>, dim3(static_cast<unsigned>(pairs)), dim3(1024), 0, st, a);
+            hipLaunchKernelGGL((fairkv_evict_kernel<ROWB, kNarrow>), dim3(static_cast<unsigned>(pairs) * 2 * (ROWB / kNarrow) + setters), dim3(256), 0, st, a);
     };
     if (rb == 64)
         move(std::integral_constant<int, 64>{});
@@ -217,8 +224,7 @@ extern "C" int fairkv_evict(const fairkv_cache *c, const fairkv_cache *into, con
         move(std::integral_constant<int, 256>{});
     else
         move(std::integral_constant<int, 512>{});
-    if (const int rc = launched()) return rc;
-    // Lengths change behind all that reads them: they may be written over the old ones.
+    if (const int rc = launched(); rc != FAIRKV_OK || !over) return rc;
     hipLaunchKernelGGL(fairkv_evict_lengths_kernel, dim3(static_cast<unsigned>(pairs)), dim3(256), 0, st, a);
     return launched();
 }
