@@ -61,17 +61,21 @@ __device__ __forceinline__ ListFound whole_list(const EvictArgs &a, int pair, in
     return *found;
 }
 // The lengths: a pair whose list is not right keeps its own (into another cache: has none there) and is counted.
-__device__ __forceinline__ void set_length(const EvictArgs &a, int pair)
+template <int NT>
+__device__ __forceinline__ void set_length(const EvictArgs &a, int pair, ListFound *found /* LDS */)
 {
-    __shared__ ListFound found;
     const int32_t len = a.len[pair], n = a.n_keep[pair];
-    const bool ok = whole_list<256>(a, pair, len, n, &found).ok != 0;
+    const bool ok = whole_list<NT>(a, pair, len, n, found).ok != 0;
     if (threadIdx.x == 0) {
         a.len_out[pair] = ok ? n : a.cap_to ? 0 : len;
         if (!ok && a.bad) atomicAdd(a.bad, 1);
     }
 }
-__global__ __launch_bounds__(256) void fairkv_evict_lengths_kernel(EvictArgs a) { set_length(a, blockIdx.x); }
+__global__ __launch_bounds__(256) void fairkv_evict_lengths_kernel(EvictArgs a)
+{
+    __shared__ ListFound found;
+    set_length<256>(a, blockIdx.x, &found);
+}
 
 // Into another cache: the line of all lists, in blocks of 64 entries, one to a lane of a wave; behind the workgroups that move are those that set a pair's
 // length, where lengths are not written over those that are read.
@@ -79,7 +83,8 @@ template <int ROWB>
 __global__ __launch_bounds__(256) void fairkv_evict_into_kernel(EvictArgs a)
 {
     constexpr int PPR = ROWB / 16, RPW = 64 / PPR, PASSES = 64 / RPW, U = PASSES < 4 ? PASSES : 4;      // pieces of a row, rows of a wave-wide move, moves of a block, at once
-    if (static_cast<int>(blockIdx.x) >= a.movers) return set_length(a, blockIdx.x - a.movers);
+    __shared__ ListFound found;
+    if (static_cast<int>(blockIdx.x) >= a.movers) return set_length<256>(a, blockIdx.x - a.movers, &found);
     const int lane = threadIdx.x & 63, piece = lane % PPR, slot = lane / PPR;
     auto count = [&](int p) __attribute__((always_inline)) {
         const int32_t n = a.n_keep[p];
@@ -92,104 +97,120 @@ __global__ __launch_bounds__(256) void fairkv_evict_into_kernel(EvictArgs a)
     int64_t first = share.begin, left = share.left;
     int32_t n = left > 0 ? count(pair) : 0;
     while (left > 0) {
-      if (first >= blocks_of(n)) {
-          pair = next_pair(pair, a.n_pairs, count), first = 0;
-          n = count(pair);
-      }
-      const int64_t end = min(first + left, blocks_of(n));
-      const int32_t len = a.len[pair];
-      for (int64_t block = first + wave; block < end; block += 4) {
-        // the lane's entry: a row that is none stays where it is
-        const int32_t i = static_cast<int32_t>(block) * 64 + lane;
-        const int32_t t = i < n ? a.keep[static_cast<int64_t>(pair) * a.max_keep + i] : -1;
-        int64_t from = t >= 0 && t < len ? a.from.row(pair, t) : -1;
-        const int64_t to = from >= 0 ? a.to.row(pair, i) : -1;
-        if (to < 0) from = -1;
-        if (a.w && from >= 0) a.w_to[to] = a.w[from];
-#pragma unroll 1
-        for (int p0 = 0; p0 < PASSES; p0 += U) {
-            if (static_cast<int32_t>(block) * 64 + p0 * RPW >= n) break;
-            int64_t at[U], out[U];
-            u32x4_row_t kk[U], vv[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                at[u] = __shfl(from, (p0 + u) * RPW + slot), out[u] = __shfl(to, (p0 + u) * RPW + slot);
-                const int64_t byte = max(at[u], static_cast<int64_t>(0)) * ROWB + piece * 16;
-                if (at[u] >= 0) {
-                    kk[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_row_t *>(a.k + byte));
-                    vv[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_row_t *>(a.v + byte));
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (at[u] >= 0) {
-                    const int64_t byte = out[u] * ROWB + piece * 16;
-                    *reinterpret_cast<u32x4_row_t *>(a.k_to + byte) = kk[u];
-                    *reinterpret_cast<u32x4_row_t *>(a.v_to + byte) = vv[u];
-                }
+        if (first >= blocks_of(n)) {
+            pair = next_pair(pair, a.n_pairs, count), first = 0;
+            n = count(pair);
         }
-      }
-      left -= end - first, first = end;
+        const int64_t end = min(first + left, blocks_of(n));
+        const int32_t len = a.len[pair];
+        for (int64_t block = first + wave; block < end; block += 4) {
+            // the lane's entry: a row that is none stays where it is
+            const int32_t i = static_cast<int32_t>(block) * 64 + lane;
+            const int32_t t = i < n ? a.keep[static_cast<int64_t>(pair) * a.max_keep + i] : -1;
+            int64_t from = t >= 0 && t < len ? a.from.row(pair, t) : -1;
+            const int64_t to = from >= 0 ? a.to.row(pair, i) : -1;
+            if (to < 0) from = -1;
+            if (a.w && from >= 0) a.w_to[to] = a.w[from];
+#pragma unroll 1
+            for (int p0 = 0; p0 < PASSES; p0 += U) {
+                if (static_cast<int32_t>(block) * 64 + p0 * RPW >= n) break;
+                int64_t at[U], out[U];
+                u32x4_row_t kk[U], vv[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    at[u] = __shfl(from, (p0 + u) * RPW + slot), out[u] = __shfl(to, (p0 + u) * RPW + slot);
+                    const int64_t byte = max(at[u], static_cast<int64_t>(0)) * ROWB + piece * 16;
+                    if (at[u] >= 0) {
+                        kk[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_row_t *>(a.k + byte));
+                        vv[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_row_t *>(a.v + byte));
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (at[u] >= 0) {
+                        const int64_t byte = out[u] * ROWB + piece * 16;
+                        *reinterpret_cast<u32x4_row_t *>(a.k_to + byte) = kk[u];
+                        *reinterpret_cast<u32x4_row_t *>(a.v_to + byte) = vv[u];
+                    }
+            }
+        }
+        left -= end - first, first = end;
     }
 }
 
 // In place.  A workgroup has so many bytes, WIDTH, of a pair's rows of K or of V: those of different workgroups have nothing to do with one another.  Rows are
-// moved in runs; a run's are in registers before one is written, and the next run's are on their way by then.
-template <int ROWB, int WIDTH>
-__global__ __launch_bounds__(256) void fairkv_evict_kernel(EvictArgs a)
+// moved in runs; a run's are in registers before one is written, and by then the next run's are on their way, the page numbers of the one behind it, and the
+// entries of the one behind that.
+template <int ROWB, int WIDTH, int NT>
+__global__ __launch_bounds__(NT) void fairkv_evict_kernel(EvictArgs a)
 {
-    constexpr int PPR = WIDTH / 16, SLICES = 2 * (ROWB / WIDTH), ROWS = 256 / PPR, U = 4, RUN = ROWS * U;
+    constexpr int PPR = WIDTH / 16, SLICES = 2 * (ROWB / WIDTH), ROWS = NT / PPR, U = 4, RUN = ROWS * U;
     __shared__ ListFound found;
-    const int blocks = a.n_pairs * SLICES;
-    if (static_cast<int>(blockIdx.x) >= blocks) return set_length(a, blockIdx.x - blocks);
+    const int movers = a.n_pairs * SLICES;
+    if (static_cast<int>(blockIdx.x) >= movers) return set_length<NT>(a, blockIdx.x - movers, &found);
     const int pair = blockIdx.x / SLICES, slice = blockIdx.x % SLICES, piece = threadIdx.x % PPR, slot = threadIdx.x / PPR;
     const int32_t len = a.len[pair], n = a.n_keep[pair];
-    const ListFound list = whole_list<256>(a, pair, len, n, &found);
+    const ListFound list = whole_list<NT>(a, pair, len, n, &found);
     if (!list.ok || list.first >= n) return;
     const int32_t *keep = a.keep + static_cast<int64_t>(pair) * a.max_keep;
     const char *const from = (slice & 1 ? a.v : a.k) + slice / 2 * WIDTH + piece * 16;
     char *const to = (slice & 1 ? a.v_to : a.k_to) + slice / 2 * WIDTH + piece * 16;
-    const bool weights = a.w && slice == 0 && piece == 0;
+    const bool weights = a.w && slice == 0 && piece == 0, paged = a.from.pages != nullptr;
+    const int64_t off = paged ? 0 : a.from.off[pair];
+    const int32_t *pages = paged ? a.from.pages + static_cast<int64_t>(pair) * a.from.max_pages : nullptr;
+    const int shift = a.from.page_shift;
+    auto entry = [&](int32_t i0, int u) __attribute__((always_inline)) { return min(i0 + u * ROWS + slot, n - 1); };      // past the last one: that one again
+    auto row = [&](int32_t id, int32_t t) __attribute__((always_inline)) { return paged ? (static_cast<int64_t>(id) << shift) + (t & ((1 << shift) - 1)) : off + t; };      // (the list is right)
+
+    struct Run {
+        int32_t t[U], page[U], page_to[U];    // entries, and the pages of their rows and of the rows that they become
+    };
+    auto ask_entries = [&](Run &r, int32_t i0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) r.t[u] = keep[entry(i0, u)];
+    };
+    auto ask_pages = [&](Run &r, int32_t i0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) r.page[u] = paged ? pages[r.t[u] >> shift] : 0, r.page_to[u] = paged ? pages[entry(i0, u) >> shift] : 0;
+    };
     u32x4_row_t x[U], x_ahead[U];
     float w[U], w_ahead[U];
-    int32_t t[U];                             // entries of the run behind
-    bool moves[U], moves_ahead[U];
-    auto entries = [&](int32_t i0) __attribute__((always_inline)) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) t[u] = keep[min(i0 + u * ROWS + slot, n - 1)];
-    };
-    auto request = [&](int32_t i0) __attribute__((always_inline)) {
+    int64_t row_to[U], row_to_ahead[U];       // -1: the row stays where it is
+    auto ask_rows = [&](const Run &r, int32_t i0) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int32_t i = i0 + u * ROWS + slot;
-            const int64_t row = a.from.row(pair, t[u]);
-            moves_ahead[u] = i < n && t[u] != i;
-            x_ahead[u] = *reinterpret_cast<const u32x4_row_t *>(from + row * ROWB);
-            w_ahead[u] = weights ? a.w[row] : 0.f;
+            const int64_t at = row(r.page[u], r.t[u]);
+            row_to_ahead[u] = i0 + u * ROWS + slot >= n || r.t[u] == entry(i0, u) ? -1 : row(r.page_to[u], entry(i0, u));
+            x_ahead[u] = *reinterpret_cast<const u32x4_row_t *>(from + at * ROWB);
+            w_ahead[u] = weights ? a.w[at] : 0.f;
         }
     };
     int32_t i0 = list.first / RUN * RUN;
-    entries(i0);
-    request(i0);
-    entries(i0 + RUN);
+    Run next, behind;
+    ask_entries(next, i0);
+    ask_entries(behind, i0 + RUN);
+    ask_pages(next, i0);
+    ask_rows(next, i0);
+    next = behind;
+    ask_pages(next, i0 + RUN);
+    ask_entries(behind, i0 + 2 * RUN);
     for (; i0 < n; i0 += RUN) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) x[u] = x_ahead[u], w[u] = w_ahead[u], moves[u] = moves_ahead[u];
-        int64_t row[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) row[u] = a.to.row(pair, min(i0 + u * ROWS + slot, n - 1));
+        for (int u = 0; u < U; ++u) x[u] = x_ahead[u], w[u] = w_ahead[u], row_to[u] = row_to_ahead[u];
 #pragma unroll
         for (int u = 0; u < U; ++u) asm volatile("" : "+v"(x[u]), "+v"(w[u]));      // have come
         __syncthreads();                      // ... to all waves: what another one is about to write has been read
         if (i0 + RUN < n) {
-            request(i0 + RUN);
-            entries(i0 + 2 * RUN);
+            ask_rows(next, i0 + RUN);
+            next = behind;
+            ask_pages(next, i0 + 2 * RUN);
+            ask_entries(behind, i0 + 3 * RUN);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (moves[u]) {
-                *reinterpret_cast<u32x4_row_t *>(to + row[u] * ROWB) = x[u];
-                if (weights) a.w_to[row[u]] = w[u];
+            if (row_to[u] >= 0) {
+                *reinterpret_cast<u32x4_row_t *>(to + row_to[u] * ROWB) = x[u];
+                if (weights) a.w_to[row_to[u]] = w[u];
             }
     }
 }

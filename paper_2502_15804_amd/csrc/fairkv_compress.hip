@@ -212,9 +212,9 @@ extern "C" int fairkv_evict(const fairkv_cache *c, const fairkv_cache *into, con
         if (into)
             hipLaunchKernelGGL(fairkv_evict_into_kernel<ROWB>, dim3(static_cast<unsigned>(a.movers) + setters), dim3(256), 0, st, a);
         else if (pairs >= 2 * static_cast<int64_t>(n_slots))
-            hipLaunchKernelGGL((fairkv_evict_kernel<ROWB, ROWB>), dim3(static_cast<unsigned>(pairs) * 2 + setters), dim3(256), 0, st, a);
+            hipLaunchKernelGGL((fairkv_evict_kernel<ROWB, ROWB, 256>), dim3(static_cast<unsigned>(pairs) * 2 + setters), dim3(256), 0, st, a);
         else
-            hipLaunchKernelGGL((fairkv_evict_kernel<ROWB, kNarrow>), dim3(static_cast<unsigned>(pairs) * 2 * (ROWB / kNarrow) + setters), dim3(256), 0, st, a);
+            hipLaunchKernelGGL((fairkv_evict_kernel<ROWB, kNarrow, 1024>), dim3(static_cast<unsigned>(pairs) * 2 * (ROWB / kNarrow) + setters), dim3(1024), 0, st, a);
     };
     if (rb == 64)
         move(std::integral_constant<int, 64>{});
