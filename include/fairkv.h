@@ -532,11 +532,13 @@ typedef struct {
  * keep       device [B][Hkv][max_keep], out: the tokens that stay, ascending; what is behind them is left as it is
  * n_keep     device [B][Hkv], out: their number; -1, and the pair counted in *bad, for a pair with more than max_keep of them, whose list then says nothing
  * bad        device counter or NULL
- * workspace  device, fairkv_select_workspace_bytes(cache, shared, n_slots) bytes, 16-byte aligned, all of it zero before the first use; every completed
- *            call leaves it so, so calls of any shapes that are ordered on one stream may share a workspace that is large enough for each
+ * workspace  device, fairkv_select_workspace_bytes(cache, shared, n_slots) bytes or more, 16-byte aligned.  Its first workspace_bytes / 3 bytes must be zero
+ *            before the first use (fairkv_select_workspace_reset); every completed call leaves them zero, and nothing else in it is kept from call to
+ *            call, so calls of any shapes that are ordered on one stream may share a workspace that is large enough for each, with one workspace_bytes
  * n_slots    the GPU's compute units
  * No synchronisation.  FAIRKV_EUNSUPPORTED: pool > 63. */
 size_t fairkv_select_workspace_bytes(const fairkv_cache *cache, int32_t shared, int32_t n_slots);
+int fairkv_select_workspace_reset(void *workspace, size_t workspace_bytes, void *hip_stream);
 int fairkv_select(const fairkv_cache *cache, const fairkv_selection *s, const float *weights, const int32_t *len, int32_t *keep,
                   int32_t max_keep, int32_t *n_keep, int32_t *bad, void *workspace, size_t workspace_bytes, int32_t n_slots,
                   void *hip_stream);

@@ -34,7 +34,7 @@ EXPORTS = ("fairkv_default_params", "fairkv_plan", "fairkv_workspace_bytes", "fa
            "fairkv_decode_attn_static", "fairkv_decode_attn_trace",
            "fairkv_place", "fairkv_pack", "fairkv_append", "fairkv_plan_grow", "fairkv_stream_probe", "fairkv_stream_probe_shape", "fairkv_workspace_reset",
            "fairkv_append_rotated", "fairkv_decode_attn_tree", "fairkv_tree_workspace_bytes", "fairkv_tree_counter_bytes", "fairkv_tree_workspace_reset", "fairkv_accept",
-           "fairkv_attn_weights", "fairkv_select", "fairkv_select_workspace_bytes", "fairkv_evict",
+           "fairkv_attn_weights", "fairkv_select", "fairkv_select_workspace_bytes", "fairkv_select_workspace_reset", "fairkv_evict",
            "fairkv_strerror", "fairkv_version")
 
 
@@ -177,6 +177,8 @@ def lib() -> ctypes.CDLL:
         L.fairkv_attn_weights.argtypes = [cache_p, vp, vp, vp, vp, vp, vp, vp, ctypes.c_float, i32, i32, i32, ctypes.c_float, vp]
         L.fairkv_select_workspace_bytes.restype = ctypes.c_size_t
         L.fairkv_select_workspace_bytes.argtypes = [cache_p, i32, i32]
+        L.fairkv_select_workspace_reset.restype = ctypes.c_int
+        L.fairkv_select_workspace_reset.argtypes = [vp, ctypes.c_size_t, vp]
         L.fairkv_select.restype = ctypes.c_int
         L.fairkv_select.argtypes = [cache_p, ctypes.POINTER(fairkv_selection), vp, vp, vp, i32, vp, vp, vp, ctypes.c_size_t, i32, vp]
         L.fairkv_evict.restype = ctypes.c_int
@@ -540,6 +542,15 @@ def fairkv_attn_weights(cache, lens, q, lse, weights, scale, tree=None, n_new=No
 def fairkv_select_workspace_bytes(cache, shared: bool, n_slots=None) -> int:
     """Bytes of the workspace of fairkv_select, which has to be zero-filled before its first use; shared: the heads of a sequence share a budget."""
     return int(lib().fairkv_select_workspace_bytes(ctypes.byref(cache.struct), int(shared), cache.n_slots if n_slots is None else int(n_slots)))
+
+
+def fairkv_select_workspace_reset(workspace, stream=None):
+    """Enqueue the kernel that zeroes what has to be zero of a device workspace of fairkv_select (see the header)."""
+    _check_dev(workspace=workspace)
+    with _torch()[0].cuda.device(workspace.get_device()):      # whichever is the current one
+        rc = lib().fairkv_select_workspace_reset(_ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream, workspace))
+    if rc != FAIRKV_OK:
+        raise FairKVError(rc, "fairkv_select_workspace_reset")
 
 
 def fairkv_select(cache, lens, weights, budget, keep, n_keep, workspace, pool=1, sink=0, recent=0, bad=None, n_slots=None, stream=None):

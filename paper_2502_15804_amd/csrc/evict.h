@@ -77,12 +77,12 @@ __global__ __launch_bounds__(256) void fairkv_evict_lengths_kernel(EvictArgs a)
     set_length<256>(a, blockIdx.x, &found);
 }
 
-// Into another cache: the line of all lists, in blocks of 64 entries, one to a lane of a wave; behind the workgroups that move are those that set a pair's
+// Into another cache: the line of all lists, in blocks of ENTRIES, one to a lane of a wave; behind the workgroups that move are those that set a pair's
 // length, where lengths are not written over those that are read.
-template <int ROWB>
+template <int ROWB, int ENTRIES>
 __global__ __launch_bounds__(256) void fairkv_evict_into_kernel(EvictArgs a)
 {
-    constexpr int PPR = ROWB / 16, RPW = 64 / PPR, PASSES = 64 / RPW, U = PASSES < 4 ? PASSES : 4;      // pieces of a row, rows of a wave-wide move, moves of a block, at once
+    constexpr int PPR = ROWB / 16, RPW = 64 / PPR, PASSES = ENTRIES / RPW > 0 ? ENTRIES / RPW : 1, U = PASSES < 4 ? PASSES : 4;      // pieces of a row, rows of a wave-wide move, moves of a block, at once
     __shared__ ListFound found;
     if (static_cast<int>(blockIdx.x) >= a.movers) return set_length<256>(a, blockIdx.x - a.movers, &found);
     const int lane = threadIdx.x & 63, piece = lane % PPR, slot = lane / PPR;
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(256) void fairkv_evict_into_kernel(EvictArgs a)
         const int32_t n = a.n_keep[p];
         return list_ok(a, p, a.len[p], n) ? n : 0;
     };
-    auto blocks_of = [](int32_t n) __attribute__((always_inline)) { return (static_cast<int64_t>(n) + 63) / 64; };
+    auto blocks_of = [](int32_t n) __attribute__((always_inline)) { return (static_cast<int64_t>(n) + ENTRIES - 1) / ENTRIES; };
     const LineShare share = line_share<256>(a.n_pairs, a.movers, blockIdx.x, [&](int p) { return blocks_of(count(p)); });
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int pair = share.pair;
@@ -105,15 +105,15 @@ __global__ __launch_bounds__(256) void fairkv_evict_into_kernel(EvictArgs a)
         const int32_t len = a.len[pair];
         for (int64_t block = first + wave; block < end; block += 4) {
             // the lane's entry: a row that is none stays where it is
-            const int32_t i = static_cast<int32_t>(block) * 64 + lane;
-            const int32_t t = i < n ? a.keep[static_cast<int64_t>(pair) * a.max_keep + i] : -1;
+            const int32_t i = static_cast<int32_t>(block) * ENTRIES + lane;
+            const int32_t t = lane < ENTRIES && i < n ? a.keep[static_cast<int64_t>(pair) * a.max_keep + i] : -1;
             int64_t from = t >= 0 && t < len ? a.from.row(pair, t) : -1;
             const int64_t to = from >= 0 ? a.to.row(pair, i) : -1;
             if (to < 0) from = -1;
             if (a.w && from >= 0) a.w_to[to] = a.w[from];
 #pragma unroll 1
             for (int p0 = 0; p0 < PASSES; p0 += U) {
-                if (static_cast<int32_t>(block) * 64 + p0 * RPW >= n) break;
+                if (static_cast<int32_t>(block) * ENTRIES + p0 * RPW >= n) break;
                 int64_t at[U], out[U];
                 u32x4_row_t kk[U], vv[U];
 #pragma unroll

@@ -10,6 +10,7 @@
 #include "evict.h"
 #include "fairkv.h"
 #include "select.h"
+#include "zero_words.h"
 
 namespace {
 
@@ -112,7 +113,11 @@ SelectShape select_shape(const fairkv_cache *c, int32_t shared, int32_t n_slots)
     s.shares = std::min<int64_t>(s.max_blocks, 4 * static_cast<int64_t>(n_slots));
     return s;
 }
-size_t select_bytes(const SelectShape &s) { return 256 + sizeof(SelectSlot) * s.slots + sizeof(SelectShare) * s.shares + sizeof(int2) * s.max_blocks; }
+// What has to be zero when a call begins lies in the first third of a workspace, whatever the call's shape, and the rest in the others.
+size_t start_bytes(const SelectShape &s) { return sizeof(SelectStart) * s.slots; }
+size_t other_bytes(const SelectShape &s) { return sizeof(SelectSlot) * s.slots + sizeof(SelectShare) * s.shares + sizeof(int2) * s.max_blocks; }
+size_t third_of(size_t workspace_bytes) { return workspace_bytes / 3 / 256 * 256; }
+size_t select_bytes(const SelectShape &s) { return 3 * ((std::max(start_bytes(s), (other_bytes(s) + 1) / 2) + 256) / 256 * 256); }
 
 template <int NT, int UNITS>
 void launch_select(const SelectArgs &a, unsigned groups, hipStream_t st)
@@ -129,6 +134,14 @@ extern "C" size_t fairkv_select_workspace_bytes(const fairkv_cache *c, int32_t s
 {
     if (check_cache(c) != FAIRKV_OK || n_slots < 1 || n_slots > kMaxSlots || shared < 0 || shared > 1) return 0;
     return select_bytes(select_shape(c, shared, n_slots));
+}
+
+extern "C" int fairkv_select_workspace_reset(void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (!workspace || !aligned(workspace, 16)) return FAIRKV_EINVAL;
+    if (workspace_bytes < select_bytes(SelectShape{})) return FAIRKV_EWORKSPACE;
+    zero_words(workspace, workspace_bytes / 3 / sizeof(uint32_t), static_cast<hipStream_t>(hip_stream));
+    return launched();
 }
 
 extern "C" int fairkv_select(const fairkv_cache *c, const fairkv_selection *s, const float *weights, const int32_t *len, int32_t *keep,
@@ -158,10 +171,11 @@ extern "C" int fairkv_select(const fairkv_cache *c, const fairkv_selection *s, c
             launch_select<512, kSmallCap>(a, static_cast<unsigned>(groups), st);
         return launched();
     }
-    char *ws = static_cast<char *>(workspace);
-    a.slots = reinterpret_cast<SelectSlot *>(ws);
-    a.shares = reinterpret_cast<SelectShare *>(ws + sizeof(SelectSlot) * shape.slots);
-    a.blocks = reinterpret_cast<int2 *>(ws + sizeof(SelectSlot) * shape.slots + sizeof(SelectShare) * shape.shares);
+    char *others = static_cast<char *>(workspace) + third_of(workspace_bytes);
+    a.starts = static_cast<SelectStart *>(workspace);
+    a.slots = reinterpret_cast<SelectSlot *>(others);
+    a.shares = reinterpret_cast<SelectShare *>(others + sizeof(SelectSlot) * shape.slots);
+    a.blocks = reinterpret_cast<int2 *>(others + sizeof(SelectSlot) * shape.slots + sizeof(SelectShare) * shape.shares);
     const dim3 grid(static_cast<unsigned>(shape.shares)), first(static_cast<unsigned>(groups + shape.shares)), threads(kLargeThreads);
     if (a.half > 0)
         hipLaunchKernelGGL((fairkv_select_first_kernel<kSmallCap, true>), first, threads, 0, st, a);
@@ -184,6 +198,12 @@ extern "C" int fairkv_evict(const fairkv_cache *c, const fairkv_cache *into, con
         if (into->B != c->B || into->Hkv != c->Hkv || into->D != c->D || into->dtype != c->dtype || into->n_scales != c->n_scales) return FAIRKV_EINVAL;
         for (int32_t h = 0; h < c->n_scales; ++h)      // bytes move as they are
             if (into->k_scale[h] != c->k_scale[h] || into->v_scale[h] != c->v_scale[h]) return FAIRKV_EINVAL;
+        // Rows are written while others are read: the caches are one pool, or apart, and where they are one their pairs' rows are not the same.
+        const bool pool = into->k == c->k && into->v == c->v && into->n_rows == c->n_rows;
+        const size_t row = static_cast<size_t>(c->D) * (c->dtype == FAIRKV_E4M3 ? 1 : c->dtype == FAIRKV_BF16 ? 2 : 4);
+        auto apart = [&](const void *x, const void *y) { return !meet(x, row * c->n_rows, y, row * into->n_rows); };
+        if (pool ? into->off == c->off && into->pages == c->pages : !(apart(c->k, into->k) && apart(c->k, into->v) && apart(c->v, into->k) && apart(c->v, into->v))) return FAIRKV_EINVAL;
+        if (weights && !(pool && weights == weights_out) && meet(weights, sizeof(float) * c->n_rows, weights_out, sizeof(float) * into->n_rows)) return FAIRKV_EINVAL;
     }
     if (!keep || !n_keep || !len || !len_out || max_keep < 1 || n_slots < 1 || (weights == nullptr) != (weights_out == nullptr)) return FAIRKV_EINVAL;
     if (n_slots > kMaxSlots) return FAIRKV_EUNSUPPORTED;
@@ -206,11 +226,16 @@ extern "C" int fairkv_evict(const fairkv_cache *c, const fairkv_cache *into, con
     // Lengths that are written over those that the move reads are set behind it, by a kernel of their own.
     const bool over = len_out == len;
     const unsigned setters = over ? 0 : static_cast<unsigned>(pairs);
-    a.movers = n_slots * kMovers;
+    // Blocks of 64 entries, or of 16 where lists as long as they can be do not give every wave one of those.
+    const int64_t most = n_slots * kMovers, few = pairs * ((static_cast<int64_t>(max_keep) + 63) / 64);
+    const bool small = few <= 4 * most;
+    a.movers = static_cast<int32_t>(std::min(most, small ? pairs * ((static_cast<int64_t>(max_keep) + 15) / 16) : few));
     auto move = [&](auto row_bytes) {
         constexpr int ROWB = decltype(row_bytes)::value, kNarrow = ROWB > 64 ? 64 : ROWB;
-        if (into)
-            hipLaunchKernelGGL(fairkv_evict_into_kernel<ROWB>, dim3(static_cast<unsigned>(a.movers) + setters), dim3(256), 0, st, a);
+        if (into && small)
+            hipLaunchKernelGGL((fairkv_evict_into_kernel<ROWB, 16>), dim3(static_cast<unsigned>(a.movers) + setters), dim3(256), 0, st, a);
+        else if (into)
+            hipLaunchKernelGGL((fairkv_evict_into_kernel<ROWB, 64>), dim3(static_cast<unsigned>(a.movers) + setters), dim3(256), 0, st, a);
         else if (pairs >= 2 * static_cast<int64_t>(n_slots))
             hipLaunchKernelGGL((fairkv_evict_kernel<ROWB, ROWB, 256>), dim3(static_cast<unsigned>(pairs) * 2 + setters), dim3(256), 0, st, a);
         else

@@ -24,18 +24,19 @@ constexpr int kMaxPairs = 64;             // of a group that one workgroup has
 constexpr int kMostHalf = 31;             // of the window
 
 // What the kernels of a large group hand on.  Slots are of groups: a group has at least min_blocks blocks, so the place of its first block in the
-// line, divided by min_blocks, is no other's.  A step's workgroups read what the step before left, in `found` of its own, and clear what nobody
-// reads any more.
+// line, divided by min_blocks, is no other's.  A step's workgroups read what the step before left.
 struct SelectFound {
     int64_t need;                         // how many stay of the candidates that share the digits found so far
     uint32_t least;                       // these digits, the rest 0; with `done`: what is larger stays
     int32_t done;                         // no more digits need be looked at
 };
+struct SelectStart {                      // of the first step, which finds it 0: the third step leaves it so
+    int32_t bins[kBins];
+    unsigned long long protected_rows;    // with a row in the cache
+};
 struct SelectSlot {
-    int32_t bins[kDigits][kBins];         // 0 between calls
-    unsigned long long protected_rows;    // with a row in the cache; 0 between calls
-    SelectFound found[kDigits];           // 0 between calls
-    int64_t listed;                       // blocks whose list is written; 0 between calls
+    int32_t bins[kDigits - 1][kBins];     // of the other digits: the first step clears them
+    SelectFound found[kDigits];
 };
 struct SelectShare {                      // of a workgroup: its blocks in the line, and of the group that the first of them is in its first block and their number
     int64_t left, block, at, group_at, group_blocks;      // left: how many; block: the first one's number in its pair
@@ -46,9 +47,10 @@ struct SelectArgs {
     const float *weights;                 // [n_rows]
     const int32_t *len, *budget;          // [B * Hkv]; [groups]
     int32_t *keep, *n_keep, *bad;         // [B * Hkv][max_keep], [B * Hkv], [1] or null
-    SelectSlot *slots;                    // null: no group can be large
-    int2 *blocks;                         // [max_blocks]: rows of a block that stay whatever ties do, and ties; 0 between calls
-    SelectShare *shares;                  // of the large groups' workgroups; 0 between calls
+    SelectStart *starts;                  // null: no group can be large
+    SelectSlot *slots;
+    int2 *blocks;                         // [max_blocks]: rows of a block that stay whatever ties do, and ties
+    SelectShare *shares;                  // of the large groups' workgroups
     int64_t max_blocks;
     int32_t n_pairs, n_groups, max_len, max_keep, half, sink, recent, per_group, cap, min_blocks;      // per_group: pairs of a group
 };
@@ -215,7 +217,7 @@ __device__ __forceinline__ void select_group(const SelectArgs &a, int group, Gro
     const int64_t off = one && !a.rows.pages ? a.rows.off[p0 + lane] : 0;
     const int64_t upto = wave_upto((static_cast<int64_t>(len) + 63) / 64), units64 = __shfl(upto, 63);
     if (n_pairs > kMaxPairs || units64 > a.cap) {     // a.cap is UNITS or less: a larger group's other kernels do it, if there can be one
-        for (int p = threadIdx.x; p < n_pairs && !a.slots; p += NT) {
+        for (int p = threadIdx.x; p < n_pairs && !a.starts; p += NT) {
             a.n_keep[p0 + p] = -1;
             if (a.bad) atomicAdd(a.bad, 1);
         }
@@ -415,10 +417,6 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
         if (threadIdx.x == 0) a.shares[slot_index] = share;
     } else {
         share = a.shares[slot_index];
-        if (STEP == kDigits + 1) {
-            __syncthreads();
-            if (threadIdx.x == 0) a.shares[slot_index] = SelectShare{0, 0, 0, 0, 0, 0};
-        }
     }
     if (share.left < 0 && STEP == kDigits + 1 && slot_index == 0)
         for (int p = threadIdx.x; p < a.n_pairs; p += NT)
@@ -429,33 +427,21 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
     if (share.left <= 0) return;
     int pair = static_cast<int>(share.pair), group = -1;
     int64_t block = share.block, at = share.at, group_at = share.group_at;      // group_at: the place of the group's first block
+    SelectStart *start = nullptr;
     SelectSlot *slot = nullptr;
     SelectFound f{0, 0, 0};
-    int32_t protected_rows = 0, blocks_here = 0;
+    int32_t protected_rows = 0;
 
     auto end_group = [&]() __attribute__((always_inline)) {
         if constexpr (kCounts) {
             __syncthreads();
             for (int i = threadIdx.x; i < kBins; i += NT)
-                if (bins[i]) atomicAdd(&slot->bins[STEP][i], bins[i]);
+                if (bins[i]) atomicAdd(STEP == 0 ? &start->bins[i] : &slot->bins[STEP > 0 ? STEP - 1 : 0][i], bins[i]);
             if constexpr (STEP == 0) {
                 const int64_t n = wave_upto(static_cast<int64_t>(protected_rows));
-                if (lane == 63 && n) atomicAdd(&slot->protected_rows, static_cast<unsigned long long>(n));
+                if (lane == 63 && n) atomicAdd(&start->protected_rows, static_cast<unsigned long long>(n));
             }
             __syncthreads();
-        }
-        if constexpr (STEP == kDigits + 1) {      // who comes last leaves all of the group's as it was found
-            const int64_t n = share.group_blocks;
-            __syncthreads();
-            if (threadIdx.x == 0) sums[0] = atomicAdd(reinterpret_cast<unsigned long long *>(&slot->listed), static_cast<unsigned long long>(blocks_here)) + blocks_here;
-            __syncthreads();
-            if (static_cast<int64_t>(sums[0]) == n) {
-                for (int64_t x = threadIdx.x; x < n; x += NT) a.blocks[group_at + x] = make_int2(0, 0);
-                for (int i = threadIdx.x; i < kBins; i += NT) slot->bins[kDigits - 1][i] = 0;
-                if (threadIdx.x < kDigits) slot->found[threadIdx.x] = SelectFound{0, 0, 0};
-                if (threadIdx.x == 0) slot->listed = 0;
-            }
-            blocks_here = 0;
         }
     };
     auto begin_group = [&]() __attribute__((always_inline)) {
@@ -465,15 +451,15 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
             group_at = share.group_at;
         }
         group = pair / a.per_group;
-        slot = a.slots + group_at / a.min_blocks;
+        start = a.starts + group_at / a.min_blocks, slot = a.slots + group_at / a.min_blocks;
         if constexpr (STEP == 1) {
-            f = {max(static_cast<int64_t>(a.budget[group]) - static_cast<int64_t>(slot->protected_rows), static_cast<int64_t>(0)), 0, 0};
+            f = {max(static_cast<int64_t>(a.budget[group]) - static_cast<int64_t>(start->protected_rows), static_cast<int64_t>(0)), 0, 0};
             if (f.need == 0) f = {0, kProtected - 1, 1};
         }
         if constexpr (STEP > 1) f = slot->found[STEP == kDigits + 1 ? kDigits - 1 : STEP - 2];
         if constexpr (STEP >= 1 && STEP <= kDigits) {
             if (!f.done) {
-                const BinFound b = find_bin<NT>(f.need, [&](int x) { return slot->bins[STEP - 1][x]; });
+                const BinFound b = find_bin<NT>(f.need, [&](int x) { return STEP == 1 ? start->bins[x] : slot->bins[STEP > 1 ? STEP - 2 : 0][x]; });
                 if (b.need == 0) {        // there are no so many candidates: all of them stay
                     f = {0, 0, 1};
                 } else {
@@ -484,9 +470,12 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
         }
         if (at == group_at) {             // this workgroup has the group's first block
             if (STEP >= 1 && STEP <= kDigits && threadIdx.x == 0) slot->found[STEP - 1] = f;
-            if (STEP == 2 && threadIdx.x == 0) slot->protected_rows = 0;
-            if constexpr (STEP == 2 || STEP == 3)
-                for (int i = threadIdx.x; i < kBins; i += NT) slot->bins[STEP - 2][i] = 0;
+            if constexpr (STEP == 0)
+                for (int i = threadIdx.x; i < (kDigits - 1) * kBins; i += NT) (&slot->bins[0][0])[i] = 0;
+            if constexpr (STEP == 2) {
+                for (int i = threadIdx.x; i < kBins; i += NT) start->bins[i] = 0;
+                if (threadIdx.x == 0) start->protected_rows = 0;
+            }
         }
         if constexpr (kCounts) {
             for (int i = threadIdx.x; i < kBins; i += NT) bins[i] = 0;
@@ -529,8 +518,12 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
             if (group >= 0) end_group();
             begin_group();
         }
-        ++blocks_here;
         if ((STEP == 1 || STEP == 2) && f.done) continue;
+        // what stays of other blocks: in front of this one, and behind it where it is the pair's first (the first of them ahead of their use)
+        const int64_t pair_at = at - block, pair_end = pair_at + blocks_of_large(len);
+        const int64_t look_from = f.need > 0 ? group_at : pair_at, look_to = block == 0 ? pair_end : at;
+        int2 look = make_int2(0, 0);
+        if (STEP == kDigits + 1 && look_from + static_cast<int64_t>(threadIdx.x) < look_to) look = a.blocks[look_from + threadIdx.x];
         if (a.half > 0) {
             __syncthreads();              // the windows of the block before have been looked at
 #pragma unroll
@@ -570,13 +563,12 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
         }
         if constexpr (STEP == kDigits + 1) {
             // ties in front of the pair, and of the block; rows in front of the block that stay anyhow; both of the whole pair
-            const int64_t pair_at = at - block, pair_end = pair_at + blocks_of_large(len);
             __syncthreads();
             if (threadIdx.x < 5) sums[threadIdx.x] = 0;
             __syncthreads();
             unsigned long long s[5] = {0, 0, 0, 0, 0};
-            for (int64_t x = (f.need > 0 ? group_at : pair_at) + threadIdx.x; x < (block == 0 ? pair_end : at); x += NT) {
-                const int2 n = a.blocks[x];
+            for (int64_t x = look_from + threadIdx.x; x < look_to; x += NT) {
+                const int2 n = x < look_from + NT ? look : a.blocks[x];
                 if (x < pair_at) s[0] += n.y;
                 if (x < at) s[1] += n.y;
                 if (x >= pair_at && x < at) s[2] += n.x;

@@ -194,7 +194,7 @@ def _check_select(s, w, budget, shared, pool=1, sink=0, recent=0, max_keep=None,
     keep = torch.full((s.B, s.Hkv, most), -9, dtype=torch.int32, device=DEV)
     n_keep, bad = torch.full((s.B, s.Hkv), -7, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
     ws = torch.zeros(F.fairkv_select_workspace_bytes(s.cache, shared, n_slots), dtype=torch.uint8, device=DEV)
-    for call in range(2):                            # the workspace is left as it was found
+    for call in range(2):                            # what has to be zero is left so
         F.fairkv_select(s.cache, s.lens, torch.from_numpy(w).to(DEV), I32(budget), keep, n_keep, ws, pool=pool, sink=sink, recent=recent, bad=bad, n_slots=n_slots)
         assert n_keep.cpu().numpy().tolist() == counts.tolist()
         got = keep.cpu().numpy().reshape(-1, most)
@@ -203,7 +203,7 @@ def _check_select(s, w, budget, shared, pool=1, sink=0, recent=0, max_keep=None,
                 assert got[p, :len(want)].tolist() == want, p
                 assert (got[p, len(want):] == -9).all()
         assert int(bad) == (call + 1) * int((counts < 0).sum())
-    assert not int(ws.max())
+    assert not int(ws[:ws.numel() // 3].max())
     return lists
 
 
