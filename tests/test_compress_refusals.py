@@ -81,9 +81,43 @@ def test_evict_refuses_a_cache_of_another_kind(kw):
     assert _evict(_cache(), into=_cache(**kw), len_out=AT) == INVALID
 
 
+FAR = 1 << 40                                # addresses that are never read on the host
+BYTES = 100 * 128 * 2                        # of the 100 rows of K
+
+
+@pytest.mark.parametrize("kw", [dict(k=FAR, v=FAR + (1 << 30)), dict(k=FAR + BYTES - 16, v=FAR + (2 << 30)), dict(k=FAR + (2 << 30), v=FAR + 16),
+                                dict(k=FAR + (2 << 30), v=FAR + (1 << 30) + BYTES - 16), dict(k=FAR + (1 << 30), v=FAR + (2 << 30))])
+def test_evict_refuses_caches_that_share_rows(kw):
+    c = _cache(k=FAR, v=FAR + (1 << 30))
+    assert _evict(c, into=_cache(**kw), len_out=AT) == INVALID      # (the first is the cache itself: the same pool, and the same rows of it)
+
+
+def test_evict_refuses_weights_that_meet_those_that_are_read():
+    c, other = _cache(k=FAR, v=FAR + (1 << 30)), _cache(k=FAR + (2 << 30), v=FAR + (3 << 30))
+    for out in (8 * AT, 8 * AT + 396, 8 * AT - 396):
+        assert _evict(c, into=other, len_out=AT, weights=8 * AT, out=out) == INVALID
+
+
 def test_evict_refuses_other_scales():
     c = lambda x: _cache(dtype=F.FAIRKV_E4M3, n_scales=2, scales=[1.0, x])
     assert _evict(c(2.0), into=c(2.5), len_out=AT) == INVALID
+
+
+def test_the_workspace_of_a_selection():
+    need = lambda shared, n_slots=256, **kw: F.lib().fairkv_select_workspace_bytes(ctypes.byref(_cache(**kw)), shared, n_slots)
+    small = need(0)
+    assert 0 < small <= 4096 and need(1) == small                    # no group of 100 rows is a large one
+    assert need(2) == need(-1) == need(0, 0) == need(0, 65537) == 0
+    for shared in (0, 1):
+        by_rows = [need(shared, n_rows=n) for n in (100, 7000, 20000, 1 << 20, 1 << 30)]
+        assert by_rows == sorted(by_rows) and by_rows[-1] < (1 << 30) * 16
+        assert _select(_cache(n_rows=1 << 20), shared=shared, ws_bytes=by_rows[3] - 1) == F.FAIRKV_EWORKSPACE
+    # what pages say of the longest pair counts, not the size of the pool
+    paged = dict(off=None, pages=AT, max_pages=64, page_rows=16, n_rows=1 << 24)
+    assert need(0, **paged) == small and need(1, **paged) == small
+    assert F.lib().fairkv_select_workspace_reset(None, 1 << 20, None) == INVALID
+    assert F.lib().fairkv_select_workspace_reset(AT + 8, 1 << 20, None) == INVALID
+    assert F.lib().fairkv_select_workspace_reset(AT, 100, None) == F.FAIRKV_EWORKSPACE
 
 
 def test_more_pairs_than_a_launch_has():

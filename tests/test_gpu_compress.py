@@ -283,6 +283,51 @@ def test_long_pairs(lens, shared, n_slots, kind):
     _check_select(s, w, np.rint(total * 0.8), shared, 1, 0, 64, n_slots=n_slots)
 
 
+@pytest.mark.parametrize("shared", [False, True])
+def test_more_heads_than_a_workgroup_keeps_in_mind(shared):
+    rng = np.random.default_rng(2)
+    s = Setup(rng.integers(0, 90, (3, 80)), 0, 64, page=16)
+    s.lens_h[1] = 0                                  # a sequence without rows
+    s.make()
+    w = _some_weights(s.n_rows, 4, "tail")
+    total = s.lens_h.sum(1) if shared else s.lens_h
+    for part, pool, sink, recent in ((0.4, 3, 2, 8), (0.0, 1, 0, 0), (2.0, 1, 0, 0)):
+        _check_select(s, w, np.rint(total * part), shared, pool, sink, recent)
+
+
+def test_pairs_that_share_rows_are_refused_not_followed_out_of_the_workspace():
+    """Rows of different pairs must not overlap; where they do, a group may have more rows than the workspace was made for."""
+    for n_pages in (40, 400):                        # no group can be a large one; one can, and has fewer blocks
+        s = Setup([[n_pages * 64]], 0, 64, page=64)
+        pages = np.arange(n_pages, dtype=np.int32)[None, None].repeat(64, 1)
+        lens = I32(np.full((1, 64), n_pages * 64))
+        cache = F.Cache(s.k, s.v, lens, pages=I32(pages), page_rows=64)
+        keep, n_keep = torch.zeros(1, 64, 8, dtype=torch.int32, device=DEV), torch.zeros(1, 64, dtype=torch.int32, device=DEV)
+        ws, bad = torch.zeros(F.fairkv_select_workspace_bytes(cache, True), dtype=torch.uint8, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+        guard = torch.full((1 << 20,), 7, dtype=torch.uint8, device=DEV)
+        F.fairkv_select(cache, lens, torch.ones(s.n_rows, device=DEV), I32([100]), keep, n_keep, ws, bad=bad)
+        assert (n_keep == -1).all() and int(bad) == 64 and bool((guard == 7).all())
+
+
+def test_one_workspace_for_calls_of_all_shapes():
+    a, b, c = Setup([[9000, 12000]], 0, 64, page=64), Setup([[300] * 8] * 3, 0, 64), Setup([[40000], [20000], [3]], 0, 64)
+    need = max(F.fairkv_select_workspace_bytes(x.cache, sh) for x in (a, b, c) for sh in (False, True))
+    ws = torch.full((need,), 255, dtype=torch.uint8, device=DEV)
+    F.fairkv_select_workspace_reset(ws)
+    for turn in range(3):
+        for s in (a, c, b):
+            for shared in (turn % 2 == 0, turn % 2 == 1):
+                w = _some_weights(s.n_rows, turn, "tail")
+                budget = np.rint((s.lens_h.sum(1) if shared else s.lens_h) * 0.3)
+                most = int(s.lens_h.max())
+                lists, counts = C.select(w.astype(np.float64), s.lens_h, budget, shared, 1, 0, 4, most, s.row)
+                keep, n_keep = torch.zeros(s.B, s.Hkv, most, dtype=torch.int32, device=DEV), torch.zeros(s.B, s.Hkv, dtype=torch.int32, device=DEV)
+                F.fairkv_select(s.cache, s.lens, torch.from_numpy(w).to(DEV), I32(budget), keep, n_keep, ws, recent=4)
+                assert n_keep.cpu().numpy().tolist() == counts.tolist()
+                got = keep.cpu().numpy().reshape(-1, most)
+                assert all(got[p, :len(x)].tolist() == x for p, x in enumerate(lists))
+
+
 # ---- evict -------------------------------------------------------------------------------------------------
 def _lists(lens, part, seed):
     rng = np.random.default_rng(seed)
@@ -500,3 +545,78 @@ def test_on_a_stream_of_the_callers():
     side.synchronize()
     torch.cuda.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(a.state(), b.state()))
+
+
+def test_two_captured_steps_that_share_a_workspace():
+    """Two sequences of long rows, each with a graph of its own, replayed in turn on one stream over one workspace."""
+    class Long:
+        def __init__(self, seed):
+            self.s = s = Setup([[9000, 7000]], 0, 64, page=64, seed=seed)
+            self.w = torch.from_numpy(_some_weights(s.n_rows, seed, "tail")).to(DEV)
+            self.keep, self.n_keep = torch.zeros(1, 2, 9000, dtype=torch.int32, device=DEV), torch.zeros(1, 2, dtype=torch.int32, device=DEV)
+            self.budget, self.bad = I32([14000]), torch.zeros(1, dtype=torch.int32, device=DEV)
+
+        def step(self, ws):
+            F.fairkv_select(self.s.cache, self.s.lens, self.w, self.budget, self.keep, self.n_keep, ws, pool=5, recent=16, bad=self.bad)
+            F.fairkv_evict(self.s.cache, self.s.lens, self.keep, self.n_keep, weights=self.w, bad=self.bad)
+            self.budget.sub_(1000)                   # a kernel of torch's, in the graph
+
+    pairs = [(Long(1), Long(1)), (Long(2), Long(2))]     # eager, captured
+    ws, eager_ws = (torch.zeros(F.fairkv_select_workspace_bytes(pairs[0][0].s.cache, True), dtype=torch.uint8, device=DEV) for _ in range(2))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graphs = []
+    for eager, captured in pairs:
+        with torch.cuda.stream(side):
+            captured.step(ws)
+        side.synchronize()
+        eager.step(eager_ws)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            captured.step(ws)
+        graphs.append(g)
+    for turn in range(4):
+        for g, (eager, captured) in zip(graphs, pairs):
+            g.replay()
+            eager.step(eager_ws)
+        torch.cuda.synchronize()
+        for eager, captured in pairs:
+            for x, y in ((eager.s.k, captured.s.k), (eager.s.v, captured.s.v), (eager.w, captured.w), (eager.s.lens, captured.s.lens), (eager.n_keep, captured.n_keep)):
+                assert torch.equal(x, y), turn
+            assert int(captured.bad) == int(eager.bad) == 0
+            assert int(captured.s.lens.sum()) == 14000 - 1000 * (turn + 1)
+
+
+def test_rows_beyond_32_bits():
+    """A pair at the end of a cache of 20 million rows: its bytes, and its weights' bytes, are beyond 32 bits."""
+    n_rows, n, D = 20_000_000, 700, 128
+    k = torch.empty(n_rows, D, dtype=torch.bfloat16, device=DEV)
+    w, first = torch.zeros(n_rows, device=DEV), n_rows - n - 5
+    g = torch.Generator().manual_seed(1)
+    k[first:] = torch.randn(n_rows - first, D, generator=g).to(torch.bfloat16).to(DEV)
+    q = torch.randn(1, 2, D, generator=g).to(torch.bfloat16).to(DEV)
+    lens, off = I32([[n]]), torch.tensor([[first]], device=DEV)
+    cache = F.Cache(k, k, I32([[n]]), off=off)
+    near = F.Cache(k[first:].clone(), k[first:].clone(), I32([[n]]), off=torch.zeros_like(off))
+    lse = torch.full((1, 2), 3.0, device=DEV)
+    F.fairkv_attn_weights(cache, lens, q, lse, w, 0.1)
+    w_near = torch.zeros(n_rows - first, device=DEV)
+    F.fairkv_attn_weights(near, lens, q, lse, w_near, 0.1)
+    assert torch.equal(w[first:], w_near) and float(w_near[:n].min()) > 0
+    lists = []
+    for c, x in ((cache, w), (near, w_near)):
+        keep, n_keep = torch.zeros(1, 1, n, dtype=torch.int32, device=DEV), torch.zeros(1, 1, dtype=torch.int32, device=DEV)
+        ws = torch.zeros(F.fairkv_select_workspace_bytes(c, False), dtype=torch.uint8, device=DEV)
+        F.fairkv_select(c, lens, x, I32([[200]]), keep, n_keep, ws, recent=10)
+        lists.append((keep, n_keep))
+    assert all(torch.equal(x, y) for x, y in zip(*lists)) and int(lists[0][1]) == 200
+    rows = (first + lists[0][0][0, 0, :200].long())
+    want = k[rows].clone()
+    out = torch.zeros_like(lens)
+    small = F.Cache(torch.zeros(200, D, dtype=torch.bfloat16, device=DEV), torch.zeros(200, D, dtype=torch.bfloat16, device=DEV), I32([[200]]), off=torch.zeros_like(off))
+    F.fairkv_evict(cache, lens, *lists[0], into=small, lens_out=out)
+    assert torch.equal(small.k, want) and torch.equal(small.v, want)
+    v = k[first:].clone()
+    apart = F.Cache(k, k.clone(), I32([[n]]), off=off)
+    F.fairkv_evict(apart, lens, *lists[0])
+    assert torch.equal(k[first:first + 200], want) and torch.equal(k[first + 200:], v[200:]) and int(lens) == 200
