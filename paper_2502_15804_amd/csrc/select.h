@@ -40,7 +40,7 @@ struct SelectSlot {
 };
 struct SelectShare {                      // of a workgroup: its blocks in the line, and of the group that the first of them is in its first block and their number
     int64_t left, block, at, group_at, group_blocks;      // left: how many; block: the first one's number in its pair
-    int64_t pair;
+    int32_t pair, len;                    // of the first one
 };
 struct SelectArgs {
     RowMap rows;
@@ -49,6 +49,7 @@ struct SelectArgs {
     int32_t *keep, *n_keep, *bad;         // [B * Hkv][max_keep], [B * Hkv], [1] or null
     SelectStart *starts;                  // null: no group can be large
     SelectSlot *slots;
+    uint32_t *keys;                       // [max_blocks][kBlockRows]: what the first step makes of the rows
     int2 *blocks;                         // [max_blocks]: rows of a block that stay whatever ties do, and ties
     SelectShare *shares;                  // of the large groups' workgroups
     int64_t max_blocks;
@@ -375,7 +376,7 @@ struct LargeGroups {
     // Where the group of a share's pair begins, and how many blocks it has.
     __device__ __forceinline__ void group_of(SelectShare &s)
     {
-        const int first = static_cast<int>(s.pair) / a.per_group * a.per_group;
+        const int first = s.pair / a.per_group * a.per_group;
         s.group_at = s.at - s.block, s.group_blocks = 0;
 #pragma unroll 8
         for (int p = first; p < first + a.per_group; ++p) {
@@ -386,8 +387,9 @@ struct LargeGroups {
     }
 };
 
+template <int STEP>
 struct LargeSpace {
-    float raw[kBlockRows + 2 * kMostHalf];
+    float raw[STEP == 0 ? kBlockRows + 2 * kMostHalf : 1];
     int32_t bins[kBins];
     int32_t counts[kBlockRows / 64];
     unsigned long long sums[5];
@@ -398,7 +400,7 @@ constexpr int kLargeThreads = 512;
 // Workgroup `slot_index` of n: STEP 0 .. 2: a digit is counted; 3: what stays of every block; 4: the lists.  The first step finds the workgroup's share of
 // the line, the others have it from there.
 template <int STEP>
-__device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index, int n_slots, LargeSpace &m)
+__device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index, int n_slots, LargeSpace<STEP> &m)
 {
     constexpr int NT = kLargeThreads, KPT = kBlockRows / NT;
     constexpr bool kCounts = STEP < kDigits;
@@ -412,8 +414,8 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
     SelectShare share;
     if constexpr (STEP == 0) {
         const LineShare l = line_share<NT>(a.n_pairs, n_slots, slot_index, [&](int p) { return blocks_of(p); });
-        share = {l.total > a.max_blocks ? -1 : l.left, l.begin, l.at, 0, 0, l.pair};      // runs of rows that overlap: so many blocks no cache has
-        if (share.left > 0) blocks_of.group_of(share);
+        share = {l.total > a.max_blocks ? -1 : l.left, l.begin, l.at, 0, 0, l.pair, 0};      // runs of rows that overlap: so many blocks no cache has
+        if (share.left > 0) blocks_of.group_of(share), share.len = select_len(a, share.pair);
         if (threadIdx.x == 0) a.shares[slot_index] = share;
     } else {
         share = a.shares[slot_index];
@@ -425,7 +427,7 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
                 if (a.bad) atomicAdd(a.bad, 1);
             }
     if (share.left <= 0) return;
-    int pair = static_cast<int>(share.pair), group = -1;
+    int pair = share.pair, group = -1;
     int64_t block = share.block, at = share.at, group_at = share.group_at;      // group_at: the place of the group's first block
     SelectStart *start = nullptr;
     SelectSlot *slot = nullptr;
@@ -485,24 +487,28 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
     };
 
     auto blocks_of_large = [&](int32_t len) __attribute__((always_inline)) { return max(1, (len + kBlockRows - 1) / kBlockRows); };
-    int32_t len = select_len(a, pair);
+    int32_t len = share.len;
     for (int64_t left = share.left; left > 0; --left, ++block, ++at) {
         if (block >= blocks_of_large(len)) {
             pair = next_pair(pair, a.n_pairs, [&](int p) { return blocks_of(p); }), block = 0;
             len = select_len(a, pair);
         }
-        // ---- values, on their way while the group's state is found ----
+        // ---- keys, on their way while the group's state is found: from the weights, or as the first step left them ----
         const int32_t t0 = static_cast<int32_t>(block) * kBlockRows;
-        const Candidates c(a, len);
+        const int e = static_cast<int>(threadIdx.x);
+        uint32_t *const keys = a.keys + at * kBlockRows + e;
         uint32_t key[KPT];
         float value[KPT], edge[1];        // edge: rows beside the block that its windows reach
-        uint32_t edge_state[1];
-        const int e = static_cast<int>(threadIdx.x);
-        if (len == 0) {                   // of a cache without rows, maybe: nothing is read
+        if constexpr (STEP > 0) {
+#pragma unroll
+            for (int i = 0; i < KPT; ++i) key[i] = keys[i * NT];
+        } else if (len == 0) {            // of a cache without rows, maybe: nothing is read
 #pragma unroll
             for (int i = 0; i < KPT; ++i) key[i] = kNone, value[i] = -INFINITY;
             edge[0] = -INFINITY;
-        } else if ((STEP == 0 || STEP > 2) || pair / a.per_group != group || !f.done) {
+        } else {
+            const Candidates c(a, len);
+            uint32_t edge_state[1];
             load_values<KPT>(a, pair, key, value, [&](int i, int32_t &t) {
                 t = min(t0 + i * NT + e, max(len - 1, 0));
                 return t0 + i * NT + e >= len ? kNone : c.has(t) ? 1u : kProtected;
@@ -524,21 +530,25 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
         const int64_t look_from = f.need > 0 ? group_at : pair_at, look_to = block == 0 ? pair_end : at;
         int2 look = make_int2(0, 0);
         if (STEP == kDigits + 1 && look_from + static_cast<int64_t>(threadIdx.x) < look_to) look = a.blocks[look_from + threadIdx.x];
-        if (a.half > 0) {
-            __syncthreads();              // the windows of the block before have been looked at
+        if constexpr (STEP == 0) {
+            if (a.half > 0) {
+                __syncthreads();              // the windows of the block before have been looked at
 #pragma unroll
-            for (int i = 0; i < KPT; ++i) raw[a.half + i * NT + e] = value[i];
-            if (e < 2 * a.half) raw[e < a.half ? e : kBlockRows + e] = edge[0];
-            __syncthreads();
-            for (int d = 0; d <= 2 * a.half; ++d) {
+                for (int i = 0; i < KPT; ++i) raw[a.half + i * NT + e] = value[i];
+                if (e < 2 * a.half) raw[e < a.half ? e : kBlockRows + e] = edge[0];
+                __syncthreads();
+                for (int d = 0; d <= 2 * a.half; ++d) {
 #pragma unroll
-                for (int i = 0; i < KPT; ++i) value[i] = fmaxf(value[i], raw[i * NT + e + d]);
+                    for (int i = 0; i < KPT; ++i) value[i] = fmaxf(value[i], raw[i * NT + e + d]);
+                }
             }
-        }
 #pragma unroll
-        for (int i = 0; i < KPT; ++i) {
-            if (key[i] == kProtected) ++protected_rows;
-            if (key[i] == 1) key[i] = order_of(value[i]);
+            for (int i = 0; i < KPT; ++i) {
+                if (key[i] == kProtected) ++protected_rows;
+                if (key[i] == 1) key[i] = order_of(value[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < KPT; ++i) keys[i * NT] = key[i];
         }
         // ---- counts ----
         if constexpr (kCounts) {
@@ -614,7 +624,7 @@ __global__ __launch_bounds__(kLargeThreads) void fairkv_select_first_kernel(Sele
 {
     __shared__ union Space {
         GroupSpace<UNITS, POOL> group;
-        LargeSpace large;
+        LargeSpace<0> large;
         __device__ Space() {}
     } m;
     if (static_cast<int>(blockIdx.x) < a.n_groups)
@@ -625,7 +635,7 @@ __global__ __launch_bounds__(kLargeThreads) void fairkv_select_first_kernel(Sele
 template <int STEP>
 __global__ __launch_bounds__(kLargeThreads) void fairkv_select_large_kernel(SelectArgs a)
 {
-    __shared__ LargeSpace m;
+    __shared__ LargeSpace<STEP> m;
     select_large<STEP>(a, blockIdx.x, gridDim.x, m);
 }
 
