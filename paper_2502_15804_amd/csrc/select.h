@@ -75,32 +75,34 @@ struct Candidates {                       // of a pair: the first token that is 
 
 // The bin, from the top, in which the need-th candidate lies (need >= 1 and at most the sum of all bins), how many are needed of that bin, and how
 // many it has.  Called by all NT threads, the bins complete; ends with a barrier behind the last look at them.
+template <class T>                        // that holds the sum
 struct BinFound {
     int32_t bin, in_bin;
-    int64_t need;
+    T need;
 };
-template <int NT, class At>
-__device__ __forceinline__ BinFound find_bin(int64_t need, At bin_at)
+template <int NT, class T, class At>
+__device__ __forceinline__ BinFound<T> find_bin(T need, At bin_at)
 {
     constexpr int PER = kBins / NT, NW = NT / 64;
     static_assert(kBins % NT == 0, "bins of a thread");
-    __shared__ int64_t totals[NW];
-    __shared__ BinFound found;
+    __shared__ T totals[NW];
+    __shared__ BinFound<T> found;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, top = kBins - 1 - static_cast<int>(threadIdx.x) * PER;
     int32_t n[PER];
     int64_t mine = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) n[i] = bin_at(top - i), mine += n[i];
-    const int64_t upto = wave_upto(mine);
+    const T upto = wave_upto(mine);
     if (lane == 63) totals[wave] = upto;
-    if (threadIdx.x == 0) found = BinFound{0, 0, 0};
+    if (threadIdx.x == 0) found = BinFound<T>{0, 0, 0};
     __syncthreads();
-    int64_t before = upto - mine;
-    for (int w = 0; w < wave; ++w) before += totals[w];
+    T before = upto - mine;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) before += w < wave ? totals[w] : 0;
     if (before < need && need <= before + mine) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            if (before < need && need <= before + n[i]) found = BinFound{top - i, n[i], need - before};
+            if (before < need && need <= before + n[i]) found = BinFound<T>{top - i, n[i], need - before};
             before += n[i];
         }
     }
@@ -274,11 +276,11 @@ __device__ __forceinline__ void select_group(const SelectArgs &a, int group, Gro
     // ---- the least that stays, and how many of those that are equal to it ----
     const int64_t room = max(static_cast<int64_t>(budget) - protected_rows, static_cast<int64_t>(0));
     uint32_t least = 0;                               // what is larger stays
-    int64_t ties = 0;
+    int32_t ties = 0;
     if (room == 0) {
         least = kProtected - 1;
     } else if (room < candidate_rows) {
-        ties = room;
+        ties = static_cast<int32_t>(room);
         for (int digit = 0; digit < kDigits; ++digit) {
             if (digit > 0) {
                 for (int i = threadIdx.x; i < kBins; i += NT) bins[i] = 0;
@@ -289,7 +291,7 @@ __device__ __forceinline__ void select_group(const SelectArgs &a, int group, Gro
                 }
                 __syncthreads();
             }
-            const BinFound b = find_bin<NT>(ties, [&](int x) { return bins[x]; });
+            const BinFound<int32_t> b = find_bin<NT>(ties, [&](int x) { return bins[x]; });
             ties = b.need;
             least |= static_cast<uint32_t>(b.bin) << kDigitShift[digit];
             if (ties == b.in_bin) {                   // all of them stay, whatever their other digits are
@@ -415,8 +417,10 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
     if constexpr (STEP == 0) {
         const LineShare l = line_share<NT>(a.n_pairs, n_slots, slot_index, [&](int p) { return blocks_of(p); });
         share = {l.total > a.max_blocks ? -1 : l.left, l.begin, l.at, 0, 0, l.pair, 0};      // runs of rows that overlap: so many blocks no cache has
-        if (share.left > 0) blocks_of.group_of(share), share.len = select_len(a, share.pair);
-        if (threadIdx.x == 0) a.shares[slot_index] = share;
+        if (share.left > 0)
+            share.len = select_len(a, share.pair);      // (its group is looked at when the first rows are on their way)
+        else if (threadIdx.x == 0)
+            a.shares[slot_index] = share;
     } else {
         share = a.shares[slot_index];
     }
@@ -447,9 +451,11 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
         }
     };
     auto begin_group = [&]() __attribute__((always_inline)) {
-        if (group >= 0) {
+        if (STEP == 0 || group >= 0) {
+            const bool first = group < 0;
             share.at = at, share.block = block, share.pair = pair;
             blocks_of.group_of(share);
+            if (first && threadIdx.x == 0) a.shares[slot_index] = share;
             group_at = share.group_at;
         }
         group = pair / a.per_group;
@@ -461,7 +467,7 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
         if constexpr (STEP > 1) f = slot->found[STEP == kDigits + 1 ? kDigits - 1 : STEP - 2];
         if constexpr (STEP >= 1 && STEP <= kDigits) {
             if (!f.done) {
-                const BinFound b = find_bin<NT>(f.need, [&](int x) { return STEP == 1 ? start->bins[x] : slot->bins[STEP > 1 ? STEP - 2 : 0][x]; });
+                const BinFound<int64_t> b = find_bin<NT>(f.need, [&](int x) { return STEP == 1 ? start->bins[x] : slot->bins[STEP > 1 ? STEP - 2 : 0][x]; });
                 if (b.need == 0) {        // there are no so many candidates: all of them stay
                     f = {0, 0, 1};
                 } else {
