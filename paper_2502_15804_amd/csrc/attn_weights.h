@@ -40,6 +40,7 @@ __global__ __launch_bounds__(NW * 64, 4) void fairkv_attn_weights_kernel(Weights
     constexpr int NT = NW * 64, TOK = 32;
     constexpr int ROWB = KV8 ? D : 2 * D, QROWB = 2 * D;      // bytes of a row of K, of a query
     constexpr int NP = ROWB / 32, NSL = D / 16, PPQ = QROWB / 16;
+    constexpr bool kMany = NW == 16 && CC < FAIRKV_MAX_DRAFT * 16;      // a pair may have more columns; the others' launches have no more
     typedef __attribute__((ext_vector_type(4))) uint32_t u4;
     __shared__ __attribute__((aligned(1024))) char qs[CC * QROWB];
     __shared__ __attribute__((aligned(16))) float minus_lse[CC];      // in log2 units
@@ -61,35 +62,46 @@ __global__ __launch_bounds__(NW * 64, 4) void fairkv_attn_weights_kernel(Weights
     const LineShare share = line_share<NT>(n_pairs, gridDim.x, blockIdx.x, [&](int p) { return tiles_of(len_of(p)); });
     int pair = share.pair;
     int64_t first = share.begin, left = share.left;
-    int32_t len = left > 0 ? len_of(pair) : 0;
+    int32_t len = left > 0 ? __builtin_amdgcn_readfirstlane(len_of(pair)) : 0;      // (the compiler does not know that it is the same for all lanes)
     while (left > 0) {
         // ---- a run of tiles of one pair ----
         if (first >= tiles_of(len)) {
             pair = next_pair(pair, n_pairs, [&](int p) { return tiles_of(len_of(p)); }), first = 0;
-            len = len_of(pair);
+            len = __builtin_amdgcn_readfirstlane(len_of(pair));
         }
         const int n_tiles = static_cast<int>(min(left, tiles_of(len) - first)), tile0 = static_cast<int>(first);
         const int b = pair / a.Hkv, h = pair - b * a.Hkv;
-        const int32_t nn = a.n_new ? min(max(a.n_new[b], 0), a.q_len) : a.q_len, base = len - nn;      // base: rows in front of the new ones
+        const int32_t nn = a.n_new ? __builtin_amdgcn_readfirstlane(min(max(a.n_new[b], 0), a.q_len)) : a.q_len, base = len - nn;      // base: rows in front of the new ones
         const int cols = nn * a.G;
         const float s_mul = KV8 ? a.scale_log2 * a.k_scale[a.n_scales > 1 ? h : 0] : a.scale_log2;
 
-        for (int turn = 0; turn * NW < n_tiles; ++turn) {
-            const int tile = tile0 + turn * NW + wave;
-            const bool mine = turn * NW + wave < n_tiles;
-            const int32_t t0 = tile * TOK;
-            // ---- rows of K, requested before the queries; where there is none the cache's first row stands in: what comes of it is not stored ----
-            const int32_t t = t0 + l32;
-            const int64_t row = mine && t < len ? a.rows.row(pair, t) : -1;
-            const char *from = a.k + max(row, static_cast<int64_t>(0)) * ROWB + hi * 16;
-            u4 raw[NP];
+        // More columns than LDS holds: the run's tiles are gone through once for each CC of them, what the others gave is added to.  (With all chunks of
+        // columns in every turn: 64 queries x 16 heads over 8 x 8 pairs of 4096 rows 160 us.)
+        for (int c_from = 0; c_from == 0 || (kMany && c_from < cols); c_from += CC) {
+            const int chunk = kMany ? c_from / CC : 0;
+            for (int turn = 0; turn * NW < n_tiles; ++turn) {
+                // What comes of the number of columns is computed in every turn: held over the loop, it would take registers that a tile wants, and they
+                // would be spilled (step over 64 x 8 pairs of 1024 rows 22 us instead of 20).
+                int some_columns = kMany ? min(CC, cols - c_from) : cols;
+                asm volatile("" : "+v"(some_columns));
+                const int n = __builtin_amdgcn_readfirstlane(some_columns);
+                const int tile = tile0 + turn * NW + wave;
+                const bool mine = turn * NW + wave < n_tiles;
+                const int32_t t0 = tile * TOK;
+                // ---- rows of K, requested before the queries; where there is none the cache's first row stands in: what comes of it is not stored ----
+                const int32_t t = t0 + l32;
+                const int64_t row = mine && t < len ? a.rows.row(pair, t) : -1;
+                const char *from = a.k + max(row, static_cast<int64_t>(0)) * ROWB + hi * 16;
+                u4 raw[NP];
 #pragma unroll
-            for (int p = 0; p < NP; ++p) raw[p] = *reinterpret_cast<const u4 *>(from + p * 32);
-            const float old = a.decay != 0.f && row >= 0 && t < base ? a.weights[row] * a.decay : 0.f;
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
-            for (int chunk = 0; chunk == 0 || chunk * CC < cols; ++chunk) {
-                const int n = min(CC, cols - chunk * CC);
-                if (turn == 0 || cols > CC) {
+                for (int p = 0; p < NP; ++p) raw[p] = *reinterpret_cast<const u4 *>(from + p * 32);
+                float old = 0.f;
+                if (kMany && chunk > 0)
+                    old = row >= 0 ? a.out[row] : 0.f;
+                else
+                    old = a.decay != 0.f && row >= 0 && t < base ? a.weights[row] * a.decay : 0.f;
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                if (turn == 0) {
                     __syncthreads();
                     for (int x = threadIdx.x; x < n * PPQ; x += NT) {
                         const int c = x / PPQ, p = x % PPQ, node = (chunk * CC + c) / a.G, g = chunk * CC + c - node * a.G;
@@ -154,9 +166,9 @@ __global__ __launch_bounds__(NW * 64, 4) void fairkv_attn_weights_kernel(Weights
                     for (int c0 = 0; c0 + 32 <= n; c0 += 32) columns(c0, std::false_type{}, std::false_type{});
                     if (n % 32 != 0) columns(n / 32 * 32, std::true_type{}, std::false_type{});
                 }
+                const float w = (sum[0] + sum[1]) + (sum[2] + sum[3]), both = w + __shfl_xor(w, 32);
+                if (hi == 0 && row >= 0) a.out[row] = old + both;
             }
-            const float w = (sum[0] + sum[1]) + (sum[2] + sum[3]), both = w + __shfl_xor(w, 32);
-            if (hi == 0 && row >= 0) a.out[row] = old + both;
         }
         left -= n_tiles, first += n_tiles;
     }

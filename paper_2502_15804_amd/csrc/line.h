@@ -71,9 +71,11 @@ __device__ __forceinline__ LineShare line_share(int n_pairs, int n_slots, int sl
         found = LineShare{p, begin - before, left, begin, total};
     }
     __syncthreads();
-    LineShare r = found;
-    r.total = total;
-    return r;
+    auto uniform = [](int64_t x) __attribute__((always_inline)) {      // the same for all lanes: in scalar registers
+        const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<int>(x)), hi = __builtin_amdgcn_readfirstlane(static_cast<int>(x >> 32));
+        return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
+    };
+    return LineShare{__builtin_amdgcn_readfirstlane(found.pair), uniform(found.begin), uniform(found.left), uniform(found.at), uniform(total)};
 }
 
 // The first pair behind `pair` that has units, n_pairs if none has: 64 are looked at at once.
