@@ -33,9 +33,13 @@ struct WeightsArgs {
     float k_scale[kCacheScales];
 };
 
-// NW waves, CC columns in LDS, four waves of a SIMD.
+// Waves of a SIMD that a launch counts on: what the registers allow.
+template <int D, int NW>
+constexpr int kWeightWaves = D == 64 && NW == 4 ? 5 : 4;
+
+// NW waves, CC columns in LDS.
 template <int D, bool KV8, int NW, int CC>
-__global__ __launch_bounds__(NW * 64, 4) void fairkv_attn_weights_kernel(WeightsArgs a)
+__global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_weights_kernel(WeightsArgs a)
 {
     constexpr int NT = NW * 64, TOK = 32;
     constexpr int ROWB = KV8 ? D : 2 * D, QROWB = 2 * D;      // bytes of a row of K, of a query

@@ -34,14 +34,14 @@ bool meet(const void *x, size_t nx, const void *y, size_t ny)
     return a < static_cast<unsigned __int128>(b) + ny && b < static_cast<unsigned __int128>(a) + nx;
 }
 
-// 16 waves of a compute unit, in as many workgroups as its LDS has room for all columns of: a workgroup's waves wait for one another only where a pair
-// begins.  64 queries x 8 heads over 64 x 8 pairs of 4096 rows: 316 us with 16 waves and 512 columns in LDS, 355 with 12; two tiles of 32 tokens a wave
+// 16 waves of a compute unit (20 with heads of 64 and few columns: 256 MB of 8-bit rows 43 us instead of 48), in as many workgroups as its LDS has room
+// for all columns of: a workgroup's waves wait for one another only where a pair begins.  64 queries x 8 heads over 64 x 8 pairs of 4096 rows: 316 us with 16 waves and 512 columns in LDS, 355 with 12; two tiles of 32 tokens a wave
 // 349 (12 waves), 365 (8) and 444 (16), with 128 columns in LDS at a time 859.  32 x 8 columns over 8 x 8 pairs of 16000 rows: 99 us in two workgroups of 8
 // waves or one of 16, 110 with 12 waves.
 template <int D, bool KV8, int NW, int CC>
 void launch_weights_kernel(const WeightsArgs &a, int32_t n_slots, hipStream_t st)
 {
-    hipLaunchKernelGGL((fairkv_attn_weights_kernel<D, KV8, NW, CC>), dim3(static_cast<unsigned>(n_slots) * (16 / NW)), dim3(NW * 64), 0, st, a);
+    hipLaunchKernelGGL((fairkv_attn_weights_kernel<D, KV8, NW, CC>), dim3(static_cast<unsigned>(n_slots) * (4 * kWeightWaves<D, NW> / NW)), dim3(NW * 64), 0, st, a);
 }
 template <int D, bool KV8>
 void launch_weights(const WeightsArgs &a, int32_t n_slots, hipStream_t st)

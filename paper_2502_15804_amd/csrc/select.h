@@ -477,7 +477,8 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
             }
         }
         if (at == group_at) {             // this workgroup has the group's first block
-            if (STEP >= 1 && STEP <= kDigits && threadIdx.x == 0) slot->found[STEP - 1] = f;
+            if constexpr (STEP >= 1 && STEP <= kDigits)
+                if (threadIdx.x == 0) slot->found[STEP - 1] = f;
             if constexpr (STEP == 0)
                 for (int i = threadIdx.x; i < (kDigits - 1) * kBins; i += NT) (&slot->bins[0][0])[i] = 0;
             if constexpr (STEP == 2) {
