@@ -510,7 +510,8 @@ int fairkv_accept(const fairkv_cache *cache, const int32_t *path, const int32_t 
  * weights      device float [n_rows]; weights_out may be weights, or must not meet it
  * n_slots      the GPU's compute units
  * Rows of no token are left as they are, and so are those of a packed pair whose run sticks out of the cache.  The sums are the same from call to
- * call.  A NaN or infinite row counts for the nodes that see it, in its own weight only.
+ * call.  A NaN or infinite row counts for the nodes that see it, in its own weight only; a node whose lse is +inf gives rows of finite scores no
+ * weight, one whose lse is NaN gives NaN to all that it sees.
  * Enqueues one kernel; no synchronisation, no workspace.  FAIRKV_EUNSUPPORTED: q_len > FAIRKV_MAX_DRAFT, an F32 cache, D, Hq / Hkv > 16.
  * FAIRKV_EINVAL also: more than 2^31 - 1 elements of q, a decay, or a scale (times a k_scale) in log2 units, that is not finite. */
 int fairkv_attn_weights(const fairkv_cache *cache, const void *q, const uint64_t *tree, const int32_t *n_new, const int32_t *len,
@@ -536,7 +537,8 @@ typedef struct {
  *            before the first use (fairkv_select_workspace_reset); every completed call leaves them zero, and nothing else in it is kept from call to
  *            call, so calls of any shapes that are ordered on one stream may share a workspace that is large enough for each, with one workspace_bytes
  * n_slots    the GPU's compute units
- * No synchronisation.  FAIRKV_EUNSUPPORTED: pool > 63. */
+ * Enqueues one kernel, or five where the sizes of the cache allow a group of more than about 7700 rows (of a paged cache max_pages * page_rows is the most
+ * that a pair has, of a packed one n_rows); no synchronisation.  FAIRKV_EUNSUPPORTED: pool > 63.  FAIRKV_EINVAL also: more than 2^21 groups. */
 size_t fairkv_select_workspace_bytes(const fairkv_cache *cache, int32_t shared, int32_t n_slots);
 int fairkv_select_workspace_reset(void *workspace, size_t workspace_bytes, void *hip_stream);
 int fairkv_select(const fairkv_cache *cache, const fairkv_selection *s, const float *weights, const int32_t *len, int32_t *keep,
@@ -544,15 +546,16 @@ int fairkv_select(const fairkv_cache *cache, const fairkv_selection *s, const fl
                   void *hip_stream);
 
 /* Row keep[p][i] of every pair becomes its row i for i < n_keep[p], K, V and, if given, its weight; len_out[p] = n_keep[p].
- * into         NULL: in place, a list has to ascend.  Else another cache of the same B, Hkv, D, type and scales, whose rows of these pairs are none that
- *              this one's tokens have (its pages may be of the same pool): lists may be in any order and name a token twice.
+ * into         NULL: in place, a list has to ascend.  Else another cache of the same B, Hkv, D, type and scales: lists may be in any order and name a token
+ *              twice.  Its k and v must not meet this one's, or be the same of as many rows (one pool); then its rows of the pairs are none that
+ *              this one's tokens have, by pages or first rows of its own.
  * keep         device [B][Hkv][max_keep], n_keep device [B][Hkv], as fairkv_select leaves them
  * len_out      device [B][Hkv]; may be len, must not meet n_keep
- * weights      device float [n_rows] and weights_out device float [n_rows of into], or both NULL; in place the same
+ * weights      device float [n_rows] and weights_out device float [n_rows of into], or both NULL; in place the same, in one pool the same or apart
  * A pair is left alone and counted in *bad, its length kept (into another cache: 0, and what is in its rows there says nothing), if n_keep[p] is not in
  * 0 .. max_keep (in place: or its length; else: or its room there), an entry not in 0 .. len - 1, not ascending (in place), or a row outside its cache.
  * Pages behind ceil(len_out / page_rows) hold no token of a pair any more.  Packed rows stay where the pair's run begins.
- * Enqueues two kernels; no synchronisation. */
+ * Enqueues one kernel, and a second one if len_out is len; no synchronisation.  FAIRKV_EINVAL also: more than 2^22 - 1 pairs. */
 int fairkv_evict(const fairkv_cache *cache, const fairkv_cache *into, const int32_t *keep, int32_t max_keep, const int32_t *n_keep,
                  const int32_t *len, int32_t *len_out, const float *weights, float *weights_out, int32_t *bad, int32_t n_slots,
                  void *hip_stream);

@@ -3,6 +3,10 @@
 // Row keep[i] of a pair becomes its row i, K and V as they are stored and the row's weight.  Only memory bounds it: what stays is read and
 // written once.  Into another cache rows may move in any order.  In place keep ascends, so row i comes from i or behind it: a workgroup that has
 // read the rows of a run of i may write them, for every later run reads behind its own i, which are behind what is written.
+//
+// Measured (MI355X): into another cache 128 x 8 pairs of 4096 8-bit rows halved, 1.02 GB read and written, 241 us (4.25 TB/s; a plain copy has 4.9); 16 x 8 pairs of
+// 16000 bf16 rows to a sixteenth 28 us (4.4 TB/s); 8 pairs of 1024 halved 5.4 us, most of it the way from lists over pages to rows.  In place the order holds it
+// back: the same 385, 50 and 9 us, 8 pairs of 131072 rows to a third 312 us (1 TB/s, 64 workgroups; 955 with 4 waves each and nothing asked for ahead).
 #pragma once
 #include "cache_rows.h"
 #include "common.h"

@@ -17,6 +17,7 @@ namespace {
 using namespace fairkv;
 
 constexpr int32_t kMovers = 8;            // workgroups of a compute unit that move rows into another cache
+constexpr int64_t kMaxGroupsOfCall = 1 << 21;      // of a selection: a grid's threads are counted in 32 bits
 constexpr int32_t kMaxSlots = 65536;      // most compute units that a caller may name
 // Units of a group whose keys lie in a workgroup's LDS: four such workgroups of 512 threads share a CU's 160 KB, and two of 1024.
 constexpr int32_t kSmallCap = 120, kLargeCap = 256;
@@ -34,10 +35,10 @@ bool meet(const void *x, size_t nx, const void *y, size_t ny)
     return a < static_cast<unsigned __int128>(b) + ny && b < static_cast<unsigned __int128>(a) + nx;
 }
 
-// 16 waves of a compute unit (20 with heads of 64 and few columns: 256 MB of 8-bit rows 43 us instead of 48), in as many workgroups as its LDS has room
-// for all columns of: a workgroup's waves wait for one another only where a pair begins.  64 queries x 8 heads over 64 x 8 pairs of 4096 rows: 316 us with 16 waves and 512 columns in LDS, 355 with 12; two tiles of 32 tokens a wave
-// 349 (12 waves), 365 (8) and 444 (16), with 128 columns in LDS at a time 859.  32 x 8 columns over 8 x 8 pairs of 16000 rows: 99 us in two workgroups of 8
-// waves or one of 16, 110 with 12 waves.
+// 16 waves of a compute unit (20 with heads of 64 and few columns: 64 x 8 pairs of 4096 8-bit rows 43 us instead of 48), in as many workgroups as its LDS
+// has room for all columns of: a workgroup's waves wait for one another only where a pair begins.  64 queries x 8 heads over 64 x 8 pairs of 4096 rows: 316 us
+// with 16 waves and 512 columns in LDS, 355 with 12; with two tiles of 32 tokens a wave 349 (12 waves), 365 (8) and 444 (16); with 128 columns in
+// LDS at a time 859.  32 x 8 columns over 8 x 8 pairs of 16000 rows: 99 us in two workgroups of 8 waves or one of 16, 110 with 12 waves.
 template <int D, bool KV8, int NW, int CC>
 void launch_weights_kernel(const WeightsArgs &a, int32_t n_slots, hipStream_t st)
 {
@@ -154,7 +155,7 @@ extern "C" int fairkv_select(const fairkv_cache *c, const fairkv_selection *s, c
     if (s->pool > 2 * kMostHalf + 1 || n_slots > kMaxSlots) return FAIRKV_EUNSUPPORTED;
     if (!aligned(weights, 4) || !aligned(workspace, 16)) return FAIRKV_EINVAL;
     const int64_t pairs = static_cast<int64_t>(c->B) * c->Hkv, groups = s->shared ? c->B : pairs;
-    if (groups > UINT32_MAX / 1024 - 4 * kMaxSlots) return FAIRKV_EINVAL;
+    if (groups > kMaxGroupsOfCall) return FAIRKV_EINVAL;
     const SelectShape shape = select_shape(c, s->shared, n_slots);
     if (!workspace || workspace_bytes < select_bytes(shape)) return FAIRKV_EWORKSPACE;
     SelectArgs a{};
@@ -165,8 +166,12 @@ extern "C" int fairkv_select(const fairkv_cache *c, const fairkv_selection *s, c
     a.cap = shape.cap, a.min_blocks = shape.min_blocks, a.max_blocks = shape.max_blocks;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (shape.max_blocks == 0) {
-        if (shape.cap == kLargeCap || groups <= n_slots)      // few: the wider workgroup is the faster one (8 pairs of 1024 rows in one group 12.5 us with 512 threads)
-            shape.cap == kLargeCap ? launch_select<1024, kLargeCap>(a, static_cast<unsigned>(groups), st) : launch_select<1024, kSmallCap>(a, static_cast<unsigned>(groups), st);
+        // Of few groups the wider workgroups are faster (8 pairs of 1024 rows in one group 10.3 us, 12.5 with 512 threads), of many the narrower ones, four of
+        // which a compute unit has at once (128 x 8 groups of 1024 rows 18 us, 25 with 1024 threads, 23 with 256).
+        if (shape.cap == kLargeCap)
+            launch_select<1024, kLargeCap>(a, static_cast<unsigned>(groups), st);
+        else if (groups <= n_slots)
+            launch_select<1024, kSmallCap>(a, static_cast<unsigned>(groups), st);
         else
             launch_select<512, kSmallCap>(a, static_cast<unsigned>(groups), st);
         return launched();
@@ -203,7 +208,8 @@ extern "C" int fairkv_evict(const fairkv_cache *c, const fairkv_cache *into, con
         const bool pool = into->k == c->k && into->v == c->v && into->n_rows == c->n_rows;
         const size_t row = static_cast<size_t>(c->D) * (c->dtype == FAIRKV_E4M3 ? 1 : c->dtype == FAIRKV_BF16 ? 2 : 4);
         auto apart = [&](const void *x, const void *y) { return !meet(x, row * c->n_rows, y, row * into->n_rows); };
-        if (pool ? into->off == c->off && into->pages == c->pages : !(apart(c->k, into->k) && apart(c->k, into->v) && apart(c->v, into->k) && apart(c->v, into->v))) return FAIRKV_EINVAL;
+        const bool all_apart = apart(c->k, into->k) && apart(c->k, into->v) && apart(c->v, into->k) && apart(c->v, into->v);
+        if (pool ? into->off == c->off && into->pages == c->pages : !all_apart) return FAIRKV_EINVAL;
         if (weights && !(pool && weights == weights_out) && meet(weights, sizeof(float) * c->n_rows, weights_out, sizeof(float) * into->n_rows)) return FAIRKV_EINVAL;
     }
     if (!keep || !n_keep || !len || !len_out || max_keep < 1 || n_slots < 1 || (weights == nullptr) != (weights_out == nullptr)) return FAIRKV_EINVAL;
@@ -227,7 +233,7 @@ extern "C" int fairkv_evict(const fairkv_cache *c, const fairkv_cache *into, con
     // Lengths that are written over those that the move reads are set behind it, by a kernel of their own.
     const bool over = len_out == len;
     const unsigned setters = over ? 0 : static_cast<unsigned>(pairs);
-    // Blocks of 64 entries, or of 16 where lists as long as they can be do not give every wave one of those.
+    // Blocks of 64 entries, or of 16 where lists as long as they can be do not give every wave one of those (8 pairs of 1024 rows halved: 5.4 us, 7.1 with 64).
     const int64_t most = n_slots * kMovers, few = pairs * ((static_cast<int64_t>(max_keep) + 63) / 64);
     const bool small = few <= 4 * most;
     a.movers = static_cast<int32_t>(std::min(most, small ? pairs * ((static_cast<int64_t>(max_keep) + 15) / 16) : few));
@@ -237,7 +243,7 @@ extern "C" int fairkv_evict(const fairkv_cache *c, const fairkv_cache *into, con
             hipLaunchKernelGGL((fairkv_evict_into_kernel<ROWB, 16>), dim3(static_cast<unsigned>(a.movers) + setters), dim3(256), 0, st, a);
         else if (into)
             hipLaunchKernelGGL((fairkv_evict_into_kernel<ROWB, 64>), dim3(static_cast<unsigned>(a.movers) + setters), dim3(256), 0, st, a);
-        else if (pairs >= 2 * static_cast<int64_t>(n_slots))
+        else if (pairs >= 2 * static_cast<int64_t>(n_slots))      // K and V of a pair by a workgroup each; of fewer pairs in slices of 64 bytes
             hipLaunchKernelGGL((fairkv_evict_kernel<ROWB, ROWB, 256>), dim3(static_cast<unsigned>(pairs) * 2 + setters), dim3(256), 0, st, a);
         else
             hipLaunchKernelGGL((fairkv_evict_kernel<ROWB, kNarrow, 1024>), dim3(static_cast<unsigned>(pairs) * 2 * (ROWB / kNarrow) + setters), dim3(1024), 0, st, a);

@@ -9,8 +9,14 @@
 // counting how many candidates have which digit among those that share the digits found so far: 11, 11 and 10 bits.  Where all candidates that
 // share some digits stay, the others need not be looked at.
 //
-// A group of up to `cap` units of 64 rows is one workgroup's, which reads its weights once and holds its values in registers.  Rows of larger groups are dealt
-// to the whole GPU in blocks: three kernels count a digit each, one counts what stays of every block, one lists it.
+// A group of up to `cap` units of 64 rows is one workgroup's, which reads its weights once and has its keys in LDS.  Rows of larger groups are dealt to
+// the whole GPU in blocks of 4096: a kernel makes keys of them, in order, and counts the first digit, two count the others, one counts what stays of
+// every block, one lists it.  Every list ascends and no sum depends on who comes first: counts are whole numbers.
+//
+// What bounds it (MI355X; times of a call in a row of them): not its bytes (a million weights are 4 MB, 1 us) but one thing after the other.  A workgroup's
+// group: 9 us from lengths over pages, weights, three digits and ties to the list, 16 us where four of them share a compute unit's issue slots (128 x 8 pairs of
+// 1024 rows; 8 pairs of 1024 rows in one group 9.4).  A large one: five kernels of 3 to 7 us each, of which the first one takes 12, for it finds the groups'
+// blocks and reads the weights (one group of 8 pairs of 131072 rows 30 us; 16 groups of 8 pairs of 16000 rows 34, 48 where every kernel read the weights).
 #pragma once
 #include "cache_rows.h"
 #include "line.h"
@@ -233,8 +239,8 @@ __device__ __forceinline__ void select_group(const SelectArgs &a, int group, Gro
     if (threadIdx.x == 0) protected_rows = candidate_rows = 0;
     __syncthreads();
 
-    // ---- values, from addresses that are always some of the arrays'.  (Two, three and four units of a wave on their way at once: 128 x 8 pairs of 1024 rows
-    //      17.8, 18.2 and 18.4 us instead of 17.5: the other waves are enough, and short pairs have no more units.) ----
+    // ---- values, from addresses that are always some of the arrays'.  (Two, three and four units of a wave on their way at once were 1.5, 4 and 5 % slower
+    //      on 128 x 8 pairs of 1024 rows: the other waves are enough, and short pairs have no more units.) ----
     int32_t is_protected = 0, is_candidate = 0;
     for (int32_t unit = wave; unit < units; unit += NW) {
         const int p = pair_of(unit);

@@ -123,6 +123,7 @@ def test_the_workspace_of_a_selection():
 def test_more_pairs_than_a_launch_has():
     many = _cache(B=1 << 20, Hkv=64)
     assert _select(many, shared=0) == INVALID and _evict(many) == INVALID
+    assert _select(_cache(B=(1 << 21) + 1, Hkv=1), shared=1) == INVALID
 
 
 # ---- the oracle ----------------------------------------------------------------------------------------------

@@ -153,6 +153,24 @@ def test_rows_that_are_no_numbers_count_where_they_are_seen():
     assert bool((out[others] <= want[others]).all())
 
 
+def test_log_sum_exps_that_are_no_numbers():
+    s = Setup([[40]], 0, 64)
+    q = torch.randn(1, 2, 2, 64, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).to(DEV)
+    rows = [s.row(0, t) for t in range(40)]
+    out, other = torch.zeros(s.n_rows, device=DEV), torch.zeros(s.n_rows, device=DEV)
+    base = torch.tensor([[[2.0, 3.0], [2.5, 1.0]]], device=DEV)
+    for value in (math.inf, -math.inf):              # either way this node gives nothing
+        lse = base.clone()
+        lse[0, 0] = value
+        F.fairkv_attn_weights(s.cache, s.lens, q, lse, out, 0.1)
+        F.fairkv_attn_weights(s.cache, s.lens, q[:, 1:].contiguous(), base[:, 1:].contiguous(), other, 0.1)
+        assert torch.equal(out[rows], other[rows])
+    lse = base.clone()
+    lse[0, 0, 0] = math.nan
+    F.fairkv_attn_weights(s.cache, s.lens, q, lse, out, 0.1)
+    assert bool(torch.isnan(out[rows[:-1]]).all()) and bool(torch.isfinite(out[rows[-1]]))      # the last row is the other node's own
+
+
 def test_a_packed_run_that_sticks_out_and_pages_that_are_none():
     s = Setup([[40, 50], [30, 20]], 0, 64)
     s.off[1] = s.n_rows - 20
