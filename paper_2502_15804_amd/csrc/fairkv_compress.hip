@@ -22,11 +22,12 @@ constexpr int32_t kMaxSlots = 65536;      // most compute units that a caller ma
 // Units of a group whose keys lie in a workgroup's LDS: four such workgroups of 512 threads share a CU's 160 KB, and two of 1024.
 constexpr int32_t kSmallCap = 120, kLargeCap = 256;
 
-// Tokens that a length can count: 2^31 - 2^16, so that what is added to a token's number does not wrap around.
+// Tokens that a length or a list can count: 2^31 - 2^16, so that what is added to a token's number does not wrap around.
+constexpr int32_t kMostTokens = INT32_MAX - 65535;
 int32_t max_len(const fairkv_cache *c)
 {
     const int64_t rows = c->n_rows < 1 ? 0 : c->pages ? static_cast<int64_t>(c->max_pages) * c->page_rows : c->n_rows;
-    return static_cast<int32_t>(std::min<int64_t>(rows, INT32_MAX - 65535));
+    return static_cast<int32_t>(std::min<int64_t>(rows, kMostTokens));
 }
 // Whether two runs of bytes share one.
 bool meet(const void *x, size_t nx, const void *y, size_t ny)
@@ -214,6 +215,7 @@ extern "C" int fairkv_evict(const fairkv_cache *c, const fairkv_cache *into, con
     }
     if (!keep || !n_keep || !len || !len_out || max_keep < 1 || n_slots < 1 || (weights == nullptr) != (weights_out == nullptr)) return FAIRKV_EINVAL;
     if (n_slots > kMaxSlots) return FAIRKV_EUNSUPPORTED;
+    if (max_keep > kMostTokens) return FAIRKV_EINVAL;
     if (!aligned(weights, 4) || !aligned(weights_out, 4) || (!into && weights_out != weights)) return FAIRKV_EINVAL;
     const int64_t pairs = static_cast<int64_t>(c->B) * c->Hkv;
     if (pairs > UINT32_MAX / 1024) return FAIRKV_EINVAL;

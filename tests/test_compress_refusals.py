@@ -92,6 +92,13 @@ def test_evict_refuses_caches_that_share_rows(kw):
     assert _evict(c, into=_cache(**kw), len_out=AT) == INVALID      # (the first is the cache itself: the same pool, and the same rows of it)
 
 
+@pytest.mark.parametrize("into", [None, _cache(k=1 << 50, v=1 << 51)])
+def test_evict_refuses_lists_whose_places_a_run_beyond_would_wrap(into):
+    out = 3 * AT if into is None else AT
+    for max_keep in (2**31 - 1, 2**31 - 65535):
+        assert _evict(_cache(), into=into, max_keep=max_keep, len_out=out) == INVALID
+
+
 def test_evict_refuses_weights_that_meet_those_that_are_read():
     c, other = _cache(k=FAR, v=FAR + (1 << 30)), _cache(k=FAR + (2 << 30), v=FAR + (3 << 30))
     for out in (8 * AT, 8 * AT + 396, 8 * AT - 396):
