@@ -9,7 +9,9 @@
 // columns 32 at a time:
 //     S[column][token] = q K^T         D / 16 instructions a tile of 32
 // A lane has one token (lane % 32) and 16 of the 32 columns, so a weight is added where it was computed; two lanes share a token.  Queries lie
-// in LDS, for all waves of the workgroup, CC columns at a time.
+// in LDS, for all waves of the workgroup, CC columns at a time.  Where fewer tiles are left than waves, several waves have one, other columns each, and one
+// of them adds up: 256 columns over 8 pairs of 1000 rows 12 us instead of 18, 1024 over 8 pairs of 2000 rows 38 instead of 72.  Columns are added 32 by 32 in one
+// order, so a weight is the same whichever waves have them.
 //
 // What bounds it (MI355X; times of a launch in a row of them).  Few columns: memory, 32 x 8 pairs of 4096 rows (bf16, heads of 128) 280 MB in 62 us
 // (4.5 TB/s), and 4 to 5 us until the first rows are there, which is all that one sequence of 8 pairs of 1024 rows costs (4.6 us).  Many columns: power.
@@ -53,10 +55,15 @@ __global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_we
     constexpr int ROWB = KV8 ? D : 2 * D, QROWB = 2 * D;      // bytes of a row of K, of a query
     constexpr int NP = ROWB / 32, NSL = D / 16, PPQ = QROWB / 16;
     constexpr bool kMany = NW == 16 && CC < FAIRKV_MAX_DRAFT * 16;      // a pair may have more columns; the others' launches have no more
+    // Tiles that several waves may have, each other columns: with up to 64 columns there are none, with all that LDS holds few.
+    constexpr bool kSplit = CC > 64;
+    constexpr int kShared = CC <= 256 ? NW / 2 : 2048 / CC;
+    constexpr int AHEAD = CC > 64 ? 4 : 1;                            // pieces of queries that a thread asks for at once
     typedef __attribute__((ext_vector_type(4))) uint32_t u4;
     __shared__ __attribute__((aligned(1024))) char qs[CC * QROWB];
     __shared__ __attribute__((aligned(16))) float minus_lse[CC];      // in log2 units
     __shared__ uint64_t sees[CC];                                     // of every column: the nodes that it sees
+    __shared__ float joins[kSplit ? kShared : 1][kSplit ? CC / 32 : 1][64];      // of tiles that several waves have, for every 32 columns
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, hi = lane >> 5;
     const int n_pairs = a.B * a.Hkv;
@@ -97,8 +104,12 @@ __global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_we
                 int some_columns = kMany ? min(CC, cols - c_from) : cols;
                 asm volatile("" : "+v"(some_columns));
                 const int n = __builtin_amdgcn_readfirstlane(some_columns);
-                const int tile = tile0 + turn * NW + wave;
-                const bool mine = turn * NW + wave < n_tiles;
+                // Where few tiles are left, 1 << shift waves have one, each every so many-th 32 of the columns.
+                const int tiles = min(NW, n_tiles - turn * NW);
+                int shift = 0;
+                while (kSplit && tiles <= kShared && tiles << (shift + 1) <= NW && 32 << shift < n) ++shift;
+                const int of_turn = wave >> shift, tile = tile0 + turn * NW + of_turn, part = wave & ((1 << shift) - 1);
+                const bool mine = of_turn < tiles;
                 const int32_t t0 = tile * TOK;
                 // ---- rows of K, requested before the queries; where there is none the cache's first row stands in: what comes of it is not stored ----
                 const int32_t t = t0 + l32;
@@ -112,13 +123,20 @@ __global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_we
                     old = row >= 0 ? a.out[row] : 0.f;
                 else
                     old = a.decay != 0.f && row >= 0 && t < base ? a.weights[row] * a.decay : 0.f;
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
                 if (turn == 0) {
                     __syncthreads();
-                    for (int x = threadIdx.x; x < n * PPQ; x += NT) {
-                        const int c = x / PPQ, p = x % PPQ, node = (chunk * CC + c) / a.G, g = chunk * CC + c - node * a.G;
-                        const size_t at = ((static_cast<size_t>(b) * a.q_len + node) * a.Hq + h * a.G + g) * QROWB;
-                        *reinterpret_cast<u4 *>(qs + c * QROWB + ((p ^ swizzle(c)) * 16)) = *reinterpret_cast<const u4 *>(a.q + at + p * 16);
+                    for (int x0 = threadIdx.x; x0 < n * PPQ; x0 += AHEAD * NT) {      // past the last piece: that one again
+                        u4 piece[AHEAD];
+#pragma unroll
+                        for (int u = 0; u < AHEAD; ++u) {
+                            const int x = min(x0 + u * NT, n * PPQ - 1), c = x / PPQ, p = x % PPQ, node = (chunk * CC + c) / a.G, g = chunk * CC + c - node * a.G;
+                            piece[u] = *reinterpret_cast<const u4 *>(a.q + ((static_cast<size_t>(b) * a.q_len + node) * a.Hq + h * a.G + g) * QROWB + p * 16);
+                        }
+#pragma unroll
+                        for (int u = 0; u < AHEAD; ++u) {
+                            const int x = min(x0 + u * NT, n * PPQ - 1), c = x / PPQ, p = x % PPQ;
+                            *reinterpret_cast<u4 *>(qs + c * QROWB + ((p ^ swizzle(c)) * 16)) = piece[u];
+                        }
                     }
                     for (int c = threadIdx.x; c < n; c += NT) {
                         const int node = (chunk * CC + c) / a.G, g = chunk * CC + c - node * a.G;
@@ -128,7 +146,7 @@ __global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_we
                     }
                     __syncthreads();
                 }
-                if (!mine) continue;
+                if (!mine && shift == 0) continue;
                 bf16x8_t k[NSL];
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
@@ -140,7 +158,8 @@ __global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_we
                     }
                 }
                 // 32 columns from c0.  some: not all of them are there; draft: some of the tile's tokens are the queries' own, and not seen by all
-                auto columns = [&](int c0, auto some, auto draft) __attribute__((always_inline)) {
+                float w = 0.f;
+                auto columns = [&](int c0, auto some, auto draft, auto joined) __attribute__((always_inline)) {
                     constexpr bool kSome = decltype(some)::value, kDraft = decltype(draft)::value;
                     const int c = kSome ? min(c0 + l32, n - 1) : c0 + l32;      // past the last one: that one again, and it does not count
                     bf16x8_t q[NSL];
@@ -156,6 +175,7 @@ __global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_we
                     for (int s = 0; s < NSL; ++s) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q[s], k[s], z, 0, 0, 0);
                     const int32_t j = t0 + l32 - base;                          // of the queries' own tokens, below 0 in front of them
                     const uint32_t *words = reinterpret_cast<const uint32_t *>(sees) + (j >= 32 ? 1 : 0);
+                    float s4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int r4 = 0; r4 < 4; ++r4) {
                         if (kSome && c0 + 8 * r4 >= n) break;
@@ -168,17 +188,33 @@ __global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_we
                             bool counts = true;
                             if constexpr (kSome) counts = cr < n;
                             if constexpr (kDraft) counts = counts && (j < 0 || (words[2 * min(cr, n - 1)] >> (j & 31) & 1) != 0);
-                            sum[x] += counts ? e : 0.f;
+                            s4[x] = r4 == 0 ? (counts ? e : 0.f) : s4[x] + (counts ? e : 0.f);
                         }
                     }
+                    const float of_32 = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                    if constexpr (decltype(joined)::value)
+                        joins[of_turn][c0 / 32][lane] = of_32;
+                    else
+                        w += of_32;
                 };
-                if (t0 + TOK > base) {
-                    for (int c0 = 0; c0 < n; c0 += 32) columns(c0, std::true_type{}, std::true_type{});
-                } else {
-                    for (int c0 = 0; c0 + 32 <= n; c0 += 32) columns(c0, std::false_type{}, std::false_type{});
-                    if (n % 32 != 0) columns(n / 32 * 32, std::true_type{}, std::false_type{});
+                auto all_columns = [&](int c0, int step, auto joined) __attribute__((always_inline)) {
+                    if (t0 + TOK > base) {
+                        for (; c0 < n; c0 += step) columns(c0, std::true_type{}, std::true_type{}, joined);
+                    } else {
+                        for (; c0 + 32 <= n; c0 += step) columns(c0, std::false_type{}, std::false_type{}, joined);
+                        if (c0 < n) columns(c0, std::true_type{}, std::false_type{}, joined);
+                    }
+                };
+                if (!kSplit || shift == 0)
+                    all_columns(0, 32, std::false_type{});
+                else if (mine)
+                    all_columns(part * 32, 32 << shift, std::integral_constant<bool, kSplit>{});
+                if (kSplit && shift > 0) {            // the same for all waves
+                    __syncthreads();
+                    if (!mine || part > 0) continue;
+                    for (int x = 0; x * 32 < n; ++x) w += joins[of_turn][x][lane];      // in the order in which one wave adds
                 }
-                const float w = (sum[0] + sum[1]) + (sum[2] + sum[3]), both = w + __shfl_xor(w, 32);
+                const float both = w + __shfl_xor(w, 32);
                 if (hi == 0 && row >= 0) a.out[row] = old + both;
             }
         }

@@ -128,6 +128,29 @@ def test_weights(case):
     assert np.array_equal(got[rest], old[rest].astype(np.float64), equal_nan=True)
 
 
+@pytest.mark.parametrize("D,G,n,ragged", [(128, 8, 9, False), (128, 5, 40, True), (128, 8, 33, True), (64, 16, 64, True), (128, 16, 64, False), (64, 8, 16, False)])
+def test_weights_are_the_same_whoever_computes_them(D, G, n, ragged):
+    """A sequence by itself and beside others, over few workgroups and many: tiles that one wave has or several, all bits the same."""
+    lens = np.array([[n + 1, 700], [33 + n, 290], [64, 1500]])
+    s = Setup(lens, 5, D, page=16, seed=n)
+    gen = torch.Generator().manual_seed(n)
+    q = torch.randn(3, n, 2 * G, D, generator=gen).to(torch.bfloat16).to(DEV)
+    lse = (3 + torch.rand(3, n, 2 * G, generator=gen)).to(DEV)
+    n_new = I32([n, n // 2, n - 1]) if ragged else None
+    want = None
+    for n_slots in (1, 2, 13, 256, 1000):
+        out = torch.full((s.n_rows,), 0.5, device=DEV)
+        F.fairkv_attn_weights(s.cache, s.lens, q, lse, out, 0.1, n_new=n_new, n_slots=n_slots)
+        want = out if want is None else want
+        assert torch.equal(out, want)
+    out = torch.full((s.n_rows,), 0.5, device=DEV)
+    for b in range(3):
+        alone = torch.zeros_like(s.lens)
+        alone[b] = s.lens[b]
+        F.fairkv_attn_weights(s.cache, alone, q, lse, out, 0.1, n_new=n_new)
+    assert torch.equal(out, want)
+
+
 def test_rows_that_are_no_numbers_count_where_they_are_seen():
     s = Setup([[70, 40]], 2, 128, page=16)
     n, Hq = 4, 4
