@@ -117,7 +117,7 @@ SelectShape select_shape(const fairkv_cache *c, int32_t shared, int32_t n_slots)
 }
 // What has to be zero when a call begins lies in the first third of a workspace, whatever the call's shape, and the rest in the others.
 size_t start_bytes(const SelectShape &s) { return sizeof(SelectStart) * s.slots; }
-size_t other_bytes(const SelectShape &s) { return sizeof(SelectSlot) * s.slots + sizeof(SelectShare) * s.shares + (sizeof(int2) + kBlockRows * sizeof(uint32_t)) * s.max_blocks; }
+size_t other_bytes(const SelectShape &s) { return sizeof(SelectSlot) * s.slots + sizeof(SelectShare) * s.shares + (sizeof(int32_t) + kLastBins * sizeof(uint16_t) + kBlockRows * sizeof(uint32_t)) * s.max_blocks; }
 size_t third_of(size_t workspace_bytes) { return workspace_bytes / 3 / 256 * 256; }
 size_t select_bytes(const SelectShape &s) { return 3 * ((std::max(start_bytes(s), (other_bytes(s) + 1) / 2) + 256) / 256 * 256); }
 
@@ -181,8 +181,9 @@ extern "C" int fairkv_select(const fairkv_cache *c, const fairkv_selection *s, c
     a.starts = static_cast<SelectStart *>(workspace);
     a.slots = reinterpret_cast<SelectSlot *>(others);
     a.shares = reinterpret_cast<SelectShare *>(others + sizeof(SelectSlot) * shape.slots);
-    a.blocks = reinterpret_cast<int2 *>(others + sizeof(SelectSlot) * shape.slots + sizeof(SelectShare) * shape.shares);
-    a.keys = reinterpret_cast<uint32_t *>(a.blocks + shape.max_blocks);
+    a.above = reinterpret_cast<int32_t *>(others + sizeof(SelectSlot) * shape.slots + sizeof(SelectShare) * shape.shares);
+    a.upto = reinterpret_cast<uint32_t *>(a.above + shape.max_blocks);
+    a.keys = a.upto + shape.max_blocks * (kLastBins / 2);
     const dim3 grid(static_cast<unsigned>(shape.shares)), first(static_cast<unsigned>(groups + shape.shares)), threads(kLargeThreads);
     if (a.half > 0)
         hipLaunchKernelGGL((fairkv_select_first_kernel<kSmallCap, true>), first, threads, 0, st, a);
@@ -191,7 +192,6 @@ extern "C" int fairkv_select(const fairkv_cache *c, const fairkv_selection *s, c
     hipLaunchKernelGGL(fairkv_select_large_kernel<1>, grid, threads, 0, st, a);
     hipLaunchKernelGGL(fairkv_select_large_kernel<2>, grid, threads, 0, st, a);
     hipLaunchKernelGGL(fairkv_select_large_kernel<3>, grid, threads, 0, st, a);
-    hipLaunchKernelGGL(fairkv_select_large_kernel<4>, grid, threads, 0, st, a);
     return launched();
 }
 

@@ -10,13 +10,14 @@
 // share some digits stay, the others need not be looked at.
 //
 // A group of up to `cap` units of 64 rows is one workgroup's, which reads its weights once and has its keys in LDS.  Rows of larger groups are dealt to
-// the whole GPU in blocks of 4096: a kernel makes keys of them, in order, and counts the first digit, two count the others, one counts what stays of
-// every block, one lists it.  Every list ascends and no sum depends on who comes first: counts are whole numbers.
+// the whole GPU in blocks of 4096: a kernel makes keys of them, in order, and counts the first digit, two count the others, the second of them block by
+// block, and one lists what stays.  Every list ascends and no sum depends on who comes first: counts are whole numbers.
 //
 // What bounds it (MI355X; times of a call in a row of them): not its bytes (a million weights are 4 MB, 1 us) but one thing after the other.  A workgroup's
 // group: 9 us from lengths over pages, weights, three digits and ties to the list, 16 us where four of them share a compute unit's issue slots (128 x 8 pairs of
-// 1024 rows; 8 pairs of 1024 rows in one group 9.4).  A large one: five kernels of 3 to 7 us each, of which the first one takes 12, for it finds the groups'
-// blocks and reads the weights (one group of 8 pairs of 131072 rows 30 us; 16 groups of 8 pairs of 16000 rows 34, 48 where every kernel read the weights).
+// 1024 rows; 8 pairs of 1024 rows in one group 9.4).  A large one: four kernels of 4 to 8 us each, of which the first one takes 12, for it finds the groups'
+// blocks and reads the weights (one group of 8 pairs of 131072 rows 27 us; 16 groups of 8 pairs of 16000 rows 32, 34 where a fifth kernel counted what stays of
+// every block, 48 where every kernel read the weights).
 #pragma once
 #include "cache_rows.h"
 #include "line.h"
@@ -24,7 +25,7 @@
 namespace fairkv {
 
 constexpr int kDigits = 3;
-constexpr int kDigitShift[kDigits] = {21, 10, 0}, kBins = 2048;      // bins of a digit, the last digit's half as many
+constexpr int kDigitShift[kDigits] = {21, 10, 0}, kBins = 2048, kLastBins = 1024;      // bins of a digit, and of the last one
 constexpr int kBlockRows = 4096;          // of a large group
 constexpr int kMaxPairs = 64;             // of a group that one workgroup has
 constexpr int kMostHalf = 31;             // of the window
@@ -42,7 +43,7 @@ struct SelectStart {                      // of the first step, which finds it 0
 };
 struct SelectSlot {
     int32_t bins[kDigits - 1][kBins];     // of the other digits: the first step clears them
-    SelectFound found[kDigits];
+    SelectFound found[kDigits - 1];
 };
 struct SelectShare {                      // of a workgroup: its blocks in the line, and of the group that the first of them is in its first block and their number
     int64_t left, block, at, group_at, group_blocks;      // left: how many; block: the first one's number in its pair
@@ -56,7 +57,8 @@ struct SelectArgs {
     SelectStart *starts;                  // null: no group can be large
     SelectSlot *slots;
     uint32_t *keys;                       // [max_blocks][kBlockRows]: what the first step makes of the rows
-    int2 *blocks;                         // [max_blocks]: rows of a block that stay whatever ties do, and ties
+    int32_t *above;                       // [max_blocks]: rows of a block that stay whatever the last digit is
+    uint32_t *upto;                       // [max_blocks][kLastBins], 16 bits each: candidates with the digits found before whose last digit is this one or more
     SelectShare *shares;                  // of the large groups' workgroups
     int64_t max_blocks;
     int32_t n_pairs, n_groups, max_len, max_keep, half, sink, recent, per_group, cap, min_blocks;      // per_group: pairs of a group
@@ -121,7 +123,7 @@ __device__ __forceinline__ void count_digit(int32_t *bins, uint32_t key, int dig
 {
     const int shift = kDigitShift[digit];
     // all digits in front are the ones found
-    if (counts && (digit == 0 || (key ^ least) >> kDigitShift[digit > 0 ? digit - 1 : 0] == 0)) atomicAdd(&bins[key >> shift & (kBins - 1) & (digit == 2 ? 1023 : ~0)], 1);
+    if (counts && (digit == 0 || (key ^ least) >> kDigitShift[digit > 0 ? digit - 1 : 0] == 0)) atomicAdd(&bins[key >> shift & (digit == kDigits - 1 ? kLastBins - 1 : kBins - 1)], 1);
 }
 
 // Weights of a thread's KPT rows, all on their way at once: first the pages' numbers, then the weights, with addresses that are always some of the
@@ -152,16 +154,6 @@ __device__ __forceinline__ void load_values(const SelectArgs &a, int pair, uint3
         value[i] = state[i] == 1 ? fmaxf(value[i], -INFINITY) : -INFINITY;      // a NaN is as low
     }
 }
-// How many of the workgroup's lanes' bits are set in all, added to *sum in LDS.
-template <int KPT, class Is>
-__device__ __forceinline__ void add_rows(int32_t *sum, Is is)
-{
-    int32_t n = 0;
-#pragma unroll
-    for (int i = 0; i < KPT; ++i) n += __builtin_popcountll(__builtin_amdgcn_ballot_w64(is(i)));
-    if ((threadIdx.x & 63) == 0 && n) atomicAdd(sum, n);
-}
-
 // Rows i NT + threadIdx.x, i < KPT, of which bit i of a thread's x says whether it is one of some: how many of them are in front of a row.
 // count_rows is called by all threads and ends with a barrier; another one stands between the last rows_before and the next count_rows.
 template <int NT, int KPT>
@@ -401,17 +393,19 @@ struct LargeSpace {
     int32_t bins[kBins];
     int32_t counts[kBlockRows / 64];
     unsigned long long sums[5];
-    int32_t total;
+    int32_t total, equals[8], aboves[8];
 };
 constexpr int kLargeThreads = 512;
 
-// Workgroup `slot_index` of n: STEP 0 .. 2: a digit is counted; 3: what stays of every block; 4: the lists.  The first step finds the workgroup's share of
+constexpr int kLists = kDigits;           // the last step
+
+// Workgroup `slot_index` of n: STEP 0 .. 2: a digit is counted, the last one in every block; 3: the lists.  The first step finds the workgroup's share of
 // the line, the others have it from there.
 template <int STEP>
 __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index, int n_slots, LargeSpace<STEP> &m)
 {
     constexpr int NT = kLargeThreads, KPT = kBlockRows / NT;
-    constexpr bool kCounts = STEP < kDigits;
+    constexpr bool kCounts = STEP < kDigits - 1, kBlocks = STEP == kDigits - 1;      // a digit of the workgroup's blocks of a group, of every block
     auto &raw = m.raw;
     auto &bins = m.bins;
     auto &counts = reinterpret_cast<int32_t (&)[KPT][NT / 64]>(m.counts);
@@ -430,7 +424,7 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
     } else {
         share = a.shares[slot_index];
     }
-    if (share.left < 0 && STEP == kDigits + 1 && slot_index == 0)
+    if (share.left < 0 && STEP == kLists && slot_index == 0)
         for (int p = threadIdx.x; p < a.n_pairs; p += NT)
             if (blocks_of(p) > 0) {
                 a.n_keep[p] = -1;
@@ -442,13 +436,13 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
     SelectStart *start = nullptr;
     SelectSlot *slot = nullptr;
     SelectFound f{0, 0, 0};
-    int32_t protected_rows = 0;
+    int32_t protected_rows = 0, last = -1, last_ties = -1;      // the last digit of what stays, and that of ties: -1 where there is none
 
     auto end_group = [&]() __attribute__((always_inline)) {
         if constexpr (kCounts) {
             __syncthreads();
             for (int i = threadIdx.x; i < kBins; i += NT)
-                if (bins[i]) atomicAdd(STEP == 0 ? &start->bins[i] : &slot->bins[STEP > 0 ? STEP - 1 : 0][i], bins[i]);
+                if (bins[i]) atomicAdd(STEP == 0 ? &start->bins[i] : &slot->bins[0][i], bins[i]);
             if constexpr (STEP == 0) {
                 const int64_t n = wave_upto(static_cast<int64_t>(protected_rows));
                 if (lane == 63 && n) atomicAdd(&start->protected_rows, static_cast<unsigned long long>(n));
@@ -470,20 +464,22 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
             f = {max(static_cast<int64_t>(a.budget[group]) - static_cast<int64_t>(start->protected_rows), static_cast<int64_t>(0)), 0, 0};
             if (f.need == 0) f = {0, kProtected - 1, 1};
         }
-        if constexpr (STEP > 1) f = slot->found[STEP == kDigits + 1 ? kDigits - 1 : STEP - 2];
-        if constexpr (STEP >= 1 && STEP <= kDigits) {
+        if constexpr (STEP > 1) f = slot->found[STEP - 2];
+        if constexpr (STEP >= 1) {
+            last = last_ties = -1;
             if (!f.done) {
-                const BinFound<int64_t> b = find_bin<NT>(f.need, [&](int x) { return STEP == 1 ? start->bins[x] : slot->bins[STEP > 1 ? STEP - 2 : 0][x]; });
+                const BinFound<int64_t> b = find_bin<NT>(f.need, [&](int x) { return STEP == 1 ? start->bins[x] : STEP == kLists && x >= kLastBins ? 0 : slot->bins[STEP > 1 ? STEP - 2 : 0][x]; });
                 if (b.need == 0) {        // there are no so many candidates: all of them stay
                     f = {0, 0, 1};
                 } else {
                     f.need = b.need, f.least |= static_cast<uint32_t>(b.bin) << kDigitShift[STEP - 1];
-                    if (f.need == b.in_bin) f = {0, f.least - 1, 1};      // all that share these digits stay
+                    last = b.bin + 1, last_ties = b.bin;
+                    if (f.need == b.in_bin) f = {0, f.least - 1, 1}, last = b.bin, last_ties = -1;      // all that share these digits stay
                 }
             }
         }
         if (at == group_at) {             // this workgroup has the group's first block
-            if constexpr (STEP >= 1 && STEP <= kDigits)
+            if constexpr (STEP >= 1 && STEP < kDigits)
                 if (threadIdx.x == 0) slot->found[STEP - 1] = f;
             if constexpr (STEP == 0)
                 for (int i = threadIdx.x; i < (kDigits - 1) * kBins; i += NT) (&slot->bins[0][0])[i] = 0;
@@ -492,13 +488,19 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
                 if (threadIdx.x == 0) start->protected_rows = 0;
             }
         }
-        if constexpr (kCounts) {
+        if constexpr (kCounts || kBlocks) {
             for (int i = threadIdx.x; i < kBins; i += NT) bins[i] = 0;
             protected_rows = 0;
             __syncthreads();
         }
     };
 
+    // Of a block: rows that stay without being ties, and ties.
+    auto counts_of = [&](int64_t x) __attribute__((always_inline)) {
+        const uint16_t *upto = reinterpret_cast<const uint16_t *>(a.upto + x * (kLastBins / 2));
+        const int32_t more = last >= 0 && last < kLastBins ? upto[last] : 0;
+        return make_int2(a.above[x] + more, last_ties >= 0 ? upto[last_ties] - more : 0);
+    };
     auto blocks_of_large = [&](int32_t len) __attribute__((always_inline)) { return max(1, (len + kBlockRows - 1) / kBlockRows); };
     int32_t len = share.len;
     for (int64_t left = share.left; left > 0; --left, ++block, ++at) {
@@ -537,12 +539,12 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
             if (group >= 0) end_group();
             begin_group();
         }
-        if ((STEP == 1 || STEP == 2) && f.done) continue;
+        if (STEP == 1 && f.done) continue;
         // what stays of other blocks: in front of this one, and behind it where it is the pair's first (the first of them ahead of their use)
         const int64_t pair_at = at - block, pair_end = pair_at + blocks_of_large(len);
         const int64_t look_from = f.need > 0 ? group_at : pair_at, look_to = block == 0 ? pair_end : at;
         int2 look = make_int2(0, 0);
-        if (STEP == kDigits + 1 && look_from + static_cast<int64_t>(threadIdx.x) < look_to) look = a.blocks[look_from + threadIdx.x];
+        if (STEP == kLists && look_from + static_cast<int64_t>(threadIdx.x) < look_to) look = counts_of(look_from + threadIdx.x);
         if constexpr (STEP == 0) {
             if (a.half > 0) {
                 __syncthreads();              // the windows of the block before have been looked at
@@ -569,29 +571,46 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
             for (int i = 0; i < KPT; ++i) count_digit(bins, key[i], STEP, f.least, key[i] != kNone && key[i] != kProtected);
             continue;
         }
+        if constexpr (kBlocks) {
+            const uint32_t most = f.done ? f.least : f.least | (kLastBins - 1);      // what is larger stays
+            int32_t above = 0;
+#pragma unroll
+            for (int i = 0; i < KPT; ++i) {
+                above += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[i] > most));
+                count_digit(bins, key[i], STEP, f.least, !f.done && key[i] != kNone && key[i] != kProtected);
+            }
+            __syncthreads();
+            // two bins of a thread, from the top; they are 0 again for the next block
+            const int wave = threadIdx.x >> 6, bin = kLastBins - 2 - 2 * static_cast<int>(threadIdx.x);
+            const int32_t high = bins[bin + 1], low = bins[bin], sum = wave_upto(high + low);
+            bins[bin + 1] = bins[bin] = 0;
+            if (lane == 63) m.equals[wave] = sum, m.aboves[wave] = above;
+            __syncthreads();
+            int32_t before = sum - high - low, all_above = 0;
+#pragma unroll
+            for (int w = 0; w < NT / 64; ++w) before += w < wave ? m.equals[w] : 0, all_above += m.aboves[w];
+            if (!f.done) {
+                a.upto[at * (kLastBins / 2) + bin / 2] = static_cast<uint32_t>(before + high + low) | static_cast<uint32_t>(before + high) << 16;
+                if (high) atomicAdd(&slot->bins[1][bin + 1], high);
+                if (low) atomicAdd(&slot->bins[1][bin], low);
+            }
+            if (threadIdx.x == 0) a.above[at] = all_above;
+            continue;
+        }
         uint32_t stays = 0, equal = 0;
 #pragma unroll
         for (int i = 0; i < KPT; ++i) {
             stays |= (key[i] > f.least ? 1u : 0u) << i;
             equal |= (f.need > 0 && key[i] == f.least ? 1u : 0u) << i;
         }
-        if constexpr (STEP == kDigits) {
-            __syncthreads();
-            if (threadIdx.x < 2) sums[threadIdx.x] = 0;
-            __syncthreads();
-            add_rows<KPT>(reinterpret_cast<int32_t *>(&sums[0]), [&](int i) { return (stays >> i & 1) != 0; });      // low halves
-            add_rows<KPT>(reinterpret_cast<int32_t *>(&sums[1]), [&](int i) { return (equal >> i & 1) != 0; });
-            __syncthreads();
-            if (threadIdx.x == 0) a.blocks[at] = make_int2(static_cast<int>(sums[0]), static_cast<int>(sums[1]));
-        }
-        if constexpr (STEP == kDigits + 1) {
+        if constexpr (STEP == kLists) {
             // ties in front of the pair, and of the block; rows in front of the block that stay anyhow; both of the whole pair
             __syncthreads();
             if (threadIdx.x < 5) sums[threadIdx.x] = 0;
             __syncthreads();
             unsigned long long s[5] = {0, 0, 0, 0, 0};
             for (int64_t x = look_from + threadIdx.x; x < look_to; x += NT) {
-                const int2 n = x < look_from + NT ? look : a.blocks[x];
+                const int2 n = x < look_from + NT ? look : counts_of(x);
                 if (x < pair_at) s[0] += n.y;
                 if (x < at) s[1] += n.y;
                 if (x >= pair_at && x < at) s[2] += n.x;
