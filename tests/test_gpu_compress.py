@@ -324,6 +324,31 @@ def test_long_pairs(lens, shared, n_slots, kind):
     _check_select(s, w, np.rint(total * 0.8), shared, 1, 0, 64, n_slots=n_slots)
 
 
+@pytest.mark.parametrize("pool", [1, 3])
+def test_groups_of_as_many_rows_as_a_workgroup_has_and_of_more(pool):
+    s = Setup([[7616], [7680], [7681], [10239], [10240], [10241], [12289], [30000], [1]], 0, 64, page=64)
+    w = _some_weights(s.n_rows, 6, "near")
+    for part in (0.03, 0.7):
+        _check_select(s, w, np.rint(s.lens_h * part), False, pool, 2, 16)
+    pairs = Setup([[5000, 5240], [5001, 5240], [1, 7680], [40, 7700]], 0, 64, page=64, seed=1)
+    _check_select(pairs, _some_weights(pairs.n_rows, 7, "near"), np.rint(pairs.lens_h.sum(1) * 0.4), True, pool, 2, 16)
+
+
+@pytest.mark.parametrize("last", [0, 1, 511, 1022, 1023])
+def test_weights_that_differ_in_their_last_bits(last):
+    """All in one bin of the first two digits; the budget ends at ties, in front of them and behind them."""
+    s = Setup([[9000, 13000], [30, 200]], 0, 64, page=64)
+    rng = np.random.default_rng(last)
+    bits = rng.integers(0, 1024, s.n_rows)
+    bits[rng.random(s.n_rows) < 0.3] = last          # ties
+    w = (np.float32(1.0).view(np.uint32) + bits.astype(np.uint32)).view(np.float32)
+    at = np.array([s.row(p, t) for p in (0, 1) for t in range(int(s.lens_h[0, p]))])
+    above, ties = int((bits[at] > last).sum()), int((bits[at] == last).sum())
+    for budget in (above + 1, above + ties // 2, above + ties, above + ties + 1, max(above, 1)):
+        _check_select(s, w, np.array([budget, 50]), True)
+    _check_select(s, w, np.rint(s.lens_h * 0.5), False)
+
+
 @pytest.mark.parametrize("shared", [False, True])
 def test_more_heads_than_a_workgroup_keeps_in_mind(shared):
     rng = np.random.default_rng(2)
