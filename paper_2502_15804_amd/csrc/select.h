@@ -261,8 +261,16 @@ __device__ __forceinline__ void select_group(const SelectArgs &a, int group, Gro
             const int p = pair_of(unit);
             const int32_t at = unit * 64 + lane, lo = __builtin_amdgcn_readlane(begins, p) * 64, hi = __builtin_amdgcn_readlane(ends, p) * 64 - 1;
             float x = raw[at];
-#pragma unroll 4
-            for (int32_t d = 1; d <= a.half; ++d) x = fmaxf(x, fmaxf(raw[max(lo, at - d)], raw[min(hi, at + d)]));
+            for (int32_t d0 = 1; d0 <= a.half; d0 += 4) {      // eight reads at once: past the window's end those of its end again
+                float y[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int32_t d = min(d0 + i, a.half);
+                    y[2 * i] = raw[max(lo, at - d)], y[2 * i + 1] = raw[min(hi, at + d)];
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x = fmaxf(x, y[i]);
+            }
             if (keys[at] == 1) {
                 keys[at] = order_of(x);
                 atomicAdd(&bins[order_of(x) >> kDigitShift[0]], 1);
