@@ -122,7 +122,9 @@ SelectShape select_shape(const fairkv_cache *c, int32_t shared, int32_t pool, in
 size_t start_bytes(const SelectShape &s) { return sizeof(SelectStart) * s.slots; }
 size_t other_bytes(const SelectShape &s) { return sizeof(SelectSlot) * s.slots + sizeof(SelectShare) * s.shares + (sizeof(int32_t) + kLastBins * sizeof(uint16_t) + kBlockRows * sizeof(uint32_t)) * s.max_blocks; }
 size_t third_of(size_t workspace_bytes) { return workspace_bytes / 3 / 256 * 256; }
-size_t select_bytes(const SelectShape &s) { return 3 * ((std::max(start_bytes(s), (other_bytes(s) + 1) / 2) + 256) / 256 * 256); }
+size_t shape_bytes(const SelectShape &s) { return 3 * ((std::max(start_bytes(s), (other_bytes(s) + 1) / 2) + 256) / 256 * 256); }
+// The same for every window: one of more than one row has the smaller cap, which takes more.
+size_t select_bytes(const fairkv_cache *c, int32_t shared, int32_t n_slots) { return shape_bytes(select_shape(c, shared, 2, n_slots)); }
 
 template <int NT, int UNITS>
 void launch_select(const SelectArgs &a, unsigned groups, hipStream_t st)
@@ -138,13 +140,13 @@ void launch_select(const SelectArgs &a, unsigned groups, hipStream_t st)
 extern "C" size_t fairkv_select_workspace_bytes(const fairkv_cache *c, int32_t shared, int32_t n_slots)
 {
     if (check_cache(c) != FAIRKV_OK || n_slots < 1 || n_slots > kMaxSlots || shared < 0 || shared > 1) return 0;
-    return select_bytes(select_shape(c, shared, 2, n_slots));      // a larger cap takes less
+    return select_bytes(c, shared, n_slots);
 }
 
 extern "C" int fairkv_select_workspace_reset(void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     if (!workspace || !aligned(workspace, 16)) return FAIRKV_EINVAL;
-    if (workspace_bytes < select_bytes(SelectShape{})) return FAIRKV_EWORKSPACE;
+    if (workspace_bytes < shape_bytes(SelectShape{})) return FAIRKV_EWORKSPACE;
     zero_words(workspace, workspace_bytes / 3 / sizeof(uint32_t), static_cast<hipStream_t>(hip_stream));
     return launched();
 }
@@ -161,7 +163,7 @@ extern "C" int fairkv_select(const fairkv_cache *c, const fairkv_selection *s, c
     const int64_t pairs = static_cast<int64_t>(c->B) * c->Hkv, groups = s->shared ? c->B : pairs;
     if (groups > kMaxGroupsOfCall) return FAIRKV_EINVAL;
     const SelectShape shape = select_shape(c, s->shared, s->pool, n_slots);
-    if (!workspace || workspace_bytes < select_bytes(shape)) return FAIRKV_EWORKSPACE;
+    if (!workspace || workspace_bytes < select_bytes(c, s->shared, n_slots)) return FAIRKV_EWORKSPACE;
     SelectArgs a{};
     a.rows = row_map(c);
     a.weights = weights, a.len = len, a.budget = s->budget, a.keep = keep, a.n_keep = n_keep, a.bad = bad;
