@@ -555,7 +555,7 @@ int fairkv_select(const fairkv_cache *cache, const fairkv_selection *s, const fl
  * A pair is left alone and counted in *bad, its length kept (into another cache: 0, and what is in its rows there says nothing), if n_keep[p] is not in
  * 0 .. max_keep (in place: or its length; else: or its room there), an entry not in 0 .. len - 1, not ascending (in place), or a row outside its cache.
  * Pages behind ceil(len_out / page_rows) hold no token of a pair any more.  Packed rows stay where the pair's run begins.
- * Enqueues one kernel, and a second one if len_out is len; no synchronisation.  FAIRKV_EINVAL also: more than 2^22 - 1 pairs, max_keep
+ * Enqueues one kernel, and a second one if len_out is len; no synchronisation.  FAIRKV_EINVAL also: more than 2^20 pairs, max_keep
  * > 2^31 - 2^16. */
 int fairkv_evict(const fairkv_cache *cache, const fairkv_cache *into, const int32_t *keep, int32_t max_keep, const int32_t *n_keep,
                  const int32_t *len, int32_t *len_out, const float *weights, float *weights_out, int32_t *bad, int32_t n_slots,

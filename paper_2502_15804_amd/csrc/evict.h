@@ -6,7 +6,8 @@
 //
 // Measured (MI355X): into another cache 128 x 8 pairs of 4096 8-bit rows halved, 1.02 GB read and written, 241 us (4.25 TB/s; a plain copy has 4.9); 16 x 8 pairs of
 // 16000 bf16 rows to a sixteenth 28 us (4.4 TB/s); 8 pairs of 1024 halved 5.4 us, most of it the way from lists over pages to rows.  In place the order holds it
-// back: the same 385, 50 and 9 us, 8 pairs of 131072 rows to a third 312 us (1 TB/s, 64 workgroups; 955 with 4 waves each and nothing asked for ahead).
+// back: the same 300, 34 and 8 us, 8 pairs of 131072 rows to a third 238 us (1.3 TB/s, 128 workgroups; 312 with 64 of 64 bytes each that went round the XCDs, 955 with 4
+// waves each and nothing asked for ahead).
 #pragma once
 #include "cache_rows.h"
 #include "common.h"
@@ -28,12 +29,13 @@ struct EvictArgs {
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_row_t;
 
-// Whether list entry i is what it has to be: a row of the pair that is in the cache, and a place for it; in place also behind the entry before.
-__device__ __forceinline__ bool entry_ok(const EvictArgs &a, int pair, int32_t len, const int32_t *keep, int32_t i)
+// Whether the pair's token t >= 0 has a row in the cache, asked for without a branch.
+__device__ __forceinline__ bool has_row(const RowMap &m, int pair, int32_t t)
 {
-    const int32_t t = keep[i];
-    if (t < 0 || t >= len || a.from.row(pair, t) < 0 || a.to.row(pair, i) < 0) return false;
-    return a.cap_to || i == 0 || t > keep[i - 1];
+    if (!m.pages) return m.row(pair, t) >= 0;
+    const int32_t page = t >> m.page_shift;
+    const bool in_pool = m.row_of_page(m.pages[static_cast<int64_t>(pair) * m.max_pages + min(page, m.max_pages - 1)], t) >= 0;
+    return in_pool && page < m.max_pages;
 }
 // Whether a pair's list can be one, before its entries are looked at.
 __device__ __forceinline__ bool list_ok(const EvictArgs &a, int pair, int32_t len, int32_t n)
@@ -54,9 +56,22 @@ __device__ __forceinline__ ListFound whole_list(const EvictArgs &a, int pair, in
         const int32_t *keep = a.keep + static_cast<int64_t>(pair) * a.max_keep;
         bool ok = true;
         int32_t first = n;
-        for (int32_t i = threadIdx.x; i < n; i += NT) {
-            ok = ok && entry_ok(a, pair, len, keep, i);
-            if (keep[i] != i) first = min(first, i);
+        // An entry is a row of the pair that is in the cache, with a place for it, and in place it is behind the entry before.  Four at once: past the last
+        // one that one again.
+        for (int32_t i0 = threadIdx.x; i0 < n; i0 += 4 * NT) {
+            int32_t t[4], before[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int32_t i = min(i0 + u * NT, n - 1);
+                t[u] = keep[i], before[u] = a.cap_to || i == 0 ? -1 : keep[i - 1];
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int32_t i = min(i0 + u * NT, n - 1);
+                const bool there = has_row(a.from, pair, max(t[u], 0)), place = has_row(a.to, pair, i);
+                ok = ok && (t[u] > before[u] || a.cap_to) && t[u] >= 0 && t[u] < len && there && place;
+                if (t[u] != i) first = min(first, i);
+            }
         }
         if (!ok) found->ok = 0;
         if (first < n) atomicMin(&found->first, first);
@@ -145,14 +160,17 @@ __global__ __launch_bounds__(256) void fairkv_evict_into_kernel(EvictArgs a)
 // In place.  A workgroup has so many bytes, WIDTH, of a pair's rows of K or of V: those of different workgroups have nothing to do with one another.  Rows are
 // moved in runs; a run's are in registers before one is written, and by then the next run's are on their way, the page numbers of the one behind it, and the
 // entries of the one behind that.
+// Workgroups go round the eight XCDs: eight pairs, one slice after the other, so that a pair's slices, which share lines of memory, are in one L2 at once.
+__host__ __device__ constexpr int evict_blocks(int n_pairs, int slices) { return (n_pairs + 7) / 8 * 8 * slices; }
 template <int ROWB, int WIDTH, int NT>
 __global__ __launch_bounds__(NT) void fairkv_evict_kernel(EvictArgs a)
 {
     constexpr int PPR = WIDTH / 16, SLICES = 2 * (ROWB / WIDTH), ROWS = NT / PPR, U = 4, RUN = ROWS * U;
     __shared__ ListFound found;
-    const int movers = a.n_pairs * SLICES;
+    const int movers = evict_blocks(a.n_pairs, SLICES);
     if (static_cast<int>(blockIdx.x) >= movers) return set_length<NT>(a, blockIdx.x - movers, &found);
-    const int pair = blockIdx.x / SLICES, slice = blockIdx.x % SLICES, piece = threadIdx.x % PPR, slot = threadIdx.x / PPR;
+    const int pair = blockIdx.x / (8 * SLICES) * 8 + blockIdx.x % 8, slice = blockIdx.x / 8 % SLICES, piece = threadIdx.x % PPR, slot = threadIdx.x / PPR;
+    if (pair >= a.n_pairs) return;
     const int32_t len = a.len[pair], n = a.n_keep[pair];
     const ListFound list = whole_list<NT>(a, pair, len, n, &found);
     if (!list.ok || list.first >= n) return;

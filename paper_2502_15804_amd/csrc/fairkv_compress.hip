@@ -18,6 +18,7 @@ using namespace fairkv;
 
 constexpr int32_t kMovers = 8;            // workgroups of a compute unit that move rows into another cache
 constexpr int64_t kMaxGroupsOfCall = 1 << 21;      // of a selection: a grid's threads are counted in 32 bits
+constexpr int64_t kMaxPairsOfCall = 1 << 20;       // of an eviction: the same
 constexpr int32_t kMaxSlots = 65536;      // most compute units that a caller may name
 // Units of a group whose keys lie in a workgroup's LDS: four such workgroups of 512 threads share a CU's 160 KB, and two of 1024.  Beside the larger groups' first
 // step, where no window doubles the space, three of 512: up to 10240 rows a workgroup is faster than the whole GPU in four steps (8 x 8 pairs of 1024 rows, shared,
@@ -200,6 +201,29 @@ extern "C" int fairkv_select(const fairkv_cache *c, const fairkv_selection *s, c
     return launched();
 }
 
+// In place.  Whole rows (of fp32, halves) by a workgroup where there are pairs enough, or else 64 bytes of them, or 32 where that leaves half of the compute units
+// without work.  128 x 8 pairs of 1024 bf16 rows halved 119 us with whole rows and 169 with 64 bytes, 8 x 8 pairs 32 and 16, 8 pairs of 131072 cut to a third 292 with 64
+// bytes and 236 with 32.  256 threads a workgroup have shorter runs, 128 x 8 pairs of 4096 8-bit rows 372 us instead of 302 with 512, but wait less for one
+// another where a list is short: of 200 rows (bf16) 27 us instead of 37.
+namespace {
+template <int ROWB, int WIDTH, int NT>
+void launch_in_place(const EvictArgs &a, unsigned setters, hipStream_t st)
+{
+    hipLaunchKernelGGL((fairkv_evict_kernel<ROWB, WIDTH, NT>), dim3(evict_blocks(a.n_pairs, 2 * (ROWB / WIDTH)) + setters), dim3(NT), 0, st, a);
+}
+template <int ROWB>
+void move_in_place(const EvictArgs &a, int32_t n_slots, unsigned setters, hipStream_t st)
+{
+    constexpr int WIDE = ROWB > 256 ? 256 : ROWB;
+    if (a.n_pairs >= 2 * static_cast<int64_t>(n_slots))
+        a.max_keep <= 1024 ? launch_in_place<ROWB, WIDE, 256>(a, setters, st) : launch_in_place<ROWB, WIDE, 512>(a, setters, st);
+    else if (static_cast<int64_t>(a.n_pairs) * 2 * (ROWB / 64) * 2 > n_slots)
+        launch_in_place<ROWB, 64, 512>(a, setters, st);
+    else
+        launch_in_place<ROWB, 32, 512>(a, setters, st);
+}
+}  // namespace
+
 extern "C" int fairkv_evict(const fairkv_cache *c, const fairkv_cache *into, const int32_t *keep, int32_t max_keep, const int32_t *n_keep,
                             const int32_t *len, int32_t *len_out, const float *weights, float *weights_out, int32_t *bad, int32_t n_slots,
                             void *hip_stream)
@@ -223,7 +247,7 @@ extern "C" int fairkv_evict(const fairkv_cache *c, const fairkv_cache *into, con
     if (max_keep > kMostTokens) return FAIRKV_EINVAL;
     if (!aligned(weights, 4) || !aligned(weights_out, 4) || (!into && weights_out != weights)) return FAIRKV_EINVAL;
     const int64_t pairs = static_cast<int64_t>(c->B) * c->Hkv;
-    if (pairs > UINT32_MAX / 1024) return FAIRKV_EINVAL;
+    if (pairs > kMaxPairsOfCall) return FAIRKV_EINVAL;
     if (meet(len_out, sizeof(int32_t) * pairs, n_keep, sizeof(int32_t) * pairs) || (len_out != len && meet(len_out, sizeof(int32_t) * pairs, len, sizeof(int32_t) * pairs)))
         return FAIRKV_EINVAL;
     EvictArgs a{};
@@ -245,15 +269,13 @@ extern "C" int fairkv_evict(const fairkv_cache *c, const fairkv_cache *into, con
     const bool small = few <= 4 * most;
     a.movers = static_cast<int32_t>(std::min(most, small ? pairs * ((static_cast<int64_t>(max_keep) + 15) / 16) : few));
     auto move = [&](auto row_bytes) {
-        constexpr int ROWB = decltype(row_bytes)::value, kNarrow = ROWB > 64 ? 64 : ROWB;
+        constexpr int ROWB = decltype(row_bytes)::value;
         if (into && small)
             hipLaunchKernelGGL((fairkv_evict_into_kernel<ROWB, 16>), dim3(static_cast<unsigned>(a.movers) + setters), dim3(256), 0, st, a);
         else if (into)
             hipLaunchKernelGGL((fairkv_evict_into_kernel<ROWB, 64>), dim3(static_cast<unsigned>(a.movers) + setters), dim3(256), 0, st, a);
-        else if (pairs >= 2 * static_cast<int64_t>(n_slots))      // K and V of a pair by a workgroup each; of fewer pairs in slices of 64 bytes
-            hipLaunchKernelGGL((fairkv_evict_kernel<ROWB, ROWB, 256>), dim3(static_cast<unsigned>(pairs) * 2 + setters), dim3(256), 0, st, a);
         else
-            hipLaunchKernelGGL((fairkv_evict_kernel<ROWB, kNarrow, 1024>), dim3(static_cast<unsigned>(pairs) * 2 * (ROWB / kNarrow) + setters), dim3(1024), 0, st, a);
+            move_in_place<ROWB>(a, n_slots, setters, st);
     };
     if (rb == 64)
         move(std::integral_constant<int, 64>{});

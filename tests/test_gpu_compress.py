@@ -438,6 +438,26 @@ def test_eviction_in_place(dtype, D, page):
             assert (s.lens if lens_out is None else lens_out).flatten().tolist() == after.tolist()
 
 
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("kv8", 64), ("kv8", 128), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("page", [0, 16])
+@pytest.mark.parametrize("n_slots", [1, 4, 1000])
+def test_eviction_in_place_however_the_rows_are_dealt(dtype, D, page, n_slots):
+    """Whole rows, 64 bytes and 32 of them by a workgroup; lists of one run and of several, of a pair among wrong ones."""
+    for lens, most in (([[9, 6000, 1], [0, 2500, 700]], 0.6), ([[300, 17, 1000]], 0.9), ([[5000]], 1.0)):
+        s = Setup(lens, 2, D, dtype, page, seed=n_slots)
+        keep, counts = _lists(s.lens_h, most, 3)
+        if most == 0.6:
+            keep[1, 1, 900] = keep[1, 1, 899]        # does not ascend, far behind the list's begin
+        after, moves, alone = C.evict(s.lens_h, keep, counts, s.row)
+        assert alone == ([4] if most == 0.6 else [])
+        w = torch.randn(s.n_rows, device=DEV)
+        want = [_moved(x, moves) for x in (s.k, s.v, w)]
+        bad = torch.zeros(1, dtype=torch.int32, device=DEV)
+        F.fairkv_evict(s.cache, s.lens, I32(keep), I32(counts), weights=w, bad=bad, n_slots=n_slots)
+        assert all(_same(x, y) for x, y in zip((s.k, s.v, w), want)) and int(bad) == len(alone)
+        assert s.lens.flatten().tolist() == after.tolist()
+
+
 @pytest.mark.parametrize("dtype,D", [("bf16", 128), ("kv8", 64), ("f32", 128)])
 @pytest.mark.parametrize("page,to_page", [(0, 0), (16, 0), (0, 32), (64, 16)])
 def test_eviction_into_another_cache(dtype, D, page, to_page):
