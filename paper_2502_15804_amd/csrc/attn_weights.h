@@ -104,10 +104,11 @@ __global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_we
                 int some_columns = kMany ? min(CC, cols - c_from) : cols;
                 asm volatile("" : "+v"(some_columns));
                 const int n = __builtin_amdgcn_readfirstlane(some_columns);
-                // Where few tiles are left, 1 << shift waves have one, each every so many-th 32 of the columns.
-                const int tiles = min(NW, n_tiles - turn * NW);
+                // Where few tiles are left, 1 << shift waves have one, each every so many-th 32 of the columns.  The shift is that of the first columns in every pass, so
+                // that a row's weight is read by the wave that wrote it.
+                const int tiles = min(NW, n_tiles - turn * NW), n_shift = kMany ? min(CC, cols) : n;
                 int shift = 0;
-                while (kSplit && tiles <= kShared && tiles << (shift + 1) <= NW && 32 << shift < n) ++shift;
+                while (kSplit && tiles <= kShared && tiles << (shift + 1) <= NW && 32 << shift < n_shift) ++shift;
                 const int of_turn = wave >> shift, tile = tile0 + turn * NW + of_turn, part = wave & ((1 << shift) - 1);
                 const bool mine = of_turn < tiles;
                 const int32_t t0 = tile * TOK;

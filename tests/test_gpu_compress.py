@@ -128,7 +128,8 @@ def test_weights(case):
     assert np.array_equal(got[rest], old[rest].astype(np.float64), equal_nan=True)
 
 
-@pytest.mark.parametrize("D,G,n,ragged", [(128, 8, 9, False), (128, 5, 40, True), (128, 8, 33, True), (64, 16, 64, True), (128, 16, 64, False), (64, 8, 16, False)])
+@pytest.mark.parametrize("D,G,n,ragged", [(128, 8, 9, False), (128, 5, 40, True), (128, 8, 33, True), (64, 16, 64, True), (128, 16, 64, False), (64, 8, 16, False), (128, 16, 40, True),
+                                          (128, 16, 33, False)])
 def test_weights_are_the_same_whoever_computes_them(D, G, n, ragged):
     """A sequence by itself and beside others, over few workgroups and many: tiles that one wave has or several, all bits the same."""
     lens = np.array([[n + 1, 700], [33 + n, 290], [64, 1500]])
