@@ -21,8 +21,8 @@ constexpr int64_t kMaxGroupsOfCall = 1 << 21;      // of a selection: a grid's t
 constexpr int64_t kMaxPairsOfCall = 1 << 20;       // of an eviction: the same
 constexpr int32_t kMaxSlots = 65536;      // most compute units that a caller may name
 // Units of a group whose keys lie in a workgroup's LDS: four such workgroups of 512 threads share a CU's 160 KB, and two of 1024.  Beside the larger groups' first
-// step, where no window doubles the space, three of 512: up to 10240 rows a workgroup is faster than the whole GPU in four steps (8 x 8 pairs of 1024 rows, shared,
-// 23 us instead of 30; with 256 units the step's own workgroups have too little room: 16 x 8 pairs of 10000 rows 37 instead of 31).
+// step three of 512: up to 10240 rows a workgroup is faster than the whole GPU in four steps (8 x 8 pairs of 1024 rows, shared, 23 us instead of 30; with 256
+// units the step's own workgroups have too little room: 16 x 8 pairs of 10000 rows 37 instead of 31).
 constexpr int32_t kSmallCap = 120, kLargeCap = 256, kMixedCap = 160;
 
 // Tokens that a length or a list can count: 2^31 - 2^16, so that what is added to a token's number does not wrap around.
@@ -101,7 +101,7 @@ struct SelectShape {
     int64_t max_blocks;           // of all larger groups, 0: there can be none
     int64_t slots, shares;        // of the large groups' kernels: groups, workgroups
 };
-SelectShape select_shape(const fairkv_cache *c, int32_t shared, int32_t pool, int32_t n_slots)
+SelectShape select_shape(const fairkv_cache *c, int32_t shared, int32_t n_slots)
 {
     const int64_t pairs = static_cast<int64_t>(c->B) * c->Hkv, per_group = shared ? c->Hkv : 1;
     const int64_t each = max_len(c), most = std::min(std::max<int64_t>(c->n_rows, 0), each * pairs), group_most = std::min(most, each * per_group);
@@ -109,7 +109,7 @@ SelectShape select_shape(const fairkv_cache *c, int32_t shared, int32_t pool, in
     auto fits = [&](int32_t cap) { return per_group <= kMaxPairs && (group_most + 63 * per_group) / 64 <= cap; };      // pairs' last units are not full
     s.cap = fits(kSmallCap) ? kSmallCap : kLargeCap;
     if (fits(s.cap)) return s;
-    s.cap = pool > 1 ? kSmallCap : kMixedCap;
+    s.cap = kMixedCap;
     // A block of a pair has at most 64 units, so a large group has more than cap / 64 blocks; its rows are more than 64 cap - 63 per_group.
     s.min_blocks = per_group > kMaxPairs ? kMaxPairs : s.cap / (kBlockRows / 64) + 1;
     const int64_t least_rows = std::max<int64_t>(1, 64 * static_cast<int64_t>(s.cap) - 63 * per_group);
@@ -123,9 +123,7 @@ SelectShape select_shape(const fairkv_cache *c, int32_t shared, int32_t pool, in
 size_t start_bytes(const SelectShape &s) { return sizeof(SelectStart) * s.slots; }
 size_t other_bytes(const SelectShape &s) { return sizeof(SelectSlot) * s.slots + sizeof(SelectShare) * s.shares + (sizeof(int32_t) + kLastBins * sizeof(uint16_t) + kBlockRows * sizeof(uint32_t)) * s.max_blocks; }
 size_t third_of(size_t workspace_bytes) { return workspace_bytes / 3 / 256 * 256; }
-size_t shape_bytes(const SelectShape &s) { return 3 * ((std::max(start_bytes(s), (other_bytes(s) + 1) / 2) + 256) / 256 * 256); }
-// The same for every window: one of more than one row has the smaller cap, which takes more.
-size_t select_bytes(const fairkv_cache *c, int32_t shared, int32_t n_slots) { return shape_bytes(select_shape(c, shared, 2, n_slots)); }
+size_t select_bytes(const SelectShape &s) { return 3 * ((std::max(start_bytes(s), (other_bytes(s) + 1) / 2) + 256) / 256 * 256); }
 
 template <int NT, int UNITS>
 void launch_select(const SelectArgs &a, unsigned groups, hipStream_t st)
@@ -141,13 +139,13 @@ void launch_select(const SelectArgs &a, unsigned groups, hipStream_t st)
 extern "C" size_t fairkv_select_workspace_bytes(const fairkv_cache *c, int32_t shared, int32_t n_slots)
 {
     if (check_cache(c) != FAIRKV_OK || n_slots < 1 || n_slots > kMaxSlots || shared < 0 || shared > 1) return 0;
-    return select_bytes(c, shared, n_slots);
+    return select_bytes(select_shape(c, shared, n_slots));
 }
 
 extern "C" int fairkv_select_workspace_reset(void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     if (!workspace || !aligned(workspace, 16)) return FAIRKV_EINVAL;
-    if (workspace_bytes < shape_bytes(SelectShape{})) return FAIRKV_EWORKSPACE;
+    if (workspace_bytes < select_bytes(SelectShape{})) return FAIRKV_EWORKSPACE;
     zero_words(workspace, workspace_bytes / 3 / sizeof(uint32_t), static_cast<hipStream_t>(hip_stream));
     return launched();
 }
@@ -163,8 +161,8 @@ extern "C" int fairkv_select(const fairkv_cache *c, const fairkv_selection *s, c
     if (!aligned(weights, 4) || !aligned(workspace, 16)) return FAIRKV_EINVAL;
     const int64_t pairs = static_cast<int64_t>(c->B) * c->Hkv, groups = s->shared ? c->B : pairs;
     if (groups > kMaxGroupsOfCall) return FAIRKV_EINVAL;
-    const SelectShape shape = select_shape(c, s->shared, s->pool, n_slots);
-    if (!workspace || workspace_bytes < select_bytes(c, s->shared, n_slots)) return FAIRKV_EWORKSPACE;
+    const SelectShape shape = select_shape(c, s->shared, n_slots);
+    if (!workspace || workspace_bytes < select_bytes(shape)) return FAIRKV_EWORKSPACE;
     SelectArgs a{};
     a.rows = row_map(c);
     a.weights = weights, a.len = len, a.budget = s->budget, a.keep = keep, a.n_keep = n_keep, a.bad = bad;
@@ -192,7 +190,7 @@ extern "C" int fairkv_select(const fairkv_cache *c, const fairkv_selection *s, c
     a.keys = a.upto + shape.max_blocks * (kLastBins / 2);
     const dim3 grid(static_cast<unsigned>(shape.shares)), first(static_cast<unsigned>(groups + shape.shares)), threads(kLargeThreads);
     if (a.half > 0)
-        hipLaunchKernelGGL((fairkv_select_first_kernel<kSmallCap, true>), first, threads, 0, st, a);
+        hipLaunchKernelGGL((fairkv_select_first_kernel<kMixedCap, true>), first, threads, 0, st, a);
     else
         hipLaunchKernelGGL((fairkv_select_first_kernel<kMixedCap, false>), first, threads, 0, st, a);
     hipLaunchKernelGGL(fairkv_select_large_kernel<1>, grid, threads, 0, st, a);

@@ -190,21 +190,22 @@ __device__ __forceinline__ int32_t rows_before(const int32_t (&counts)[KPT][NT /
 
 // ---- a group that one workgroup has ----
 // Its rows in units of 64, a pair's last one not full, so that all lanes of a wave are in one pair; wave w has units w, w + NW, ...  What a pair's
-// rows need to know is held in lanes: lane p has pair p.  Keys lie in LDS.
-template <int UNITS, bool POOL>
+// rows need to know is held in lanes: lane p has pair p.  Keys lie in LDS.  With a window they are first the floats' bits, NaN for rows that are no
+// candidates, which a maximum passes over; what becomes of them waits in registers until all windows have been looked at.  (A second array in LDS
+// leaves a compute unit half its workgroups: 128 x 8 pairs of 1000 rows, window 7, 24 us instead of 20; one group of 8000 rows 17 instead of 18.)
+constexpr uint32_t kRawNone = 0x7fc00001u, kRawProtected = 0x7fc00002u;
+template <int UNITS>
 struct GroupSpace {
-    uint32_t keys[UNITS * 64];                        // first: kNone, 1 for a candidate, kProtected
-    float raw[POOL ? UNITS * 64 : 1];
+    uint32_t keys[UNITS * 64];
     int32_t bins[kBins];
     int32_t counts[UNITS];
     int32_t total, protected_rows, candidate_rows;
 };
 template <int NT, int UNITS, bool POOL>
-__device__ __forceinline__ void select_group(const SelectArgs &a, int group, GroupSpace<UNITS, POOL> &m)
+__device__ __forceinline__ void select_group(const SelectArgs &a, int group, GroupSpace<UNITS> &m)
 {
     constexpr int NW = NT / 64, PER = (UNITS + 63) / 64;
     auto &keys = m.keys;
-    auto &raw = m.raw;
     auto &bins = m.bins;
     auto &counts = m.counts;
     int32_t &total = m.total, &protected_rows = m.protected_rows, &candidate_rows = m.candidate_rows;
@@ -250,31 +251,45 @@ __device__ __forceinline__ void select_group(const SelectArgs &a, int group, Gro
         value = fmaxf(candidate ? value : -INFINITY, -INFINITY);      // a NaN is as low
         is_candidate += __builtin_popcountll(__builtin_amdgcn_ballot_w64(candidate));
         is_protected += __builtin_popcountll(__builtin_amdgcn_ballot_w64(stays));
-        if constexpr (POOL) raw[unit * 64 + lane] = value;
-        keys[unit * 64 + lane] = stays ? kProtected : !candidate ? kNone : POOL ? 1u : order_of(value);
-        if (!POOL && candidate) atomicAdd(&bins[order_of(value) >> kDigitShift[0]], 1);
+        if constexpr (POOL) {
+            keys[unit * 64 + lane] = stays ? kRawProtected : candidate ? __float_as_uint(value) : kRawNone;
+        } else {
+            keys[unit * 64 + lane] = stays ? kProtected : candidate ? order_of(value) : kNone;
+            if (candidate) atomicAdd(&bins[order_of(value) >> kDigitShift[0]], 1);
+        }
     }
     if (lane == 0) atomicAdd(&candidate_rows, is_candidate), atomicAdd(&protected_rows, is_protected);
     __syncthreads();
-    if constexpr (POOL) {                             // rows that are no candidates have -inf there; the window ends where the pair does
-        for (int32_t unit = wave; unit < units; unit += NW) {
+    if constexpr (POOL) {                             // the window ends where the pair does
+        constexpr int EACH = (UNITS + NW - 1) / NW;
+        uint32_t key[EACH];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int32_t unit = wave + i * NW;
+            if (unit >= units) break;
             const int p = pair_of(unit);
             const int32_t at = unit * 64 + lane, lo = __builtin_amdgcn_readlane(begins, p) * 64, hi = __builtin_amdgcn_readlane(ends, p) * 64 - 1;
-            float x = raw[at];
+            const uint32_t own = keys[at];
+            float x = __uint_as_float(own);
             for (int32_t d0 = 1; d0 <= a.half; d0 += 4) {      // eight reads at once: past the window's end those of its end again
                 float y[8];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int32_t d = min(d0 + i, a.half);
-                    y[2 * i] = raw[max(lo, at - d)], y[2 * i + 1] = raw[min(hi, at + d)];
+                for (int u = 0; u < 4; ++u) {
+                    const int32_t d = min(d0 + u, a.half);
+                    y[2 * u] = __uint_as_float(keys[max(lo, at - d)]), y[2 * u + 1] = __uint_as_float(keys[min(hi, at + d)]);
                 }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x = fmaxf(x, y[i]);
+                for (int u = 0; u < 8; ++u) x = fmaxf(x, y[u]);
             }
-            if (keys[at] == 1) {
-                keys[at] = order_of(x);
-                atomicAdd(&bins[order_of(x) >> kDigitShift[0]], 1);
-            }
+            key[i] = own == kRawProtected ? kProtected : own == kRawNone ? kNone : order_of(x);
+            if (key[i] != kNone && key[i] != kProtected) atomicAdd(&bins[key[i] >> kDigitShift[0]], 1);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int32_t unit = wave + i * NW;
+            if (unit >= units) break;
+            keys[unit * 64 + lane] = key[i];
         }
         __syncthreads();
     }
@@ -356,8 +371,8 @@ __device__ __forceinline__ void select_group(const SelectArgs &a, int group, Gro
 template <int NT, int UNITS, bool POOL>
 __global__ __launch_bounds__(NT) void fairkv_select_kernel(SelectArgs a)
 {
-    __shared__ GroupSpace<UNITS, POOL> m;
-    select_group<NT>(a, blockIdx.x, m);
+    __shared__ GroupSpace<UNITS> m;
+    select_group<NT, UNITS, POOL>(a, blockIdx.x, m);
 }
 
 // ---- large groups: the line of their blocks ----
@@ -660,15 +675,15 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
 
 // The first step of the large groups, and beside it the groups that one workgroup has.
 template <int UNITS, bool POOL>
-__global__ __launch_bounds__(kLargeThreads) void fairkv_select_first_kernel(SelectArgs a)
+__global__ __launch_bounds__(kLargeThreads, 6) void fairkv_select_first_kernel(SelectArgs a)
 {
     __shared__ union Space {
-        GroupSpace<UNITS, POOL> group;
+        GroupSpace<UNITS> group;
         LargeSpace<0> large;
         __device__ Space() {}
     } m;
     if (static_cast<int>(blockIdx.x) < a.n_groups)
-        select_group<kLargeThreads>(a, blockIdx.x, m.group);
+        select_group<kLargeThreads, UNITS, POOL>(a, blockIdx.x, m.group);
     else
         select_large<0>(a, blockIdx.x - a.n_groups, gridDim.x - a.n_groups, m.large);
 }
