@@ -32,8 +32,8 @@ def compiled(tmp_path_factory):
 
 def test_every_variant_is_there(compiled):
     count = lambda part: sum(part in name for name in compiled)
-    assert count("attn_weights") == 16 and count("select_kernel") == 6 and count("select_first") == 2 and count("select_large") == 4
-    assert count("evict_into") == 8 and count("evict_kernel") == 8 and count("evict_lengths") == 1
+    assert count("attn_weights") == 16 and count("select_kernel") == 6 and count("select_first") == 2 and count("select_large") == 3
+    assert count("evict_into") == 8 and count("evict_kernel") == 15 and count("evict_lengths") == 1
 
 
 def test_registers_lds_and_wait_states(compiled):
