@@ -537,6 +537,7 @@ typedef struct {
  *            before the first use (fairkv_select_workspace_reset); every completed call leaves them zero, and nothing else in it is kept from call to
  *            call, so calls of any shapes that are ordered on one stream may share a workspace that is large enough for each, with one workspace_bytes
  * n_slots    the GPU's compute units
+ * keep, n_keep, bad and workspace must not meet one another, or weights, len, budget or the cache's off or pages.
  * Enqueues one kernel, or four where the sizes of the cache allow a group of more than about 16000 rows (of a paged cache max_pages * page_rows is the most
  * that a pair has, of a packed one n_rows); no synchronisation.  FAIRKV_EUNSUPPORTED: pool > 63.  FAIRKV_EINVAL also: more than 2^21 groups. */
 size_t fairkv_select_workspace_bytes(const fairkv_cache *cache, int32_t shared, int32_t n_slots);

@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 
 #include "attn_weights.h"
 #include "cache_check.h"
@@ -37,6 +38,19 @@ bool meet(const void *x, size_t nx, const void *y, size_t ny)
 {
     const auto a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y);
     return a < static_cast<unsigned __int128>(b) + ny && b < static_cast<unsigned __int128>(a) + nx;
+}
+struct Bytes {
+    const void *at;
+    size_t n;
+};
+// Whether something that a call writes shares a byte with what it reads or with something else that it writes.  Those that are null are not there.
+bool written_over(std::initializer_list<Bytes> written, std::initializer_list<Bytes> read)
+{
+    for (auto w = written.begin(); w != written.end(); ++w) {
+        auto meets = [&](const Bytes &x) { return w->at && x.at && meet(w->at, w->n, x.at, x.n); };
+        if (std::any_of(read.begin(), read.end(), meets) || std::any_of(w + 1, written.end(), meets)) return true;
+    }
+    return false;
 }
 
 // 16 waves of a compute unit (20 with heads of 64 and few columns: 64 x 8 pairs of 4096 8-bit rows 43 us instead of 48), in as many workgroups as its LDS
@@ -163,6 +177,11 @@ extern "C" int fairkv_select(const fairkv_cache *c, const fairkv_selection *s, c
     if (groups > kMaxGroupsOfCall) return FAIRKV_EINVAL;
     const SelectShape shape = select_shape(c, s->shared, n_slots);
     if (!workspace || workspace_bytes < select_bytes(shape)) return FAIRKV_EWORKSPACE;
+    // Workgroups read lengths, weights and tables while others write their lists.
+    constexpr size_t word = sizeof(int32_t);
+    if (written_over({{keep, word * pairs * max_keep}, {n_keep, word * pairs}, {bad, word}, {workspace, workspace_bytes}},
+                     {{weights, sizeof(float) * c->n_rows}, {len, word * pairs}, {s->budget, word * groups}, {c->off, sizeof(int64_t) * pairs}, {c->pages, word * pairs * c->max_pages}}))
+        return FAIRKV_EINVAL;
     SelectArgs a{};
     a.rows = row_map(c);
     a.weights = weights, a.len = len, a.budget = s->budget, a.keep = keep, a.n_keep = n_keep, a.bad = bad;
