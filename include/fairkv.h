@@ -551,10 +551,11 @@ int fairkv_select(const fairkv_cache *cache, const fairkv_selection *s, const fl
  *              twice.  Its k and v must not meet this one's, or be the same of as many rows (one pool); then its rows of the pairs are none that
  *              this one's tokens have, by pages or first rows of its own.
  * keep         device [B][Hkv][max_keep], n_keep device [B][Hkv], as fairkv_select leaves them
- * len_out      device [B][Hkv]; may be len, must not meet n_keep
+ * len_out      device [B][Hkv]; may be len
  * weights      device float [n_rows] and weights_out device float [n_rows of into], or both NULL; in place the same, in one pool the same or apart
  * A pair is left alone and counted in *bad, its length kept (into another cache: 0, and what is in its rows there says nothing), if n_keep[p] is not in
  * 0 .. max_keep (in place: or its length; else: or its room there), an entry not in 0 .. len - 1, not ascending (in place), or a row outside its cache.
+ * len_out, bad and weights_out must not meet one another, or keep, n_keep or the caches' off or pages or into's cap.
  * Pages behind ceil(len_out / page_rows) hold no token of a pair any more.  Packed rows stay where the pair's run begins.
  * Enqueues one kernel, and a second one if len_out is len; no synchronisation.  FAIRKV_EINVAL also: more than 2^20 pairs, max_keep
  * > 2^31 - 2^16. */

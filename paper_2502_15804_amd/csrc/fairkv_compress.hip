@@ -265,10 +265,15 @@ extern "C" int fairkv_evict(const fairkv_cache *c, const fairkv_cache *into, con
     if (!aligned(weights, 4) || !aligned(weights_out, 4) || (!into && weights_out != weights)) return FAIRKV_EINVAL;
     const int64_t pairs = static_cast<int64_t>(c->B) * c->Hkv;
     if (pairs > kMaxPairsOfCall) return FAIRKV_EINVAL;
-    if (meet(len_out, sizeof(int32_t) * pairs, n_keep, sizeof(int32_t) * pairs) || (len_out != len && meet(len_out, sizeof(int32_t) * pairs, len, sizeof(int32_t) * pairs)))
+    const fairkv_cache *to = into ? into : c;
+    const size_t words = sizeof(int32_t) * pairs;
+    if (len_out != len && meet(len_out, words, len, words)) return FAIRKV_EINVAL;
+    // Entries are read again once a list has been found right, while other workgroups write lengths, counts and weights.
+    if (written_over({{len_out, words}, {bad, sizeof(int32_t)}, {weights_out, sizeof(float) * to->n_rows}},
+                     {{keep, words * max_keep}, {n_keep, words}, {c->off, 2 * words}, {c->pages, words * c->max_pages}, {to->off, 2 * words}, {to->pages, words * to->max_pages},
+                      {into ? into->cap : nullptr, words}}))
         return FAIRKV_EINVAL;
     EvictArgs a{};
-    const fairkv_cache *to = into ? into : c;
     a.k = static_cast<const char *>(c->k), a.v = static_cast<const char *>(c->v);
     a.k_to = static_cast<char *>(to->k), a.v_to = static_cast<char *>(to->v);
     a.w = weights, a.w_to = weights_out;

@@ -26,7 +26,7 @@ WRITTEN = ("keep", "n_keep", "bad", "ws")
 
 
 @pytest.mark.parametrize("out", WRITTEN)
-@pytest.mark.parametrize("other", SIZES)
+@pytest.mark.parametrize("other", ("weights", "len", "budget", "off") + WRITTEN)
 def test_select_refuses_to_write_over_what_it_reads_or_writes(out, other):
     if out == other:
         return
@@ -37,3 +37,33 @@ def test_select_refuses_to_write_over_what_it_reads_or_writes(out, other):
 
 def test_select_refuses_lists_over_pages():
     assert _select(pages=True, n_keep=PLACES["off"] + 4 * PAIRS * 2 - 4) == INVALID
+
+
+def _evict(other_cache=False, pages=False, **places):
+    p = dict(PLACES, **places)
+    where = dict(off=None, pages=p["off"], max_pages=2, page_rows=16) if pages else dict(off=p["off"])
+    c = _cache(k=p["k"], v=p["v"], cap=p["cap"], n_rows=ROWS, **where)
+    into = _cache(k=p["k"] + (1 << 38), v=p["v"] + (1 << 38), cap=p["into_cap"], off=p["into_off"], n_rows=ROWS) if other_cache else None
+    return F.lib().fairkv_evict(ctypes.byref(c), ctypes.byref(into) if into else None, p["keep"], MOST, p["n_keep"], p["len"], p["len_out"], p["weights"],
+                                p["weights_out"] if other_cache else p["weights"], p["bad"], 256, None)
+
+
+PLACES.update(into_off=AT + (60 << 30), into_cap=AT + (61 << 30))
+SIZES.update(len_out=4 * PAIRS, weights_out=4 * ROWS, into_off=8 * PAIRS, into_cap=4 * PAIRS)
+
+
+@pytest.mark.parametrize("other_cache", [False, True])
+@pytest.mark.parametrize("out", ["len_out", "bad", "weights_out"])
+@pytest.mark.parametrize("other", ["keep", "n_keep", "off", "into_off", "into_cap", "len_out", "bad", "weights_out"])
+def test_evict_refuses_to_write_over_what_it_reads_or_writes(out, other, other_cache):
+    if out == other or (not other_cache and (other.startswith("into") or "weights_out" in (out, other))):
+        return
+    for by in (0, (SIZES[other] - 1) // 4 * 4, -((SIZES[out] - 1) // 4 * 4)):
+        assert _evict(other_cache, **{out: PLACES[other] + by}) == INVALID, by
+
+
+def test_evict_in_place_refuses_weights_over_lists_and_lengths_over_pages():
+    for name in ("keep", "n_keep", "off", "len_out", "bad"):
+        assert _evict(weights=PLACES[name]) == INVALID, name
+    assert _evict(pages=True, len_out=PLACES["off"] + 4 * PAIRS * 2 - 4) == INVALID
+    assert _evict(pages=True, bad=PLACES["off"] + 4) == INVALID
