@@ -547,6 +547,7 @@ int fairkv_select(const fairkv_cache *cache, const fairkv_selection *s, const fl
                   void *hip_stream);
 
 /* Row keep[p][i] of every pair becomes its row i for i < n_keep[p], K, V and, if given, its weight; len_out[p] = n_keep[p].
+ * K and V of the cache that rows move in, or into, must not meet each other.
  * into         NULL: in place, a list has to ascend.  Else another cache of the same B, Hkv, D, type and scales: lists may be in any order and name a token
  *              twice.  Its k and v must not meet this one's, or be the same of as many rows (one pool); then its rows of the pairs are none that
  *              this one's tokens have, by pages or first rows of its own.

@@ -246,6 +246,7 @@ extern "C" int fairkv_evict(const fairkv_cache *c, const fairkv_cache *into, con
                             void *hip_stream)
 {
     if (const int rc = check_cache(c)) return rc;
+    const size_t row_bytes = static_cast<size_t>(c->D) * (c->dtype == FAIRKV_E4M3 ? 1 : c->dtype == FAIRKV_BF16 ? 2 : 4);
     if (into) {
         if (const int rc = check_cache(into)) return rc;
         if (into->B != c->B || into->Hkv != c->Hkv || into->D != c->D || into->dtype != c->dtype || into->n_scales != c->n_scales) return FAIRKV_EINVAL;
@@ -253,8 +254,7 @@ extern "C" int fairkv_evict(const fairkv_cache *c, const fairkv_cache *into, con
             if (into->k_scale[h] != c->k_scale[h] || into->v_scale[h] != c->v_scale[h]) return FAIRKV_EINVAL;
         // Rows are written while others are read: the caches are one pool, or apart, and where they are one their pairs' rows are not the same.
         const bool pool = into->k == c->k && into->v == c->v && into->n_rows == c->n_rows;
-        const size_t row = static_cast<size_t>(c->D) * (c->dtype == FAIRKV_E4M3 ? 1 : c->dtype == FAIRKV_BF16 ? 2 : 4);
-        auto apart = [&](const void *x, const void *y) { return !meet(x, row * c->n_rows, y, row * into->n_rows); };
+        auto apart = [&](const void *x, const void *y) { return !meet(x, row_bytes * c->n_rows, y, row_bytes * into->n_rows); };
         const bool all_apart = apart(c->k, into->k) && apart(c->k, into->v) && apart(c->v, into->k) && apart(c->v, into->v);
         if (pool ? into->off == c->off && into->pages == c->pages : !all_apart) return FAIRKV_EINVAL;
         if (weights && !(pool && weights == weights_out) && meet(weights, sizeof(float) * c->n_rows, weights_out, sizeof(float) * into->n_rows)) return FAIRKV_EINVAL;
@@ -273,6 +273,8 @@ extern "C" int fairkv_evict(const fairkv_cache *c, const fairkv_cache *into, con
                      {{keep, words * max_keep}, {n_keep, words}, {c->off, 2 * words}, {c->pages, words * c->max_pages}, {to->off, 2 * words}, {to->pages, words * to->max_pages},
                       {into ? into->cap : nullptr, words}}))
         return FAIRKV_EINVAL;
+    // Rows of K and of V are moved by workgroups that do not wait for one another.
+    if (meet(to->k, row_bytes * to->n_rows, to->v, row_bytes * to->n_rows)) return FAIRKV_EINVAL;
     EvictArgs a{};
     a.k = static_cast<const char *>(c->k), a.v = static_cast<const char *>(c->v);
     a.k_to = static_cast<char *>(to->k), a.v_to = static_cast<char *>(to->v);
@@ -282,7 +284,6 @@ extern "C" int fairkv_evict(const fairkv_cache *c, const fairkv_cache *into, con
     a.keep = keep, a.n_keep = n_keep, a.len = len, a.len_out = len_out, a.bad = bad;
     a.n_pairs = static_cast<int32_t>(pairs), a.max_keep = max_keep;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const int rb = c->D * (c->dtype == FAIRKV_E4M3 ? 1 : c->dtype == FAIRKV_BF16 ? 2 : 4);
     // Lengths that are written over those that the move reads are set behind it, by a kernel of their own.
     const bool over = len_out == len;
     const unsigned setters = over ? 0 : static_cast<unsigned>(pairs);
@@ -299,11 +300,11 @@ extern "C" int fairkv_evict(const fairkv_cache *c, const fairkv_cache *into, con
         else
             move_in_place<ROWB>(a, n_slots, setters, st);
     };
-    if (rb == 64)
+    if (row_bytes == 64)
         move(std::integral_constant<int, 64>{});
-    else if (rb == 128)
+    else if (row_bytes == 128)
         move(std::integral_constant<int, 128>{});
-    else if (rb == 256)
+    else if (row_bytes == 256)
         move(std::integral_constant<int, 256>{});
     else
         move(std::integral_constant<int, 512>{});

@@ -67,3 +67,14 @@ def test_evict_in_place_refuses_weights_over_lists_and_lengths_over_pages():
         assert _evict(weights=PLACES[name]) == INVALID, name
     assert _evict(pages=True, len_out=PLACES["off"] + 4 * PAIRS * 2 - 4) == INVALID
     assert _evict(pages=True, bad=PLACES["off"] + 4) == INVALID
+
+
+@pytest.mark.parametrize("dtype,row", [(F.FAIRKV_BF16, 256), (F.FAIRKV_F32, 512)])
+def test_evict_refuses_keys_that_meet_values(dtype, row):
+    """In place, or in the cache that rows go to; where they come from does not matter."""
+    p = {name: at + (1 << 39) for name, at in PLACES.items()}
+    cache = lambda k, v: ctypes.byref(_cache(k=k, v=v, cap=p["cap"], off=p["off"], n_rows=ROWS, dtype=dtype))
+    call = lambda c, into: F.lib().fairkv_evict(c, into, p["keep"], MOST, p["n_keep"], p["len"], p["len_out"], None, None, None, 256, None)
+    for by in (0, 16, row * ROWS - 16, -(row * ROWS - 16)):
+        assert call(cache(AT, AT + by), None) == INVALID, by
+        assert call(cache(AT + (1 << 36), AT + (1 << 37)), cache(AT, AT + by)) == INVALID, by
