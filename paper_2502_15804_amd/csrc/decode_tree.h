@@ -298,7 +298,7 @@ __global__ __launch_bounds__(WC *WT * 64, 1) void fairkv_decode_tree_kernel(Tree
     int solo_most = kSolo;                            // tiles of a pair that one wave has alone
     if constexpr (kSolo > 0) {
         const int tiles = tiles_of(entry.x);
-        const int64_t first = at - wave_upto(tiles + overhead(tiles)) + overhead(tiles);      // place of the lane's pair
+        const int64_t first = at - wave_upto(static_cast<int64_t>(tiles) + overhead(tiles)) + overhead(tiles);      // place of the lane's pair; 64 pairs may have more than 31 bits hold
         const bool fits = lane <= pair && tiles <= kSoloMany && first - overhead(tiles) >= begin && first + tiles <= end;
         if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(fits)) >= 3) solo_most = kSoloMany;
     }
