@@ -506,7 +506,7 @@ int fairkv_accept(const fairkv_cache *cache, const int32_t *path, const int32_t 
  * is as in fairkv_decode_attn_tree, whose lse of the same queries it takes.
  * q            device bf16 [B][q_len][Hq][D], 16-byte aligned; Hq a multiple of Hkv, any Hq / Hkv up to 16
  * tree, n_new  as in fairkv_decode_attn_tree; queries and lse of nodes i >= n are not read
- * lse          device float [B][q_len][Hq]; -inf for a node that sees nothing, which gives no weight
+ * lse          device float [B][q_len][Hq]; -inf for a node that sees nothing, which gives no weight to any row, whatever is in it
  * weights      device float [n_rows]; weights_out may be weights, or must not meet it
  * n_slots      the GPU's compute units
  * Rows of no token are left as they are, and so are those of a packed pair whose run sticks out of the cache.  The sums are the same from call to

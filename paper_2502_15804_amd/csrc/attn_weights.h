@@ -25,6 +25,8 @@
 #include "decode_mfma.h"
 #include "line.h"
 
+#include <cfloat>
+
 namespace fairkv {
 
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
@@ -61,7 +63,8 @@ __global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_we
     constexpr int AHEAD = CC > 64 ? 4 : 1;                            // pieces of queries that a thread asks for at once
     typedef __attribute__((ext_vector_type(4))) uint32_t u4;
     __shared__ __attribute__((aligned(1024))) char qs[CC * QROWB];
-    __shared__ __attribute__((aligned(16))) float minus_lse[CC];      // in log2 units
+    __shared__ __attribute__((aligned(16))) float minus_lse[CC];      // in log2 units; +inf: of a node that sees nothing, and no other's
+    __shared__ int32_t blind;                                         // the last run and pass whose columns had such a node
     __shared__ uint64_t sees[CC];                                     // of every column: the nodes that it sees
     __shared__ float joins[kSplit ? kShared : 1][kSplit ? CC / 32 : 1][64];      // of tiles that several waves have, for every 32 columns
 
@@ -78,6 +81,7 @@ __global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_we
     // Piece p of column c lies at piece p ^ swizzle(c): a row per lane, 16 of them take all banks.
     auto swizzle = [](int c) __attribute__((always_inline)) { return c / (256 / QROWB) % PPQ; };
 
+    if (threadIdx.x == 0) blind = -1;
     const LineShare share = line_share<NT>(n_pairs, gridDim.x, blockIdx.x, [&](int p) { return tiles_of(len_of(p)); });
     int pair = share.pair;
     int64_t first = share.begin, left = share.left;
@@ -142,12 +146,14 @@ __global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_we
                     for (int c = threadIdx.x; c < n; c += NT) {
                         const int node = (chunk * CC + c) / a.G, g = chunk * CC + c - node * a.G;
                         const float lse = a.lse[(static_cast<size_t>(b) * a.q_len + node) * a.Hq + h * a.G + g];
-                        minus_lse[c] = lse == -INFINITY ? -INFINITY : -lse * kLog2e;      // a node that sees nothing gives no weight
+                        minus_lse[c] = lse == -INFINITY ? INFINITY : lse < 0.f ? fminf(-lse * kLog2e, FLT_MAX) : -lse * kLog2e;
+                        if (lse == -INFINITY) blind = 2 * pair + chunk;
                         sees[c] = a.tree ? static_cast<uint64_t>(a.tree[static_cast<size_t>(b) * a.q_len + node]) : ~0ull >> (63 - node);
                     }
                     __syncthreads();
                 }
                 if (!mine && shift == 0) continue;
+                const bool some_blind = __builtin_amdgcn_readfirstlane(blind) == 2 * pair + chunk;
                 bf16x8_t k[NSL];
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
@@ -158,10 +164,11 @@ __global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_we
                         k[p] = __builtin_bit_cast(bf16x8_t, raw[p]);
                     }
                 }
-                // 32 columns from c0.  some: not all of them are there; draft: some of the tile's tokens are the queries' own, and not seen by all
+                // 32 columns from c0.  some: not all of them are there; draft: some of the tile's tokens are the queries' own, and not seen by all; rare: some of
+                // the columns are of nodes that see nothing, which infinite rows and NaN ones would give NaN
                 float w = 0.f;
-                auto columns = [&](int c0, auto some, auto draft, auto joined) __attribute__((always_inline)) {
-                    constexpr bool kSome = decltype(some)::value, kDraft = decltype(draft)::value;
+                auto columns = [&](int c0, auto some, auto draft, auto rare, auto joined) __attribute__((always_inline)) {
+                    constexpr bool kSome = decltype(some)::value, kDraft = decltype(draft)::value, kRare = decltype(rare)::value;
                     const int c = kSome ? min(c0 + l32, n - 1) : c0 + l32;      // past the last one: that one again, and it does not count
                     bf16x8_t q[NSL];
 #pragma unroll
@@ -189,6 +196,7 @@ __global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_we
                             bool counts = true;
                             if constexpr (kSome) counts = cr < n;
                             if constexpr (kDraft) counts = counts && (j < 0 || (words[2 * min(cr, n - 1)] >> (j & 31) & 1) != 0);
+                            if constexpr (kRare) counts = counts && ml[x] != INFINITY;
                             s4[x] = r4 == 0 ? (counts ? e : 0.f) : s4[x] + (counts ? e : 0.f);
                         }
                     }
@@ -199,11 +207,15 @@ __global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_we
                         w += of_32;
                 };
                 auto all_columns = [&](int c0, int step, auto joined) __attribute__((always_inline)) {
-                    if (t0 + TOK > base) {
-                        for (; c0 < n; c0 += step) columns(c0, std::true_type{}, std::true_type{}, joined);
+                    constexpr std::true_type yes;
+                    constexpr std::false_type no;
+                    if (some_blind) {
+                        for (; c0 < n; c0 += step) columns(c0, yes, yes, yes, joined);
+                    } else if (t0 + TOK > base) {
+                        for (; c0 < n; c0 += step) columns(c0, yes, yes, no, joined);
                     } else {
-                        for (; c0 + 32 <= n; c0 += step) columns(c0, std::false_type{}, std::false_type{}, joined);
-                        if (c0 < n) columns(c0, std::true_type{}, std::false_type{}, joined);
+                        for (; c0 + 32 <= n; c0 += step) columns(c0, no, no, no, joined);
+                        if (c0 < n) columns(c0, yes, no, no, joined);
                     }
                 };
                 if (!kSplit || shift == 0)
