@@ -528,10 +528,11 @@ typedef struct {
 /* The first `sink` and the last `recent` tokens of a pair are protected and stay, whatever the budget.  Of the others, the candidates, each has the value
  * max weights[row of u] over the candidates u of its pair with |u - t| <= pool / 2, and the largest values of a pair (shared: of a sequence) stay, as many
  * as the budget leaves room for behind the protected tokens.  Of equal values that of the lower head stays, then that of the lower token; -0 is
- * 0, and a NaN is as low as -inf.  A token that has no row in the cache does not stay and takes no part.
+ * 0, and a NaN is as low as -inf.  A token that has no row in the cache does not stay and takes no part.  Lengths count as in fairkv_decode_attn_tree.
  * weights    device float [n_rows]
  * keep       device [B][Hkv][max_keep], out: the tokens that stay, ascending; what is behind them is left as it is
- * n_keep     device [B][Hkv], out: their number; -1, and the pair counted in *bad, for a pair with more than max_keep of them, whose list then says nothing
+ * n_keep     device [B][Hkv], out: their number; -1, and the pair counted in *bad, for a pair with more than max_keep of them, whose list then says nothing.
+ *            Pairs whose rows overlap, which they must not, may get it too
  * bad        device counter or NULL
  * workspace  device, fairkv_select_workspace_bytes(cache, shared, n_slots) bytes or more, 16-byte aligned.  Its first workspace_bytes / 3 bytes must be zero
  *            before the first use (fairkv_select_workspace_reset); every completed call leaves them zero, and nothing else in it is kept from call to
@@ -539,7 +540,8 @@ typedef struct {
  * n_slots    the GPU's compute units
  * keep, n_keep, bad and workspace must not meet one another, or weights, len, budget or the cache's off or pages.
  * Enqueues one kernel, or four where the sizes of the cache allow a group of more than about 16000 rows (of a paged cache max_pages * page_rows is the most
- * that a pair has, of a packed one n_rows); no synchronisation.  FAIRKV_EUNSUPPORTED: pool > 63.  FAIRKV_EINVAL also: more than 2^21 groups. */
+ * that a pair has, of a packed one n_rows); no synchronisation.  Tokens without rows cost time where they make the pairs of a budget longer than the cache's rows: 0.2 to 3 ms for
+ * 131072 of them a pair.  FAIRKV_EUNSUPPORTED: pool > 63.  FAIRKV_EINVAL also: more than 2^21 groups. */
 size_t fairkv_select_workspace_bytes(const fairkv_cache *cache, int32_t shared, int32_t n_slots);
 int fairkv_select_workspace_reset(void *workspace, size_t workspace_bytes, void *hip_stream);
 int fairkv_select(const fairkv_cache *cache, const fairkv_selection *s, const float *weights, const int32_t *len, int32_t *keep,

@@ -11,7 +11,7 @@
 //
 // A group of up to `cap` units of 64 rows is one workgroup's, which reads its weights once and has its keys in LDS.  Rows of larger groups are dealt to
 // the whole GPU in blocks of 4096: a kernel makes keys of them, in order, and counts the first digit, two count the others, the second of them block by
-// block, and one lists what stays.  Every list ascends and no sum depends on who comes first: counts are whole numbers.
+// block, and one lists what stays.  A group that is longer than the cache has rows, because tokens of it have none, is gone through by one workgroup, slowly.  Every list ascends and no sum depends on who comes first: counts are whole numbers.
 //
 // What bounds it (MI355X; times of a call in a row of them): not its bytes (a million weights are 4 MB, 1 us) but one thing after the other.  A workgroup's
 // group: 9 us from lengths over pages, weights, three digits and ties to the list, 16 us where four of them share a compute unit's issue slots (128 x 8 pairs of
@@ -54,7 +54,7 @@ struct SelectArgs {
     const float *weights;                 // [n_rows]
     const int32_t *len, *budget;          // [B * Hkv]; [groups]
     int32_t *keep, *n_keep, *bad;         // [B * Hkv][max_keep], [B * Hkv], [1] or null
-    SelectStart *starts;                  // null: no group can be large
+    SelectStart *starts;
     SelectSlot *slots;
     uint32_t *keys;                       // [max_blocks][kBlockRows]: what the first step makes of the rows
     int32_t *above;                       // [max_blocks]: rows of a block that stay whatever the last digit is
@@ -188,6 +188,137 @@ __device__ __forceinline__ int32_t rows_before(const int32_t (&counts)[KPT][NT /
     return counts[i][threadIdx.x >> 6] + __builtin_popcountll(__builtin_amdgcn_ballot_w64((x >> i & 1) != 0) & ((1ull << (threadIdx.x & 63)) - 1));
 }
 
+// The kernel's arguments (these are all that its kernels have), read again: for what is hardly ever done, so that nothing of it is kept in scalar registers by
+// those that do not come there (one sequence of 8 pairs of 1024 rows 9.6 us instead of 9.4).
+__device__ __forceinline__ SelectArgs select_args_again()
+{
+    typedef __attribute__((address_space(4))) const uint64_t *words_t;
+    struct Words {
+        uint64_t x[sizeof(SelectArgs) / sizeof(uint64_t)];
+    } words;
+    static_assert(sizeof(Words) == sizeof(SelectArgs), "whole words");
+    uint64_t at = reinterpret_cast<uint64_t>(__builtin_amdgcn_kernarg_segment_ptr());
+    asm volatile("" : "+s"(at));
+#pragma unroll
+    for (size_t i = 0; i < sizeof(SelectArgs) / sizeof(uint64_t); ++i) words.x[i] = reinterpret_cast<words_t>(at)[i];
+    return __builtin_bit_cast(SelectArgs, words);
+}
+
+// ---- a group that is longer than the host has counted on ----
+// The host counts on no more rows than the cache has, but tokens count whether they have one or not.  Here a workgroup goes through a group's tokens once for
+// every digit and once for the lists, and makes a token's key anew each time: what this takes from the kernels around it is kept small, not its time (8 pairs of
+// 131072 tokens of which the last 1024 have rows: 1.7 ms in one group, 0.2 in 8).  A group that has more rows than the cache is refused: its pairs' rows overlap.
+template <int NT>
+__device__ __forceinline__ void select_slowly(const SelectArgs &a, int group, int32_t *bins, int32_t *counts /* both in LDS, kBins and NT / 64 */)
+{
+    __shared__ unsigned long long rows, protected_rows;
+    const int p0 = group * a.per_group, p1 = p0 + a.per_group, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    auto key_of = [&](int pair, const Candidates &c, int32_t t) __attribute__((always_inline)) {
+        const int64_t row = a.rows.row(pair, t);
+        if (row < 0) return kNone;
+        if (!c.has(t)) return kProtected;
+        float x = fmaxf(a.weights[row], -INFINITY);
+#pragma unroll 1
+        for (int32_t u = a.half > 0 ? max(t - a.half, c.first) : c.end; u < min(t + a.half + 1, c.end); ++u) {
+            const int64_t beside = a.rows.row(pair, u);
+            if (beside >= 0) x = fmaxf(x, a.weights[beside]);
+        }
+        return order_of(x);
+    };
+    auto clear_bins = [&]() __attribute__((always_inline)) {
+#pragma unroll 1
+        for (int i = threadIdx.x; i < kBins; i += NT) bins[i] = 0;
+    };
+    __syncthreads();                      // the group before
+    clear_bins();
+    if (threadIdx.x == 0) rows = protected_rows = 0;
+    __syncthreads();
+    uint32_t least = 0;                   // what is larger stays
+    int32_t need = 0;                     // how many of those that are equal to it
+#pragma unroll 1
+    for (int digit = 0; digit < kDigits; ++digit) {
+        int32_t n = 0, n_protected = 0;   // of a thread
+#pragma unroll 1
+        for (int p = p0; p < p1; ++p) {
+            const int32_t len = select_len(a, p);
+            const Candidates c(a, len);
+#pragma unroll 1
+            for (int32_t t = threadIdx.x; t < len; t += NT) {
+                const uint32_t key = key_of(p, c, t);
+                n += key != kNone, n_protected += key == kProtected;
+                count_digit(bins, key, digit, least, key != kNone && key != kProtected);
+            }
+        }
+        if (digit == 0) atomicAdd(&rows, static_cast<unsigned long long>(n)), atomicAdd(&protected_rows, static_cast<unsigned long long>(n_protected));
+        __syncthreads();
+        if (digit == 0) {
+            if (rows > static_cast<unsigned long long>(a.rows.n_rows)) {
+                for (int p = p0 + threadIdx.x; p < p1; p += NT) {
+                    a.n_keep[p] = -1;
+                    if (a.bad) atomicAdd(a.bad, 1);
+                }
+                return;
+            }
+            need = static_cast<int32_t>(max(static_cast<int64_t>(a.budget[group]) - static_cast<int64_t>(protected_rows), static_cast<int64_t>(0)));
+            if (need == 0) {
+                least = kProtected - 1;
+                break;
+            }
+        }
+        const BinFound<int32_t> b = find_bin<NT>(need, [&](int x) { return bins[x]; });
+        need = b.need;
+        if (need == 0) break;             // there are no so many candidates: all of them stay
+        least |= static_cast<uint32_t>(b.bin) << kDigitShift[digit];
+        if (need == b.in_bin) {           // all that share these digits stay
+            least -= 1, need = 0;
+            break;
+        }
+        clear_bins();
+        __syncthreads();
+    }
+    // NT tokens of a pair at a time: how many of those that `is` says are in front of the thread's, and all of them
+    auto place = [&](bool is, int32_t &all) __attribute__((always_inline)) {
+        const uint64_t here = __builtin_amdgcn_ballot_w64(is);
+        __syncthreads();                  // the counts before have been read
+        if (lane == 0) counts[wave] = __builtin_popcountll(here);
+        __syncthreads();
+        int32_t before = __builtin_popcountll(here & ((1ull << lane) - 1));
+        all = 0;
+#pragma unroll 1
+        for (int w = 0; w < NT / 64; ++w) {
+            if (w < wave) before += counts[w];
+            all += counts[w];
+        }
+        return before;
+    };
+    int32_t ties = 0;                     // of the group, so far: no more than are needed count
+#pragma unroll 1
+    for (int p = p0; p < p1; ++p) {
+        const int32_t len = select_len(a, p);
+        const Candidates c(a, len);
+        int32_t kept = 0, all;
+#pragma unroll 1
+        for (int32_t t0 = 0; t0 < len; t0 += NT) {
+            const int32_t t = t0 + static_cast<int32_t>(threadIdx.x);
+            const uint32_t key = t < len ? key_of(p, c, t) : kNone;
+            bool stays = key > least;
+            if (ties < need) {
+                const bool equal = key == least;
+                const int32_t before = place(equal, all);
+                stays = stays || (equal && before < need - ties);
+                ties += min(all, need - ties);
+            }
+            const int32_t n = kept + place(stays, all);
+            if (stays && n < a.max_keep) a.keep[static_cast<int64_t>(p) * a.max_keep + n] = t;
+            kept += all;
+        }
+        if (threadIdx.x == 0) {
+            a.n_keep[p] = kept <= a.max_keep ? kept : -1;
+            if (kept > a.max_keep && a.bad) atomicAdd(a.bad, 1);
+        }
+    }
+}
+
 // ---- a group that one workgroup has ----
 // Its rows in units of 64, a pair's last one not full, so that all lanes of a wave are in one pair; wave w has units w, w + NW, ...  What a pair's
 // rows need to know is held in lanes: lane p has pair p.  Keys lie in LDS.  With a window they are first the floats' bits, NaN for rows that are no
@@ -201,7 +332,7 @@ struct GroupSpace {
     int32_t counts[UNITS];
     int32_t total, protected_rows, candidate_rows;
 };
-template <int NT, int UNITS, bool POOL>
+template <int NT, int UNITS, bool POOL, bool ALONE>      // ALONE: no other kernel has larger groups
 __device__ __forceinline__ void select_group(const SelectArgs &a, int group, GroupSpace<UNITS> &m)
 {
     constexpr int NW = NT / 64, PER = (UNITS + 63) / 64;
@@ -218,11 +349,8 @@ __device__ __forceinline__ void select_group(const SelectArgs &a, int group, Gro
     const int32_t len = one ? select_len(a, p0 + lane) : 0;
     const int64_t off = one && !a.rows.pages ? a.rows.off[p0 + lane] : 0;
     const int64_t upto = wave_upto((static_cast<int64_t>(len) + 63) / 64), units64 = __shfl(upto, 63);
-    if (n_pairs > kMaxPairs || units64 > a.cap) {     // a.cap is UNITS or less: a larger group's other kernels do it, if there can be one
-        for (int p = threadIdx.x; p < n_pairs && !a.starts; p += NT) {
-            a.n_keep[p0 + p] = -1;
-            if (a.bad) atomicAdd(a.bad, 1);
-        }
+    if (n_pairs > kMaxPairs || units64 > a.cap) {     // a.cap is UNITS or less
+        if constexpr (ALONE) select_slowly<NT>(select_args_again(), group, bins, counts);
         return;
     }
     const int32_t units = __builtin_amdgcn_readfirstlane(static_cast<int>(units64));
@@ -369,10 +497,10 @@ __device__ __forceinline__ void select_group(const SelectArgs &a, int group, Gro
 }
 
 template <int NT, int UNITS, bool POOL>
-__global__ __launch_bounds__(NT) void fairkv_select_kernel(SelectArgs a)
+__global__ __launch_bounds__(NT, 8) void fairkv_select_kernel(SelectArgs a)
 {
     __shared__ GroupSpace<UNITS> m;
-    select_group<NT, UNITS, POOL>(a, blockIdx.x, m);
+    select_group<NT, UNITS, POOL, true>(a, blockIdx.x, m);
 }
 
 // ---- large groups: the line of their blocks ----
@@ -439,7 +567,7 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
     SelectShare share;
     if constexpr (STEP == 0) {
         const LineShare l = line_share<NT>(a.n_pairs, n_slots, slot_index, [&](int p) { return blocks_of(p); });
-        share = {l.total > a.max_blocks ? -1 : l.left, l.begin, l.at, 0, 0, l.pair, 0};      // runs of rows that overlap: so many blocks no cache has
+        share = {l.total > a.max_blocks ? -1 : l.left, l.begin, l.at, 0, 0, l.pair, 0};      // tokens without rows: more blocks than the workspace has
         if (share.left > 0)
             share.len = select_len(a, share.pair);      // (its group is looked at when the first rows are on their way)
         else if (threadIdx.x == 0)
@@ -447,12 +575,15 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
     } else {
         share = a.shares[slot_index];
     }
-    if (share.left < 0 && STEP == kLists && slot_index == 0)
-        for (int p = threadIdx.x; p < a.n_pairs; p += NT)
-            if (blocks_of(p) > 0) {
-                a.n_keep[p] = -1;
-                if (a.bad) atomicAdd(a.bad, 1);
-            }
+    if constexpr (STEP == kLists)
+        if (share.left < 0) {
+            const SelectArgs again = select_args_again();
+            LargeGroups blocks(again);
+#pragma unroll 1
+            for (int g = slot_index; g < again.n_groups; g += n_slots)
+                if (blocks(g * again.per_group) > 0) select_slowly<NT>(again, g, bins, m.counts);
+            return;
+        }
     if (share.left <= 0) return;
     int pair = share.pair, group = -1;
     int64_t block = share.block, at = share.at, group_at = share.group_at;      // group_at: the place of the group's first block
@@ -683,7 +814,7 @@ __global__ __launch_bounds__(kLargeThreads, 6) void fairkv_select_first_kernel(S
         __device__ Space() {}
     } m;
     if (static_cast<int>(blockIdx.x) < a.n_groups)
-        select_group<kLargeThreads, UNITS, POOL>(a, blockIdx.x, m.group);
+        select_group<kLargeThreads, UNITS, POOL, false>(a, blockIdx.x, m.group);
     else
         select_large<0>(a, blockIdx.x - a.n_groups, gridDim.x - a.n_groups, m.large);
 }
