@@ -489,6 +489,10 @@ int fairkv_decode_attn_tree(const fairkv_cache *cache, const void *q, const uint
 int fairkv_accept(const fairkv_cache *cache, const int32_t *path, const int32_t *n_path, const int32_t *n_new, const int32_t *len,
                   int32_t *len_out, int32_t q_len, int32_t *bad, void *hip_stream);
 
+/* The same, and the weights of the rows that move (fairkv_attn_weights, below) move with them: device float [n_rows], or NULL, which is fairkv_accept. */
+int fairkv_accept_weights(const fairkv_cache *cache, float *weights, const int32_t *path, const int32_t *n_path, const int32_t *n_new,
+                          const int32_t *len, int32_t *len_out, int32_t q_len, int32_t *bad, void *hip_stream);
+
 /* ---- compression of a growing cache: which rows matter, which stay, and away with the others ---------
  *
  * What makes a cache one that is compressed per head (the setting above) and keeps it one while it grows.  Three calls, which read lengths and lists
@@ -498,7 +502,14 @@ int fairkv_accept(const fairkv_cache *cache, const int32_t *path, const int32_t 
  *     fairkv_select          which rows of every pair stay, under a budget of the pair or of the sequence
  *     fairkv_evict           these rows move to the front of their pair, or into another cache
  *
- * Weights lie as the rows do: weights[row] belongs to row `row` of the cache, whichever pair and token that is. */
+ * Weights lie as the rows do: weights[row] belongs to row `row` of the cache, whichever pair and token that is, so what moves rows has to move them:
+ * fairkv_evict does, and fairkv_accept_weights.
+ * A draft is scored in one of two orders.  fairkv_accept, then fairkv_attn_weights with the queries and log-sum-exps of the accepted nodes, gathered in
+ * the order of the path (from a root on), tree NULL and n_new = n_path: rows have what the accepted tokens gave them.  Or fairkv_attn_weights with the
+ * draft's tree, then fairkv_accept_weights: rows keep what rejected nodes gave them, too.
+ * A row that was appended and not scored has what its place in weights held before, a dropped token's weight maybe, and that counts (times decay) from
+ * the next call on.  So every step is scored, or weights of rows that are appended without are set by the caller; a call with decay 0 sets those of
+ * all tokens. */
 
 /* For every token t of every pair, over the q_len queries of a sequence (its last n = n_new[b] tokens, whose rows are in the cache already):
  *     weights_out[row] = decay * weights[row] + sum over the nodes i < n that see t, and the heads g of the group, of exp(scale * q . k_t - lse)

@@ -33,7 +33,7 @@ EXPORTS = ("fairkv_default_params", "fairkv_plan", "fairkv_workspace_bytes", "fa
            "fairkv_decode_attn_multi", "fairkv_decode_attn_kv8", "fairkv_decode_attn_kv8_per_head",
            "fairkv_decode_attn_static", "fairkv_decode_attn_trace",
            "fairkv_place", "fairkv_pack", "fairkv_append", "fairkv_plan_grow", "fairkv_stream_probe", "fairkv_stream_probe_shape", "fairkv_workspace_reset",
-           "fairkv_append_rotated", "fairkv_decode_attn_tree", "fairkv_tree_workspace_bytes", "fairkv_tree_counter_bytes", "fairkv_tree_workspace_reset", "fairkv_accept",
+           "fairkv_append_rotated", "fairkv_decode_attn_tree", "fairkv_tree_workspace_bytes", "fairkv_tree_counter_bytes", "fairkv_tree_workspace_reset", "fairkv_accept", "fairkv_accept_weights",
            "fairkv_attn_weights", "fairkv_select", "fairkv_select_workspace_bytes", "fairkv_select_workspace_reset", "fairkv_evict",
            "fairkv_strerror", "fairkv_version")
 
@@ -173,6 +173,8 @@ def lib() -> ctypes.CDLL:
         L.fairkv_decode_attn_tree.argtypes = [cache_p, vp, vp, vp, vp, vp, ctypes.c_size_t, i32, vp, vp, i32, i32, i32, ctypes.c_float, vp]
         L.fairkv_accept.restype = ctypes.c_int
         L.fairkv_accept.argtypes = [cache_p, vp, vp, vp, vp, vp, i32, vp, vp]
+        L.fairkv_accept_weights.restype = ctypes.c_int
+        L.fairkv_accept_weights.argtypes = [cache_p, vp, vp, vp, vp, vp, vp, i32, vp, vp]
         L.fairkv_attn_weights.restype = ctypes.c_int
         L.fairkv_attn_weights.argtypes = [cache_p, vp, vp, vp, vp, vp, vp, vp, ctypes.c_float, i32, i32, i32, ctypes.c_float, vp]
         L.fairkv_select_workspace_bytes.restype = ctypes.c_size_t
@@ -334,7 +336,7 @@ def _native():
         m.init(ITEM_DTYPE, *(ctypes.cast(f, ctypes.c_void_p).value for f in (
             L.fairkv_decode_attn_multi, L.fairkv_decode_attn_static, L.fairkv_decode_attn_trace, L.fairkv_decode_attn_kv8,
             L.fairkv_decode_attn_kv8_per_head, L.fairkv_pack, L.fairkv_append, L.fairkv_append_rotated, L.fairkv_decode_attn_tree,
-            L.fairkv_accept, L.fairkv_attn_weights, L.fairkv_select, L.fairkv_evict)))
+            L.fairkv_accept_weights, L.fairkv_attn_weights, L.fairkv_select, L.fairkv_evict)))
         _native_module = m
     return _native_module
 
@@ -518,11 +520,14 @@ def fairkv_decode_attn_tree(cache, lens, q, workspace, out, lse, scale, tree=Non
         raise FairKVError(rc, "fairkv_decode_attn_tree")
 
 
-def fairkv_accept(cache, lens, path, n_path, n_new=None, lens_out=None, bad=None, stream=None):
+def fairkv_accept(cache, lens, path, n_path, n_new=None, lens_out=None, bad=None, stream=None, weights=None):
     """Enqueue the end of a step: of the draft's rows those of the accepted path are kept (see the header).
 
-    path int32 [B, q_len], n_path int32 [B]; n_new as in the step's append; lens, lens_out int32 [B, Hkv] (lens_out=None: in place); bad int32 [1]."""
-    rc = (_native_module or _native()).accept((_pt or _torch())[1], cache.address, cache.device, lens, path, n_path, n_new, lens_out, bad, stream)
+    path int32 [B, q_len], n_path int32 [B]; n_new as in the step's append; lens, lens_out int32 [B, Hkv] (lens_out=None: in place); bad int32 [1].
+    weights float32 [n_rows]: those that fairkv_attn_weights has given the draft's rows move with them; None where it is called behind this, with the
+    accepted path's queries."""
+    rc = (_native_module or _native()).accept((_pt or _torch())[1], cache.address, cache.device, lens, path, n_path, n_new, lens_out, bad, weights,
+                                              stream)
     if rc != FAIRKV_OK:
         raise FairKVError(rc, "fairkv_accept")
 

@@ -321,6 +321,7 @@ struct AcceptArgs {
     int32_t *len_out, *bad;
     RowMap rows;
     int32_t B, Hkv, q_len;
+    float *weights;                       // [n_rows] or null: they move with their rows
 };
 
 // Row base + path[i] of a pair to row base + i, base being the length without the draft.  A workgroup has whole pairs and all
@@ -337,6 +338,8 @@ __global__ __launch_bounds__(256) void fairkv_accept_kernel(AcceptArgs a)
     __syncthreads();
     u4 kk[kPasses], vv[kPasses];
     int64_t to[kPasses];
+    float w[kPasses];
+    const bool weights = a.weights && piece == 0;
 #pragma unroll
     for (int u = 0; u < kPasses; ++u) {
         const int r = slot + u * kSlots, own = r / a.q_len, pair = first + own, i = r % a.q_len;
@@ -354,6 +357,7 @@ __global__ __launch_bounds__(256) void fairkv_accept_kernel(AcceptArgs a)
             if (ok && from != i) {
                 kk[u] = *reinterpret_cast<const u4 *>(a.k + source * ROWB + piece * 16);
                 vv[u] = *reinterpret_cast<const u4 *>(a.v + source * ROWB + piece * 16);
+                if (weights) w[u] = a.weights[source];
             } else {
                 to[u] = -1;                // in its place already, or refused
             }
@@ -371,6 +375,7 @@ __global__ __launch_bounds__(256) void fairkv_accept_kernel(AcceptArgs a)
         if (to[u] < 0 || refused[own]) continue;
         *reinterpret_cast<u4 *>(a.k + to[u] * ROWB + piece * 16) = kk[u];
         *reinterpret_cast<u4 *>(a.v + to[u] * ROWB + piece * 16) = vv[u];
+        if (weights) a.weights[to[u]] = w[u];
     }
     if (counts) {
         const int pair = first + threadIdx.x, b = pair / a.Hkv;

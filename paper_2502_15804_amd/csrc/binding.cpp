@@ -29,7 +29,7 @@ decltype(&fairkv_pack) pack_rows;
 decltype(&fairkv_append) append_rows;
 decltype(&fairkv_append_rotated) append_rotated_rows;
 decltype(&fairkv_decode_attn_tree) decode_tree_attn;
-decltype(&fairkv_accept) accept_rows;
+decltype(&fairkv_accept_weights) accept_rows;
 decltype(&fairkv_attn_weights) attn_weights_rows;
 decltype(&fairkv_select) select_rows;
 decltype(&fairkv_evict) evict_rows;
@@ -461,21 +461,22 @@ PyObject *decode_tree(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// (current, cache, device, lens, path, n_path, n_new, lens_out, bad, stream)
+// (current, cache, device, lens, path, n_path, n_new, lens_out, bad, weights, stream)
 PyObject *accept(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    return guarded(n, 10, [&]() -> int {
+    return guarded(n, 11, [&]() -> int {
         const CacheArg cache(a[1], a[2]);
         const int64_t B = cache.c->B;
         const at::Tensor &lens = cache.flat(a[3], "lens", at::kInt, cache.pairs()), &path = cache.flat(a[4], "path", at::kInt, -1),
                          &n_path = cache.flat(a[5], "n_path", at::kInt, B), &count = cache.flat(a[6], "n_new", at::kInt, B, true),
-                         &lens_out = cache.flat(a[7], "lens_out", at::kInt, cache.pairs(), true), &bad = cache.flat(a[8], "bad", at::kInt, 1, true);
+                         &lens_out = cache.flat(a[7], "lens_out", at::kInt, cache.pairs(), true), &bad = cache.flat(a[8], "bad", at::kInt, 1, true),
+                         &weights = cache.flat(a[9], "weights", at::kFloat, cache.c->n_rows, true);
         if (path.dim() != 2 || path.size(0) != B || path.size(1) > INT32_MAX) refuse(PyExc_ValueError, "path must be [B, q_len]");
-        void *st = stream_of(a[9], a[0], path);
+        void *st = stream_of(a[10], a[0], path);
         const c10::DeviceGuard guard = cache.guard();
         return unlocked([&] {
-            return accept_rows(cache.c, data<const int32_t>(path), data<const int32_t>(n_path), data<const int32_t>(count), data<const int32_t>(lens),
-                               data<int32_t>(lens_out.defined() ? lens_out : lens), static_cast<int32_t>(path.size(1)), data<int32_t>(bad), st);
+            return accept_rows(cache.c, data<float>(weights), data<const int32_t>(path), data<const int32_t>(n_path), data<const int32_t>(count),
+                               data<const int32_t>(lens), data<int32_t>(lens_out.defined() ? lens_out : lens), static_cast<int32_t>(path.size(1)), data<int32_t>(bad), st);
         });
     });
 }

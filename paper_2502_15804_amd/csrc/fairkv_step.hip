@@ -88,13 +88,14 @@ extern "C" int fairkv_append_rotated(const fairkv_cache *c, const fairkv_rotatio
     return launched();
 }
 
-extern "C" int fairkv_accept(const fairkv_cache *c, const int32_t *path, const int32_t *n_path, const int32_t *n_new, const int32_t *len,
-                             int32_t *len_out, int32_t q_len, int32_t *bad, void *hip_stream)
+extern "C" int fairkv_accept_weights(const fairkv_cache *c, float *weights, const int32_t *path, const int32_t *n_path, const int32_t *n_new,
+                                     const int32_t *len, int32_t *len_out, int32_t q_len, int32_t *bad, void *hip_stream)
 {
     if (const int rc = check_cache(c)) return rc;
     if (!path || !n_path || !len || !len_out || q_len < 1) return FAIRKV_EINVAL;
     if (q_len > FAIRKV_MAX_DRAFT) return FAIRKV_EUNSUPPORTED;
-    const AcceptArgs a{static_cast<char *>(c->k), static_cast<char *>(c->v), path, n_path, n_new, len, len_out, bad, row_map(c), c->B, c->Hkv, q_len};
+    if (!aligned(weights, 4)) return FAIRKV_EINVAL;
+    const AcceptArgs a{static_cast<char *>(c->k), static_cast<char *>(c->v), path, n_path, n_new, len, len_out, bad, row_map(c), c->B, c->Hkv, q_len, weights};
     const int rb = c->D * (c->dtype == FAIRKV_E4M3 ? 1 : c->dtype == FAIRKV_BF16 ? 2 : 4), slots = 256 / (rb / 16), each = std::max(1, slots / q_len);
     const int64_t groups = (static_cast<int64_t>(c->B) * c->Hkv + each - 1) / each;
     if (groups > kMaxGroups) return FAIRKV_EINVAL;
@@ -109,6 +110,12 @@ extern "C" int fairkv_accept(const fairkv_cache *c, const int32_t *path, const i
     else
         hipLaunchKernelGGL(fairkv_accept_kernel<512>, grid, dim3(256), 0, st, a);
     return launched();
+}
+
+extern "C" int fairkv_accept(const fairkv_cache *c, const int32_t *path, const int32_t *n_path, const int32_t *n_new, const int32_t *len,
+                             int32_t *len_out, int32_t q_len, int32_t *bad, void *hip_stream)
+{
+    return fairkv_accept_weights(c, nullptr, path, n_path, n_new, len, len_out, q_len, bad, hip_stream);
 }
 
 // ---- attention of a draft tree --------------------------------------------------------------------
