@@ -45,8 +45,8 @@ struct SelectSlot {
     int32_t bins[kDigits - 1][kBins];     // of the other digits: the first step clears them
     SelectFound found[kDigits - 1];
 };
-struct SelectShare {                      // of a workgroup: its blocks in the line, and of the group that the first of them is in its first block and their number
-    int64_t left, block, at, group_at, group_blocks;      // left: how many; block: the first one's number in its pair
+struct SelectShare {                      // of a workgroup: its blocks in the line, and the place of the first block of the group that the first of them is in
+    int64_t left, block, at, group_at;    // left: how many, -1: the line is longer than the workspace has room for; block: the first one's number in its pair
     int32_t pair, len;                    // of the first one
 };
 struct SelectArgs {
@@ -524,17 +524,12 @@ struct LargeGroups {
         }
         return large ? max(1, (select_len(a, pair) + kBlockRows - 1) / kBlockRows) : 0;      // one of an empty pair too: its list is one
     }
-    // Where the group of a share's pair begins, and how many blocks it has.
+    // Where the group of a share's pair begins.
     __device__ __forceinline__ void group_of(SelectShare &s)
     {
-        const int first = s.pair / a.per_group * a.per_group;
-        s.group_at = s.at - s.block, s.group_blocks = 0;
+        s.group_at = s.at - s.block;
 #pragma unroll 8
-        for (int p = first; p < first + a.per_group; ++p) {
-            const int32_t n = max(1, (select_len(a, p) + kBlockRows - 1) / kBlockRows);
-            s.group_blocks += n;
-            if (p < s.pair) s.group_at -= n;
-        }
+        for (int p = s.pair / a.per_group * a.per_group; p < s.pair; ++p) s.group_at -= max(1, (select_len(a, p) + kBlockRows - 1) / kBlockRows);
     }
 };
 
@@ -562,12 +557,12 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
     auto &counts = reinterpret_cast<int32_t (&)[KPT][NT / 64]>(m.counts);
     auto &sums = m.sums;
     int32_t &total = m.total;
-    const int lane = threadIdx.x & 63;
+    [[maybe_unused]] const int lane = threadIdx.x & 63;
     LargeGroups blocks_of(a);
     SelectShare share;
     if constexpr (STEP == 0) {
         const LineShare l = line_share<NT>(a.n_pairs, n_slots, slot_index, [&](int p) { return blocks_of(p); });
-        share = {l.total > a.max_blocks ? -1 : l.left, l.begin, l.at, 0, 0, l.pair, 0};      // tokens without rows: more blocks than the workspace has
+        share = {l.total > a.max_blocks ? -1 : l.left, l.begin, l.at, 0, l.pair, 0};      // tokens without rows: more blocks than the workspace has
         if (share.left > 0)
             share.len = select_len(a, share.pair);      // (its group is looked at when the first rows are on their way)
         else if (threadIdx.x == 0)
@@ -757,51 +752,48 @@ __device__ __forceinline__ void select_large(const SelectArgs &a, int slot_index
             stays |= (key[i] > f.least ? 1u : 0u) << i;
             equal |= (f.need > 0 && key[i] == f.least ? 1u : 0u) << i;
         }
-        if constexpr (STEP == kLists) {
-            // ties in front of the pair, and of the block; rows in front of the block that stay anyhow; both of the whole pair
-            __syncthreads();
-            if (threadIdx.x < 5) sums[threadIdx.x] = 0;
-            __syncthreads();
-            unsigned long long s[5] = {0, 0, 0, 0, 0};
-            for (int64_t x = look_from + threadIdx.x; x < look_to; x += NT) {
-                const int2 n = x < look_from + NT ? look : counts_of(x);
-                if (x < pair_at) s[0] += n.y;
-                if (x < at) s[1] += n.y;
-                if (x >= pair_at && x < at) s[2] += n.x;
-                if (x >= pair_at) s[3] += n.y, s[4] += n.x;
-            }
+        // ties in front of the pair, and of the block; rows in front of the block that stay anyhow; both of the whole pair
+        __syncthreads();
+        if (threadIdx.x < 5) sums[threadIdx.x] = 0;
+        __syncthreads();
+        unsigned long long s[5] = {0, 0, 0, 0, 0};
+        for (int64_t x = look_from + threadIdx.x; x < look_to; x += NT) {
+            const int2 n = x < look_from + NT ? look : counts_of(x);
+            if (x < pair_at) s[0] += n.y;
+            if (x < at) s[1] += n.y;
+            if (x >= pair_at && x < at) s[2] += n.x;
+            if (x >= pair_at) s[3] += n.y, s[4] += n.x;
+        }
 #pragma unroll
-            for (int i = 0; i < 5; ++i) {
-                const int64_t n = wave_upto(static_cast<int64_t>(s[i]));
-                if (lane == 63 && n) atomicAdd(&sums[i], static_cast<unsigned long long>(n));
-            }
-            __syncthreads();
-            const int64_t ties_pair = sums[0], ties_block = sums[1];
-            const int64_t from = static_cast<int64_t>(sums[2]) + min(f.need, ties_block) - min(f.need, ties_pair);
-            if (block == 0 && threadIdx.x == 0) {
-                const int64_t n = static_cast<int64_t>(sums[4]) + min(f.need, ties_pair + static_cast<int64_t>(sums[3])) - min(f.need, ties_pair);
-                a.n_keep[pair] = n <= a.max_keep ? static_cast<int32_t>(n) : -1;
-                if (n > a.max_keep && a.bad) atomicAdd(a.bad, 1);
-            }
-            if (f.need > 0) {
-                count_rows<NT, KPT>(counts, equal, &total);
-#pragma unroll
-                for (int i = 0; i < KPT; ++i) {
-                    const int32_t n = rows_before<NT, KPT>(counts, equal, i);
-                    if ((equal >> i & 1) && ties_block + n < f.need) stays |= 1u << i;
-                }
-                __syncthreads();
-            }
-            count_rows<NT, KPT>(counts, stays, &total);
+        for (int i = 0; i < 5; ++i) {
+            const int64_t n = wave_upto(static_cast<int64_t>(s[i]));
+            if (lane == 63 && n) atomicAdd(&sums[i], static_cast<unsigned long long>(n));
+        }
+        __syncthreads();
+        const int64_t ties_pair = sums[0], ties_block = sums[1];
+        const int64_t from = static_cast<int64_t>(sums[2]) + min(f.need, ties_block) - min(f.need, ties_pair);
+        if (block == 0 && threadIdx.x == 0) {
+            const int64_t n = static_cast<int64_t>(sums[4]) + min(f.need, ties_pair + static_cast<int64_t>(sums[3])) - min(f.need, ties_pair);
+            a.n_keep[pair] = n <= a.max_keep ? static_cast<int32_t>(n) : -1;
+            if (n > a.max_keep && a.bad) atomicAdd(a.bad, 1);
+        }
+        if (f.need > 0) {
+            count_rows<NT, KPT>(counts, equal, &total);
 #pragma unroll
             for (int i = 0; i < KPT; ++i) {
-                const int64_t n = from + rows_before<NT, KPT>(counts, stays, i);
-                if ((stays >> i & 1) && n < a.max_keep) a.keep[static_cast<int64_t>(pair) * a.max_keep + n] = t0 + i * NT + static_cast<int32_t>(threadIdx.x);
+                const int32_t n = rows_before<NT, KPT>(counts, equal, i);
+                if ((equal >> i & 1) && ties_block + n < f.need) stays |= 1u << i;
             }
+            __syncthreads();
+        }
+        count_rows<NT, KPT>(counts, stays, &total);
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) {
+            const int64_t n = from + rows_before<NT, KPT>(counts, stays, i);
+            if ((stays >> i & 1) && n < a.max_keep) a.keep[static_cast<int64_t>(pair) * a.max_keep + n] = t0 + i * NT + static_cast<int32_t>(threadIdx.x);
         }
     }
     end_group();
-    (void)lane;
 }
 
 // The first step of the large groups, and beside it the groups that one workgroup has.
