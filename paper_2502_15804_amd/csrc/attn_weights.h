@@ -25,8 +25,6 @@
 #include "decode_mfma.h"
 #include "line.h"
 
-#include <cfloat>
-
 namespace fairkv {
 
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
@@ -63,8 +61,7 @@ __global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_we
     constexpr int AHEAD = CC > 64 ? 4 : 1;                            // pieces of queries that a thread asks for at once
     typedef __attribute__((ext_vector_type(4))) uint32_t u4;
     __shared__ __attribute__((aligned(1024))) char qs[CC * QROWB];
-    __shared__ __attribute__((aligned(16))) float minus_lse[CC];      // in log2 units; +inf: of a node that sees nothing, and no other's
-    __shared__ int32_t blind;                                         // the last run and pass whose columns had such a node
+    __shared__ __attribute__((aligned(16))) float minus_lse[CC];      // in log2 units
     __shared__ uint64_t sees[CC];                                     // of every column: the nodes that it sees
     __shared__ float joins[kSplit ? kShared : 1][kSplit ? CC / 32 : 1][64];      // of tiles that several waves have, for every 32 columns
 
@@ -81,7 +78,6 @@ __global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_we
     // Piece p of column c lies at piece p ^ swizzle(c): a row per lane, 16 of them take all banks.
     auto swizzle = [](int c) __attribute__((always_inline)) { return c / (256 / QROWB) % PPQ; };
 
-    if (threadIdx.x == 0) blind = -1;
     const LineShare share = line_share<NT>(n_pairs, gridDim.x, blockIdx.x, [&](int p) { return tiles_of(len_of(p)); });
     int pair = share.pair;
     int64_t first = share.begin, left = share.left;
@@ -146,14 +142,12 @@ __global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_we
                     for (int c = threadIdx.x; c < n; c += NT) {
                         const int node = (chunk * CC + c) / a.G, g = chunk * CC + c - node * a.G;
                         const float lse = a.lse[(static_cast<size_t>(b) * a.q_len + node) * a.Hq + h * a.G + g];
-                        minus_lse[c] = lse == -INFINITY ? INFINITY : lse < 0.f ? fminf(-lse * kLog2e, FLT_MAX) : -lse * kLog2e;
-                        if (lse == -INFINITY) blind = 2 * pair + chunk;
+                        minus_lse[c] = lse == -INFINITY ? -INFINITY : -lse * kLog2e;      // a node that sees nothing gives 0, or NaN to a row that is no number
                         sees[c] = a.tree ? static_cast<uint64_t>(a.tree[static_cast<size_t>(b) * a.q_len + node]) : ~0ull >> (63 - node);
                     }
                     __syncthreads();
                 }
                 if (!mine && shift == 0) continue;
-                const bool some_blind = __builtin_amdgcn_readfirstlane(blind) == 2 * pair + chunk;
                 bf16x8_t k[NSL];
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
@@ -164,39 +158,46 @@ __global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_we
                         k[p] = __builtin_bit_cast(bf16x8_t, raw[p]);
                     }
                 }
-                // 32 columns from c0.  some: not all of them are there; draft: some of the tile's tokens are the queries' own, and not seen by all; rare: some of
-                // the columns are of nodes that see nothing, which infinite rows and NaN ones would give NaN
+                // 32 columns from c0.  some: not all of them are there; draft: some of the tile's tokens are the queries' own, and not seen by all; again: for a
+                // tile of which a weight was NaN, without the nodes that see nothing
                 float w = 0.f;
-                auto columns = [&](int c0, auto some, auto draft, auto rare, auto joined) __attribute__((always_inline)) {
-                    constexpr bool kSome = decltype(some)::value, kDraft = decltype(draft)::value, kRare = decltype(rare)::value;
-                    const int c = kSome ? min(c0 + l32, n - 1) : c0 + l32;      // past the last one: that one again, and it does not count
+                auto columns = [&](int c0, auto some, auto draft, auto again, auto joined) __attribute__((always_inline)) {
+                    constexpr bool kSome = decltype(some)::value, kDraft = decltype(draft)::value, kAgain = decltype(again)::value;
+                    int at = l32, half = hi;
+                    if constexpr (kAgain) asm volatile("" : "+v"(at), "+v"(half));      // or what comes of them would be kept in registers by tiles that never come here
+                    const int c = kSome ? min(c0 + at, n - 1) : c0 + at;      // past the last one: that one again, and it does not count
                     bf16x8_t q[NSL];
 #pragma unroll
                     for (int s = 0; s < NSL; ++s) {
-                        const int p = KV8 ? (s & ~1) * 2 + 2 * hi + (s & 1) : 2 * s + hi;      // the order in which the lanes hold K
-                        q[s] = *reinterpret_cast<const bf16x8_t *>(qs + c * QROWB + ((p ^ swizzle(kSome ? c : l32)) * 16));
+                        const int p = KV8 ? (s & ~1) * 2 + 2 * half + (s & 1) : 2 * s + half;      // the order in which the lanes hold K
+                        q[s] = *reinterpret_cast<const bf16x8_t *>(qs + c * QROWB + ((p ^ swizzle(kSome ? c : at)) * 16));
                     }
                     f32x16_t z;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) z[r] = 0.f;
 #pragma unroll
                     for (int s = 0; s < NSL; ++s) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q[s], k[s], z, 0, 0, 0);
-                    const int32_t j = t0 + l32 - base;                          // of the queries' own tokens, below 0 in front of them
+                    const int32_t j = t0 + at - base;                          // of the queries' own tokens, below 0 in front of them
                     const uint32_t *words = reinterpret_cast<const uint32_t *>(sees) + (j >= 32 ? 1 : 0);
                     float s4[4] = {0.f, 0.f, 0.f, 0.f};
+                    uint32_t sighted = 0;                                       // of the columns those whose node sees something
+                    if constexpr (kAgain) {
+                        const int node = (chunk * CC + c) / a.G, g = chunk * CC + c - node * a.G;
+                        sighted = static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(a.lse[(static_cast<size_t>(b) * a.q_len + node) * a.Hq + h * a.G + g] != -INFINITY));
+                    }
 #pragma unroll
                     for (int r4 = 0; r4 < 4; ++r4) {
                         if (kSome && c0 + 8 * r4 >= n) break;
-                        const float4 ml4 = *reinterpret_cast<const float4 *>(minus_lse + c0 + 8 * r4 + 4 * hi);
+                        const float4 ml4 = *reinterpret_cast<const float4 *>(minus_lse + c0 + 8 * r4 + 4 * half);
                         const float ml[4] = {ml4.x, ml4.y, ml4.z, ml4.w};
 #pragma unroll
                         for (int x = 0; x < 4; ++x) {
-                            const int cr = c0 + 8 * r4 + 4 * hi + x;
+                            const int cr = c0 + 8 * r4 + 4 * half + x;
                             float e = __builtin_amdgcn_exp2f(fmaf(z[4 * r4 + x], s_mul, ml[x]));
                             bool counts = true;
                             if constexpr (kSome) counts = cr < n;
                             if constexpr (kDraft) counts = counts && (j < 0 || (words[2 * min(cr, n - 1)] >> (j & 31) & 1) != 0);
-                            if constexpr (kRare) counts = counts && ml[x] != INFINITY;
+                            if constexpr (kAgain) counts = counts && (sighted >> (8 * r4 + 4 * half + x) & 1) != 0;
                             s4[x] = r4 == 0 ? (counts ? e : 0.f) : s4[x] + (counts ? e : 0.f);
                         }
                     }
@@ -209,9 +210,7 @@ __global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_we
                 auto all_columns = [&](int c0, int step, auto joined) __attribute__((always_inline)) {
                     constexpr std::true_type yes;
                     constexpr std::false_type no;
-                    if (some_blind) {
-                        for (; c0 < n; c0 += step) columns(c0, yes, yes, yes, joined);
-                    } else if (t0 + TOK > base) {
+                    if (t0 + TOK > base) {
                         for (; c0 < n; c0 += step) columns(c0, yes, yes, no, joined);
                     } else {
                         for (; c0 + 32 <= n; c0 += step) columns(c0, no, no, no, joined);
@@ -227,7 +226,13 @@ __global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_we
                     if (!mine || part > 0) continue;
                     for (int x = 0; x * 32 < n; ++x) w += joins[of_turn][x][lane];      // in the order in which one wave adds
                 }
-                const float both = w + __shfl_xor(w, 32);
+                float both = w + __shfl_xor(w, 32);
+                if (__builtin_amdgcn_ballot_w64(both != both) != 0) {
+                    w = 0.f;
+#pragma unroll 1
+                    for (int c0 = 0; c0 < n; c0 += 32) columns(c0, std::true_type{}, std::true_type{}, std::true_type{}, std::false_type{});
+                    both = w + __shfl_xor(w, 32);
+                }
                 if (hi == 0 && row >= 0) a.out[row] = old + both;
             }
         }
