@@ -571,6 +571,7 @@ int fairkv_select(const fairkv_cache *cache, const fairkv_selection *s, const fl
  * 0 .. max_keep (in place: or its length; else: or its room there), an entry not in 0 .. len - 1, not ascending (in place), or a row outside its cache.
  * len_out, bad and weights_out must not meet one another, or keep, n_keep or the caches' off or pages or into's cap.
  * Pages behind ceil(len_out / page_rows) hold no token of a pair any more.  Packed rows stay where the pair's run begins.
+ * What n_keep says is known on the GPU only, so the host chooses how rows are dealt by max_keep: one not much larger than the lists are serves best.
  * Enqueues one kernel, and a second one if len_out is len; no synchronisation.  FAIRKV_EINVAL also: more than 2^20 pairs, max_keep
  * > 2^31 - 2^16. */
 int fairkv_evict(const fairkv_cache *cache, const fairkv_cache *into, const int32_t *keep, int32_t max_keep, const int32_t *n_keep,

@@ -6,7 +6,7 @@
 //
 // Measured (MI355X): into another cache 128 x 8 pairs of 4096 8-bit rows halved, 1.02 GB read and written, 241 us (4.25 TB/s; a plain copy has 4.9); 16 x 8 pairs of
 // 16000 bf16 rows to a sixteenth 28 us (4.4 TB/s); 8 pairs of 1024 halved 5.4 us, most of it the way from lists over pages to rows.  In place the order holds it
-// back: the same 300, 34 and 8 us, 8 pairs of 131072 rows to a third 238 us (1.3 TB/s, 128 workgroups; 312 with 64 of 64 bytes each that went round the XCDs, 955 with 4
+// back: the same 300, 35 and 9 us, 8 pairs of 131072 rows to a third 238 us (1.3 TB/s, 128 workgroups; 312 with 64 of 64 bytes each that went round the XCDs, 955 with 4
 // waves each and nothing asked for ahead).
 #pragma once
 #include "cache_rows.h"

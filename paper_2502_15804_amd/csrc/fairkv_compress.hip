@@ -54,7 +54,7 @@ bool written_over(std::initializer_list<Bytes> written, std::initializer_list<By
 }
 
 // 16 waves of a compute unit (20 with heads of 64 and few columns: 64 x 8 pairs of 4096 8-bit rows 43 us instead of 48), in as many workgroups as its LDS
-// has room for all columns of: a workgroup's waves wait for one another only where a pair begins.  64 queries x 8 heads over 64 x 8 pairs of 4096 rows: 316 us
+// has room for all columns of: a workgroup's waves wait for one another only where a pair begins.  64 queries x 8 heads over 64 x 8 pairs of 4096 rows, on one card: 316 us
 // with 16 waves and 512 columns in LDS, 355 with 12; with two tiles of 32 tokens a wave 349 (12 waves), 365 (8) and 444 (16); with 128 columns in
 // LDS at a time 859.  32 x 8 columns over 8 x 8 pairs of 16000 rows: 99 us in two workgroups of 8 waves or one of 16, 110 with 12 waves.
 template <int D, bool KV8, int NW, int CC>

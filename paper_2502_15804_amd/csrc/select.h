@@ -14,7 +14,7 @@
 // block, and one lists what stays.  A group that is longer than the cache has rows, because tokens of it have none, is gone through by one workgroup, slowly.  Every list ascends and no sum depends on who comes first: counts are whole numbers.
 //
 // What bounds it (MI355X; times of a call in a row of them): not its bytes (a million weights are 4 MB, 1 us) but one thing after the other.  A workgroup's
-// group: 9 us from lengths over pages, weights, three digits and ties to the list, 16 us where four of them share a compute unit's issue slots (128 x 8 pairs of
+// group: 9 us from lengths over pages, weights, three digits and ties to the list, 16 us with four of them on a compute unit, whose waves wait in 64 % of their cycles (128 x 8 pairs of
 // 1024 rows; 8 pairs of 1024 rows in one group 9.4).  A large one: four kernels of 4 to 8 us each, of which the first one takes 12, for it finds the groups'
 // blocks and reads the weights (one group of 8 pairs of 131072 rows 27 us; 16 groups of 8 pairs of 16000 rows 32, 34 where a fifth kernel counted what stays of
 // every block, 48 where every kernel read the weights).
