@@ -15,14 +15,14 @@
 //
 // What bounds it (MI355X; times of a launch in a row of them).  Few columns: memory, 32 x 8 pairs of 4096 rows (bf16, heads of 128) 280 MB in 62 us
 // (4.5 TB/s), and 4 to 5 us until the first rows are there, which is all that one sequence of 8 pairs of 1024 rows costs (4.6 us).  Many columns: power.
-// 64 x 8 pairs of 4096 rows and 512 columns 316 to 336 us by card (830 to 880 TFLOP/s; a library's matrix product of 8192 rows has 1167) are 612 thousand cycles at 1.95 GHz, 266 thousand
-// of matrix instructions beside 360 thousand of others, with 12 KB from LDS a wave for every 32 columns; the same instructions over numbers that are
+// 64 x 8 pairs of 4096 rows and 512 columns 316 to 336 us by card (830 to 880 TFLOP/s; a library's matrix product of 8192 rows has 1167) are 620 thousand
+// cycles at 1.95 GHz, 266 thousand of matrix instructions beside 360 thousand of others, with 12 KB from LDS a wave for every 32 columns; the same instructions over numbers that are
 // all alike take 530 thousand at 2.4 GHz.  In between, both: 256 columns over 8 x 8 pairs of 16000 rows 97 us (2.8 TB/s, 690 TFLOP/s), 67 without the columns'
-// work, 90 without the rows' way from memory; matrix and other vector instructions are 158 of its 204 thousand cycles.  In short pairs waves wait (two thirds of
-// their cycles: 32 trees of 8 over 8 pairs of 512 rows 18 us): the line is dealt in tiles, but four waves take a turn together, and the longest workgroup has 4
-// turns where 2 would do.  More columns than LDS holds wait half of the time (1024 over 8 x 8 pairs of 4096 rows, heads of 128, 134 us): one workgroup on a compute
-// unit, which brings in 128 KB of queries and reads K in each of two passes.  Tried and slower there: the next tile's rows in registers (spills at four waves of a SIMD, fewer waves
-// without) or in LDS (fewer waves), two tiles a wave, scores of the next columns beside the weights of these, wave priorities.
+// work, 90 without the rows' way from memory; matrix and other vector instructions are 158 of its 207 thousand cycles.  In short pairs waves wait (two thirds of
+// their cycles: 32 trees of up to 8 nodes, heads of 64, 18 us): the line is dealt in tiles, but four waves take a turn together, and the longest workgroup has 4
+// turns where 2 would do.  More columns than LDS holds wait half of the time (1024 over 8 x 8 pairs of 4096 rows, heads of 128, 131 us): one workgroup on a compute
+// unit, which brings in 128 KB of queries and reads K in each of two passes.  Tried and slower: the next tile's rows in registers (spills at four waves of
+// a SIMD, fewer waves without) or in LDS (fewer waves), two tiles a wave, scores of the next columns beside the weights of these, wave priorities.
 #pragma once
 #include "cache_rows.h"
 #include "decode_mfma.h"
