@@ -230,7 +230,7 @@ __global__ __launch_bounds__(NW * 64, (kWeightWaves<D, NW>)) void fairkv_attn_we
                     for (int x = 0; x * 32 < n; ++x) w += joins[of_turn][x][lane];      // in the order in which one wave adds
                 }
                 float both = w + __shfl_xor(w, 32);
-                if (__builtin_amdgcn_ballot_w64(both != both) != 0) {
+                if (__builtin_amdgcn_ballot_w64(row >= 0 && both != both) != 0) {
                     w = 0.f;
 #pragma unroll 1
                     for (int c0 = 0; c0 < n; c0 += 32) columns(c0, std::true_type{}, std::true_type{}, std::true_type{}, std::false_type{});
